@@ -86,6 +86,53 @@ typedef struct xs_window {
 int xs_route_topk_softmax(const float* logits, int32_t T, int32_t E, int32_t k,
                           int32_t renormalize, int32_t* topk_idx, float* topk_w, void* stream);
 
+/* ----------------------------------------------------------------------------- routing gates
+ * Routing by a trained gate (softmax top-k over plain logits is xs_route_topk_softmax):
+ *   score      s_e = softmax(logits)_e or sigmoid(logit_e); 0 for a masked expert (logit -inf)
+ *   bias       optional device fp32 [E], added to the scores for the selection only (a balance
+ *              bias; it has no gradient)
+ *   groups     E experts in n_group groups of consecutive experts; the topk_group groups with the
+ *              largest group score (the largest biased score in it, or the sum of its two largest,
+ *              one if it has one unmasked expert) are kept, ties to the lower group
+ *   selection  the k experts of the kept groups with the largest biased scores in descending order,
+ *              ties to the lower index; masked experts come after every other one. Scores are
+ *              compared in 64 bits (to 42 bits at least: closer ones count as equal)
+ *   weights    w_j = scale s_j, with renormalize != 0 scale s_j / sum_i s_i over the k selected (0
+ *              where that sum is 0)
+ * A row that is masked whole selects its lowest indices with weights 0. A NaN logit counts as masked
+ * in the selection (and makes softmax weights of its row NaN). */
+enum { XS_SCORE_SOFTMAX = 0, XS_SCORE_SIGMOID = 1 };
+enum { XS_GROUP_MAX = 0, XS_GROUP_TOP2 = 1 };
+enum { XS_TYPE_BF16 = 0, XS_TYPE_F32 = 1 };
+
+typedef struct xs_gate {
+  int32_t E, k;
+  int32_t score;              /* XS_SCORE_* */
+  int32_t n_group, topk_group; /* 1, 1: no groups */
+  int32_t group_score;        /* XS_GROUP_* */
+  int32_t renormalize;
+  int32_t logits_type;        /* XS_TYPE_* of logits and of their gradient */
+  float scale;
+  int32_t reserved;           /* 0 */
+  const float* bias;          /* device fp32 [E] or NULL */
+} xs_gate;
+
+/* logits device [T][E], rows ld elements apart; topk_idx device int32 [T][k] out; topk_w device fp32
+ * [T][k] out. Requires E <= 1024, 1 <= k <= min(E, 32), E % n_group == 0, n_group <= 64, 1 <= topk_group
+ * <= n_group, k <= topk_group E / n_group, a finite scale, logits aligned to their type: otherwise
+ * XS_EINVAL and nothing is launched. */
+int xs_route_gate(const xs_gate* g, const void* logits, int64_t ld, int32_t T, int32_t* topk_idx,
+                  float* topk_w, void* stream);
+
+/* Gradient of the weights in the logits, the selection held fixed: d_logits device [T][E] (rows ld_d
+ * elements apart, of logits_type; every element is written; may be logits itself) from d_topk_w device
+ * fp32 [T][k] and the forward call's g, logits and topk_idx. An expert listed twice by a token gets both
+ * slots' terms; an index outside [0, E) sets XS_EBADINPUT in dev_status and its slot counts as absent.
+ * Argument errors as above. */
+int xs_route_gate_backward(const xs_gate* g, const void* logits, int64_t ld, int32_t T,
+                           const int32_t* topk_idx, const float* d_topk_w, void* d_logits,
+                           int64_t ld_d, int32_t* dev_status, void* stream);
+
 /* ----------------------------------------------------------------------------- layout
  * Destination-window layout of every (source, token, slot) (the Dispatch exchange,
  * Sec. 2.2 and Sec. 4.3: expert-parallel tokens go to the ranks owning their experts).
@@ -536,6 +583,75 @@ int xs_quantize_mx_grouped(const void* x, int64_t rows, int32_t cols, int64_t ld
 int xs_gemm_mx(const void* a, int64_t lda, const void* a_scales, int64_t lda_s, const void* b,
                int64_t ldb, const void* b_scales, int64_t ldb_s, int32_t b_fmt, void* c,
                int64_t ldc, int32_t M, int32_t N, int32_t K, const xs_trace* trace, void* stream);
+
+/* ----------------------------------------------------------------------------- E4M3, blocks of 128
+ * E4M3 values (OCP "FN", largest 448) with one fp32 scale per block of 128: 1 x 128 (activations and
+ * gradients) or 128 x 128 (weights). A matrix [rows][cols] of 1 x 128 blocks is codes [rows][ceil(cols /
+ * 128) * 128] (ld bytes per row, a multiple of 16) and scales fp32 [rows][ceil(cols / 128)] (ld_s floats
+ * per row, a multiple of 4), both 16-byte aligned; the codes past cols are zero. A matrix of 128 x 128
+ * blocks has scales [ceil(rows / 128)][ceil(cols / 128)].
+ * Quantization: scale = max(amax, 2^-60) / 448 rounded to fp32, code = E4M3(x / scale), the quotient
+ * rounded to fp32 and then to nearest even. A block with an infinity or a NaN gets the scale NaN and zero
+ * codes, so every product with it is NaN. */
+enum { XS_BLOCK_ROW = 0, XS_BLOCK_TILE = 1 };   /* 1 x 128, 128 x 128 */
+
+/* x device bf16 [rows][cols] (ldx elements per row, 16-byte aligned rows) quantized in 1 x 128 blocks:
+ * along its rows into codes / scales, and along its columns, transposed, into codes_t [cols][ceil(rows /
+ * 128) * 128] / scales_t [cols][ceil(rows / 128)] (the operands of a weight's gradient, whose sum runs
+ * over the rows). Either pair may be NULL, not both. x is read once. cols a multiple of 8, else
+ * XS_EUNSUPPORTED. XS_EINVAL on other bad arguments; nothing is launched on an error. */
+int xs_quantize_fp8(const void* x, int64_t rows, int32_t cols, int64_t ldx, void* codes, int64_t ld_codes,
+                    float* scales, int64_t ld_scales, void* codes_t, int64_t ld_codes_t, float* scales_t,
+                    int64_t ld_scales_t, void* stream);
+
+/* The same in 128 x 128 blocks (weights): scales [ceil(rows / 128)][ceil(cols / 128)], scales_t its
+ * transpose (the transposed weight is the operand of the input's gradient). */
+int xs_quantize_fp8_tile(const void* x, int64_t rows, int32_t cols, int64_t ldx, void* codes,
+                         int64_t ld_codes, float* scales, int64_t ld_scales, void* codes_t,
+                         int64_t ld_codes_t, float* scales_t, int64_t ld_scales_t, void* stream);
+
+/* C = A B^T of block-scaled operands: a E4M3 [M][K] in 1 x 128 blocks, b E4M3 [N][K] in 1 x 128 blocks
+ * (b_block XS_BLOCK_ROW, scales [N][K / 128]) or 128 x 128 (XS_BLOCK_TILE, scales [ceil(N / 128)][K /
+ * 128]); c [M][N] bf16 or fp32 (c_type, ldc elements per row, 16-byte aligned). Blocks' sums are scaled and
+ * added in fp32 in ascending K (small M: in parallel parts of K, joined in a fixed order), one rounding
+ * at the end. Within a block: for an fp32 result exact products summed in fp32; for a bf16 result the 8-bit
+ * matrix unit, at twice the rate, which cuts the products of eight consecutive K elements below 2^-13 of
+ * the largest one's exponent (about 1e-5 of the result).
+ * How a product is split follows from M, N, K and the device's CU count alone. K counts whole blocks (the
+ * padded columns of a quantized matrix).
+ * Requires K % 128 == 0, N % 8 == 0, rows of at most 2^22 bytes (else XS_EUNSUPPORTED); ldc % 8 == 0 and
+ * the layout above (else XS_EINVAL). */
+int xs_gemm_fp8(const void* a, int64_t lda, const float* a_scales, int64_t lda_s, const void* b, int64_t ldb,
+                const float* b_scales, int64_t ldb_s, int32_t b_block, void* c, int64_t ldc, int32_t c_type,
+                int32_t M, int32_t N, int32_t K, void* stream);
+
+/* The grouped product of xs_grouped_gemm on such operands: rows [seg_offsets[s], + seg_rows[s]) of a times
+ * B_s^T into the same rows of c (bf16), B_s = b + s N K bytes [N][K] in 128 x 128 blocks, its scales at
+ * b_scales + s ceil(N / 128) ldb_s. XS_EPI_STORE or XS_EPI_SWIGLU (gate rows [0, N / 2), up rows [N / 2,
+ * N); c [M][N / 2]). Segments, their errors and the rows outside every segment as xs_grouped_gemm.
+ * Requires K % 128 == 0, N % 8 == 0 (STORE) or N % 256 == 0 (SWIGLU). The input's gradient is the same
+ * call on transposed weights (xs_quantize_fp8_tile's codes_t), a segment's weight gradient xs_gemm_fp8 on
+ * transposed rows. How rows are tiled follows from M, n_seg, N, K and the device's CU count alone. */
+int xs_grouped_gemm_fp8(const void* a, int64_t lda, const float* a_scales, int64_t lda_s, int32_t M,
+                        const int32_t* seg_offsets, const int32_t* seg_rows, int32_t n_seg, const void* b,
+                        const float* b_scales, int64_t ldb_s, int32_t N, int32_t K, void* c, int64_t ldc,
+                        int32_t epilogue, int32_t* dev_status, void* stream);
+
+/* SwiGLU between two such products: gu device bf16 [rows][2 I] (gate, then up; ld_gu elements per row,
+ * 16-byte aligned) -> h = silu(gate) up quantized in 1 x 128 blocks (h_codes [rows][I], h_scales), and, with
+ * ck_codes non-NULL, an 8-bit checkpoint of gu for the backward pass: gu quantized in 1 x 128 blocks
+ * (ck_codes [rows][2 I], ck_scales [rows][2 I / 128]), half the bytes of gu. h comes from gu itself.
+ * Requires I % 128 == 0 (else XS_EUNSUPPORTED). */
+int xs_swiglu_fp8(const void* gu, int64_t ld_gu, int64_t rows, int32_t I, void* h_codes, int64_t ld_h,
+                  float* h_scales, int64_t ld_hs, void* ck_codes, int64_t ld_ck, float* ck_scales,
+                  int64_t ld_cks, void* stream);
+
+/* Its gradient from the checkpoint: d_gu bf16 [rows][2 I] from dh bf16 [rows][I] and the checkpoint's gate g
+ * and up u: d_gate = dh u sig(g) (1 + g (1 - sig(g))), d_up = dh silu(g); with h non-NULL also h = silu(g) u
+ * bf16 [rows][I], recomputed for the second product's weight gradient. Requires I % 128 == 0. */
+int xs_swiglu_fp8_backward(const void* ck_codes, int64_t ld_ck, const float* ck_scales, int64_t ld_cks,
+                           const void* dh, int64_t ld_dh, int64_t rows, int32_t I, void* d_gu, int64_t ld_dgu,
+                           void* h, int64_t ld_h, void* stream);
 
 /* ----------------------------------------------------------------------------- X-Stage
  * Burst-Gap model (Sec. 3.3-3.5). Units: bytes and microseconds.

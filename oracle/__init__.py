@@ -21,6 +21,8 @@ Modules:
   ep_mx           the quantized EP layer (W8A8 MXFP8, W4A8 with E2M1 weights)
   ring            dispatch through bounded destination rings, with optional per-destination
                   token dedup
+  gate            routing gates (sigmoid or softmax, bias, groups) and their gradient
+  fp8             E4M3 blocks of 128 with fp32 scales: quantizer, products, SwiGLU checkpoints
   mx              microscaled formats (E4M3 / E2M1 elements, E8M0 block scales) of the
                   quantized EP path: encode, decode, block quantizer, dequantized GEMM
 
@@ -28,4 +30,4 @@ Parity status: every function here is pinned by tests under ``tests/`` against
 closed forms, worked numbers the paper prints, brute force or library routines,
 except where a function's docstring says "parity unpinned".
 """
-from . import attention, ep, ep_mx, mx, ring, scatter, xstage_model, schedule  # noqa: F401
+from . import attention, ep, ep_mx, fp8, gate, mx, ring, scatter, xstage_model, schedule  # noqa: F401

@@ -1,0 +1,87 @@
+"""Oracle of the E4M3 blocks of 128 with fp32 scales: quantizer, dequantized values, products, SwiGLU
+with its checkpoint and gradient.
+
+scale = max(amax, 2^-60) / 448 and x / scale are rounded to fp32 (numpy's division), the code to the
+nearest E4M3 value, ties to even; a block that holds an infinity or a NaN has the scale NaN and zero
+codes. Everything after that is fp64."""
+from __future__ import annotations
+
+import numpy as np
+
+from . import mx
+
+__all__ = ["BLOCK", "quantize", "values", "silu", "swiglu", "swiglu_backward", "product_bound"]
+
+BLOCK = 128
+
+
+def _blocks(n):
+    return -(-n // BLOCK)
+
+
+def quantize(x, down=1):
+    """x: values that fp32 holds, [rows][cols]. Blocks of `down` rows x 128 columns. Returns (codes uint8
+    [rows][padded cols], scales fp32 [ceil(rows / down)][blocks])."""
+    x = np.asarray(x, dtype=np.float32)
+    rows, cols = x.shape
+    R, B = -(-rows // down), _blocks(cols)
+    full = np.zeros((R * down, B * BLOCK), dtype=np.float32)
+    full[:rows, :cols] = x
+    v = full.reshape(R, down, B, BLOCK)
+    with np.errstate(invalid="ignore"):
+        amax = np.abs(v).max((1, 3))
+    bad = ~np.isfinite(amax)
+    s = (np.maximum(np.where(bad, np.float32(0), amax), np.float32(2.0 ** -60)) / np.float32(448)).astype(np.float32)
+    with np.errstate(invalid="ignore", over="ignore"):
+        q = np.where(bad[:, None, :, None], np.float32(0), v) / s[:, None, :, None]
+    assert q.dtype == np.float32
+    codes = np.where(np.broadcast_to(bad[:, None, :, None], v.shape), np.uint8(0), mx.encode(q.astype(np.float64), mx.E4M3))
+    return (codes.reshape(R * down, B * BLOCK)[:rows].astype(np.uint8),
+            np.where(bad, np.float32(np.nan), s).astype(np.float32))
+
+
+def values(codes, scales, down=1):
+    """fp64 values of codes [rows][K] under scales [ceil(rows / down)][>= K / 128]."""
+    c = mx.decode(codes, mx.E4M3)
+    rows, K = c.shape
+    s = np.asarray(scales, dtype=np.float64)[np.arange(rows) // down][:, :K // BLOCK]
+    return c * np.repeat(s, BLOCK, axis=1)
+
+
+def silu(g):
+    with np.errstate(over="ignore"):
+        return g / (1.0 + np.exp(-g))
+
+
+def swiglu(gu):
+    g, u = np.split(np.asarray(gu, dtype=np.float64), 2, axis=1)
+    return silu(g) * u
+
+
+def swiglu_backward(gu, dh):
+    """(d_gu, h, magnitude of d_gu's terms) in fp64."""
+    g, u = np.split(np.asarray(gu, dtype=np.float64), 2, axis=1)
+    with np.errstate(over="ignore"):
+        sig = 1.0 / (1.0 + np.exp(-g))
+    dh = np.asarray(dh, dtype=np.float64)
+    d = np.concatenate([dh * u * sig * (1 + g * (1 - sig)), dh * g * sig], axis=1)
+    mag = np.concatenate([np.abs(dh * u) * sig * (1 + np.abs(g) * (1 - sig)), np.abs(dh * g * sig)], axis=1)
+    return d, g * sig * u, mag
+
+
+def product_bound(A, B, exact):
+    """Bound of the error of A B^T before its final rounding. A product passes at most 128 additions in its
+    block, one per block and (parts of K joined) eight more, and three roundings by the scales; doubled for
+    the matrix unit's own order of additions. Unless `exact`, the 8-bit matrix unit also cuts each of eight
+    consecutive products below 2^-13 of the largest's exponent (its magnitude bounds that): at most 8 2^-13
+    of a group's largest product."""
+    K = A.shape[1]
+    A, B = np.abs(A), np.abs(B)
+    bound = 2 * (128 + K // BLOCK + 11) * 2.0 ** -24 * (A @ B.T)
+    if not exact:
+        for k in range(0, K, 8):
+            largest = np.zeros((A.shape[0], B.shape[0]))
+            for i in range(k, k + 8):
+                np.maximum(largest, A[:, i, None] * B[None, :, i], out=largest)
+            bound += 2.0 ** -10 * largest
+    return bound

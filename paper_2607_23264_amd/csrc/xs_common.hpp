@@ -113,6 +113,9 @@ __device__ __forceinline__ void wait_vm() {   // s_waitcnt vmcnt(V) only
   asm volatile("" ::: "memory");
 }
 
+// The workgroup's number in a grid of xs_host::grid_of(n).
+__device__ __forceinline__ int64_t block_number() { return blockIdx.x + static_cast<int64_t>(gridDim.x) * blockIdx.y; }
+
 // Busy-wait for `ticks` wall-clock ticks without touching memory.
 __device__ __forceinline__ void spin_ticks(uint64_t ticks) {
   if (!ticks) return;
@@ -133,5 +136,13 @@ int launch_status();                      // XS_OK, or XS_EHIP if the last launc
 double wall_rate_hz();                    // wall-clock tick rate of the current device
 int num_cus();                            // compute units of the current device
 int64_t ns_to_ticks(int64_t ns);
+
+// At least n workgroups in two dimensions (a dimension has at most 2^32 - 1 threads); n < 2^35, the
+// kernel leaves the last dimension's surplus out.
+inline dim3 grid_of(int64_t n) {
+  const int64_t x = n < (1 << 20) ? n : 1 << 20;
+  return dim3(static_cast<unsigned>(x), static_cast<unsigned>((n + x - 1) / x));
+}
+constexpr int64_t kMaxBlocks = int64_t(1) << 35;
 
 }  // namespace xs_host

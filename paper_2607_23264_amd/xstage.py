@@ -31,6 +31,10 @@ XS_ATTN_LOCAL, XS_ATTN_WINDOWS, XS_ATTN_WINDOWS_COUPLED = 0, 1, 2
 XS_FMT_E4M3, XS_FMT_E2M1 = 0, 1
 XS_PREC_BF16, XS_PREC_MXFP8, XS_PREC_W4A8 = 0, 1, 2
 XS_EPI_STORE, XS_EPI_SWIGLU = 0, 1
+XS_SCORE_SOFTMAX, XS_SCORE_SIGMOID = 0, 1
+XS_GROUP_MAX, XS_GROUP_TOP2 = 0, 1
+XS_TYPE_BF16, XS_TYPE_F32 = 0, 1
+XS_BLOCK_ROW, XS_BLOCK_TILE = 0, 1
 
 vp = C.c_void_p
 i32 = C.c_int32
@@ -76,6 +80,11 @@ class xs_attn(C.Structure):
     _fields_ = [("heads", i32), ("M", i32), ("head_dim", i32), ("W", i32), ("scale", C.c_float),
                 ("max_producers", i32), ("q", vp), ("k", vp), ("v", vp), ("o", vp),
                 ("win", C.POINTER(xs_window))]
+
+
+class xs_gate(C.Structure):
+    _fields_ = [("E", i32), ("k", i32), ("score", i32), ("n_group", i32), ("topk_group", i32), ("group_score", i32),
+                ("renormalize", i32), ("logits_type", i32), ("scale", C.c_float), ("reserved", i32), ("bias", vp)]
 
 
 class xs_scatter_desc(C.Structure):
@@ -178,8 +187,19 @@ xs_burst_gap = _sig("xs_burst_gap", C.c_int, P(xs_model), f64, f64, P(f64), P(f6
 xs_recovery_audit = _sig("xs_recovery_audit", C.c_int, P(xs_model), f64, i32, f64, f64, i32, P(xs_recovery))
 xs_pacing_audit_run = _sig("xs_pacing_audit_run", C.c_int, P(xs_ep_layer), P(xs_pacing), P(xs_pacing_audit))
 xs_trace_tile_times = _sig("xs_trace_tile_times", C.c_int, vp, vp, i64, i32, P(f64), P(f64), P(f64))
+xs_route_gate = _sig("xs_route_gate", C.c_int, P(xs_gate), vp, i64, i32, vp, vp, vp)
+xs_route_gate_backward = _sig("xs_route_gate_backward", C.c_int, P(xs_gate), vp, i64, i32, vp, vp, vp, i64, vp, vp)
+xs_quantize_fp8 = _sig("xs_quantize_fp8", C.c_int, vp, i64, i32, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp)
+xs_quantize_fp8_tile = _sig("xs_quantize_fp8_tile", C.c_int, vp, i64, i32, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp)
+xs_gemm_fp8 = _sig("xs_gemm_fp8", C.c_int, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, i32, i32, i32, i32, vp)
+xs_grouped_gemm_fp8 = _sig("xs_grouped_gemm_fp8", C.c_int, vp, i64, vp, i64, i32, vp, vp, i32, vp, vp, i64, i32, i32, vp,
+                           i64, i32, vp, vp)
+xs_swiglu_fp8 = _sig("xs_swiglu_fp8", C.c_int, vp, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp)
+xs_swiglu_fp8_backward = _sig("xs_swiglu_fp8_backward", C.c_int, vp, i64, vp, i64, vp, i64, i64, i32, vp, i64, vp, i64, vp)
 
-EXPORTED = ["xs_strerror", "xs_version", "xs_route_topk_softmax", "xs_dispatch_layout_workspace_bytes",
+EXPORTED = ["xs_route_gate", "xs_route_gate_backward", "xs_quantize_fp8", "xs_quantize_fp8_tile", "xs_gemm_fp8",
+            "xs_grouped_gemm_fp8", "xs_swiglu_fp8", "xs_swiglu_fp8_backward",
+            "xs_strerror", "xs_version", "xs_route_topk_softmax", "xs_dispatch_layout_workspace_bytes",
             "xs_dispatch_layout", "xs_dispatch", "xs_ep_layer_workspace_bytes", "xs_expert_ffn",
             "xs_combine_send", "xs_combine_reduce", "xs_fused_ep_layer", "xs_gemm", "xs_gemm_scatter",
             "xs_scatter_copy", "xs_attention", "xs_ulysses_copy", "xs_quantize_mx", "xs_quantize_mx_grouped", "xs_gemm_mx", "xs_dispatch_rows",
@@ -227,6 +247,14 @@ def windows(ws) -> C.Array:
     for i, w in enumerate(ws):
         arr[i] = w
     return arr
+
+
+def gate(E, k, score=XS_SCORE_SOFTMAX, n_group=1, topk_group=1, group_score=XS_GROUP_MAX, renormalize=0, scale=1.0,
+         bias=None, logits_type=XS_TYPE_F32) -> xs_gate:
+    """A routing gate; keeps the bias tensor alive."""
+    g = xs_gate(E, k, score, n_group, topk_group, group_score, int(renormalize), logits_type, scale, 0, ptr(bias))
+    g._bias_ref = bias
+    return g
 
 
 def trace(buf, count) -> xs_trace:
