@@ -96,11 +96,10 @@ int xs_route_topk_softmax(const float* logits, int32_t T, int32_t E, int32_t k,
  *              one if it has one unmasked expert) are kept, ties to the lower group
  *   selection  the k experts of the kept groups with the largest biased scores in descending order,
  *              ties to the lower index; masked experts come after every other one. Scores are
- *              compared in 64 bits (to 42 bits at least: closer ones count as equal)
- *   weights    w_j = scale s_j, with renormalize != 0 scale s_j / sum_i s_i over the k selected (0
- *              where that sum is 0)
+ *              compared as computed in 64 bits (within 2^127; below that counts as masked)
+ *   weights    w_j = scale s_j, with renormalize != 0 scale s_j / sum_i s_i over the k selected
  * A row that is masked whole selects its lowest indices with weights 0. A NaN logit counts as masked
- * in the selection (and makes softmax weights of its row NaN). */
+ * in the selection; weights that depend on it are NaN. */
 enum { XS_SCORE_SOFTMAX = 0, XS_SCORE_SIGMOID = 1 };
 enum { XS_GROUP_MAX = 0, XS_GROUP_TOP2 = 1 };
 enum { XS_TYPE_BF16 = 0, XS_TYPE_F32 = 1 };

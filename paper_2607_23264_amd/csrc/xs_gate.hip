@@ -5,9 +5,16 @@
 //   key_e = s_e + b_e          group score = the largest key, or the sum of the two largest
 //   w_j = scale s_j            or, renormalized, scale s_j / S with S = sum_i s_i over the k chosen
 //
-// Gradient, g_j = dL/dw_j:  ds_j = scale g_j, or scale (g_j - sum_i g_i s_i / S) / S;
-//   sigmoid  dl_e = sum_{j: e_j = e} ds_j s_e (1 - s_e)
-//   softmax  dl_e = s_e (sum_{j: e_j = e} ds_j - sum_j ds_j s_j)   (renormalized: the second sum is 0)
+// A factor that all k scores have cancels in s_j / S: renormalized weights r_j are computed from exp(l_j - c)
+// with c the largest of the k logits (sigmoid: where that is below 0), so scores that underflow fp32
+// still have their weights.
+//
+// Gradient, g_j = scale dL/dw_j; sums over the slots j of expert e, all other elements 0 but for plain softmax:
+//   sigmoid               dl_e = sum g_j s_e (1 - s_e)
+//   softmax               dl_e = s_e (sum g_j - sum_i g_i s_i)          (every e)
+//   renormalized, d_j = (g_j - sum_i g_i r_i) r_j:
+//     sigmoid             dl_e = sum d_j (1 - s_e)
+//     softmax             dl_e = sum d_j
 #include <algorithm>
 #include <cmath>
 
@@ -36,29 +43,97 @@ __device__ __forceinline__ const char* logit_row(const void* logits, int64_t ld,
   return static_cast<const char*>(logits) + t * ld * static_cast<int64_t>(sizeof(LT));
 }
 
-// Keys are finite: a masked expert (logit -inf or NaN, key NaN or below) has the lowest, one outside
-// the chosen groups -inf.
-constexpr double kMaskedKey = -3.4028234663852886e38;
+// Keys lie within 2^127: a masked expert (logit -inf or NaN, key NaN or below) has the lowest, and one
+// outside the chosen groups a lower value yet.
+constexpr double kMaskedKey = -0x1p127;
 __device__ __forceinline__ double finite_key(double key, bool masked) {
   return masked || !(key > kMaskedKey) ? kMaskedKey : fmin(key, -kMaskedKey);
 }
 
-// One wave per token, everything in 64 bits: any E, k and groups.
+template <int CTRL>
+__device__ __forceinline__ float dpp32(float f) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(f), CTRL, 0xF, 0xF, false));
+}
+constexpr int kRor8 = 0x128, kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;   // over the 16 lanes of a DPP row
+// Sums and maxima over a token's lanes: 16 (a DPP row) or 64; the same bits in every lane.
+template <int LPT>
+__device__ __forceinline__ float lanes_sum(float v) {
+  v += dpp32<kRor8>(v);
+  v += dpp32<kRor4>(v);
+  v += dpp32<kRor2>(v);
+  v += dpp32<kRor1>(v);
+  if constexpr (LPT == 64) {
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+  }
+  return v;
+}
+template <int LPT>
+__device__ __forceinline__ float lanes_max(float v) {
+  v = fmaxf(v, dpp32<kRor8>(v));
+  v = fmaxf(v, dpp32<kRor4>(v));
+  v = fmaxf(v, dpp32<kRor2>(v));
+  v = fmaxf(v, dpp32<kRor1>(v));
+  if constexpr (LPT == 64) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    v = fmaxf(v, __shfl_xor(v, 32));
+  }
+  return v;
+}
+
+// A slot's renormalized weight r_j among its token's lanes (0 without a live slot); l: its logit.
+template <int LPT>
+__device__ __forceinline__ float renormalized(bool softmax, bool slot, float l) {
+  slot = slot && l != -INFINITY;
+  float c = lanes_max<LPT>(slot ? l : -INFINITY);
+  if (!softmax) c = fminf(c, 0.f);
+  float s = 0.f;
+  if (slot) s = softmax ? expf(l - c) : l > 0.f ? 1.f / (1.f + expf(-l)) : expf(l - c) / (1.f + expf(l));
+  const float total = lanes_sum<LPT>(s);
+  return total == 0.f ? 0.f : s / total;
+}
+// Its score; m and inv: the row's largest logit and the reciprocal of its softmax sum.
+__device__ __forceinline__ float slot_score(bool softmax, bool slot, float l, float m, float inv) {
+  if (!slot || l == -INFINITY) return 0.f;
+  return softmax ? expf(l - m) * inv : 1.f / (1.f + expf(-l));
+}
+
+template <int CTRL>
+__device__ __forceinline__ double dpp64(double d) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, d);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, 0xF, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ double wave_max(double v) {
+  v = fmax(v, dpp64<kRor8>(v));
+  v = fmax(v, dpp64<kRor4>(v));
+  v = fmax(v, dpp64<kRor2>(v));
+  v = fmax(v, dpp64<kRor1>(v));
+  v = fmax(v, __shfl_xor(v, 16));
+  return fmax(v, __shfl_xor(v, 32));
+}
+template <int CTRL>
+__device__ __forceinline__ int min_dpp(int v) { return min(v, __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false)); }
+__device__ __forceinline__ int wave_min(int v) {
+  v = min_dpp<kRor1>(min_dpp<kRor2>(min_dpp<kRor4>(min_dpp<kRor8>(v))));
+  v = min(v, __shfl_xor(v, 16));
+  return min(v, __shfl_xor(v, 32));
+}
+
+// One token by a whole wave, keys in 64 bits: any E, k and groups. key: E doubles of LDS, this wave's
+// own. A reduction is a maximum, then the lowest index that has it.
 template <typename LT>
-__global__ __launch_bounds__(256) void gate_wave_kernel(GateArgs g) {
-  extern __shared__ double gate_keys[];   // [4][E]
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t t = block_number() * 4 + w;
-  if (t >= g.T) return;                   // whole waves; there is no barrier below
-  double* const key = gate_keys + w * g.E;
+__device__ void gate_token(const GateArgs& g, int64_t t, double* key) {
+  const int lane = threadIdx.x & 63;
   const char* const row = logit_row<LT>(g.logits, g.ld, t);
   const int E = g.E;
+  const bool softmax = g.score == XS_SCORE_SOFTMAX;
   float m = -INFINITY;
   double sum = 0.;
-  if (g.score == XS_SCORE_SOFTMAX) {
+  if (softmax) {
     for (int e = lane; e < E; e += 64) m = fmaxf(m, load_logit<LT>(row, e));
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+    m = lanes_max<64>(m);
     for (int e = lane; e < E; e += 64) {
       const float l = load_logit<LT>(row, e);
       if (l != -INFINITY) sum += exp(static_cast<double>(l) - static_cast<double>(m));
@@ -66,55 +141,39 @@ __global__ __launch_bounds__(256) void gate_wave_kernel(GateArgs g) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
   }
-  const auto score = [&](float l) -> double {
-    if (l == -INFINITY) return 0.;
-    if (g.score == XS_SCORE_SIGMOID) return 1. / (1. + exp(-static_cast<double>(l)));
-    return exp(static_cast<double>(l) - static_cast<double>(m)) / sum;
-  };
   // without a bias the logits have the scores' order, and no rounding
   const bool by_logit = !g.bias && (g.n_group == 1 || !g.top2);
   for (int e = lane; e < E; e += 64) {
     const float l = load_logit<LT>(row, e);
-    double v = by_logit ? static_cast<double>(l) : score(l);
+    const bool masked = l == -INFINITY || l != l;
+    double v = static_cast<double>(l);
+    if (!by_logit && !masked) v = softmax ? exp(v - static_cast<double>(m)) / sum : 1. / (1. + exp(-v));
     if (g.bias) v += static_cast<double>(g.bias[e]);
-    key[e] = finite_key(v, l == -INFINITY || l != l);
+    key[e] = finite_key(v, masked);
   }
   __builtin_amdgcn_wave_barrier();
-  const auto best = [&](double& bv, int& bi) {   // over the wave; ties to the lower index
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-      const double ov = __shfl_xor(bv, off);
-      const int oi = __shfl_xor(bi, off);
-      if (ov > bv || (ov == bv && oi < bi)) {
-        bv = ov;
-        bi = oi;
-      }
-    }
-  };
-  const int Eg = E / g.n_group;
   if (g.n_group > 1) {
-    // lane = group: its two largest keys
-    double gs = -INFINITY;
-    if (lane < g.n_group) {
-      double a = -INFINITY, b = -INFINITY;
-      for (int i = 0; i < Eg; ++i) {
-        const double v = key[lane * Eg + i];
-        if (v > a) {
-          b = a;
-          a = v;
-        } else if (v > b) {
-          b = v;
-        }
+    // lanes 2^s per group: its two largest keys; then group = lane
+    const int Eg = E / g.n_group, lanes = 64 >> (32 - __builtin_clz(g.n_group - 1));
+    const int grp = lane / lanes;
+    double a = -INFINITY, b = -INFINITY;
+    if (grp < g.n_group)
+      for (int i = lane % lanes; i < Eg; i += lanes) {
+        const double v = key[grp * Eg + i];
+        b = fmax(b, fmin(a, v));
+        a = fmax(a, v);
       }
-      gs = g.top2 && b > kMaskedKey ? a + b : a;
+    for (int off = 1; off < lanes; off <<= 1) {
+      const double oa = __shfl_xor(a, off), ob = __shfl_xor(b, off);
+      b = fmax(fmin(a, oa), fmax(b, ob));
+      a = fmax(a, oa);
     }
+    double left = __shfl(g.top2 && b > kMaskedKey ? a + b : a, (lane * lanes) & 63);
+    if (lane >= g.n_group) left = -INFINITY;
     bool kept = false;
-    double left = gs;
     for (int j = 0; j < g.topk_group; ++j) {
-      double bv = left;
-      int bi = lane < g.n_group && !kept ? lane : 64 + lane;
-      best(bv, bi);
-      if (bi == lane) {
+      const double most = wave_max(left);
+      if (wave_min(left == most ? lane : 64) == lane) {
         kept = true;
         left = -INFINITY;
       }
@@ -122,13 +181,12 @@ __global__ __launch_bounds__(256) void gate_wave_kernel(GateArgs g) {
     const unsigned long long keep = __ballot(kept);
     for (int e = lane; e < E; e += 64)
       if (!((keep >> (e / Eg)) & 1ull)) key[e] = -INFINITY;
+    __builtin_amdgcn_wave_barrier();
   }
-  __builtin_amdgcn_wave_barrier();
   int my_idx = 0;
-  double my_s = 0.;
   for (int j = 0; j < g.k; ++j) {
     double bv = -INFINITY;
-    int bi = 0x7fffffff;
+    int bi = E;
     for (int e = lane; e < E; e += 64) {
       const double v = key[e];
       if (v > bv) {
@@ -136,22 +194,267 @@ __global__ __launch_bounds__(256) void gate_wave_kernel(GateArgs g) {
         bi = e;
       }
     }
-    best(bv, bi);
+    bi = wave_min(bv == wave_max(bv) ? bi : E);
     if ((bi & 63) == lane) key[bi] = -INFINITY;
-    if (lane == j) {
-      my_idx = bi;
-      my_s = score(load_logit<LT>(row, bi));
+    if (lane == j) my_idx = bi;
+  }
+  const bool slot = lane < g.k;
+  const float l = slot ? load_logit<LT>(row, my_idx) : 0.f;
+  const float s = g.renorm ? renormalized<64>(softmax, slot, l) : slot_score(softmax, slot, l, m, static_cast<float>(1. / sum));
+  if (slot) {
+    g.idx[t * g.k + lane] = my_idx;
+    g.w[t * g.k + lane] = s * g.scale;
+  }
+}
+
+template <typename LT>
+__global__ __launch_bounds__(256) void gate_wave_kernel(GateArgs g) {
+  extern __shared__ double gate_keys[];   // [4][E]
+  const int w = threadIdx.x >> 6;
+  const int64_t t = block_number() * 4 + w;
+  if (t < g.T) gate_token<LT>(g, t, gate_keys + w * g.E);   // whole waves, no barrier
+}
+
+// ------------------------------------------------------------------------------ sixteen lanes a token
+// A key, cut to 14 bits of mantissa, and its expert in an integer: larger is earlier (a larger cut key or,
+// of equal ones, the lower index; E <= 512).
+__device__ __forceinline__ int pack_key(float key, int e) {
+  const int u = __float_as_int(key);
+  return ((u ^ ((u >> 31) & 0x7FFFFFFF)) & ~511) | (511 - e);
+}
+__device__ __forceinline__ int key_expert(int p) { return 511 - (p & 511); }
+constexpr int kNoKey = -0x7FFFFFFF - 1;
+
+__device__ __forceinline__ void order(int& a, int& b) {   // the larger first
+  const int hi = max(a, b), lo = min(a, b);
+  a = hi;
+  b = lo;
+}
+// A list whose halves' maxima are placed (a bitonic sequence) into descending order.
+template <int N>
+__device__ __forceinline__ void order_bitonic(int (&v)[N]) {
+#pragma unroll
+  for (int d = N / 2; d >= 1; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (!(i & d)) order(v[i], v[i + d]);
+}
+// Descending order of any list (Batcher's odd-even merge sort).
+template <int N>
+__device__ __forceinline__ void order_all(int (&v)[N]) {
+#pragma unroll
+  for (int p = 1; p < N; p <<= 1)
+#pragma unroll
+    for (int k = p; k >= 1; k >>= 1)
+#pragma unroll
+      for (int j = k % p; j + k < N; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) order(v[i + j], v[i + j + k]);
+}
+// The N largest of two descending lists, in descending order.
+template <int N>
+__device__ __forceinline__ void keep_largest(int (&v)[N], const int (&o)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = max(v[i], o[N - 1 - i]);
+  order_bitonic(v);
+}
+template <int CTRL, int N>
+__device__ __forceinline__ void merge_lanes(int (&v)[N]) {
+  int o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = __builtin_amdgcn_update_dpp(0, v[i], CTRL, 0xF, 0xF, false);
+  keep_largest(v, o);
+}
+
+// VP consecutive values of T from p: in pieces of 16 bytes where `vec`.
+template <int VPL, typename LT>
+__device__ __forceinline__ void load_run(const void* base, int first, int VP, int E, bool vec, float other, float (&v)[VPL]) {
+  constexpr int kPiece = sizeof(LT) == 2 && VPL >= 8 ? 8 : 4;
+  if (vec) {
+    const char* const p = static_cast<const char*>(base) + static_cast<int64_t>(first) * static_cast<int64_t>(sizeof(LT));
+#pragma unroll
+    for (int i = 0; i < VPL; i += kPiece) {
+#pragma unroll
+      for (int c = 0; c < kPiece; ++c) v[i + c] = other;
+      if (i < VP && first + i < E) {
+        if constexpr (sizeof(LT) == 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(p + i * 4);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[i + c] = x[c];
+        } else if constexpr (kPiece == 8) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(p + i * 2);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[i + 2 * c] = bf_lo(x[c]), v[i + 2 * c + 1] = bf_hi(x[c]);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(p + i * 2);
+          v[i] = bf_lo(x.x), v[i + 1] = bf_hi(x.x), v[i + 2] = bf_lo(x.y), v[i + 3] = bf_hi(x.y);
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) v[i] = i < VP && first + i < E ? load_logit<LT>(base, first + i) : other;
+  }
+}
+
+// Sixteen lanes per token, four tokens per wave; lane `sub` has the VP = ceil(E / 16) consecutive experts
+// from VP sub on, so a group is whole lanes (E % 16 == 0 where there are groups, of 1, 2, 4 or 8 lanes).
+//
+// The k largest keys are found by a sorting network on 32-bit words, each a key cut to 14 bits with its
+// expert; then every lane looks up one of them whole, and the order is decided again where neighbours lie
+// close. That order is the 64-bit one: with s off by at most sigma (below) and a key by sigma + 2^-24 |key|,
+// two keys further apart than twice that are in the right order. If every neighbouring pair of the k
+// is, and no other key comes as near to the last, and the groups' scores where they decide are as far
+// apart, the selection is the 64-bit one. A token where that fails (about one in two hundred for 256
+// sigmoid scores, by the cut keys at the k-th) is done again in 64 bits by its wave. Without a bias the
+// logits are the keys, exactly (bf16 ones also when cut).
+//   sigmoid: exp(-l) is off by 2^-23 and, from its argument, |l| 2^-23; times s (1 - s), with s (1 - s) |l|
+//     <= 0.224; the sum and the reciprocal 2^-24 + 2^-23 of s: together below 2^-22 (s <= 1).
+//   softmax: e^-d is off by d 2^-22 + 2^-23 (d e^-d <= 0.37), the sum of up to 512 terms (32 in a
+//     lane, four levels) by 2^-19 of itself at most: below 2^-18 of the largest score.
+template <typename LT, int VPL, int KL>
+__global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int vec) {
+  extern __shared__ double gate_keys[];   // [4][E], for tokens done again
+  const int sub = threadIdx.x & 15, w = threadIdx.x >> 6;
+  const int64_t t_raw = block_number() * 16 + (threadIdx.x >> 4);
+  const bool live = t_raw < g.T;
+  const int64_t t = live ? t_raw : g.T - 1;   // every lane takes part in its row's reductions
+  const char* const row = logit_row<LT>(g.logits, g.ld, t);
+  const int first = VP * sub;
+  const bool softmax = g.score == XS_SCORE_SOFTMAX;
+  const bool by_logit = !g.bias && (g.n_group == 1 || !g.top2);
+  constexpr float kMasked = static_cast<float>(kMaskedKey), kDropped = 1.5f * kMasked;
+  float v[VPL];
+  load_run<VPL, LT>(row, first, VP, g.E, vec, -INFINITY, v);
+  float m = 0.f, inv = 1.f, sigma = 0x1p-22f;
+  if (softmax) {
+    m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) m = fmaxf(m, v[i]);
+    m = lanes_max<16>(m);
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) s += v[i] == -INFINITY ? 0.f : __expf(v[i] - m);
+    inv = 1.f / lanes_sum<16>(s);
+    sigma = 0x1p-18f * inv;
+  }
+  // the key of a logit: clamped, and the lowest for NaN (med3 takes the lower bound) and masked ones
+  const auto key_of = [&](float l, float b) {
+    float s = l;
+    if (!by_logit) s = (softmax ? __expf(l - m) * inv : __builtin_amdgcn_rcpf(1.f + __expf(-l))) + b;
+    s = __builtin_amdgcn_fmed3f(s, kMasked, -kMasked);
+    return l == -INFINITY ? kMasked : s;
+  };
+  {
+    float b[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) b[i] = 0.f;
+    if (g.bias) load_run<VPL, float>(g.bias, first, VP, g.E, vec && (reinterpret_cast<uintptr_t>(g.bias) & 15) == 0, 0.f, b);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) v[i] = key_of(v[i], b[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < VPL; ++i)
+    if (i >= VP || first + i >= g.E) v[i] = kDropped;
+  bool unsure = false;
+  if (g.n_group > 1) {
+    const int lanes = 16 / g.n_group;
+    float a = -INFINITY, b = -INFINITY;     // the group's two largest keys
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      b = fmaxf(b, fminf(a, v[i]));
+      a = fmaxf(a, v[i]);
+    }
+    for (int off = 1; off < lanes; off <<= 1) {
+      const float oa = __shfl_xor(a, off), ob = __shfl_xor(b, off);
+      b = fmaxf(fminf(a, oa), fmaxf(b, ob));
+      a = fmaxf(a, oa);
+    }
+    const float gs = g.top2 && b > kMasked ? a + b : a;
+    // off by both keys' errors and the sum's rounding, on both sides
+    const float tol = by_logit ? 0.f : 4.f * sigma + 0x1p-21f * (fabsf(a) + (b > kMasked ? fabsf(b) : 0.f));
+    int above = 0, near = 0;                // groups surely before this one, groups that may be
+    for (int r = lanes; r < 16; r += lanes) {
+      const int os = (sub + r) & 15;
+      const float o = __shfl(gs, os, 16), ot = __shfl(tol, os, 16);
+      const float far = fmaxf(tol, ot);
+      if (by_logit) {
+        const bool before = o > gs || (o == gs && os / lanes < sub / lanes);
+        above += before;
+        near += before;
+      } else {
+        above += o - gs > far;
+        near += !(gs - o > far);
+      }
+    }
+    unsure = above < g.topk_group && near >= g.topk_group;
+    if (near >= g.topk_group) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) v[i] = kDropped;
     }
   }
-  if (g.renorm) {
-    double total = lane < g.k ? my_s : 0.;
+  // the KL largest of a lane's keys, then of the sixteen lanes'
+  int top[KL];
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
-    my_s = total == 0. ? 0. : my_s / total;
+  for (int i = 0; i < KL; ++i) top[i] = i < VPL ? pack_key(v[i < VPL ? i : 0], first + i) : kNoKey;
+  order_all(top);
+#pragma unroll
+  for (int c = KL; c < VPL; c += KL) {
+    int more[KL];
+#pragma unroll
+    for (int i = 0; i < KL; ++i) more[i] = c + i < VPL ? pack_key(v[c + i < VPL ? c + i : 0], first + c + i) : kNoKey;
+    order_all(more);
+    keep_largest(top, more);
   }
-  if (lane < g.k) {
-    g.idx[t * g.k + lane] = my_idx;
-    g.w[t * g.k + lane] = static_cast<float>(my_s * g.scale);
+  merge_lanes<kRor8>(top);
+  merge_lanes<kRor4>(top);
+  merge_lanes<kRor2>(top);
+  merge_lanes<kRor1>(top);
+  int mine = top[0];                        // lane j has the j-th
+#pragma unroll
+  for (int i = 1; i < KL; ++i) mine = sub == i ? top[i] : mine;
+  const bool slot = sub < g.k;
+  const int e = slot ? key_expert(mine) : 512 + sub;
+  const float l = slot ? load_logit<LT>(row, e) : -INFINITY;
+  const float key = slot ? key_of(l, g.bias ? g.bias[e] : 0.f) : kDropped;
+  const float largest = lanes_max<16>(key);
+  const float last = -lanes_max<16>(slot ? -key : -INFINITY);
+  const float tol = by_logit ? 0.f : 2.f * sigma + 0x1p-22f * fmaxf(fabsf(largest), last > kMasked ? fabsf(last) : 0.f);
+  // masked keys are equal without doubt, and a masked last one means that nothing else is left
+  const auto before = [&](float a, int ea, float b, int eb) { return a > b || (a == b && ea < eb); };
+  int rank = sub;
+  {
+    const float next = __shfl(key, (sub + 1) & 15, 16);
+    const int en = __shfl(e, (sub + 1) & 15, 16);
+    const bool clear = tol == 0.f || next == kMasked ? before(key, e, next, en) : key - next > tol;
+    if (__ballot(sub + 1 < g.k && !clear)) {
+      rank = 0;
+      for (int r = 1; r < 16; ++r) {
+        const float o = __shfl(key, (sub + r) & 15, 16);
+        const int eo = __shfl(e, (sub + r) & 15, 16);
+        rank += before(o, eo, key, e);
+        if (tol != 0.f && key > kMasked && slot) unsure |= fabsf(o - key) <= tol;
+      }
+    }
+  }
+  if (!(by_logit && sizeof(LT) == 2) && last > kMasked) {
+    float n = 0.f;                          // keys that may be among the k: the k, if all is clear
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) n += v[i] >= last - tol ? 1.f : 0.f;
+    unsure |= lanes_sum<16>(n) != static_cast<float>(g.k);
+  }
+  unsure |= !(tol >= 0.f);                  // a NaN among softmax logits
+  const float s = g.renorm ? renormalized<16>(softmax, slot, l) : slot_score(softmax, slot, l, m, inv);
+  unsigned long long again = __ballot(unsure && live);
+  if (slot && live && !((again >> (threadIdx.x & 48)) & 0xFFFFull)) {
+    g.idx[t * g.k + rank] = e;
+    g.w[t * g.k + rank] = s * g.scale;
+  }
+  while (again) {
+    const int q = (__ffsll(static_cast<long long>(again)) - 1) >> 4;
+    again &= ~(0xFFFFull << (16 * q));
+    gate_token<LT>(g, block_number() * 16 + 4 * w + q, gate_keys + w * g.E);
   }
 }
 
@@ -167,23 +470,9 @@ struct GateGradArgs {
   int* status;
 };
 
-template <int LPT>
-__device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int off = LPT / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-  return v;
-}
-template <int LPT>
-__device__ __forceinline__ float lanes_max(float v) {
-#pragma unroll
-  for (int off = LPT / 2; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-  return v;
-}
-
 // LPT lanes per token; lane `sub` has the experts 4 LPT q + 4 sub + c (q < NQ, c < 4), a vector load or
-// store for each q where rows are aligned. Slot j of a token is lane j % LPT's (slots j and, with more
-// slots than lanes, none: k <= LPT). The row's logits are read for softmax only; the chosen experts'
-// are read one by one for sigmoid. Every lane adds the k slots to its own experts in ascending j, so
+// store for each q where rows are aligned. Slot j of a token is lane j's (k <= LPT). A plain softmax reads
+// the row; the others only the chosen experts' logits. Every lane adds the k slots to its own experts in ascending j, so
 // an expert that is listed twice gets both terms and the order of the sum is fixed.
 template <typename LT, int LPT, int NQ, bool VEC>
 __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs g) {
@@ -207,7 +496,8 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs g) {
   }
   float v[4 * NQ];
   float m = -INFINITY, inv = 0.f;
-  if (softmax) {
+  const bool whole = softmax && !g.renorm;
+  if (whole) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       const int e = 4 * LPT * q + 4 * sub;
@@ -242,17 +532,16 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs g) {
     s = lanes_sum<LPT>(s);
     inv = s == 0.f ? 0.f : 1.f / s;        // a row that is masked whole has no gradient
   }
-  float s_j = 0.f;
-  if (l_j != -INFINITY) s_j = softmax ? expf(l_j - m) * inv : 1.f / (1.f + expf(-l_j));
-  float ds = gj;
+  float add, shared = 0.f;                 // of the slot's expert, and of every expert of the row
   if (g.renorm) {
-    const float S = lanes_sum<LPT>(s_j);
-    const float dot = lanes_sum<LPT>(gj * s_j);
-    ds = S == 0.f ? 0.f : (gj - dot / S) / S;
+    const float r = renormalized<LPT>(softmax, e_j >= 0, l_j);
+    add = (gj - lanes_sum<LPT>(gj * r)) * r;
+    if (!softmax) add *= 1.f / (1.f + expf(l_j));
+  } else {
+    const float s_j = slot_score(softmax, e_j >= 0, l_j, m, inv);
+    if (softmax) shared = lanes_sum<LPT>(gj * s_j);
+    add = softmax ? gj : gj * s_j * (1.f - s_j);
   }
-  // softmax: the part that every expert of the row gets; the renormalized weights' is zero
-  const float shared = softmax && !g.renorm ? lanes_sum<LPT>(ds * s_j) : 0.f;
-  const float add = softmax ? ds : ds * s_j * (1.f - s_j);
   float d[4 * NQ];
 #pragma unroll
   for (int i = 0; i < 4 * NQ; ++i) d[i] = 0.f;
@@ -264,7 +553,7 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs g) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) d[4 * q + c] += e == 4 * LPT * q + 4 * sub + c ? a : 0.f;
   }
-  if (softmax) {
+  if (whole) {
 #pragma unroll
     for (int i = 0; i < 4 * NQ; ++i) d[i] = v[i] * inv * (d[i] - shared);
   }
@@ -315,6 +604,25 @@ int gate_ok(const xs_gate* g, const void* logits, int64_t ld, int32_t T) {
   return XS_OK;
 }
 
+template <typename LT, int VPL>
+void launch_rows(const GateArgs& a, size_t lds, hipStream_t st) {
+  const int VP = (a.E + 15) / 16;
+  constexpr int kPiece = sizeof(LT) == 2 && VPL >= 8 ? 8 : 4;
+  // whole pieces: of each lane's run, and (the last lane's) of the row
+  const int vec = VP % kPiece == 0 && a.E % kPiece == 0 && a.ld % kPiece == 0 && aligned_to(a.logits, kPiece * sizeof(LT));
+  const dim3 grid = xs_host::grid_of((static_cast<int64_t>(a.T) + 15) / 16);
+  if (a.k <= 8) hipLaunchKernelGGL((gate_rows_kernel<LT, VPL, 8>), grid, dim3(256), lds, st, a, VP, vec);
+  else hipLaunchKernelGGL((gate_rows_kernel<LT, VPL, 16>), grid, dim3(256), lds, st, a, VP, vec);
+}
+
+template <typename LT>
+void launch_rows(const GateArgs& a, size_t lds, hipStream_t st) {
+  if (a.E <= 64) launch_rows<LT, 4>(a, lds, st);
+  else if (a.E <= 128) launch_rows<LT, 8>(a, lds, st);
+  else if (a.E <= 256) launch_rows<LT, 16>(a, lds, st);
+  else launch_rows<LT, 32>(a, lds, st);
+}
+
 template <typename LT, int LPT, int NQ>
 void launch_grad(const GateGradArgs& a, bool vec, hipStream_t st) {
   const int per = 256 / LPT;
@@ -349,8 +657,16 @@ extern "C" int xs_route_gate(const xs_gate* g, const void* logits, int64_t ld, i
   const GateArgs a{logits, ld, g->bias, T, g->E, g->k, g->score, g->n_group, g->topk_group,
                    g->group_score == XS_GROUP_TOP2, g->renormalize != 0, g->scale, topk_idx, topk_w};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const dim3 grid = xs_host::grid_of((static_cast<int64_t>(T) + 3) / 4);
   const size_t lds = 4 * sizeof(double) * g->E;
+  // Sixteen lanes per token where each lane has at most 32 consecutive experts and groups are whole lanes;
+  // one wave per token otherwise (32,768 tokens, top-8 of 256 in groups: 28 us against 120).
+  const bool whole_lanes = a.n_group == 1 || (a.E % 16 == 0 && 16 % a.n_group == 0);
+  if (a.E <= 512 && a.k <= 16 && whole_lanes) {
+    if (g->logits_type == XS_TYPE_BF16) launch_rows<uint16_t>(a, lds, st);
+    else launch_rows<float>(a, lds, st);
+    return xs_host::launch_status();
+  }
+  const dim3 grid = xs_host::grid_of((static_cast<int64_t>(T) + 3) / 4);
   if (g->logits_type == XS_TYPE_BF16) hipLaunchKernelGGL((gate_wave_kernel<uint16_t>), grid, dim3(256), lds, st, a);
   else hipLaunchKernelGGL((gate_wave_kernel<float>), grid, dim3(256), lds, st, a);
   return xs_host::launch_status();
