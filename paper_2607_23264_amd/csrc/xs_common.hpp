@@ -84,6 +84,12 @@ __device__ __forceinline__ void load_lds16(v4i rsrc, uint32_t voff, int soff, co
                :: "v"(voff), "s"(rsrc), "s"(soff), "{m0}"(m0v) : "memory");
 }
 
+// The same with one dword per lane, into LDS at dst + 4 lane.
+__device__ __forceinline__ void load_lds4(v4i rsrc, uint32_t voff, const lds_char* dst) {
+  const uint32_t m0v = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(dst));
+  asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" :: "v"(voff), "s"(rsrc), "{m0}"(m0v) : "memory");
+}
+
 // A store past the L2 (agent scope, written through to memory): once it has completed (vmcnt), an
 // agent-scope acquire on any XCD sees it, without the release that writes back the whole L2. Not
 // counted by the compiler: the kernel waits with wait_vm. (The registers of a store of more than 64

@@ -1,5 +1,6 @@
 // GEMM and grouped GEMM on block-scaled E4M3 (xs_gemm_fp8.hpp).
 #include <algorithm>
+#include <cmath>
 
 #include "xs_gemm_fp8.hpp"
 
@@ -25,18 +26,29 @@ struct GemmArgs {
   int* status;
 };
 
-// Work index t -> (segment, row block, column tile): segments in order, within one the row blocks
-// vary fastest (neighbouring tiles share the weight's columns). Every wave scans the segments itself.
+// Work index t -> (segment, row block, column tile): segments in order; within one, groups of eight row
+// blocks, the row blocks of a group varying fastest (32 consecutive tiles, one XCD's, are then 8 x 4: twelve
+// operand panels for its L2). Every wave scans the segments itself.
 struct Where {
   int seg, m0, rows, nb;
 };
+constexpr int kGroupRows = 8;
+__device__ __forceinline__ void in_groups(int64_t t, int blocks, int nt, int* mb, int* nb) {
+  const int64_t per = static_cast<int64_t>(kGroupRows) * nt;
+  const int first = static_cast<int>(t / per) * kGroupRows, local = static_cast<int>(t % per);
+  const int gm = min(kGroupRows, blocks - first);
+  *mb = first + local % gm;
+  *nb = local / gm;
+}
 template <int BM>
 __device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, Where& at) {
   if (!p.seg_off) {
     const int blocks = (p.M + BM - 1) / BM;
-    const int mb = static_cast<int>(t % blocks);
-    at = Where{0, mb * BM, min(BM, p.M - mb * BM), static_cast<int>(t / blocks)};
-    return at.nb < nt;
+    if (t >= static_cast<int64_t>(blocks) * nt) return false;
+    int mb, nb;
+    in_groups(t, blocks, nt, &mb, &nb);
+    at = Where{0, mb * BM, min(BM, p.M - mb * BM), nb};
+    return true;
   }
   const int lane = threadIdx.x & 63;
   int64_t base = 0;
@@ -64,11 +76,12 @@ __device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, 
       const int rows = __shfl(r, l), off = __shfl(o, l);
       const int64_t local = t - (base + __shfl(incl, l) - __shfl(tiles, l));
       const int blocks = (rows + BM - 1) / BM;
-      const int mb = static_cast<int>(local % blocks);
+      int mb, nb;
+      in_groups(local, blocks, nt, &mb, &nb);
       at.seg = __builtin_amdgcn_readfirstlane(s0 + l);
       at.m0 = __builtin_amdgcn_readfirstlane(off + mb * BM);
       at.rows = __builtin_amdgcn_readfirstlane(min(BM, rows - mb * BM));
-      at.nb = __builtin_amdgcn_readfirstlane(static_cast<int>(local / blocks));
+      at.nb = __builtin_amdgcn_readfirstlane(nb);
       return true;
     }
     base += __shfl(incl, 63);
@@ -77,7 +90,7 @@ __device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, 
 }
 
 template <class T, bool ROW, bool SWIGLU, bool F32>
-__global__ __launch_bounds__(T::kThreads) void gemm_kernel(GemmArgs p) {
+__global__ __launch_bounds__(T::kThreads, 2) void gemm_kernel(GemmArgs p) {
   __shared__ __attribute__((aligned(16))) char lds[T::kLds];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = w / T::kWN, wn = w % T::kWN;
@@ -85,7 +98,9 @@ __global__ __launch_bounds__(T::kThreads) void gemm_kernel(GemmArgs p) {
   const int n_out = SWIGLU ? p.N / 2 : p.N;
   const int nt = (n_out + kCols - 1) / kCols;
   Where at;
-  for (int64_t t = blockIdx.x; find_tile<T::kBM>(p, t, nt, at); t += gridDim.x) {
+  // consecutive workgroups go to different XCDs: each XCD takes a run of consecutive tiles
+  const int G = gridDim.x, b = blockIdx.x;
+  for (int64_t t = G % 8 ? b : (b % 8) * (G / 8) + b / 8; find_tile<T::kBM>(p, t, nt, at); t += G) {
     const int n0 = at.nb * kCols;
     const Product q{p.a + at.m0 * p.lda, p.lda, p.a_s + at.m0 * p.lda_s, p.lda_s, at.rows,
                     p.b + at.seg * p.b_seg, p.ldb, p.b_s + at.seg * p.b_s_seg, p.ldb_s, n0, p.N, p.N / 2, p.K};
@@ -139,6 +154,154 @@ __global__ __launch_bounds__(T::kThreads) void gemm_kernel(GemmArgs p) {
   }
 }
 
+// Products with few output tiles: a workgroup takes 16 NB rows and 16 NJ columns and splits the K blocks
+// over its four waves, whose scaled fp32 sums meet in LDS once and are added in wave order. Each wave
+// stages its own blocks (one 128-byte line of every row, and the rows' scales) kDepth deep in a slice of
+// LDS of its own, by direct loads, and needs no barrier until the end. SWIGLU: columns y < NJ / 2 are the
+// gate's, the others the same columns of up.
+constexpr uint32_t kNone = 1u << 30;   // an offset past every buffer (the host sees to that); twice it does not wrap
+template <int NB, int NJ, int kDepth, bool ROW, bool SWIGLU, bool F32>
+__global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
+  constexpr int kWaves = 4, kRows = 16 * NB, kCols = 16 * NJ, kPitch = kCols + 4;
+  constexpr int kPiece = (kRows + kCols) * 128 + 512;      // B rows, A rows, 64 scales of A, 64 of B
+  constexpr int kLoads = 2 * (NB + NJ) + 2;
+  constexpr int kStage = kWaves * kDepth * kPiece, kRed = kWaves * kRows * kPitch * 4;
+  constexpr int kHalf = SWIGLU ? kCols / 2 : kCols;        // output columns of the workgroup
+  __shared__ __attribute__((aligned(16))) char smem[kStage > kRed ? kStage : kRed];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.x * kHalf, n_out = SWIGLU ? p.N / 2 : p.N;
+  Where at;
+  if (!find_tile<kRows>(p, blockIdx.y, 1, at)) return;     // the whole workgroup
+  const int rows = at.rows, cols = min(kHalf, n_out - n0);
+  lds_char* const lds = (lds_char*)smem + w * kDepth * kPiece;
+  const uint8_t* const b = p.b + at.seg * p.b_seg;
+  const float* const b_s = p.b_s + at.seg * p.b_s_seg;
+  const int nk = p.K / 128;
+  const auto span = [&](int64_t rows_, int64_t ld, int64_t last) { return static_cast<uint32_t>((rows_ - 1) * ld + last); };
+  const v4i ra = buffer_rsrc(p.a + at.m0 * p.lda, span(rows, p.lda, p.K));
+  const v4i rb = buffer_rsrc(b + n0 * p.ldb, span(cols, p.ldb, p.K));
+  const v4i rb2 = buffer_rsrc(b + (n0 + (SWIGLU ? n_out : 0)) * p.ldb, span(cols, p.ldb, p.K));
+  const v4i rsa = buffer_rsrc(p.a_s + at.m0 * p.lda_s, span(rows, p.lda_s * 4, nk * 4));
+  // scales of B: one per column, or of the workgroup's 128 x 128 block (and of up's)
+  const int sb_rows = ROW ? cols : 1;
+  const v4i rsb = buffer_rsrc(b_s + (ROW ? n0 : n0 / 128) * p.ldb_s,
+                              span(SWIGLU ? n_out / 128 + 1 : sb_rows, p.ldb_s * 4, nk * 4));
+  // load n of an operand fills its rows 8 n .. + 7 of a piece; past the buffers' ends nothing is fetched
+  uint32_t oa[2 * NB], ob[2 * NJ];
+  const int lr = lane >> 3, lp = lane & 7;
+#pragma unroll
+  for (int n = 0; n < 2 * NB; ++n) oa[n] = static_cast<uint32_t>((8 * n + lr) * p.lda + ((lp ^ ((4 * n + (lr >> 1)) & 7)) << 4));
+#pragma unroll
+  for (int n = 0; n < 2 * NJ; ++n) {
+    const int r = SWIGLU && n >= NJ ? 8 * (n - NJ) : 8 * n;
+    ob[n] = static_cast<uint32_t>((r + lr) * p.ldb + ((lp ^ ((4 * n + (lr >> 1)) & 7)) << 4));
+  }
+  const uint32_t osa = lane < kRows ? static_cast<uint32_t>(lane * p.lda_s * 4) : kNone;
+  uint32_t osb = kNone;
+  if (ROW ? lane < kCols : lane < (SWIGLU ? 2 : 1)) osb = static_cast<uint32_t>((SWIGLU ? lane * (n_out / 128) : lane) * p.ldb_s * 4);
+  const int k0 = nk * w / kWaves, k1 = nk * (w + 1) / kWaves;   // this wave's blocks
+  f32x4 acc[NB][NJ];
+#pragma unroll
+  for (int x = 0; x < NB; ++x)
+#pragma unroll
+    for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // block k into slot s; past the wave's range every lane points past the buffers, so the number of loads
+  // in flight stays the same
+  const auto load = [&](int s, int k) {
+    const uint32_t kb = k < k1 ? static_cast<uint32_t>(k) * 128u : kNone, ks = k < k1 ? static_cast<uint32_t>(k) * 4u : kNone;
+    lds_char* const at_ = lds + s * kPiece;
+#pragma unroll
+    for (int n = 0; n < 2 * NJ; ++n) load_lds16(SWIGLU && n >= NJ ? rb2 : rb, ob[n] + kb, at_ + n * 1024);
+#pragma unroll
+    for (int n = 0; n < 2 * NB; ++n) load_lds16(ra, oa[n] + kb, at_ + kCols * 128 + n * 1024);
+    load_lds4(rsa, osa + ks, at_ + (kRows + kCols) * 128);
+    load_lds4(rsb, osb + ks, at_ + (kRows + kCols) * 128 + 256);
+  };
+  const int swz = (i >> 1) & 7;
+  typedef __attribute__((address_space(3))) v4i_ lds_v4i;
+  typedef __attribute__((address_space(3))) float lds_float;
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+  const auto frag = [&](const lds_char* row) {
+    const v4i_ lo = *(const lds_v4i*)(row + ((g ^ swz) << 4)), hi = *(const lds_v4i*)(row + (((g + 4) ^ swz) << 4));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+#pragma unroll
+  for (int s = 0; s < kDepth; ++s) load(s, k0 + s);
+  for (int k = k0; k < k1; k += kDepth) {
+#pragma unroll
+    for (int s = 0; s < kDepth; ++s) {
+      if (k + s >= k1) break;
+      wait_vm<(kDepth - 1) * kLoads>();                    // block k + s has landed
+      const lds_char* const at_ = lds + s * kPiece;
+      const lds_char* const sc = at_ + (kRows + kCols) * 128;
+      v8i bc[NJ], ac[NB];
+      float sa[NB];
+      f32x4 sb[ROW ? NJ : 1];
+#pragma unroll
+      for (int y = 0; y < NJ; ++y) bc[y] = frag(at_ + (16 * y + i) * 128);
+#pragma unroll
+      for (int x = 0; x < NB; ++x) {
+        ac[x] = frag(at_ + (kCols + 16 * x + i) * 128);
+        sa[x] = *(const lds_float*)(sc + (16 * x + i) * 4);
+      }
+      if constexpr (ROW) {
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) sb[y] = *(const lds_f32x4*)(sc + 256 + (16 * y + 4 * g) * 4);
+      } else {
+        sb[0][0] = *(const lds_float*)(sc + 256);
+        sb[0][1] = SWIGLU ? *(const lds_float*)(sc + 260) : 0.f;
+      }
+      __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the slot has been read
+      asm volatile("" ::: "memory");
+      load(s, k + s + kDepth);
+      std::conditional_t<F32, Wide, v8i> bf[NJ], af;
+#pragma unroll
+      for (int y = 0; y < NJ; ++y) as_operand(bc[y], bf[y]);
+#pragma unroll
+      for (int x = 0; x < NB; ++x) {
+        as_operand(ac[x], af);
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) {
+          const f32x4 v = block_sum(bf[y], af);
+          const float f = ROW ? sa[x] : sa[x] * sb[0][SWIGLU && y >= NJ / 2 ? 1 : 0];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[x][y][c] = __builtin_fmaf(ROW ? v[c] * sb[y][c] : v[c], f, acc[x][y][c]);
+        }
+      }
+    }
+  }
+  wait_vm<0>();
+  __syncthreads();                                         // no load is in flight: the LDS is free
+  float* const red = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int x = 0; x < NB; ++x)
+#pragma unroll
+    for (int y = 0; y < NJ; ++y)
+      *reinterpret_cast<f32x4*>(red + (w * kRows + 16 * x + i) * kPitch + 16 * y + 4 * g) = acc[x][y];
+  __syncthreads();
+  const auto sum = [&](int r, int c) {
+    f32x4 v = *reinterpret_cast<const f32x4*>(red + r * kPitch + c);
+#pragma unroll
+    for (int x = 1; x < kWaves; ++x) v += *reinterpret_cast<const f32x4*>(red + (x * kRows + r) * kPitch + c);
+    return v;
+  };
+  for (int u = tid; u < rows * (kHalf / 4); u += 256) {
+    const int r = u / (kHalf / 4), c = 4 * (u % (kHalf / 4));
+    if (n0 + c >= n_out) continue;
+    f32x4 v = sum(r, c);
+    if constexpr (SWIGLU) {
+      const f32x4 up = sum(r, c + kHalf);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = v[q] * __builtin_amdgcn_rcpf(1.f + __expf(-v[q])) * up[q];
+    }
+    const int64_t to = (at.m0 + r) * p.ldc + n0 + c;
+    if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.c) + to) = v;
+    else *reinterpret_cast<uint2*>(p.c + to * 2) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
+}
+
 }  // namespace f8
 }  // namespace xs
 
@@ -152,20 +315,95 @@ namespace {
 
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+typedef f8::Tile<256, 256, 2, 4> Big;
 typedef f8::Tile<128, 128, 2, 2> Mid;
 
+template <int NB, int NJ, int kDepth, bool ROW, bool SWIGLU, bool F32>
+int launch_split(const f8::GemmArgs& p, hipStream_t st) {
+  const int cols = SWIGLU ? 8 * NJ : 16 * NJ, n_out = SWIGLU ? p.N / 2 : p.N;
+  const int64_t blocks = (static_cast<int64_t>(p.M) + 16 * NB - 1) / (16 * NB) + (p.seg_off ? p.n_seg : 0);
+  hipLaunchKernelGGL((f8::split_kernel<NB, NJ, kDepth, ROW, SWIGLU, F32>),
+                     dim3((n_out + cols - 1) / cols, static_cast<unsigned>(blocks)), dim3(256), 0, st, p);
+  return xs_host::launch_status();
+}
+
 template <class T, bool ROW, bool SWIGLU, bool F32>
-int launch(const f8::GemmArgs& p, hipStream_t st) {
+int launch_tiles(const f8::GemmArgs& p, int per_cu, hipStream_t st) {
   const int cols = SWIGLU ? T::kBN / 2 : T::kBN;
   const int64_t nt = ((SWIGLU ? p.N / 2 : p.N) + cols - 1) / cols;
   const int64_t blocks = (static_cast<int64_t>(p.M) + T::kBM - 1) / T::kBM + (p.seg_off ? p.n_seg : 0);
-  const int grid = static_cast<int>(std::min<int64_t>(blocks * nt, 2 * xs_host::persistent_grid(0)));
+  const int grid = static_cast<int>(std::min<int64_t>(blocks * nt, static_cast<int64_t>(per_cu) * xs_host::persistent_grid(0)));
   hipLaunchKernelGGL((f8::gemm_kernel<T, ROW, SWIGLU, F32>), dim3(grid), dim3(T::kThreads), 0, st, p);
   return xs_host::launch_status();
 }
 
+enum Form { kSplit12, kSplit21, kSplit22, kSplit24, kSplit44, kMid, kBig };
+
+// The cheapest form by a model of its time in us, from M, N, K and the CU count (grouped: with exponential
+// segment lengths, n / (1 - exp(-rows n / M)) row blocks of n segments). A split form takes its rounds of
+// workgroups, each a start and a join that grow with its outputs, and its rows of K bytes at the rate of a
+// CU's memory path; tiles take K / 128 blocks a round, of one 256 x 256 or up to two 128 x 128 tiles a CU.
+// Weights past the caches (grouped products that touch over 100 MB) come more slowly. Measured, us, split
+// 1x2 / 2x4 / 4x4, 128- and 256-tiles, N = 4096, K = 7168: M = 24 8.4 / 12.0 / 16.8 / 37 / 71; 128 26 / 13.5 / 18.6 / 42 /
+// 71; 512 93 / 45 / 34 / 45 / 74; 2048 - / 171 / 131 / 62 / 82; 4093 - / - / - / 134 / 118. K = 512, M = 1024: - / 24 / 19 / 8.7 / 12.
+// 32 segments, K = 7168: 64 rows in all 137 / 131 / 141 / 141 / 179; 1024 342 / 211 / 197 / 160 / 196; 16,384 - / - / 1299 /
+// 763 / 556.
+Form choose(const f8::GemmArgs& p, bool swiglu, bool f32) {
+  const double cus = xs_host::persistent_grid(0), nk = p.K / 128, n_out = swiglu ? p.N / 2 : p.N;
+  const double segs = p.seg_off ? std::min(p.n_seg, p.M) : 1;
+  const auto blocks = [&](int rows) {
+    return segs > 1 ? std::ceil(segs / (1 - std::exp(-rows * segs / p.M))) : std::ceil(static_cast<double>(p.M) / rows);
+  };
+  const bool far = segs * p.N * p.K > 100e6 && p.seg_off;
+  double best = 1e300;
+  Form form = kMid;
+  const auto offer = [&](Form f, double us) {
+    if (us < best) {
+      best = us;
+      form = f;
+    }
+  };
+  // offsets of the split form's buffers stay below f8::kNone, its row blocks in a grid's second dimension
+  if ((n_out / 128 + 1) * p.ldb_s * 4 < f8::kNone) {
+    constexpr int forms[5][2] = {{1, 2}, {2, 1}, {2, 2}, {2, 4}, {4, 4}};
+    const double rate = f32 ? 55e3 : far ? 47e3 : 70e3;
+    for (int f = 0; f < 5; ++f) {
+      const int rows = 16 * forms[f][0], cols = 16 * forms[f][1];
+      if ((swiglu && f == kSplit21) || static_cast<double>(p.M) / rows + p.n_seg > 65535) continue;   // gate and up take two blocks
+      const double wgs = blocks(rows) * std::ceil(p.N / static_cast<double>(cols));
+      const double idle = (static_cast<double>(p.M) / rows + p.n_seg) * std::ceil(p.N / static_cast<double>(cols)) - wgs;
+      offer(static_cast<Form>(f), 2 + (p.seg_off ? 0.5 * std::max(0.0, idle) / cus : 0) + std::ceil(wgs / cus) * (1.45 + 5.5e-4 * rows * cols + (rows + cols) * static_cast<double>(p.K) / rate));
+    }
+  }
+  const auto tiles = [&](int bm, int bn) { return blocks(bm) * std::ceil(p.N / static_cast<double>(bn)); };
+  const double mid = tiles(128, 128), rest = std::fmod(mid, 2 * cus) / cus;
+  const double part = rest == 0 ? 0 : rest <= 1 ? 0.62 : 0.62 + 0.48 * (rest - 1);
+  offer(kMid, 6 + nk * (std::floor(mid / (2 * cus)) * 1.1 + part) * (f32 ? 1.9 : far ? 1.2 : 1));
+  if (!f32) {                                            // exact sums do not fit its registers
+    const double big = tiles(256, 256), left = std::fmod(big, cus) / cus;
+    offer(kBig, 6 + nk * (std::floor(big / cus) * 1.85 + (left == 0 ? 0 : 1.25 + 0.6 * left)));
+  }
+  return form;
+}
+
+template <bool ROW, bool SWIGLU, bool F32>
+int launch(const f8::GemmArgs& p, hipStream_t st) {
+  switch (choose(p, SWIGLU, F32)) {
+    case kSplit12: return launch_split<1, 2, 4, ROW, SWIGLU, F32>(p, st);
+    case kSplit21:
+      if constexpr (!SWIGLU) return launch_split<2, 1, 4, ROW, SWIGLU, F32>(p, st);
+    case kSplit22: return launch_split<2, 2, 3, ROW, SWIGLU, F32>(p, st);
+    case kSplit24: return launch_split<2, 4, 2, ROW, SWIGLU, F32>(p, st);
+    case kSplit44: return launch_split<4, 4, 2, ROW, SWIGLU, F32>(p, st);
+    case kMid: return launch_tiles<Mid, ROW, SWIGLU, F32>(p, 2, st);
+    case kBig:
+      if constexpr (!F32) return launch_tiles<Big, ROW, SWIGLU, F32>(p, 1, st);
+  }
+  return launch_tiles<Mid, ROW, SWIGLU, F32>(p, 2, st);
+}
+
 // Byte offsets inside a tile are 32-bit: up to 256 rows of at most 2^22 bytes.
-constexpr int64_t kMaxRow = int64_t(1) << 22;
+constexpr int64_t kMaxRow = int64_t(1) << 22, kMaxSpan = 0x7FFFFF00;
 
 int operand_ok(const void* codes, int64_t ld, const float* scales, int64_t ld_s, int32_t K) {
   if (!codes || !scales) return XS_EINVAL;
@@ -192,8 +430,8 @@ extern "C" int xs_gemm_fp8(const void* a, int64_t lda, const float* a_scales, in
                        b_scales, ldb_s, 0, static_cast<char*>(c), ldc, M, N, K, nullptr, nullptr, 1, nullptr};
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (b_block == XS_BLOCK_ROW)
-    return c_type == XS_TYPE_F32 ? launch<Mid, true, false, true>(p, st) : launch<Mid, true, false, false>(p, st);
-  return c_type == XS_TYPE_F32 ? launch<Mid, false, false, true>(p, st) : launch<Mid, false, false, false>(p, st);
+    return c_type == XS_TYPE_F32 ? launch<true, false, true>(p, st) : launch<true, false, false>(p, st);
+  return c_type == XS_TYPE_F32 ? launch<false, false, true>(p, st) : launch<false, false, false>(p, st);
 }
 
 extern "C" int xs_grouped_gemm_fp8(const void* a, int64_t lda, const float* a_scales, int64_t lda_s, int32_t M,
@@ -209,11 +447,13 @@ extern "C" int xs_grouped_gemm_fp8(const void* a, int64_t lda, const float* a_sc
   int rc = operand_ok(a, lda, a_scales, lda_s, K);
   if (!rc) rc = operand_ok(b, K, b_scales, ldb_s, K);
   if (rc) return rc;
+  // a tile's gate and up rows in one buffer range
+  if (swiglu && ((n_out + 128) * static_cast<int64_t>(K) > kMaxSpan || (n_out / 128 + 1) * ldb_s * 4 > kMaxSpan)) return XS_EUNSUPPORTED;
   if (ldc < n_out || ldc % 8 || !aligned_to(c, 16)) return XS_EINVAL;
   if (M == 0 || n_seg == 0) return XS_OK;
   const f8::GemmArgs p{static_cast<const uint8_t*>(a), lda, a_scales, lda_s, static_cast<const uint8_t*>(b), K,
                        static_cast<int64_t>(N) * K, b_scales, ldb_s, static_cast<int64_t>((N + 127) / 128) * ldb_s,
                        static_cast<char*>(c), ldc, M, N, K, seg_offsets, seg_rows, n_seg, dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  return swiglu ? launch<Mid, false, true, false>(p, st) : launch<Mid, false, false, false>(p, st);
+  return swiglu ? launch<false, true, false>(p, st) : launch<false, false, false>(p, st);
 }

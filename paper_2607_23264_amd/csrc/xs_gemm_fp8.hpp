@@ -97,52 +97,59 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w / T::kWN, wn = w % T::kWN;
   const int nk = p.K / 128;
-  const auto b_row = [&](int r) { return min(b_row_map(r, p.n0, p.half, SWIGLU), p.b_end - 1); };
+  // Buffers from the tile's first row on; rows past the valid ones are not fetched (their slots of LDS
+  // hold anything, and only outputs that are not stored come from them). Scales come four blocks at a
+  // time, 16 aligned bytes.
+  const auto span = [&](int64_t rows, int64_t ld, int64_t last) { return static_cast<uint32_t>((rows - 1) * ld + last); };
+  const int b_rows = SWIGLU ? p.half + T::kBN / 2 : min(T::kBN, p.b_end - p.n0);
+  const v4i ra = buffer_rsrc(p.a, span(p.rows, p.lda, p.K));
+  const v4i rb = buffer_rsrc(p.b + p.n0 * p.ldb, span(b_rows, p.ldb, p.K));
+  const int s_bytes = (nk + 3) / 4 * 16;
   // load i of wave w fills rows 8 (kWaves i + w) .. + 7: lane -> row lane / 8, physical piece lane % 8
   uint32_t oa[T::kALoads], ob[T::kBLoads], os[T::kSLoads];
   const int lr = lane >> 3, lp = lane & 7;
 #pragma unroll
   for (int i = 0; i < T::kALoads; ++i) {
     const int r = 8 * (T::kWaves * i + w) + lr;
-    oa[i] = static_cast<uint32_t>(min(r, p.rows - 1) * p.lda + ((lp ^ ((r >> 1) & 7)) << 4));
+    oa[i] = static_cast<uint32_t>(r * p.lda + ((lp ^ ((r >> 1) & 7)) << 4));
   }
 #pragma unroll
   for (int i = 0; i < T::kBLoads; ++i) {
     const int r = 8 * (T::kWaves * i + w) + lr;
-    ob[i] = static_cast<uint32_t>(b_row(r) * p.ldb + ((lp ^ ((r >> 1) & 7)) << 4));
+    ob[i] = static_cast<uint32_t>(b_row_map(r, 0, p.half, SWIGLU) * p.ldb + ((lp ^ ((r >> 1) & 7)) << 4));
   }
-  // scale load i of wave w: rows 64 (kWaves i + w) .. + 63 of A, then of B
-  const char* sbase[T::kSLoads];
+  // scale load i of wave w: rows 64 (kWaves i + w) .. + 63 of A, then of B (128 x 128 blocks: each row's)
+  v4i rs[T::kSLoads];
 #pragma unroll
   for (int i = 0; i < T::kSLoads; ++i) {
     const int r0 = 64 * (T::kWaves * i + w);
     if (r0 < T::kBM) {
-      sbase[i] = reinterpret_cast<const char*>(p.a_s);
-      os[i] = static_cast<uint32_t>(min(r0 + lane, p.rows - 1) * p.lda_s * 4);
+      rs[i] = buffer_rsrc(p.a_s, span(p.rows, p.lda_s * 4, s_bytes));
+      os[i] = static_cast<uint32_t>((r0 + lane) * p.lda_s * 4);
     } else {
-      const int n = b_row(r0 - T::kBM + lane);
-      sbase[i] = reinterpret_cast<const char*>(p.b_s);
-      os[i] = static_cast<uint32_t>((ROW ? n : n / 128) * p.ldb_s * 4);
+      const int first = ROW ? p.n0 : p.n0 / 128;
+      const int n = min(b_row_map(r0 - T::kBM + lane, p.n0, p.half, SWIGLU), p.b_end - 1);
+      const int last = min(p.n0 + b_rows, p.b_end) - 1;
+      rs[i] = buffer_rsrc(p.b_s + first * p.ldb_s, span((ROW ? last : last / 128) - first + 1, p.ldb_s * 4, s_bytes));
+      os[i] = static_cast<uint32_t>(((ROW ? n : n / 128) - first) * p.ldb_s * 4);
     }
   }
   char* const scales = lds + 2 * T::kStage;
+  lds_char* const to = (lds_char*)lds + w * 1024;
+  const auto issue_one = [&](int kt, int n) {
+    lds_char* const st = to + (kt & 1) * T::kStage;
+    if (n < T::kALoads) load_lds16(ra, oa[n], kt * 128, st + T::kWaves * n * 1024);
+    else load_lds16(rb, ob[n - T::kALoads], kt * 128, st + T::kBM * 128 + T::kWaves * (n - T::kALoads) * 1024);
+  };
+  constexpr int kPerStep = (T::kALoads + T::kBLoads + T::kNJ - 1) / T::kNJ;
   const auto issue = [&](int kt) {
-    char* const st = lds + (kt & 1) * T::kStage;
-    const char* const a = reinterpret_cast<const char*>(p.a) + static_cast<int64_t>(kt) * 128;
-    const char* const b = reinterpret_cast<const char*>(p.b) + static_cast<int64_t>(kt) * 128;
 #pragma unroll
-    for (int i = 0; i < T::kALoads; ++i)
-      __builtin_amdgcn_global_load_lds((glob_void*)(a + oa[i]), (lds_void*)(st + (T::kWaves * i + w) * 1024), 16, 0, 0);
-#pragma unroll
-    for (int i = 0; i < T::kBLoads; ++i)
-      __builtin_amdgcn_global_load_lds((glob_void*)(b + ob[i]),
-                                       (lds_void*)(st + T::kBM * 128 + (T::kWaves * i + w) * 1024), 16, 0, 0);
+    for (int n = 0; n < T::kALoads + T::kBLoads; ++n) issue_one(kt, n);
   };
   const auto issue_scales = [&](int g) {
 #pragma unroll
     for (int i = 0; i < T::kSLoads; ++i)
-      __builtin_amdgcn_global_load_lds((glob_void*)(sbase[i] + static_cast<int64_t>(g) * 16 + os[i]),
-                                       (lds_void*)(scales + (g & 1) * T::kScales + (T::kWaves * i + w) * 1024), 16, 0, 0);
+      load_lds16(rs[i], os[i], g * 16, to + 2 * T::kStage + (g & 1) * T::kScales + T::kWaves * i * 1024);
   };
   const int l16 = lane & 15, g4 = lane >> 4, swz = (l16 >> 1) & 7;
   const int ar = wm * T::kMI * 16 + l16, br = wn * T::kNJ * 16 + l16;
@@ -151,50 +158,126 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
     const v4i_ hi = *reinterpret_cast<const v4i_*>(rows + r * 128 + (((g4 + 4) ^ swz) << 4));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
+  constexpr int kMI = T::kMI, kNJ = T::kNJ, kF = SWIGLU ? 2 : 1;
+  static_assert(kMI % 2 == 0, "row blocks alternate between two fragment and two sum buffers");
 #pragma unroll
-  for (int i = 0; i < T::kMI; ++i)
+  for (int i = 0; i < kMI; ++i)
 #pragma unroll
-    for (int j = 0; j < T::kNJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < kNJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  std::conditional_t<EXACT, Wide, v8i> bf[kNJ], af[2];
+  float sa[kMI], sb[kF], f[2][kF];          // f: the factor of the row block whose sums are in v[same]
+  f32x4 sbr[ROW ? kNJ : 1], v[2][kNJ];
+  const auto read_b = [&](const char* st, int j) { as_operand(frag(st + T::kBM * 128, br + 16 * j), bf[j]); };
+  const auto read_a = [&](const char* st, int i) { as_operand(frag(st, ar + 16 * i), af[i & 1]); };
+  const auto read_scales = [&](int kt) {
+    const char* const sc = scales + ((kt >> 2) & 1) * T::kScales + (kt & 3) * 4;
+#pragma unroll
+    for (int i = 0; i < kMI; ++i) sa[i] = *reinterpret_cast<const float*>(sc + (ar + 16 * i) * 16);
+    if constexpr (ROW) {
+#pragma unroll
+      for (int j = 0; j < kNJ; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          sbr[j][c] = *reinterpret_cast<const float*>(sc + (T::kBM + wn * kNJ * 16 + 16 * j + 4 * g4 + c) * 16);
+    } else {
+#pragma unroll
+      for (int h = 0; h < kF; ++h) sb[h] = *reinterpret_cast<const float*>(sc + (T::kBM + wn * kNJ * 16 + 32 * h) * 16);
+    }
+  };
+  // sums of row block i, column block j into the accumulators
+  const auto add = [&](int i, int j) {
+    const float s = f[i & 1][SWIGLU ? (j >> 1) & 1 : 0];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[i][j][c] = __builtin_fmaf(v[i & 1][j][c], s, acc[i][j][c]);
+  };
+  // One K block. Row block i's MFMAs are each followed by the multiply-adds of row block i - 1's sums (the
+  // last one's in the next stage), and by reads or loads that run ahead: the next row block's fragment;
+  // in the last row block, behind the barrier, the next stage's weight fragments, each into the registers
+  // that the MFMA before it has read, its scales, and the loads of the stage after next, into this stage's
+  // buffers, which every wave has read.
+  const auto stage = [&](int kt, auto next_c, auto issue_c) {
+    constexpr bool kNext = decltype(next_c)::value, kIssue = decltype(issue_c)::value;
+    const char* const st = lds + (kt & 1) * T::kStage;
+    const char* const nx = lds + ((kt + 1) & 1) * T::kStage;
+    // (a branch further down would let the compiler sink the multiply-adds behind it, all sums live)
+    if constexpr (kIssue)
+      if (((kt + 2) & 3) == 0) issue_scales((kt + 2) >> 2);
+#pragma unroll
+    for (int i = 0; i < kMI; ++i) {
+      const int pi = (i + kMI - 1) % kMI;
+      __builtin_amdgcn_sched_barrier(0);
+      if (i == kMI - 1 && kNext) {
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): the next stage has landed, this one is read
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      float cur[kF];
+#pragma unroll
+      for (int h = 0; h < kF; ++h) cur[h] = ROW ? sa[i] : sa[i] * sb[h];
+#pragma unroll
+      for (int j = 0; j < kNJ; ++j) {
+        v[i & 1][j] = block_sum(bf[j], af[i & 1]);
+        if (ROW && i > 0) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[pi & 1][j][c] *= sbr[ROW ? j : 0][c];
+        }
+        add(pi, j);
+        if (i < kMI - 1) {
+          if (j == 0) read_a(st, i + 1);
+        } else {
+          if constexpr (kNext) {
+            if (j == 0) read_a(nx, 0);
+            if constexpr (!ROW) read_b(nx, j);
+          }
+          if constexpr (kIssue) {
+#pragma unroll
+            for (int n = 0; n < kPerStep; ++n)
+              if (j * kPerStep + n < T::kALoads + T::kBLoads) issue_one(kt + 2, j * kPerStep + n);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int h = 0; h < kF; ++h) f[i & 1][h] = cur[h];
+      if (i == kMI - 1) {
+        if constexpr (ROW) {
+          // its column scales are the next stage's from here on: this stage's last sums take theirs now
+#pragma unroll
+          for (int j = 0; j < kNJ; ++j) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[i & 1][j][c] *= sbr[j][c];
+            if constexpr (kNext) read_b(nx, j);
+          }
+        }
+        if constexpr (kNext) read_scales(kt + 1);
+      }
+    }
+  };
   issue(0);
   issue_scales(0);
   wait_vm0();
   __builtin_amdgcn_s_barrier();
-  for (int kt = 0; kt < nk; ++kt) {
-    if (kt + 1 < nk) issue(kt + 1);
-    if ((kt & 3) == 0 && kt + 4 < nk) issue_scales((kt >> 2) + 1);
-    const char* const st = lds + (kt & 1) * T::kStage;
-    const char* const sc = scales + ((kt >> 2) & 1) * T::kScales + (kt & 3) * 4;
-    std::conditional_t<EXACT, Wide, v8i> bf[T::kNJ], af;
+  if (nk > 1) issue(1);
 #pragma unroll
-    for (int j = 0; j < T::kNJ; ++j) as_operand(frag(st + T::kBM * 128, br + 16 * j), bf[j]);
-    float sb[ROW ? T::kNJ : (SWIGLU ? 2 : 1)][ROW ? 4 : 1];
-    if constexpr (ROW) {
+  for (int j = 0; j < kNJ; ++j) read_b(lds, j);
+  read_a(lds, 0);
+  read_scales(0);
 #pragma unroll
-      for (int j = 0; j < T::kNJ; ++j)
+  for (int j = 0; j < kNJ; ++j) v[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          sb[j][c] = *reinterpret_cast<const float*>(sc + (T::kBM + wn * T::kNJ * 16 + 16 * j + 4 * g4 + c) * 16);
-    } else {
-      sb[0][0] = *reinterpret_cast<const float*>(sc + (T::kBM + wn * T::kNJ * 16) * 16);
-      if constexpr (SWIGLU) sb[1][0] = *reinterpret_cast<const float*>(sc + (T::kBM + wn * T::kNJ * 16 + 32) * 16);
-    }
-#pragma unroll
-    for (int i = 0; i < T::kMI; ++i) {
-      as_operand(frag(st, ar + 16 * i), af);
-      const float sa = *reinterpret_cast<const float*>(sc + (ar + 16 * i) * 16);
-#pragma unroll
-      for (int j = 0; j < T::kNJ; ++j) {
-        const f32x4 v = block_sum(bf[j], af);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          if constexpr (ROW) acc[i][j][c] = __builtin_fmaf(v[c] * sb[j][c], sa, acc[i][j][c]);
-          else acc[i][j][c] = __builtin_fmaf(v[c], sa * sb[SWIGLU ? (j >> 1) & 1 : 0][0], acc[i][j][c]);
-        }
-      }
-    }
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): the next stage has landed, this one is read
-    __builtin_amdgcn_s_barrier();
+  for (int h = 0; h < kF; ++h) f[1][h] = 0.f;
+  const std::true_type yes;
+  const std::false_type no;
+  int kt = 0;
+  for (; kt + 2 < nk; ++kt) stage(kt, yes, yes);
+  if (kt + 1 < nk) {
+    stage(kt, yes, no);
+    ++kt;
   }
+  stage(kt, no, no);
+#pragma unroll
+  for (int j = 0; j < kNJ; ++j) add(kMI - 1, j);
+  __syncthreads();
 }
 
 }  // namespace f8

@@ -82,7 +82,8 @@ def test_gemms():
     for bad in (dict(a=None), dict(sa=None), dict(o=None), dict(r=None), dict(n=-1), dict(n=1025), dict(b=None), dict(sb=None),
                 dict(lsb=2), dict(c=None), dict(ldc=248), dict(ldc=260), dict(epi=2), dict(M=-1), dict(c=A + 8), dict(lda=500)):
         assert g(**bad) == X.XS_EINVAL, bad
-    for bad in (dict(K=500), dict(N=252), dict(N=384, epi=X.XS_EPI_SWIGLU)):
+    for bad in (dict(K=500), dict(N=252), dict(N=384, epi=X.XS_EPI_SWIGLU),
+                dict(N=1 << 23, ldc=1 << 22, epi=X.XS_EPI_SWIGLU)):
         assert g(**bad) == X.XS_EUNSUPPORTED, bad
     assert g(M=0) == X.XS_OK and g(n=0) == X.XS_OK
 
