@@ -24,6 +24,7 @@ struct GemmArgs {
   const int* seg_rows;
   int n_seg;
   int* status;
+  int one_each;                // one tile per workgroup, not a persistent grid
 };
 
 // Work index t -> (segment, row block, column tile): segments in order; within one, groups of eight row
@@ -32,7 +33,8 @@ struct GemmArgs {
 struct Where {
   int seg, m0, rows, nb;
 };
-constexpr int kGroupRows = 8;
+constexpr int kGroupRows = 8, kRun = 32;
+constexpr int64_t kNoTile = int64_t(1) << 50;
 __device__ __forceinline__ void in_groups(int64_t t, int blocks, int nt, int* mb, int* nb) {
   const int64_t per = static_cast<int64_t>(kGroupRows) * nt;
   const int first = static_cast<int>(t / per) * kGroupRows, local = static_cast<int>(t % per);
@@ -98,9 +100,14 @@ __global__ __launch_bounds__(T::kThreads, 2) void gemm_kernel(GemmArgs p) {
   const int n_out = SWIGLU ? p.N / 2 : p.N;
   const int nt = (n_out + kCols - 1) / kCols;
   Where at;
-  // consecutive workgroups go to different XCDs: each XCD takes a run of consecutive tiles
+  // Consecutive workgroups go to different XCDs: each XCD takes runs of consecutive tiles, of the grid's eighth
+  // or (one tile per workgroup) of kRun. 128-tiles come two to a CU, and a last round of one to a CU is quicker,
+  // which dealing a tile to each workgroup as it starts makes use of (7 tiles per CU: 262 us persistent, 238
+  // so); the 256-tiles' workgroups gain nothing by it.
   const int G = gridDim.x, b = blockIdx.x;
-  for (int64_t t = G % 8 ? b : (b % 8) * (G / 8) + b / 8; find_tile<T::kBM>(p, t, nt, at); t += G) {
+  int64_t t = G % 8 ? b : (b % 8) * (G / 8) + b / 8;
+  if (p.one_each) t = (static_cast<int64_t>(b / 8 / kRun) * 8 + b % 8) * kRun + b / 8 % kRun;
+  for (; find_tile<T::kBM>(p, t, nt, at); t += p.one_each ? kNoTile : G) {
     const int n0 = at.nb * kCols;
     const Product q{p.a + at.m0 * p.lda, p.lda, p.a_s + at.m0 * p.lda_s, p.lda_s, at.rows,
                     p.b + at.seg * p.b_seg, p.ldb, p.b_s + at.seg * p.b_s_seg, p.ldb_s, n0, p.N, p.N / 2, p.K};
@@ -328,11 +335,13 @@ int launch_split(const f8::GemmArgs& p, hipStream_t st) {
 }
 
 template <class T, bool ROW, bool SWIGLU, bool F32>
-int launch_tiles(const f8::GemmArgs& p, int per_cu, hipStream_t st) {
+int launch_tiles(f8::GemmArgs p, int per_cu, hipStream_t st) {
   const int cols = SWIGLU ? T::kBN / 2 : T::kBN;
   const int64_t nt = ((SWIGLU ? p.N / 2 : p.N) + cols - 1) / cols;
   const int64_t blocks = (static_cast<int64_t>(p.M) + T::kBM - 1) / T::kBM + (p.seg_off ? p.n_seg : 0);
-  const int grid = static_cast<int>(std::min<int64_t>(blocks * nt, static_cast<int64_t>(per_cu) * xs_host::persistent_grid(0)));
+  const int64_t runs = (blocks * nt + 8 * f8::kRun - 1) / (8 * f8::kRun) * (8 * f8::kRun);
+  p.one_each = per_cu > 1 && !p.seg_off && runs < (1 << 22);
+  const int grid = static_cast<int>(p.one_each ? runs : std::min<int64_t>(blocks * nt, static_cast<int64_t>(per_cu) * xs_host::persistent_grid(0)));
   hipLaunchKernelGGL((f8::gemm_kernel<T, ROW, SWIGLU, F32>), dim3(grid), dim3(T::kThreads), 0, st, p);
   return xs_host::launch_status();
 }
@@ -378,7 +387,7 @@ Form choose(const f8::GemmArgs& p, bool swiglu, bool f32) {
   const auto tiles = [&](int bm, int bn) { return blocks(bm) * std::ceil(p.N / static_cast<double>(bn)); };
   const double mid = tiles(128, 128), rest = std::fmod(mid, 2 * cus) / cus;
   const double part = rest == 0 ? 0 : rest <= 1 ? 0.62 : 0.62 + 0.48 * (rest - 1);
-  offer(kMid, 6 + nk * (std::floor(mid / (2 * cus)) * 1.1 + part) * (f32 ? 1.9 : far ? 1.2 : 1));
+  offer(kMid, 6 + nk * (std::floor(mid / (2 * cus)) * 1.1 + part) * (f32 ? 1.75 : far ? 1.2 : 1));
   if (!f32) {                                            // exact sums do not fit its registers
     const double big = tiles(256, 256), left = std::fmod(big, cus) / cus;
     offer(kBig, 6 + nk * (std::floor(big / cus) * 1.85 + (left == 0 ? 0 : 1.25 + 0.6 * left)));
@@ -427,7 +436,7 @@ extern "C" int xs_gemm_fp8(const void* a, int64_t lda, const float* a_scales, in
   if (ldc < N || ldc % 8 || !aligned_to(c, 16)) return XS_EINVAL;
   if (M == 0) return XS_OK;
   const f8::GemmArgs p{static_cast<const uint8_t*>(a), lda, a_scales, lda_s, static_cast<const uint8_t*>(b), ldb, 0,
-                       b_scales, ldb_s, 0, static_cast<char*>(c), ldc, M, N, K, nullptr, nullptr, 1, nullptr};
+                       b_scales, ldb_s, 0, static_cast<char*>(c), ldc, M, N, K, nullptr, nullptr, 1, nullptr, 0};
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (b_block == XS_BLOCK_ROW)
     return c_type == XS_TYPE_F32 ? launch<true, false, true>(p, st) : launch<true, false, false>(p, st);
@@ -453,7 +462,7 @@ extern "C" int xs_grouped_gemm_fp8(const void* a, int64_t lda, const float* a_sc
   if (M == 0 || n_seg == 0) return XS_OK;
   const f8::GemmArgs p{static_cast<const uint8_t*>(a), lda, a_scales, lda_s, static_cast<const uint8_t*>(b), K,
                        static_cast<int64_t>(N) * K, b_scales, ldb_s, static_cast<int64_t>((N + 127) / 128) * ldb_s,
-                       static_cast<char*>(c), ldc, M, N, K, seg_offsets, seg_rows, n_seg, dev_status};
+                       static_cast<char*>(c), ldc, M, N, K, seg_offsets, seg_rows, n_seg, dev_status, 0};
   hipStream_t st = static_cast<hipStream_t>(stream);
   return swiglu ? launch<false, true, false>(p, st) : launch<false, false, false>(p, st);
 }
