@@ -393,6 +393,13 @@ int xs_fused_ep_layer(const xs_ep_layer* L, const xs_pacing* pacing, const xs_tr
                       void* workspace, int64_t workspace_bytes, int32_t* dev_status,
                       void* stream);
 
+/* The same layer routed by a gate (see "routing gates") instead of top-k softmax: L->logits holds the gate's
+ * logits [n_src][T][E] in its logits_type, L->renormalize is not used. gate->E and gate->k are L's (else
+ * XS_EINVAL); otherwise as xs_fused_ep_layer and xs_route_gate. */
+int xs_fused_ep_layer_gated(const xs_ep_layer* L, const xs_gate* gate, const xs_pacing* pacing,
+                            const xs_trace* trace, void* workspace, int64_t workspace_bytes,
+                            int32_t* dev_status, void* stream);
+
 /* The same layer for callers that cannot allocate (code under HIP graph capture, tight serving
  * loops, harnesses that forbid hipMalloc): no workspace argument; the layer's scratch (layout
  * partial counts, tile tables, readiness and claim counters, MX token-row staging) lives in a

@@ -1081,13 +1081,20 @@ extern "C" int xs_combine_send(const xs_ep_layer* L, const xs_pacing* pacing, in
   return xs_host::signal_windows(cws, st);
 }
 
-static int fused_ep_layer(const xs_ep_layer* L, const xs_pacing* pacing, const xs_trace* trace,
+static int fused_ep_layer(const xs_ep_layer* L, const xs_gate* gate, const xs_pacing* pacing, const xs_trace* trace,
                           void* workspace, int64_t workspace_bytes, int32_t* dev_status, void* stream);
 
 extern "C" int xs_fused_ep_layer(const xs_ep_layer* L, const xs_pacing* pacing,
                                  const xs_trace* trace, void* workspace, int64_t workspace_bytes,
                                  int32_t* dev_status, void* stream) {
-  return fused_ep_layer(L, pacing, trace, workspace, workspace_bytes, dev_status, stream);
+  return fused_ep_layer(L, nullptr, pacing, trace, workspace, workspace_bytes, dev_status, stream);
+}
+
+extern "C" int xs_fused_ep_layer_gated(const xs_ep_layer* L, const xs_gate* gate, const xs_pacing* pacing,
+                                       const xs_trace* trace, void* workspace, int64_t workspace_bytes,
+                                       int32_t* dev_status, void* stream) {
+  if (!L || !gate || gate->E != L->E || gate->k != L->k) return XS_EINVAL;
+  return fused_ep_layer(L, gate, pacing, trace, workspace, workspace_bytes, dev_status, stream);
 }
 
 // ------------------------------------------------------------------------------ no-alloc layer
@@ -1123,10 +1130,10 @@ extern "C" int xs_fused_ep_layer_noalloc(const xs_ep_layer* L, const xs_pacing* 
   if (need > XS_STATIC_SCRATCH_BYTES) return XS_EWORKSPACE;
   void* ws = nullptr;
   if ((rc = scratch_of_current_device(&ws))) return rc;
-  return fused_ep_layer(L, pacing, trace, ws, XS_STATIC_SCRATCH_BYTES, dev_status, stream);
+  return fused_ep_layer(L, nullptr, pacing, trace, ws, XS_STATIC_SCRATCH_BYTES, dev_status, stream);
 }
 
-static int fused_ep_layer(const xs_ep_layer* L, const xs_pacing* pacing, const xs_trace* trace,
+static int fused_ep_layer(const xs_ep_layer* L, const xs_gate* gate, const xs_pacing* pacing, const xs_trace* trace,
                           void* workspace, int64_t workspace_bytes, int32_t* dev_status, void* stream) {
   int rc = validate(L, true);
   if (rc) return rc;
@@ -1145,9 +1152,12 @@ static int fused_ep_layer(const xs_ep_layer* L, const xs_pacing* pacing, const x
   if (rc) return rc;
   const int64_t n_all = static_cast<int64_t>(L->n_src) * L->T;
   if (n_all > 0x7fffffff) return XS_EINVAL;
+  // a gate's own argument errors before anything is launched
+  if (gate && (rc = xs_route_gate(gate, L->logits, L->E, 0, L->topk_idx, L->topk_w, stream))) return rc;
   if ((rc = record_event(L, XS_EV_ROUTE, st))) return rc;
-  rc = xs_route_topk_softmax(L->logits, static_cast<int32_t>(n_all), L->E, L->k, L->renormalize,
-                             L->topk_idx, L->topk_w, stream);
+  rc = gate ? xs_route_gate(gate, L->logits, L->E, static_cast<int32_t>(n_all), L->topk_idx, L->topk_w, stream)
+            : xs_route_topk_softmax(L->logits, static_cast<int32_t>(n_all), L->E, L->k, L->renormalize,
+                                    L->topk_idx, L->topk_w, stream);
   if (rc) return rc;
   if ((rc = record_event(L, XS_EV_LAYOUT, st))) return rc;
   // The layout's scan launch also plans the expert FFN, and the dispatch launch finishes the

@@ -49,7 +49,11 @@ class EPLayer:
 
     def __init__(self, s: Shape, device="cuda", combine_host: bool = False, sentinel: bool = True,
                  precision: int = X.XS_PREC_BF16, ready_flags: bool = False,
-                 host_combine_sources=None):
+                 host_combine_sources=None, gate=None):
+        # a routing gate (X.gate(...)) in place of top-k softmax; its logits are float32 or bfloat16
+        if gate is not None and (gate.E != s.E or gate.k != s.k):
+            raise ValueError(f"gate of top-{gate.k} of {gate.E} experts in a layer of top-{s.k} of {s.E}")
+        self.gate = gate
         self.s = s
         self.precision = precision
         mxp = precision in (X.XS_PREC_MXFP8, X.XS_PREC_W4A8)
@@ -69,7 +73,8 @@ class EPLayer:
         self.cap = cap
         d = self.dev
         i32 = torch.int32
-        self.logits = torch.zeros((s.n_src, s.T, s.E), dtype=torch.float32, device=d)
+        bf16_logits = gate is not None and gate.logits_type == X.XS_TYPE_BF16
+        self.logits = torch.zeros((s.n_src, s.T, s.E), dtype=torch.bfloat16 if bf16_logits else torch.float32, device=d)
         self.x_all = torch.zeros((s.n_src, s.T, s.H), dtype=torch.int16, device=d)
         self.w1 = torch.zeros((s.n_experts, 2 * s.I, s.H), dtype=torch.int16, device=d) \
             if s.expert_mode == X.XS_EXPERT_SWIGLU else None
@@ -211,6 +216,10 @@ class EPLayer:
     # -------------------------------------------------------------------------- steps
     def route(self):
         s = self.s
+        if self.gate is not None:
+            X.check(X.xs_route_gate(self.gate, self.logits.data_ptr(), s.E, s.n_src * s.T, self.topk_idx.data_ptr(),
+                                    self.topk_w.data_ptr(), self.stream), "route gate")
+            return
         X.check(X.xs_route_topk_softmax(self.logits.data_ptr(), s.n_src * s.T, s.E, s.k, s.renormalize,
                                         self.topk_idx.data_ptr(), self.topk_w.data_ptr(), self.stream),
                 "route")
@@ -268,6 +277,11 @@ class EPLayer:
 
     def fused(self, pacing: X.xs_pacing | None = None, trace: X.xs_trace | None = None):
         ws = self.workspace
+        if self.gate is not None:
+            X.check(X.xs_fused_ep_layer_gated(C.byref(self.L), self.gate, C.byref(pacing) if pacing is not None else None,
+                                              C.byref(trace) if trace is not None else None, ws.data_ptr(),
+                                              ws.numel(), self.status.data_ptr(), self.stream), "fused_ep_layer_gated")
+            return
         X.check(X.xs_fused_ep_layer(C.byref(self.L), C.byref(pacing) if pacing is not None else None,
                                     C.byref(trace) if trace is not None else None, ws.data_ptr(),
                                     ws.numel(), self.status.data_ptr(), self.stream), "fused_ep_layer")

@@ -189,6 +189,8 @@ xs_pacing_audit_run = _sig("xs_pacing_audit_run", C.c_int, P(xs_ep_layer), P(xs_
 xs_trace_tile_times = _sig("xs_trace_tile_times", C.c_int, vp, vp, i64, i32, P(f64), P(f64), P(f64))
 xs_route_gate = _sig("xs_route_gate", C.c_int, P(xs_gate), vp, i64, i32, vp, vp, vp)
 xs_route_gate_backward = _sig("xs_route_gate_backward", C.c_int, P(xs_gate), vp, i64, i32, vp, vp, vp, i64, vp, vp)
+xs_fused_ep_layer_gated = _sig("xs_fused_ep_layer_gated", C.c_int, P(xs_ep_layer), P(xs_gate), P(xs_pacing), P(xs_trace),
+                               vp, i64, vp, vp)
 xs_quantize_fp8 = _sig("xs_quantize_fp8", C.c_int, vp, i64, i32, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp)
 xs_quantize_fp8_tile = _sig("xs_quantize_fp8_tile", C.c_int, vp, i64, i32, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp)
 xs_gemm_fp8 = _sig("xs_gemm_fp8", C.c_int, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, i32, i32, i32, i32, vp)
@@ -197,7 +199,7 @@ xs_grouped_gemm_fp8 = _sig("xs_grouped_gemm_fp8", C.c_int, vp, i64, vp, i64, i32
 xs_swiglu_fp8 = _sig("xs_swiglu_fp8", C.c_int, vp, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp)
 xs_swiglu_fp8_backward = _sig("xs_swiglu_fp8_backward", C.c_int, vp, i64, vp, i64, vp, i64, i64, i32, vp, i64, vp, i64, vp)
 
-EXPORTED = ["xs_route_gate", "xs_route_gate_backward", "xs_quantize_fp8", "xs_quantize_fp8_tile", "xs_gemm_fp8",
+EXPORTED = ["xs_fused_ep_layer_gated", "xs_route_gate", "xs_route_gate_backward", "xs_quantize_fp8", "xs_quantize_fp8_tile", "xs_gemm_fp8",
             "xs_grouped_gemm_fp8", "xs_swiglu_fp8", "xs_swiglu_fp8_backward",
             "xs_strerror", "xs_version", "xs_route_topk_softmax", "xs_dispatch_layout_workspace_bytes",
             "xs_dispatch_layout", "xs_dispatch", "xs_ep_layer_workspace_bytes", "xs_expert_ffn",
