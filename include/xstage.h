@@ -124,8 +124,8 @@ int xs_route_gate(const xs_gate* g, const void* logits, int64_t ld, int32_t T, i
                   float* topk_w, void* stream);
 
 /* Gradient of the weights in the logits, the selection held fixed: d_logits device [T][E] (rows ld_d
- * elements apart, of logits_type; every element is written; may be logits itself) from d_topk_w device
- * fp32 [T][k] and the forward call's g, logits and topk_idx. An expert listed twice by a token gets both
+ * elements apart, of logits_type; every element is written; may be logits itself, then with ld_d = ld) from
+ * d_topk_w device fp32 [T][k] and the forward call's g, logits and topk_idx. An expert listed twice by a token gets both
  * slots' terms; an index outside [0, E) sets XS_EBADINPUT in dev_status and its slot counts as absent.
  * Argument errors as above. */
 int xs_route_gate_backward(const xs_gate* g, const void* logits, int64_t ld, int32_t T,

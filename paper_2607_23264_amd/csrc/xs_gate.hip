@@ -346,8 +346,9 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
   }
   // the key of a logit: clamped, and the lowest for NaN (med3 takes the lower bound) and masked ones
   const auto key_of = [&](float l, float b) {
-    float s = l;
-    if (!by_logit) s = (softmax ? __expf(l - m) * inv : __builtin_amdgcn_rcpf(1.f + __expf(-l))) + b;
+    float s;
+    if (by_logit) s = l + 0.f;              // -0 becomes 0: as integers they differ
+    else s = (softmax ? __expf(l - m) * inv : __builtin_amdgcn_rcpf(1.f + __expf(-l))) + b;
     s = __builtin_amdgcn_fmed3f(s, kMasked, -kMasked);
     return l == -INFINITY ? kMasked : s;
   };
@@ -474,8 +475,8 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
   const float last = -lanes_max<16>(slot ? -key : -INFINITY);
   const float tol = by_logit ? 0.f : 2.f * sigma + 0x1p-22f * fmaxf(fabsf(largest), last > kMasked ? fabsf(last) : 0.f);
   const auto before = [&](auto a, int ea, auto b, int eb) { return a > b || (a == b && ea < eb); };
-  // Keys that may be among the k: the k, if all is clear. (A masked last one: nothing else is left; whole keys
-  // in the network: they are.)
+  // Keys that may be among the k: the k, if all is clear. (A masked last one: nothing else is left, as no key
+  // above -2^127 is cut down to it; whole keys in the network: they are.)
   int n = g.k;
   if (!(by_logit && sizeof(LT) == 2) && last > kMasked) {
     float c = 0.f;
@@ -772,7 +773,7 @@ extern "C" int xs_route_gate_backward(const xs_gate* g, const void* logits, int6
   int rc = gate_ok(g, logits, ld, T);
   if (rc) return rc;
   if (!topk_idx || !d_topk_w || !d_logits || ld_d < g->E || ld_d > (int64_t(1) << 40)) return XS_EINVAL;
-  if (!aligned_to(d_logits, g->logits_type == XS_TYPE_BF16 ? 2 : 4)) return XS_EINVAL;
+  if (!aligned_to(d_logits, g->logits_type == XS_TYPE_BF16 ? 2 : 4) || (d_logits == logits && ld_d != ld)) return XS_EINVAL;
   if (T == 0) return XS_OK;
   const GateGradArgs a{logits, ld, T, g->E, g->k, g->score, g->renormalize != 0, g->scale, topk_idx, d_topk_w,
                        d_logits, ld_d, dev_status};

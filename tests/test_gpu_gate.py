@@ -256,3 +256,37 @@ def test_gates_in_a_graph_and_on_another_stream():
             assert all(torch.equal(a, b) for a, b in zip((idx, w, d), want))
         else:
             assert np.array_equal(idx.cpu().numpy(), gate.select(_logits(T, E, "f32", 9)[1], k, "sigmoid", 8, 4, True))
+
+
+@pytest.mark.parametrize("E,k", [(8, 1), (8, 3), (64, 8), (256, 5), (512, 16), (700, 20)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_signed_zeros_are_equal(E, k, dtype):
+    """Logits of 0 and -0 tie, whichever comes first."""
+    l = torch.full((4, E), -1.0)
+    l[0, ::2] = 0.0
+    l[0, 1::2] = -0.0
+    l[1, ::2] = -0.0
+    l[1, 1::2] = 0.0
+    l[2, :] = -0.0
+    l[2, E - 1] = 0.0
+    l[3, 1] = -0.0
+    l[3, E - 1] = 0.0
+    l = l.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    for kind in ("softmax", "sigmoid"):
+        idx, _ = _route(_gate(E, k, kind, dtype=dtype), l.cuda(), 4)
+        assert np.array_equal(idx, gate.route(l.double().numpy(), k, kind)[0])
+
+
+@pytest.mark.parametrize("E,k", [(16, 4), (64, 8), (256, 8), (512, 16), (640, 8)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lowest_keys_come_before_masked_ones(E, k, dtype):
+    """Finite logits just above -2^127 at the highest indices, behind masked ones."""
+    l = torch.full((3, E), float("-inf"))
+    low = -(2.0 ** 127) * (1 - 2.0 ** (-7 if dtype == "bf16" else -20))
+    l[0, E - k - 1:] = low
+    l[1, E - k // 2:] = low
+    l[2, E - k // 2:] = low
+    l[2, E // 2] = 3.0
+    l = l.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    idx, _ = _route(_gate(E, k, "softmax", renorm=True, dtype=dtype), l.cuda(), 3)
+    assert np.array_equal(idx, gate.route(l.double().numpy(), k, "softmax", renorm=True)[0])

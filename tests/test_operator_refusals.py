@@ -108,3 +108,11 @@ def test_swiglu_checkpoints():
         assert b(**bad) == X.XS_EINVAL, bad
     assert b(I=192) == X.XS_EUNSUPPORTED
     assert b(rows=0) == X.XS_OK
+
+
+def test_gradient_over_its_logits():
+    """In place, rows of the gradient lie where the logits' rows do."""
+    X = xs()
+    g = _gate()
+    assert X.xs_route_gate_backward(g, A, 64, 4, A, A, A, 72, None, None) == X.XS_EINVAL
+    assert X.xs_route_gate_backward(g, A, 72, 4, A, A, A, 64, None, None) == X.XS_EINVAL
