@@ -623,8 +623,10 @@ int xs_quantize_fp8_tile(const void* x, int64_t rows, int32_t cols, int64_t ldx,
  * at the end. Within a block: for an fp32 result exact products summed in fp32; for a bf16 result the 8-bit
  * matrix unit, at twice the rate, which cuts the products of eight consecutive K elements below 2^-13 of
  * the largest one's exponent (about 1e-5 of the result).
- * How a product is split follows from M, N, K, c_type, ldb_s and the device's CU count alone. K counts whole blocks (the
- * padded columns of a quantized matrix).
+ * With 128 x 128 blocks a row's and a block's scale are one fp32 factor: finite, and not below fp32's normal
+ * range, where the largest magnitudes of the two blocks multiply to between 2^-108 and 2^145.
+ * How a product is split follows from M, N, K, c_type, ldb_s and the device's CU count alone. K counts
+ * whole blocks (the padded columns of a quantized matrix).
  * Requires K % 128 == 0, N % 8 == 0, rows of at most 2^22 bytes (else XS_EUNSUPPORTED); ldc % 8 == 0 and
  * the layout above (else XS_EINVAL). */
 int xs_gemm_fp8(const void* a, int64_t lda, const float* a_scales, int64_t lda_s, const void* b, int64_t ldb,
@@ -636,10 +638,9 @@ int xs_gemm_fp8(const void* a, int64_t lda, const float* a_scales, int64_t lda_s
  * b_scales + s ceil(N / 128) ldb_s. XS_EPI_STORE or XS_EPI_SWIGLU (gate rows [0, N / 2), up rows [N / 2,
  * N); c [M][N / 2]). Segments, their errors and the rows outside every segment as xs_grouped_gemm.
  * Requires K % 128 == 0, N % 8 == 0 (STORE) or N % 256 == 0 and N / 2 rows of K bytes below 2^31 (SWIGLU).
- * The input's gradient is the same
- * call on transposed weights (xs_quantize_fp8_tile's codes_t), a segment's weight gradient xs_gemm_fp8 on
- * transposed rows. How rows are tiled follows from M, n_seg, N, K, ldb_s and the
- * device's CU count alone. */
+ * The input's gradient is the same call on transposed weights (xs_quantize_fp8_tile's codes_t), a segment's
+ * weight gradient xs_gemm_fp8 on transposed rows. How rows are tiled follows from M, n_seg, N, K, ldb_s and
+ * the device's CU count alone. */
 int xs_grouped_gemm_fp8(const void* a, int64_t lda, const float* a_scales, int64_t lda_s, int32_t M,
                         const int32_t* seg_offsets, const int32_t* seg_rows, int32_t n_seg, const void* b,
                         const float* b_scales, int64_t ldb_s, int32_t N, int32_t K, void* c, int64_t ldc,

@@ -484,7 +484,7 @@ extern "C" int xs_swiglu_fp8_backward(const void* ck_codes, int64_t ld_ck, const
     return XS_EINVAL;
   if (h && (ld_h < I || ld_h % 8 || !aligned_to(h, 16))) return XS_EINVAL;
   if (rows == 0) return XS_OK;
-  if (rows > kMaxRows || (rows * (I / 8) + 255) / 256 > xs_host::kMaxBlocks) return XS_EUNSUPPORTED;
+  if (rows > kMaxRows || (rows * (I / 128) + 15) / 16 > xs_host::kMaxBlocks) return XS_EUNSUPPORTED;
   const f8::SwigluGradArgs a{static_cast<const uint8_t*>(ck_codes), ld_ck, ck_scales, ld_cks, static_cast<const uint16_t*>(dh), ld_dh,
                              rows, I, static_cast<uint16_t*>(d_gu), ld_dgu, static_cast<uint16_t*>(h), ld_h};
   const dim3 grid = xs_host::grid_of((rows * (I / 8) + 255) / 256);

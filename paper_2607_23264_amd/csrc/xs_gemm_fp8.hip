@@ -45,7 +45,7 @@ __device__ __forceinline__ void in_groups(int64_t t, int blocks, int nt, int* mb
 template <int BM>
 __device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, Where& at) {
   if (!p.seg_off) {
-    const int blocks = (p.M + BM - 1) / BM;
+    const int blocks = static_cast<int>((static_cast<int64_t>(p.M) + BM - 1) / BM);
     if (t >= static_cast<int64_t>(blocks) * nt) return false;
     int mb, nb;
     in_groups(t, blocks, nt, &mb, &nb);
@@ -77,7 +77,7 @@ __device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, 
       const int l = __ffsll(static_cast<long long>(hit)) - 1;
       const int rows = __shfl(r, l), off = __shfl(o, l);
       const int64_t local = t - (base + __shfl(incl, l) - __shfl(tiles, l));
-      const int blocks = (rows + BM - 1) / BM;
+      const int blocks = static_cast<int>((static_cast<int64_t>(rows) + BM - 1) / BM);
       int mb, nb;
       in_groups(local, blocks, nt, &mb, &nb);
       at.seg = __builtin_amdgcn_readfirstlane(s0 + l);
@@ -372,8 +372,9 @@ Form choose(const f8::GemmArgs& p, bool swiglu, bool f32) {
       form = f;
     }
   };
-  // offsets of the split form's buffers stay below f8::kNone, its row blocks in a grid's second dimension
-  if ((n_out / 128 + 1) * p.ldb_s * 4 < f8::kNone) {
+  // offsets of the split form's buffers stay below f8::kNone, its column blocks (of 16 or more, 256 threads) in a
+  // grid's first dimension of 2^32 - 1 threads, its row blocks in the second
+  if ((n_out / 128 + 1) * p.ldb_s * 4 < f8::kNone && p.N < (1 << 28)) {
     constexpr int forms[5][2] = {{1, 2}, {2, 1}, {2, 2}, {2, 4}, {4, 4}};
     const double rate = f32 ? 55e3 : far ? 47e3 : 70e3;
     for (int f = 0; f < 5; ++f) {

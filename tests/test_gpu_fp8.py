@@ -419,3 +419,26 @@ def test_a_weights_gradient_in_a_graph_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(dw, first)
+
+
+def test_more_columns_than_a_grid_of_the_split_form_has():
+    """2^28 + 8 columns: sixteen of them to a workgroup of 256 threads would be more threads than a grid's
+    dimension has. Repeating rows of b give repeating columns of c."""
+    N, K, n = (1 << 28) + 8, 128, 1 << 20
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    X = xs()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    base = (torch.randint(0, 2, (n, K), device="cuda", generator=g) * 0x38).to(torch.uint8)        # 0 or 1
+    b = torch.empty((N, K), dtype=torch.uint8, device="cuda")
+    b[:1 << 28].view(-1, n, K).copy_(base)
+    b[1 << 28:] = base[:8]
+    sb = torch.ones((N // 128 + 1, 4), device="cuda")
+    a, sa = torch.full((1, K), 0x38, dtype=torch.uint8, device="cuda"), torch.full((1, 4), 0.5, device="cuda")
+    c = torch.full((1, N), -7.0, dtype=torch.bfloat16, device="cuda")
+    X.check(X.xs_gemm_fp8(a.data_ptr(), K, sa.data_ptr(), 4, b.data_ptr(), K, sb.data_ptr(), 4, X.XS_BLOCK_TILE, c.data_ptr(), N,
+                          X.XS_TYPE_BF16, 1, N, K, _stream()))
+    want = ((base != 0).sum(1).float() * 0.5).to(torch.bfloat16)                                 # at most 64: exact
+    assert torch.equal(c[0, :1 << 28].view(-1, n), want.expand(1 << 8, n)) and torch.equal(c[0, 1 << 28:], want[:8])
+    del a, b, c, sb, base
+    torch.cuda.empty_cache()

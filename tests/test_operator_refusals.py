@@ -116,3 +116,12 @@ def test_gradient_over_its_logits():
     g = _gate()
     assert X.xs_route_gate_backward(g, A, 64, 4, A, A, A, 72, None, None) == X.XS_EINVAL
     assert X.xs_route_gate_backward(g, A, 72, 4, A, A, A, 64, None, None) == X.XS_EINVAL
+
+
+def test_sizes_past_a_grid():
+    """Row and column counts whose product passes 64 bits or a grid are refused, not wrapped."""
+    X = xs()
+    r, i = 1 << 37, 1 << 29
+    assert X.xs_swiglu_fp8_backward(A, 2 * i, A, i, A, i, r, i, A, 2 * i, None, 0, None) == X.XS_EUNSUPPORTED
+    assert X.xs_swiglu_fp8(A, 2 * i, r, i, A, i, A, i, None, 0, None, 0, None) == X.XS_EUNSUPPORTED
+    assert X.xs_quantize_fp8(A, r, 1 << 30, 1 << 30, A, 1 << 30, A, 1 << 23, None, 0, None, 0, None) == X.XS_EUNSUPPORTED
