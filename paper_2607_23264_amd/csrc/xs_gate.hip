@@ -17,6 +17,7 @@
 //     softmax             dl_e = sum d_j
 #include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "xs_common.hpp"
 
@@ -31,6 +32,12 @@ struct GateArgs {
   int* idx;
   float* w;
 };
+
+// f(kRor + r, r) for r = 1 .. 15
+template <class F, int... I>
+__device__ __forceinline__ void each_rotation(const F& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, 0x121 + I>(), I + 1), ...);
+}
 
 template <typename LT>
 __device__ __forceinline__ float load_logit(const void* row, int e) {
@@ -57,7 +64,14 @@ template <int CTRL>
 __device__ __forceinline__ float dpp32(float f) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(f), CTRL, 0xF, 0xF, false));
 }
-constexpr int kRor8 = 0x128, kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;   // over the 16 lanes of a DPP row
+template <int CTRL>
+__device__ __forceinline__ int dpp32(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false);
+}
+// Within the 16 lanes of a DPP row: rotations by r (kRor + r, a lane takes the value r lanes below its own,
+// around the row), the lane's neighbours in its pair and in its four, and its mirror in its eight.
+constexpr int kRor = 0x120, kRor8 = 0x128, kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;
+constexpr int kPair = 0xB1, kFour = 0x4E, kMirror8 = 0x141;
 // Sums and maxima over a token's lanes: 16 (a DPP row) or 64; the same bits in every lane.
 template <int LPT>
 __device__ __forceinline__ float lanes_sum(float v) {
@@ -89,11 +103,17 @@ template <int LPT>
 __device__ __forceinline__ float renormalized(bool softmax, bool slot, float l) {
   slot = slot && l != -INFINITY;
   float c = lanes_max<LPT>(slot ? l : -INFINITY);
-  if (!softmax) c = fminf(c, 0.f);
   float s = 0.f;
-  if (slot) s = softmax ? expf(l - c) : l > 0.f ? 1.f / (1.f + expf(-l)) : expf(l - c) / (1.f + expf(l));
+  if (softmax) {
+    if (slot) s = expf(l - c);
+  } else {
+    // e^-|l| once; below all of the k, e^(l - c) comes with c = 0 from it too
+    c = fminf(c, 0.f);
+    const float t = expf(-fabsf(l));
+    if (slot) s = (l > 0.f ? 1.f : c == 0.f ? t : expf(l - c)) * __builtin_amdgcn_rcpf(1.f + t);
+  }
   const float total = lanes_sum<LPT>(s);
-  return total == 0.f ? 0.f : s / total;
+  return total == 0.f ? 0.f : s * __builtin_amdgcn_rcpf(total);
 }
 // Its score; m and inv: the row's largest logit and the reciprocal of its softmax sum.
 __device__ __forceinline__ float slot_score(bool softmax, bool slot, float l, float m, float inv) {
@@ -219,14 +239,15 @@ __global__ __launch_bounds__(256) void gate_wave_kernel(GateArgs g) {
 }
 
 // ------------------------------------------------------------------------------ sixteen lanes a token
-// A key, cut to 14 bits of mantissa, and its expert in an integer: larger is earlier (a larger cut key or,
-// of equal ones, the lower index; E <= 512).
-__device__ __forceinline__ int pack_key(float key, int e) {
-  const int u = __float_as_int(key);
-  return ((u ^ ((u >> 31) & 0x7FFFFFFF)) & ~511) | (511 - e);
-}
+// fp32 values as integers of the same order (and back: the map is its own inverse), and such a key, cut to 14
+// bits of mantissa, with its expert: larger is earlier (a larger cut key or, of equal ones, the lower
+// index; E <= 512).
+__device__ __forceinline__ int ordered(int bits) { return bits ^ ((bits >> 31) & 0x7FFFFFFF); }
+__device__ __forceinline__ int ordered(float f) { return ordered(__float_as_int(f)); }
+__device__ __forceinline__ float from_ordered(int o) { return __int_as_float(ordered(o)); }
+__device__ __forceinline__ int pack_key(int o, int e) { return (o & ~511) | (511 - e); }
 __device__ __forceinline__ int key_expert(int p) { return 511 - (p & 511); }
-constexpr int kNoKey = -0x7FFFFFFF - 1;
+constexpr int kNoKey = -0x7FFFFFFF - 1, kUnknown = 0x7FFFFFFF;
 
 __device__ __forceinline__ void order(int& a, int& b) {   // the larger first
   const int hi = max(a, b), lo = min(a, b);
@@ -262,25 +283,24 @@ __device__ __forceinline__ void keep_largest(int (&v)[N], const int (&o)[N]) {
   for (int i = 0; i < N; ++i) v[i] = max(v[i], o[N - 1 - i]);
   order_bitonic(v);
 }
-template <int CTRL, int N>
-__device__ __forceinline__ void merge_lanes(int (&v)[N]) {
-  int o[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) o[i] = __builtin_amdgcn_update_dpp(0, v[i], CTRL, 0xF, 0xF, false);
-  keep_largest(v, o);
+__device__ __forceinline__ int lanes_max16(int v) {
+  v = max(v, dpp32<kRor8>(v));
+  v = max(v, dpp32<kRor4>(v));
+  v = max(v, dpp32<kRor2>(v));
+  return max(v, dpp32<kRor1>(v));
 }
 
 // VP consecutive values of T from p: in pieces of 16 bytes where `vec`.
-template <int VPL, typename LT>
+template <int VPL, typename LT, bool FULL>
 __device__ __forceinline__ void load_run(const void* base, int first, int VP, int E, bool vec, float other, float (&v)[VPL]) {
   constexpr int kPiece = sizeof(LT) == 2 && VPL >= 8 ? 8 : 4;
-  if (vec) {
+  if (FULL || vec) {
     const char* const p = static_cast<const char*>(base) + static_cast<int64_t>(first) * static_cast<int64_t>(sizeof(LT));
 #pragma unroll
     for (int i = 0; i < VPL; i += kPiece) {
 #pragma unroll
       for (int c = 0; c < kPiece; ++c) v[i + c] = other;
-      if (i < VP && first + i < E) {
+      if (FULL || (i < VP && first + i < E)) {
         if constexpr (sizeof(LT) == 4) {
           const f32x4 x = *reinterpret_cast<const f32x4*>(p + i * 4);
 #pragma unroll
@@ -311,14 +331,20 @@ __device__ __forceinline__ void load_run(const void* base, int first, int VP, in
 // Elsewhere (one token in a hundred for 256 sigmoid scores, by the cut) the keys within reach of the last,
 // if they are at most sixteen, are done again in 64 bits, one a lane; so are the groups' scores where it is
 // unclear which are kept. What remains (softmax with a bias, whose sum would have to be in 64 bits too, more
-// candidates, a group's second key too near its third) is done again by the token's whole wave (gate_token). Without a bias the logits are
-// the keys, exactly (bf16 ones also when cut).
+// candidates, a group's second key too near its third) is done again by the token's whole wave (gate_token).
+// Without a bias the logits are the keys, exactly (bf16 ones also when cut).
+//
+// Bound by vector instructions (32,768 tokens, top-8 of 256 biased sigmoid scores in groups: 850 for four
+// tokens, 12 us at full rate; 17.8 us, 2.0 TB/s): so what a token needs is fixed when the kernel is compiled
+// (the kind of key, whole rows), the lanes exchange by DPP, and the keys are integers throughout.
 //   sigmoid: exp(-l) is off by 2^-23 and, from its argument, |l| 2^-23; times s (1 - s), with s (1 - s) |l|
 //     <= 0.224; the sum and the reciprocal 2^-24 + 2^-23 of s: together below 2^-22 (s <= 1).
 //   softmax: e^-d is off by d 2^-22 + 2^-23 (d e^-d <= 0.37), the sum of up to 512 terms (32 in a
 //     lane, four levels) by 2^-19 of itself at most: below 2^-18 of the largest score.
-template <typename LT, int VPL, int KL>
-__global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int vec) {
+// MODE: the keys are the logits, sigmoid scores or softmax scores. FULL: E = 16 VPL experts in aligned rows.
+enum { kByLogit, kSigmoid, kSoftmax };
+template <typename LT, int VPL, int KL, int MODE, bool FULL>
+__global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int vec, int bias_vec) {
   extern __shared__ double gate_keys[];   // [4][E], for tokens done again
   __shared__ int candidates[16][16];
   const int sub = threadIdx.x & 15, w = threadIdx.x >> 6;
@@ -326,12 +352,13 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
   const bool live = t_raw < g.T;
   const int64_t t = live ? t_raw : g.T - 1;   // every lane takes part in its row's reductions
   const char* const row = logit_row<LT>(g.logits, g.ld, t);
-  const int first = VP * sub;
-  const bool softmax = g.score == XS_SCORE_SOFTMAX;
-  const bool by_logit = !g.bias && (g.n_group == 1 || !g.top2);
+  const int first = (FULL ? VPL : VP) * sub;
+  constexpr bool by_logit = MODE == kByLogit;
+  const bool softmax = by_logit ? g.score == XS_SCORE_SOFTMAX : MODE == kSoftmax;
   constexpr float kMasked = static_cast<float>(kMaskedKey), kDropped = 1.5f * kMasked;
+  constexpr int kDroppedKey = static_cast<int>(0xFF400000u) ^ 0x7FFFFFFF;
   float v[VPL];
-  load_run<VPL, LT>(row, first, VP, g.E, vec, -INFINITY, v);
+  load_run<VPL, LT, FULL>(row, first, VP, g.E, vec, -INFINITY, v);
   float m = 0.f, inv = 1.f, sigma = 0x1p-22f;
   if (softmax) {
     m = -INFINITY;
@@ -352,49 +379,54 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
     s = __builtin_amdgcn_fmed3f(s, kMasked, -kMasked);
     return l == -INFINITY ? kMasked : s;
   };
+  int o[VPL];                               // the keys, ordered
   {
     float b[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) b[i] = 0.f;
-    if (g.bias) load_run<VPL, float>(g.bias, first, VP, g.E, vec && (reinterpret_cast<uintptr_t>(g.bias) & 15) == 0, 0.f, b);
+    if (!by_logit && g.bias) load_run<VPL, float, FULL>(g.bias, first, VP, g.E, bias_vec, 0.f, b);
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) v[i] = key_of(v[i], b[i]);
+    for (int i = 0; i < VPL; ++i)
+      o[i] = FULL || (i < VP && first + i < g.E) ? ordered(key_of(v[i], b[i])) : kDroppedKey;
   }
-#pragma unroll
-  for (int i = 0; i < VPL; ++i)
-    if (i >= VP || first + i >= g.E) v[i] = kDropped;
+  const auto key_at = [&](int i) { return from_ordered(o[i]); };
+  bool kept = true;                         // the lane's group
   bool unsure = false;
   if (g.n_group > 1) {
     const int lanes = 16 / g.n_group;
-    float a = -INFINITY, b = -INFINITY;     // the group's two largest keys
+    int a = kNoKey, b = kNoKey;             // the group's two largest keys
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-      b = fmaxf(b, fminf(a, v[i]));
-      a = fmaxf(a, v[i]);
+      b = max(b, min(a, o[i]));
+      a = max(a, o[i]);
     }
-    for (int off = 1; off < lanes; off <<= 1) {
-      const float oa = __shfl_xor(a, off), ob = __shfl_xor(b, off);
-      b = fmaxf(fminf(a, oa), fmaxf(b, ob));
-      a = fmaxf(a, oa);
-    }
-    const float gs = g.top2 && b > kMasked ? a + b : a;
+    const auto join = [&](int oa, int ob) {
+      b = max(min(a, oa), max(b, ob));
+      a = max(a, oa);
+    };
+    if (lanes > 1) join(dpp32<kPair>(a), dpp32<kPair>(b));
+    if (lanes > 2) join(dpp32<kFour>(a), dpp32<kFour>(b));
+    if (lanes > 4) join(dpp32<kMirror8>(a), dpp32<kMirror8>(b));
+    const float ka = from_ordered(a), kb = from_ordered(b);   // (one expert to a group: b is dropped, or NaN)
+    const float gs = g.top2 && kb > kMasked ? ka + kb : ka;
     // off by both keys' errors and the sum's rounding, on both sides
-    const float tol = by_logit ? 0.f : 4.f * sigma + 0x1p-21f * (fabsf(a) + (b > kMasked ? fabsf(b) : 0.f));
+    const float tol = by_logit ? 0.f : 4.f * sigma + 0x1p-21f * (fabsf(ka) + (kb > kMasked ? fabsf(kb) : 0.f));
     int above = 0, near = 0;                // groups surely before this one, groups that may be
-    for (int r = lanes; r < 16; r += lanes) {
-      const int os = (sub + r) & 15;
-      const float o = __shfl(gs, os, 16), ot = __shfl(tol, os, 16);
-      const float far = fmaxf(tol, ot);
+    const auto compare = [&](auto ctrl, int r) {
+      if (r % lanes) return;                // (the same in every lane)
+      const int os = dpp32<decltype(ctrl)::value>(sub);
+      const float other = dpp32<decltype(ctrl)::value>(gs), far = fmaxf(tol, dpp32<decltype(ctrl)::value>(tol));
       if (by_logit) {
-        const bool before = o > gs || (o == gs && os / lanes < sub / lanes);
+        const bool before = other > gs || (other == gs && os < sub);
         above += before;
         near += before;
       } else {
-        above += o - gs > far;
-        near += !(gs - o > far);
+        above += other - gs > far;
+        near += !(gs - other > far);
       }
-    }
-    bool kept = near < g.topk_group;
+    };
+    each_rotation(compare, std::make_integer_sequence<int, 15>());
+    kept = near < g.topk_group;
     const unsigned long long doubts = __ballot(above < g.topk_group && !kept);
     if (doubts) {
       // the groups' scores in 64 bits, from the largest keys, if those are clear of the next one
@@ -414,7 +446,7 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
         }
       };
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) insert(v[i], first + i);
+      for (int i = 0; i < VPL; ++i) insert(key_at(i), first + i);
       for (int off = 1; off < lanes; off <<= 1) {
         const float o1 = __shfl_xor(k1, off), o2 = __shfl_xor(k2, off), o3 = __shfl_xor(k3, off);
         const int i1 = __shfl_xor(e1, off), i2 = __shfl_xor(e2, off);
@@ -442,31 +474,34 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
         unsure = !fine;
       }
     }
-    if (!kept) {
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) v[i] = kDropped;
-    }
   }
-  // the KL largest of a lane's keys, then of the sixteen lanes'
+  // The KL largest of a lane's keys in order; then the sixteen lanes' largest first keys one by one, each taken
+  // from its lane's list (merging the lists in a network over the lanes instead: 19.5 us where this takes 17.8).
   int top[KL];
 #pragma unroll
-  for (int i = 0; i < KL; ++i) top[i] = i < VPL ? pack_key(v[i < VPL ? i : 0], first + i) : kNoKey;
+  for (int i = 0; i < KL; ++i) top[i] = i < VPL ? pack_key(o[i < VPL ? i : 0], first + i) : kNoKey;
   order_all(top);
 #pragma unroll
   for (int c = KL; c < VPL; c += KL) {
     int more[KL];
 #pragma unroll
-    for (int i = 0; i < KL; ++i) more[i] = c + i < VPL ? pack_key(v[c + i < VPL ? c + i : 0], first + c + i) : kNoKey;
+    for (int i = 0; i < KL; ++i) more[i] = c + i < VPL ? pack_key(o[c + i < VPL ? c + i : 0], first + c + i) : kNoKey;
     order_all(more);
     keep_largest(top, more);
   }
-  merge_lanes<kRor8>(top);
-  merge_lanes<kRor4>(top);
-  merge_lanes<kRor2>(top);
-  merge_lanes<kRor1>(top);
-  int mine = top[0];                        // lane j has the j-th
 #pragma unroll
-  for (int i = 1; i < KL; ++i) mine = sub == i ? top[i] : mine;
+  for (int i = 0; i < KL; ++i) top[i] = kept ? top[i] : kDroppedKey & ~511;
+  int mine = kNoKey;                        // lane j has the j-th
+#pragma unroll
+  for (int j = 0; j < KL; ++j) {
+    if (j >= g.k) break;
+    const int most = lanes_max16(top[0]);
+    mine = sub == j ? most : mine;
+    const bool mine_too = top[0] == most;   // (keys in use are all different)
+#pragma unroll
+    for (int i = 0; i < KL - j; ++i) top[i] = mine_too ? (i + 1 < KL ? top[i + 1 < KL ? i + 1 : 0] : kUnknown) : top[i];
+  }
+  const int rest = lanes_max16(top[0]);     // kUnknown: one lane had them all
   bool slot = sub < g.k;
   int e = slot ? key_expert(mine) : 512 + sub;
   float l = slot ? load_logit<LT>(row, e) : -INFINITY;
@@ -475,41 +510,39 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
   const float last = -lanes_max<16>(slot ? -key : -INFINITY);
   const float tol = by_logit ? 0.f : 2.f * sigma + 0x1p-22f * fmaxf(fabsf(largest), last > kMasked ? fabsf(last) : 0.f);
   const auto before = [&](auto a, int ea, auto b, int eb) { return a > b || (a == b && ea < eb); };
-  // Keys that may be among the k: the k, if all is clear. (A masked last one: nothing else is left, as no key
-  // above -2^127 is cut down to it; whole keys in the network: they are.)
-  int n = g.k;
-  if (!(by_logit && sizeof(LT) == 2) && last > kMasked) {
-    float c = 0.f;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) c += v[i] >= last - tol ? 1.f : 0.f;
-    n = static_cast<int>(lanes_sum<16>(c));
-  }
-  const float next = __shfl(key, (sub + 1) & 15, 16);
-  const int en = __shfl(e, (sub + 1) & 15, 16);
+  // No key of the rest is above the next cut one's largest value: those may not come near the last. (A masked
+  // last one: nothing else is left, as no key above -2^127 is cut down to it; whole keys in the network: they
+  // are in order.)
+  const bool whole = by_logit && sizeof(LT) == 2;
+  const bool apart = whole || last <= kMasked || from_ordered(rest | 511) < last - tol;
+  const float next = dpp32<kRor + 15>(key);         // of the lane above
+  const int en = dpp32<kRor + 15>(e);
   // masked keys are equal without doubt
   const bool clear = tol == 0.f || next == kMasked ? before(key, e, next, en) : key - next > tol;
   int rank = sub;
-  bool doubt = n != g.k || (sub + 1 < g.k && !clear) || !(tol >= 0.f);   // (a NaN among softmax logits)
+  bool doubt = !apart || (sub + 1 < g.k && !clear) || !(tol >= 0.f);   // (a NaN among softmax logits)
   const unsigned long long doubts = __ballot(doubt);
   if (doubts) {
     doubt = (doubts >> (threadIdx.x & 48)) & 0xFFFFull;                  // of the token
-    // up to sixteen candidates, one a lane, in 64 bits
-    const bool few = doubt && n <= 16 && last > kMasked && tol >= 0.f && (by_logit || !softmax);
-    unsure |= doubt && !few;
+    // the keys that may be among the k: up to sixteen, one a lane, in 64 bits
+    const int from = ordered(last - tol);
     int c = 0;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) c += v[i] >= last - tol ? 1 : 0;
+    for (int i = 0; i < VPL; ++i) c += kept && o[i] >= from ? 1 : 0;
     int at = c;                             // candidates of the lanes up to this one
 #pragma unroll
     for (int off = 1; off < 16; off <<= 1) {
-      const int o = __shfl_up(at, off, 16);
-      if (sub >= off) at += o;
+      const int below = __shfl_up(at, off, 16);
+      if (sub >= off) at += below;
     }
+    const int n = __shfl(at, 15, 16);
     at -= c;
+    const bool few = doubt && n <= 16 && last > kMasked && tol >= 0.f && (by_logit || !softmax);
+    unsure |= doubt && !few;
     if (few) {
 #pragma unroll
       for (int i = 0; i < VPL; ++i)
-        if (v[i] >= last - tol) candidates[threadIdx.x >> 4][at++] = first + i;
+        if (kept && o[i] >= from) candidates[threadIdx.x >> 4][at++] = first + i;
     }
     wave_order();
     if (few) {
@@ -697,15 +730,30 @@ int gate_ok(const xs_gate* g, const void* logits, int64_t ld, int32_t T) {
   return XS_OK;
 }
 
-template <typename LT, int VPL>
+template <typename LT, int VPL, int KL, int MODE>
 void launch_rows(const GateArgs& a, size_t lds, hipStream_t st) {
   const int VP = (a.E + 15) / 16;
   constexpr int kPiece = sizeof(LT) == 2 && VPL >= 8 ? 8 : 4;
   // whole pieces: of each lane's run, and (the last lane's) of the row
   const int vec = VP % kPiece == 0 && a.E % kPiece == 0 && a.ld % kPiece == 0 && aligned_to(a.logits, kPiece * sizeof(LT));
+  const int bias_vec = VP % 4 == 0 && a.E % 4 == 0 && aligned_to(a.bias, 16);
   const dim3 grid = xs_host::grid_of((static_cast<int64_t>(a.T) + 15) / 16);
-  if (a.k <= 8) hipLaunchKernelGGL((gate_rows_kernel<LT, VPL, 8>), grid, dim3(256), lds, st, a, VP, vec);
-  else hipLaunchKernelGGL((gate_rows_kernel<LT, VPL, 16>), grid, dim3(256), lds, st, a, VP, vec);
+  if (a.E == 16 * VPL && vec && bias_vec)
+    hipLaunchKernelGGL((gate_rows_kernel<LT, VPL, KL, MODE, true>), grid, dim3(256), lds, st, a, VP, vec, bias_vec);
+  else hipLaunchKernelGGL((gate_rows_kernel<LT, VPL, KL, MODE, false>), grid, dim3(256), lds, st, a, VP, vec, bias_vec);
+}
+
+template <typename LT, int VPL, int MODE>
+void launch_rows(const GateArgs& a, size_t lds, hipStream_t st) {
+  if (a.k <= 8) launch_rows<LT, VPL, 8, MODE>(a, lds, st);
+  else launch_rows<LT, VPL, 16, MODE>(a, lds, st);
+}
+
+template <typename LT, int VPL>
+void launch_rows(const GateArgs& a, size_t lds, hipStream_t st) {
+  if (!a.bias && (a.n_group == 1 || !a.top2)) launch_rows<LT, VPL, kByLogit>(a, lds, st);
+  else if (a.score == XS_SCORE_SOFTMAX) launch_rows<LT, VPL, kSoftmax>(a, lds, st);
+  else launch_rows<LT, VPL, kSigmoid>(a, lds, st);
 }
 
 template <typename LT>
@@ -754,7 +802,7 @@ extern "C" int xs_route_gate(const xs_gate* g, const void* logits, int64_t ld, i
   hipStream_t st = static_cast<hipStream_t>(stream);
   const size_t lds = 4 * sizeof(double) * g->E;
   // Sixteen lanes per token where each lane has at most 32 consecutive experts and groups are whole lanes;
-  // one wave per token otherwise (32,768 tokens, top-8 of 256 in groups: 23 us against 120).
+  // one wave per token otherwise (32,768 tokens, top-8 of 256 in groups: 18 us against 120).
   const bool whole_lanes = a.n_group == 1 || (a.E % 16 == 0 && 16 % a.n_group == 0);
   if (a.E <= 512 && a.k <= 16 && whole_lanes) {
     if (g->logits_type == XS_TYPE_BF16) launch_rows<uint16_t>(a, lds, st);
