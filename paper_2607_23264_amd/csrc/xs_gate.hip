@@ -33,10 +33,10 @@ struct GateArgs {
   float* w;
 };
 
-// f(kRor + r, r) for r = 1 .. 15
+// f of the constants I... in turn
 template <class F, int... I>
-__device__ __forceinline__ void each_rotation(const F& f, std::integer_sequence<int, I...>) {
-  (f(std::integral_constant<int, 0x121 + I>(), I + 1), ...);
+__device__ __forceinline__ void each_of(const F& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
 }
 
 template <typename LT>
@@ -290,6 +290,19 @@ __device__ __forceinline__ int lanes_max16(int v) {
   return max(v, dpp32<kRor1>(v));
 }
 
+// From the sixteen lanes' descending lists, the J-th largest key and on to the k-th into lane J's, J + 1's ...
+// `mine`, each taken from its list (keys in use are all different); kUnknown follows a list's end.
+template <int J, int KL>
+__device__ __forceinline__ void take_largest(int (&top)[KL], int k, int sub, int& mine) {
+  if (J >= k) return;
+  const int most = lanes_max16(top[0]);
+  mine = sub == J ? most : mine;
+  const bool from_here = top[0] == most;
+#pragma unroll
+  for (int i = 0; i < KL - J; ++i) top[i] = from_here ? (i + 1 < KL ? top[i + 1 < KL ? i + 1 : 0] : kUnknown) : top[i];
+  if constexpr (J + 1 < KL) take_largest<J + 1>(top, k, sub, mine);
+}
+
 // VP consecutive values of T from p: in pieces of 16 bytes where `vec`.
 template <int VPL, typename LT, bool FULL>
 __device__ __forceinline__ void load_run(const void* base, int first, int VP, int E, bool vec, float other, float (&v)[VPL]) {
@@ -330,7 +343,7 @@ __device__ __forceinline__ void load_run(const void* base, int first, int VP, in
 // in the right order, so no other key may come that near to the last of the k, and no neighbours among them.
 // Elsewhere (one token in a hundred for 256 sigmoid scores, by the cut) the keys within reach of the last,
 // if they are at most sixteen, are done again in 64 bits, one a lane; so are the groups' scores where it is
-// unclear which are kept. What remains (softmax with a bias, whose sum would have to be in 64 bits too, more
+// unclear which are kept. What remains (softmax scores, whose sum would have to be in 64 bits too, more
 // candidates, a group's second key too near its third) is done again by the token's whole wave (gate_token).
 // Without a bias the logits are the keys, exactly (bf16 ones also when cut).
 //
@@ -412,10 +425,11 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
     // off by both keys' errors and the sum's rounding, on both sides
     const float tol = by_logit ? 0.f : 4.f * sigma + 0x1p-21f * (fabsf(ka) + (kb > kMasked ? fabsf(kb) : 0.f));
     int above = 0, near = 0;                // groups surely before this one, groups that may be
-    const auto compare = [&](auto ctrl, int r) {
+    const auto compare = [&](auto rc) {
+      constexpr int r = decltype(rc)::value + 1, ctrl = kRor + r;
       if (r % lanes) return;                // (the same in every lane)
-      const int os = dpp32<decltype(ctrl)::value>(sub);
-      const float other = dpp32<decltype(ctrl)::value>(gs), far = fmaxf(tol, dpp32<decltype(ctrl)::value>(tol));
+      const int os = dpp32<ctrl>(sub);
+      const float other = dpp32<ctrl>(gs), far = fmaxf(tol, dpp32<ctrl>(tol));
       if (by_logit) {
         const bool before = other > gs || (other == gs && os < sub);
         above += before;
@@ -425,7 +439,7 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
         near += !(gs - other > far);
       }
     };
-    each_rotation(compare, std::make_integer_sequence<int, 15>());
+    each_of(compare, std::make_integer_sequence<int, 15>());
     kept = near < g.topk_group;
     const unsigned long long doubts = __ballot(above < g.topk_group && !kept);
     if (doubts) {
@@ -492,15 +506,7 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
 #pragma unroll
   for (int i = 0; i < KL; ++i) top[i] = kept ? top[i] : kDroppedKey & ~511;
   int mine = kNoKey;                        // lane j has the j-th
-#pragma unroll
-  for (int j = 0; j < KL; ++j) {
-    if (j >= g.k) break;
-    const int most = lanes_max16(top[0]);
-    mine = sub == j ? most : mine;
-    const bool mine_too = top[0] == most;   // (keys in use are all different)
-#pragma unroll
-    for (int i = 0; i < KL - j; ++i) top[i] = mine_too ? (i + 1 < KL ? top[i + 1 < KL ? i + 1 : 0] : kUnknown) : top[i];
-  }
+  take_largest<0>(top, g.k, sub, mine);
   const int rest = lanes_max16(top[0]);     // kUnknown: one lane had them all
   bool slot = sub < g.k;
   int e = slot ? key_expert(mine) : 512 + sub;
