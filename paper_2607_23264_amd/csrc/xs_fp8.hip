@@ -127,9 +127,11 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const uint16_t* __re
 // this takes 105 (16,381 rows of 7168 both ways: 4.5 TB/s, a copy's rate being 5.2).
 constexpr int kPitchT = 144;
 // Regions in order: 32 row blocks of a column block, then the next column block, so that the 128-byte
-// pieces of a transposed row are written together. Measured with 1 / 4 / 8 / 32 / 128 row blocks (16,384
-// rows of 7168): transposed 87.6 / 89.3 / 89.0 / 78.3 / 78.7 us, both ways 107.6 / 109.1 / 108.1 / 105.2 /
-// 109.1, tiles both ways 105.5 / 104.2 / 100.4 / 97.0 / 98.4, tiles alone 67.2 / 67.1 / 67.9 / 68.8 / 72.8.
+// pieces of a transposed row are written together; each XCD (consecutive workgroups go to different ones)
+// takes four consecutive row blocks, whose scales of a column are neighbours. Measured with 16 / 32 / 64 /
+// 128 row blocks (16,384 rows of 7168): transposed 87.0 / 77.8 / 76.0 / 73.9 us, both ways 109.1 / 105.2 /
+// 107.6 / 107.0, tiles both ways 100.0 / 94.6 / 97.4 / 96.8, tiles alone 68.1 / 68.2 / 70.4 / 72.6; with
+// consecutive row blocks on different XCDs 78.6, 105.6, 96.9, 68.5.
 constexpr int kGroupR = 32;
 struct RegionArgs {
   const uint16_t* x;
@@ -152,14 +154,13 @@ __global__ __launch_bounds__(256, 4) void quantize_region_kernel(RegionArgs a) {
   __shared__ __attribute__((aligned(16))) uint32_t red[4][64];     // per wave: column maxima (packed pairs)
   __shared__ __attribute__((aligned(16))) float2 col_s[COLS && !TILE ? 128 : 1];
   const int tid = threadIdx.x, w = tid >> 6, rg = tid >> 4, cg = tid & 15;
-  // kGroupR row blocks of a column block after one another, then the next column block
   const int64_t id = block_number(), per_group = static_cast<int64_t>(kGroupR) * a.col_blocks;
   const int64_t first = id / per_group * kGroupR, in = id % per_group;
   const int64_t left = (a.rows + 127) / 128 - first;
   if (left <= 0) return;                            // the whole workgroup (surplus of the grid)
   const int gm = static_cast<int>(min(left, static_cast<int64_t>(kGroupR)));
   const int cb = static_cast<int>(in / gm);
-  const int64_t rb = first + in % gm;
+  const int64_t rb = first + (gm == kGroupR ? in % 8 * (kGroupR / 8) + in / 8 % (kGroupR / 8) : in % gm);
   if (cb >= a.col_blocks) return;
   const int64_t row0 = rb * 128;
   const int col = cb * 128 + cg * 8;
