@@ -324,6 +324,10 @@ bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t
 
 typedef f8::Tile<256, 256, 2, 4> Big;
 typedef f8::Tile<128, 128, 2, 2> Mid;
+// For tiles that have a CU to themselves: four stages, since a K block's products (0.2 us) are much shorter than a
+// load's way (1024 x 4096 x 7168: 43.5 us with two stages, 35.7; 512 rows 43.4, in 64 x 128 27.2).
+typedef f8::Tile<128, 128, 4, 2, 4> Deep;
+typedef f8::Tile<64, 128, 2, 2, 4> Low;
 
 template <int NB, int NJ, int kDepth, bool ROW, bool SWIGLU, bool F32>
 int launch_split(const f8::GemmArgs& p, hipStream_t st) {
@@ -346,17 +350,20 @@ int launch_tiles(f8::GemmArgs p, int per_cu, hipStream_t st) {
   return xs_host::launch_status();
 }
 
-enum Form { kSplit12, kSplit21, kSplit22, kSplit24, kSplit44, kMid, kBig };
+enum Form { kSplit12, kSplit21, kSplit22, kSplit24, kSplit44, kLow, kDeep, kMid, kBig };
 
 // The cheapest form by a model of its time in us, from M, N, K and the CU count (grouped: with exponential
 // segment lengths, n / (1 - exp(-rows n / M)) row blocks of n segments). A split form takes its rounds of
 // workgroups, each a start and a join that grow with its outputs, and its rows of K bytes at the rate of a
-// CU's memory path; tiles take K / 128 blocks a round, of one 256 x 256 or up to two 128 x 128 tiles a CU.
-// Weights past the caches (grouped products that touch over 100 MB) come more slowly. Measured, us, split
-// 1x2 / 2x4 / 4x4, 128- and 256-tiles, N = 4096, K = 7168: M = 24 8.4 / 12.0 / 16.8 / 37 / 71; 128 26 / 13.5 / 18.6 / 42 /
-// 71; 512 93 / 45 / 34 / 45 / 74; 2048 - / 171 / 131 / 62 / 82; 4093 - / - / - / 134 / 118. K = 512, M = 1024: - / 24 / 19 / 8.7 / 12.
-// 32 segments, K = 7168: 64 rows in all 137 / 131 / 141 / 141 / 179; 1024 342 / 211 / 197 / 160 / 196; 16,384 - / - / 1299 /
-// 763 / 556.
+// CU's memory path; tiles take K / 128 blocks a round, of one 256 x 256, up to two 128 x 128 or one tile of four
+// stages a CU. Weights past the caches (grouped products that touch over 100 MB) come more slowly. Measured, us,
+// split 1x2 / 2x4 / 4x4, 64 x 128 and 128 x 128 of four stages, 128- and 256-tiles, N = 4096, K = 7168:
+//   M = 24  8.4 / 12.0 / 16.8 / 25 / 24 / 37 / 71        M = 128  26 / 13.3 / 18.1 / 25.6 / 27.8 / 42 / 71
+//   M = 512  93 / 46 / 35 / 27.2 / 28.3 / 43 / 74        M = 1024  - / 86 / 67 / 52 / 35.7 / 44 / -
+//   M = 2048  - / 171 / 131 / 101 / 71 / 62 / 82         M = 4093  - / - / - / 198 / 146 / 134 / 105
+//   K = 1024: M = 512  - / 16.3 / 12.6 / 8.3 / 9.2 / 11.1 / -
+// 32 segments with SwiGLU: 64 rows in all  137 / 128 / 137 / 127 / 129 / 143 / 178; 1024  342 / 211 / 197 / 170 /
+// 163 / 159 / 189; 8192  - / 909 / 701 / 496 / 371 / 346 / 323.
 Form choose(const f8::GemmArgs& p, bool swiglu, bool f32) {
   const double cus = xs_host::persistent_grid(0), nk = p.K / 128, n_out = swiglu ? p.N / 2 : p.N;
   const double segs = p.seg_off ? std::min(p.n_seg, p.M) : 1;
@@ -390,6 +397,21 @@ Form choose(const f8::GemmArgs& p, bool swiglu, bool f32) {
   const double part = rest == 0 ? 0 : rest <= 1 ? 0.62 : 0.62 + 0.48 * (rest - 1);
   offer(kMid, 6 + nk * (std::floor(mid / (2 * cus)) * 1.1 + part) * (f32 ? 1.75 : far ? 1.2 : 1));
   if (!f32) {                                            // exact sums do not fit its registers
+    // one tile a CU at a time; grouped, a round's end is not the same for all, half a round lost on the average
+    const auto lone = [&](Form f, int rows, double start, double per, double full, double far_per) {
+      const double nt = std::ceil(p.N / 128.);
+      double us = 0;
+      if (segs > 1) {
+        const double x = segs / (1 - std::exp(-rows * segs / p.M)) * nt / cus, rounds = x <= 1.05 ? 1 : x + 0.5;
+        us = start + nk * (far ? far_per : full) * rounds + 5 * (rounds - 1);
+      } else {
+        const double x = blocks(rows) * nt / cus, whole = std::floor(x), rest = x - whole;
+        us = start + nk * (whole * full + (rest == 0 ? 0 : per + (full - per) * std::max(0., 2 * rest - 1))) + 5 * (std::ceil(x) - 1);
+      }
+      offer(f, us);
+    };
+    lone(kLow, 64, 5.2, 0.37, 0.395, 0.56);
+    lone(kDeep, 128, 6.3, 0.38, 0.51, 0.62);
     const double big = tiles(256, 256), left = std::fmod(big, cus) / cus;
     offer(kBig, 6 + nk * (std::floor(big / cus) * 1.85 + (left == 0 ? 0 : 1.25 + 0.6 * left)));
   }
@@ -405,6 +427,10 @@ int launch(const f8::GemmArgs& p, hipStream_t st) {
     case kSplit22: return launch_split<2, 2, 3, ROW, SWIGLU, F32>(p, st);
     case kSplit24: return launch_split<2, 4, 2, ROW, SWIGLU, F32>(p, st);
     case kSplit44: return launch_split<4, 4, 2, ROW, SWIGLU, F32>(p, st);
+    case kLow:
+      if constexpr (!F32) return launch_tiles<Low, ROW, SWIGLU, F32>(p, 1, st);
+    case kDeep:
+      if constexpr (!F32) return launch_tiles<Deep, ROW, SWIGLU, F32>(p, 1, st);
     case kMid: return launch_tiles<Mid, ROW, SWIGLU, F32>(p, 2, st);
     case kBig:
       if constexpr (!F32) return launch_tiles<Big, ROW, SWIGLU, F32>(p, 1, st);

@@ -22,7 +22,7 @@
 // 128 x 128 tiles, 4096 x 7168 x 4096 (235 us): two conversions and two multiplications by scales for each MFMA, of whose
 // 15.0 ns issuing these five instructions takes 12.1.
 //
-// LDS: two stages of one K block, A rows then B rows of 128 bytes (16-byte piece c of row r at c ^ ((r >>
+// LDS: two stages (four where a tile has a CU to itself) of one K block, A rows then B rows of 128 bytes (16-byte piece c of row r at c ^ ((r >>
 // 1) & 7): the 16 rows of a fragment read hit 16 distinct bank groups), and two buffers of scales, each
 // the 16 bytes of four blocks per row. All arrive by direct global -> LDS loads.
 #pragma once
@@ -69,16 +69,17 @@ __device__ __forceinline__ f32x4 block_sum(const Wide& b, const Wide& a) {
 __device__ __forceinline__ void as_operand(v8i v, v8i& out) { out = v; }
 __device__ __forceinline__ void as_operand(v8i v, Wide& out) { out = widen(v); }
 
-template <int BM_, int BN_, int WM_, int WN_>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_ = 2>
 struct Tile {
-  static constexpr int kBM = BM_, kBN = BN_, kWM = WM_, kWN = WN_;
+  static constexpr int kBM = BM_, kBN = BN_, kWM = WM_, kWN = WN_, kStages = STAGES_;
+  static_assert(STAGES_ == 2 || STAGES_ == 4, "a stage's buffer by masking; scales come four blocks at a time");
   static constexpr int kWaves = WM_ * WN_, kThreads = kWaves * 64;
   static constexpr int kMI = BM_ / WM_ / 16, kNJ = BN_ / WN_ / 16;
   static constexpr int kALoads = BM_ / 8 / kWaves, kBLoads = BN_ / 8 / kWaves;   // 8 rows a load
-  static constexpr int kSLoads = (BM_ + BN_) / 64 / kWaves;                      // 64 rows' scales a load
+  static constexpr int kSParts = (BM_ + BN_) / 64, kSLoads = (kSParts + kWaves - 1) / kWaves;   // 64 rows' scales a load
   static constexpr int kStage = (BM_ + BN_) * 128, kScales = (BM_ + BN_) * 16;
   static constexpr int kPitch = (BN_ + 8) * 2;                                   // staged bf16 output row
-  static constexpr int kOperands = 2 * kStage + 2 * kScales, kOut = BM_ * kPitch;
+  static constexpr int kOperands = kStages * kStage + 2 * kScales, kOut = BM_ * kPitch;
   static constexpr int kLds = kOperands > kOut ? kOperands : kOut;
   typedef f32x4 Acc[kMI][kNJ];
 };
@@ -129,7 +130,10 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
 #pragma unroll
   for (int i = 0; i < T::kSLoads; ++i) {
     const int r0 = 64 * (T::kWaves * i + w);
-    if (r0 < T::kBM) {
+    if (T::kSParts % T::kWaves && r0 >= T::kBM + T::kBN) {
+      rs[i] = buffer_rsrc(p.b_s, 0);        // (not loaded)
+      os[i] = 0;
+    } else if (r0 < T::kBM) {
       rs[i] = buffer_rsrc(p.a_s, span(p.rows, p.lda_s * 4, s_bytes));
       os[i] = static_cast<uint32_t>((r0 + lane) * p.lda_s * 4);
     } else {
@@ -140,10 +144,11 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
       os[i] = static_cast<uint32_t>(((ROW ? n : n / 128) - first) * p.ldb_s * 4);
     }
   }
-  char* const scales = lds + 2 * T::kStage;
+  constexpr int kStages = T::kStages;
+  char* const scales = lds + kStages * T::kStage;
   lds_char* const to = (lds_char*)lds + w * 1024;
   const auto issue_one = [&](int kt, int n) {
-    lds_char* const st = to + (kt & 1) * T::kStage;
+    lds_char* const st = to + (kt & (kStages - 1)) * T::kStage;
     if (n < T::kALoads) load_lds16(ra, oa[n], kt * 128, st + T::kWaves * n * 1024);
     else load_lds16(rb, ob[n - T::kALoads], kt * 128, st + T::kBM * 128 + T::kWaves * (n - T::kALoads) * 1024);
   };
@@ -155,7 +160,8 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
   const auto issue_scales = [&](int g) {
 #pragma unroll
     for (int i = 0; i < T::kSLoads; ++i)
-      load_lds16(rs[i], os[i], g * 16, to + 2 * T::kStage + (g & 1) * T::kScales + T::kWaves * i * 1024);
+      if (T::kSParts % T::kWaves == 0 || T::kWaves * i + w < T::kSParts)
+        load_lds16(rs[i], os[i], g * 16, to + kStages * T::kStage + (g & 1) * T::kScales + T::kWaves * i * 1024);
   };
   const int l16 = lane & 15, g4 = lane >> 4, swz = (l16 >> 1) & 7;
   const int ar = wm * T::kMI * 16 + l16, br = wn * T::kNJ * 16 + l16;
@@ -196,6 +202,12 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
 #pragma unroll
     for (int c = 0; c < 4; ++c) acc[i][j][c] = __builtin_fmaf(v[i & 1][j][c], s, acc[i][j][c]);
   };
+  // Waits for the next stage's loads: of those issued since, all kStages - 2 stages' may still fly, but near the
+  // end, where there are fewer, none (scales are issued before their first stage: they have landed too).
+  const auto landed = [&](auto issue_c) {
+    constexpr int kFly = decltype(issue_c)::value ? (kStages - 2) * (T::kALoads + T::kBLoads) : 0;
+    wait_vm<kFly>();
+  };
   // One K block. Row block i's MFMAs are each followed by the multiply-adds of row block i - 1's sums (the
   // last one's in the next stage), and by reads or loads that run ahead: the next row block's fragment;
   // in the last row block, behind the barrier, the next stage's weight fragments, each into the registers
@@ -203,17 +215,18 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
   // buffers, which every wave has read.
   const auto stage = [&](int kt, auto next_c, auto issue_c) {
     constexpr bool kNext = decltype(next_c)::value, kIssue = decltype(issue_c)::value;
-    const char* const st = lds + (kt & 1) * T::kStage;
-    const char* const nx = lds + ((kt + 1) & 1) * T::kStage;
+    const char* const st = lds + (kt & (kStages - 1)) * T::kStage;
+    const char* const nx = lds + ((kt + 1) & (kStages - 1)) * T::kStage;
     // (a branch further down would let the compiler sink the multiply-adds behind it, all sums live)
     if constexpr (kIssue)
-      if (((kt + 2) & 3) == 0) issue_scales((kt + 2) >> 2);
+      if (((kt + kStages) & 3) == 0) issue_scales((kt + kStages) >> 2);
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
       const int pi = (i + kMI - 1) % kMI;
       __builtin_amdgcn_sched_barrier(0);
       if (i == kMI - 1 && kNext) {
-        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): the next stage has landed, this one is read
+        landed(issue_c);                      // the next stage; and this one is read
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -238,7 +251,7 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
           if constexpr (kIssue) {
 #pragma unroll
             for (int n = 0; n < kPerStep; ++n)
-              if (j * kPerStep + n < T::kALoads + T::kBLoads) issue_one(kt + 2, j * kPerStep + n);
+              if (j * kPerStep + n < T::kALoads + T::kBLoads) issue_one(kt + kStages, j * kPerStep + n);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -259,19 +272,28 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
       }
     }
   };
-  issue(0);
+  const std::true_type yes;
+  const std::false_type no;
   issue_scales(0);
-  wait_vm0();
+  if (nk >= kStages) {
+#pragma unroll
+    for (int kt = 0; kt < kStages; ++kt) issue(kt);
+    wait_vm<(kStages - 1) * (T::kALoads + T::kBLoads)>();
+  } else {
+    for (int kt = 0; kt < nk; ++kt) issue(kt);
+    wait_vm<0>();
+  }
   __builtin_amdgcn_s_barrier();
-  if (nk > 1) issue(1);
   if (p.rows <= wm * kMI * 16) {
     // no row of this wave's is valid: its loads and barriers only, the SIMD's other wave has the matrix unit
     // (32 experts' 32,768 rows 931 -> 917 us)
     for (int kt = 0; kt + 1 < nk; ++kt) {
-      if (kt + 2 < nk && ((kt + 2) & 3) == 0) issue_scales((kt + 2) >> 2);
-      wait_vm0();
+      const bool more = kt + kStages < nk;
+      if (more && ((kt + kStages) & 3) == 0) issue_scales((kt + kStages) >> 2);
+      if (more) landed(yes);
+      else landed(no);
       __builtin_amdgcn_s_barrier();
-      if (kt + 2 < nk) issue(kt + 2);
+      if (more) issue(kt + kStages);
     }
     __syncthreads();
     return;
@@ -284,14 +306,9 @@ __device__ __forceinline__ void mainloop(const Product& p, typename T::Acc& acc,
   for (int j = 0; j < kNJ; ++j) v[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int h = 0; h < kF; ++h) f[1][h] = 0.f;
-  const std::true_type yes;
-  const std::false_type no;
   int kt = 0;
-  for (; kt + 2 < nk; ++kt) stage(kt, yes, yes);
-  if (kt + 1 < nk) {
-    stage(kt, yes, no);
-    ++kt;
-  }
+  for (; kt + kStages < nk; ++kt) stage(kt, yes, yes);
+  for (; kt + 1 < nk; ++kt) stage(kt, yes, no);
   stage(kt, no, no);
 #pragma unroll
   for (int j = 0; j < kNJ; ++j) add(kMI - 1, j);

@@ -442,3 +442,11 @@ def test_more_columns_than_a_grid_of_the_split_form_has():
     assert torch.equal(c[0, :1 << 28].view(-1, n), want.expand(1 << 8, n)) and torch.equal(c[0, 1 << 28:], want[:8])
     del a, b, c, sb, base
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("M,N,blocks", [(384, 4096, 1), (391, 4088, 2), (450, 4096, 3), (333, 4104, 5), (401, 4096, 8), (500, 2048, 18),
+                                        (700, 4096, 2), (769, 4088, 3), (900, 4096, 4), (1000, 3976, 5), (1024, 4096, 9), (257, 7168, 11)])
+@pytest.mark.parametrize("block", ["tile", "row"])
+def test_gemm_of_about_a_tile_to_a_cu(M, N, blocks, block):
+    """Fewer blocks of K than stages, as many, more; whole and ragged last tiles."""
+    test_gemm(M, N, blocks * B, block, "bf16")
