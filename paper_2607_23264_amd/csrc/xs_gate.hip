@@ -334,8 +334,8 @@ __device__ __forceinline__ void load_run(const void* base, int first, int VP, in
   }
 }
 
-// Sixteen lanes per token, four tokens per wave; lane `sub` has the VP = ceil(E / 16) consecutive experts
-// from VP sub on, so a group is whole lanes (E % 16 == 0 where there are groups, of 1, 2, 4 or 8 lanes).
+// Sixteen lanes per token, four tokens per wave. A group of experts has 16 / n_group whole lanes, each with up to VP
+// = ceil(E / n_group / lanes) of its consecutive experts; lanes are in the experts' order.
 //
 // The k largest keys are found by a sorting network on 32-bit words, each a key cut to 14 bits with its
 // expert; then every lane looks up one of them whole. Their order is the 64-bit one where it is clear: with s
@@ -365,13 +365,15 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
   const bool live = t_raw < g.T;
   const int64_t t = live ? t_raw : g.T - 1;   // every lane takes part in its row's reductions
   const char* const row = logit_row<LT>(g.logits, g.ld, t);
-  const int first = (FULL ? VPL : VP) * sub;
+  const int lanes = 16 / g.n_group;         // of a group
+  const int group_end = g.E / g.n_group * ((sub >> __builtin_ctz(lanes)) + 1);
+  const int first = FULL ? VPL * sub : group_end - g.E / g.n_group + VP * (sub & (lanes - 1));
   constexpr bool by_logit = MODE == kByLogit;
   const bool softmax = by_logit ? g.score == XS_SCORE_SOFTMAX : MODE == kSoftmax;
   constexpr float kMasked = static_cast<float>(kMaskedKey), kDropped = 1.5f * kMasked;
   constexpr int kDroppedKey = static_cast<int>(0xFF400000u) ^ 0x7FFFFFFF;
   float v[VPL];
-  load_run<VPL, LT, FULL>(row, first, VP, g.E, vec, -INFINITY, v);
+  load_run<VPL, LT, FULL>(row, first, VP, group_end, vec, -INFINITY, v);
   float m = 0.f, inv = 1.f, sigma = 0x1p-22f;
   if (softmax) {
     m = -INFINITY;
@@ -397,16 +399,15 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
     float b[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) b[i] = 0.f;
-    if (!by_logit && g.bias) load_run<VPL, float, FULL>(g.bias, first, VP, g.E, bias_vec, 0.f, b);
+    if (!by_logit && g.bias) load_run<VPL, float, FULL>(g.bias, first, VP, group_end, bias_vec, 0.f, b);
 #pragma unroll
     for (int i = 0; i < VPL; ++i)
-      o[i] = FULL || (i < VP && first + i < g.E) ? ordered(key_of(v[i], b[i])) : kDroppedKey;
+      o[i] = FULL || (i < VP && first + i < group_end) ? ordered(key_of(v[i], b[i])) : kDroppedKey;
   }
   const auto key_at = [&](int i) { return from_ordered(o[i]); };
   bool kept = true;                         // the lane's group
   bool unsure = false;
   if (g.n_group > 1) {
-    const int lanes = 16 / g.n_group;
     int a = kNoKey, b = kNoKey;             // the group's two largest keys
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
@@ -738,11 +739,11 @@ int gate_ok(const xs_gate* g, const void* logits, int64_t ld, int32_t T) {
 
 template <typename LT, int VPL, int KL, int MODE>
 void launch_rows(const GateArgs& a, size_t lds, hipStream_t st) {
-  const int VP = (a.E + 15) / 16;
+  const int lanes = 16 / a.n_group, Eg = a.E / a.n_group, VP = (Eg + lanes - 1) / lanes;
   constexpr int kPiece = sizeof(LT) == 2 && VPL >= 8 ? 8 : 4;
-  // whole pieces: of each lane's run, and (the last lane's) of the row
-  const int vec = VP % kPiece == 0 && a.E % kPiece == 0 && a.ld % kPiece == 0 && aligned_to(a.logits, kPiece * sizeof(LT));
-  const int bias_vec = VP % 4 == 0 && a.E % 4 == 0 && aligned_to(a.bias, 16);
+  // whole pieces: of each lane's run, and (the last lane's) of the group
+  const int vec = VP % kPiece == 0 && Eg % kPiece == 0 && a.ld % kPiece == 0 && aligned_to(a.logits, kPiece * sizeof(LT));
+  const int bias_vec = VP % 4 == 0 && Eg % 4 == 0 && aligned_to(a.bias, 16);
   const dim3 grid = xs_host::grid_of((static_cast<int64_t>(a.T) + 15) / 16);
   if (a.E == 16 * VPL && vec && bias_vec)
     hipLaunchKernelGGL((gate_rows_kernel<LT, VPL, KL, MODE, true>), grid, dim3(256), lds, st, a, VP, vec, bias_vec);
@@ -764,9 +765,10 @@ void launch_rows(const GateArgs& a, size_t lds, hipStream_t st) {
 
 template <typename LT>
 void launch_rows(const GateArgs& a, size_t lds, hipStream_t st) {
-  if (a.E <= 64) launch_rows<LT, 4>(a, lds, st);
-  else if (a.E <= 128) launch_rows<LT, 8>(a, lds, st);
-  else if (a.E <= 256) launch_rows<LT, 16>(a, lds, st);
+  const int lanes = 16 / a.n_group, VP = (a.E / a.n_group + lanes - 1) / lanes;
+  if (VP <= 4) launch_rows<LT, 4>(a, lds, st);
+  else if (VP <= 8) launch_rows<LT, 8>(a, lds, st);
+  else if (VP <= 16) launch_rows<LT, 16>(a, lds, st);
   else launch_rows<LT, 32>(a, lds, st);
 }
 
@@ -808,9 +810,9 @@ extern "C" int xs_route_gate(const xs_gate* g, const void* logits, int64_t ld, i
   hipStream_t st = static_cast<hipStream_t>(stream);
   const size_t lds = 4 * sizeof(double) * g->E;
   // Sixteen lanes per token where each lane has at most 32 consecutive experts and groups are whole lanes;
-  // one wave per token otherwise (32,768 tokens, top-8 of 256 in groups: 18 us against 120).
-  const bool whole_lanes = a.n_group == 1 || (a.E % 16 == 0 && 16 % a.n_group == 0);
-  if (a.E <= 512 && a.k <= 16 && whole_lanes) {
+  // one wave per token otherwise (32,768 tokens, top-8 of 256 in groups: 18 us against 120; 16,384, top-4 of 60 in
+  // 4 groups: 8.4 against 18).
+  if (a.E <= 512 && a.k <= 16 && 16 % a.n_group == 0) {
     if (g->logits_type == XS_TYPE_BF16) launch_rows<uint16_t>(a, lds, st);
     else launch_rows<float>(a, lds, st);
     return xs_host::launch_status();

@@ -290,3 +290,13 @@ def test_lowest_keys_come_before_masked_ones(E, k, dtype):
     l = l.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
     idx, _ = _route(_gate(E, k, "softmax", renorm=True, dtype=dtype), l.cuda(), 3)
     assert np.array_equal(idx, gate.route(l.double().numpy(), k, "softmax", renorm=True)[0])
+
+
+@pytest.mark.parametrize("E,k,n_group,topk_group,top2", [(30, 4, 2, 1, True), (36, 5, 4, 2, False), (40, 6, 8, 3, True), (48, 4, 16, 5, True),
+                                                         (500, 9, 4, 3, True), (502, 16, 2, 1, False), (504, 8, 8, 4, True), (12, 2, 4, 2, True),
+                                                         (8, 2, 8, 3, False), (264, 7, 8, 5, True), (2, 1, 2, 1, True)])
+@pytest.mark.parametrize("kind,dtype,biased", [("sigmoid", "f32", True), ("softmax", "bf16", False), ("softmax", "f32", True), ("sigmoid", "bf16", True)])
+def test_groups_that_do_not_fill_their_lanes(E, k, n_group, topk_group, top2, kind, dtype, biased):
+    test_selection_and_weights(E, k, n_group, topk_group, top2, kind, dtype, biased, True, 1.5)
+    if E >= 14 and topk_group * (E // n_group) >= 6:               # that test's one unmasked expert, and its k
+        test_ties_masks_and_scores_an_ulp_apart(E, n_group, topk_group, top2, kind, biased)
