@@ -343,8 +343,8 @@ __device__ __forceinline__ void load_run(const void* base, int first, int VP, in
 // in the right order, so no other key may come that near to the last of the k, and no neighbours among them.
 // Elsewhere (one token in a hundred for 256 sigmoid scores, by the cut) the keys within reach of the last,
 // if they are at most sixteen, are done again in 64 bits, one a lane; so are the groups' scores where it is
-// unclear which are kept. What remains (softmax scores, whose sum would have to be in 64 bits too, more
-// candidates, a group's second key too near its third) is done again by the token's whole wave (gate_token).
+// unclear which are kept. What remains (more candidates, a group's second key too near its third) is done again
+// by the token's whole wave (gate_token).
 // Without a bias the logits are the keys, exactly (bf16 ones also when cut).
 //
 // Bound by vector instructions (32,768 tokens, top-8 of 256 biased sigmoid scores in groups: 850 for four
@@ -406,6 +406,24 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
   }
   const auto key_at = [&](int i) { return from_ordered(o[i]); };
   bool kept = true;                         // the lane's group
+  // In doubt: a score in 64 bits, of a softmax with its row's sum (by the token's sixteen lanes).
+  const auto sum64 = [&]() -> double {
+    if (!softmax) return 1.;
+    double s = 0.;
+#pragma unroll 4
+    for (int i = 0; i < VPL; ++i)
+      if (FULL || (i < VP && first + i < group_end)) {
+        const float l = load_logit<LT>(row, first + i);
+        if (l != -INFINITY) s += exp(static_cast<double>(l) - static_cast<double>(m));
+      }
+    s += dpp64<kRor8>(s);
+    s += dpp64<kRor4>(s);
+    s += dpp64<kRor2>(s);
+    return s + dpp64<kRor1>(s);
+  };
+  const auto score64 = [&](float l, double sum) -> double {
+    return softmax ? exp(static_cast<double>(l) - static_cast<double>(m)) / sum : 1. / (1. + exp(-static_cast<double>(l)));
+  };
   bool unsure = false;
   if (g.n_group > 1) {
     int a = kNoKey, b = kNoKey;             // the group's two largest keys
@@ -470,10 +488,11 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
         k3 = fmaxf(k3, o3);
       }
       const float used = g.top2 && k2 > kMasked ? k2 : k1, unused = g.top2 ? k3 : k2;
-      bool fine = !softmax && (unused <= kMasked || used - unused > 2.f * sigma + 0x1p-22f * fmaxf(fabsf(used), fabsf(unused)));
+      const bool fine = unused <= kMasked || used - unused > 2.f * sigma + 0x1p-22f * fmaxf(fabsf(used), fabsf(unused));
+      const double sum = by_logit ? 1. : sum64();
       const auto exact = [&](float k, int e) -> double {
         if (k <= kMasked) return kMaskedKey;
-        const double x = 1. / (1. + exp(-static_cast<double>(load_logit<LT>(row, e))));
+        const double x = score64(load_logit<LT>(row, e), sum);
         return finite_key(g.bias ? x + static_cast<double>(g.bias[e]) : x, false);
       };
       const double d1 = exact(k1, e1), d2 = exact(k2, e2), most = fmax(d1, d2);
@@ -544,7 +563,8 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
     }
     const int n = __shfl(at, 15, 16);
     at -= c;
-    const bool few = doubt && n <= 16 && last > kMasked && tol >= 0.f && (by_logit || !softmax);
+    const bool few = doubt && n <= 16 && last > kMasked && tol >= 0.f;
+    const double sum = by_logit ? 1. : sum64();
     unsure |= doubt && !few;
     if (few) {
 #pragma unroll
@@ -558,7 +578,7 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
     }
     double kd = -INFINITY;
     if (few && sub < n) {
-      const double x = by_logit ? static_cast<double>(l) : 1. / (1. + exp(-static_cast<double>(l)));
+      const double x = by_logit ? static_cast<double>(l) : score64(l, sum);
       kd = finite_key(g.bias ? x + static_cast<double>(g.bias[e]) : x, l == -INFINITY || l != l);
     }
     int r0 = 0;
