@@ -79,9 +79,17 @@ def product_bound(A, B, exact):
     A, B = np.abs(A), np.abs(B)
     bound = 2 * (128 + K // BLOCK + 11) * 2.0 ** -24 * (A @ B.T)
     if not exact:
-        for k in range(0, K, 8):
-            largest = np.zeros((A.shape[0], B.shape[0]))
-            for i in range(k, k + 8):
-                np.maximum(largest, A[:, i, None] * B[None, :, i], out=largest)
-            bound += 2.0 ** -10 * largest
+        # in fp32, 64 rows at a time (memory that stays in a cache); a scaling by powers of two keeps it in range
+        sa, sb = (2.0 ** -np.floor(np.log2(max(X.max(), 2.0 ** -1000))) for X in (A, B))
+        a, b = ((X * s).astype(np.float32).T.copy() for X, s in ((A, sa), (B, sb)))
+        for r in range(0, A.shape[0], 64):
+            total = np.zeros((min(64, A.shape[0] - r), B.shape[0]), dtype=np.float32)
+            largest, product = np.empty_like(total), np.empty_like(total)
+            for k in range(0, K, 8):
+                np.multiply(a[k, r:r + 64, None], b[k], out=largest)
+                for i in range(k + 1, min(k + 8, K)):
+                    np.multiply(a[i, r:r + 64, None], b[i], out=product)
+                    np.maximum(largest, product, out=largest)
+                total += largest
+            bound[r:r + 64] += 2.0 ** -10 * (1 + K * 2.0 ** -24) * total / sa / sb
     return bound
