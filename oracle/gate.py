@@ -64,7 +64,7 @@ def backward(logits, idx, d_w, kind, renorm=False, scale=1.0):
     count as absent."""
     l = np.asarray(logits, dtype=np.float64)
     T, E = l.shape
-    s = scores(l, kind)
+    s, rest = scores(l, kind), scores(-l, "sigmoid")     # rest: 1 - sigmoid, near 1 too
     grad, mag = np.zeros((T, E)), np.zeros((T, E))
     for t in range(T):
         slots = [(int(e), float(g) * scale) for e, g in zip(idx[t], d_w[t]) if 0 <= e < E]
@@ -79,8 +79,8 @@ def backward(logits, idx, d_w, kind, renorm=False, scale=1.0):
                 terms.append((e, g, abs(g)))
         if kind == "sigmoid":
             for e, d, a in terms:
-                grad[t, e] += d * s[t, e] * (1 - s[t, e])
-                mag[t, e] += a * s[t, e]
+                grad[t, e] += d * s[t, e] * rest[t, e]
+                mag[t, e] += a * s[t, e] * rest[t, e]
         else:
             shared = 0.0 if renorm else sum(d * s[t, e] for e, d, _ in terms)
             grad[t] -= s[t] * shared

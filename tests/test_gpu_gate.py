@@ -300,3 +300,25 @@ def test_groups_that_do_not_fill_their_lanes(E, k, n_group, topk_group, top2, ki
     test_selection_and_weights(E, k, n_group, topk_group, top2, kind, dtype, biased, True, 1.5)
     if E >= 14 and topk_group * (E // n_group) >= 6:               # that test's one unmasked expert, and its k
         test_ties_masks_and_scores_an_ulp_apart(E, n_group, topk_group, top2, kind, biased)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_gradient_of_saturated_sigmoids(dtype, renorm):
+    """Scores near 1 keep their slope, about e^-l, to a relative error: logits of 8 to 30 and of -30 to -8. Two
+    exponentials, two quotients and three products are below 2^-20 of a slope's terms; renormalized, the difference
+    g - sum g r adds 2^-19 of them (r as the weights: three roundings of an exponential, a quotient, a sum of four)."""
+    T, E, k = 24, 64, 4
+    g = torch.Generator().manual_seed(7)
+    l = torch.rand((T, E), generator=g) * 22 + 8
+    l[T // 2:] *= -1
+    l = l.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    l64 = l.double().numpy()
+    idx = gate.select(l64, k, "sigmoid")
+    idx[3] = [9, 9, 9, 10]
+    d_w = np.random.default_rng(3).standard_normal((T, k)).astype(np.float32)
+    got, status = _backward(_gate(E, k, "sigmoid", renorm=renorm, scale=2.5, dtype=dtype), _device(l, E), T, idx, d_w)
+    assert status == 0
+    want, mag = gate.backward(l64, idx, d_w, "sigmoid", renorm, 2.5)
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    assert np.all(np.abs(got - want) <= half * np.abs(want) + 2.0 ** -18 * mag)

@@ -68,3 +68,11 @@ def test_gradient_of_rows_without_weights():
         for renorm in (False, True):
             grad, _ = gate.backward(l, np.array([[0, 1]]), np.ones((1, 2)), kind, renorm)
             assert not grad.any()
+
+
+def test_gradient_of_saturated_sigmoids():
+    """s (1 - s) = 1 / (2 + e^l + e^-l) where 1 - s cancels in 64 bits too."""
+    l = np.array([[40.0, 30.0, -40.0, 8.0]])
+    grad, mag = gate.backward(l, np.array([[0, 1, 2, 3]]), np.ones((1, 4)), "sigmoid")
+    want = 1 / (2 + np.exp(l) + np.exp(-l))
+    assert np.allclose(grad, want, rtol=1e-14, atol=0) and np.allclose(mag, want, rtol=1e-14, atol=0)
