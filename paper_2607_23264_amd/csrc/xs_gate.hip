@@ -683,15 +683,15 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs g) {
   }
   // of a slot: its own term, and (whole) its expert's score and what every element gets by its score
   float add, s_j = 0.f, shared = 0.f;
+  // 1 - s of a sigmoid as 1 / (1 + e^l): the difference loses a score near 1 (6 % of the slope at l = 16, all from 17 on)
+  const float rest = softmax ? 1.f : 1.f / (1.f + expf(l_j));
   if (g.renorm) {
     const float r = renormalized<LPT>(softmax, e_j >= 0, l_j);
-    add = (gj - lanes_sum<LPT>(gj * r)) * r;
-    if (!softmax) add *= 1.f / (1.f + expf(l_j));
+    add = (gj - lanes_sum<LPT>(gj * r)) * r * rest;
   } else {
     s_j = slot_score(softmax, e_j >= 0, l_j, m, inv);
     if (softmax) shared = lanes_sum<LPT>(gj * s_j);
-    // 1 - s of a sigmoid as 1 / (1 + e^l): the difference loses a score near 1 (6 % of the slope at l = 16, all from 17 on)
-    add = softmax ? gj : gj * s_j / (1.f + expf(l_j));
+    add = softmax ? gj : gj * s_j * rest;
   }
   float sum = 0.f;                          // over the slots of the same expert
   for (int j = 0; j < g.k; ++j) {
