@@ -51,8 +51,10 @@ __device__ __forceinline__ const char* logit_row(const void* logits, int64_t ld,
 }
 
 // Keys lie within 2^127: a masked expert (logit -inf or NaN, key NaN or below) has the lowest, and one
-// outside the chosen groups a lower value yet.
-constexpr double kMaskedKey = -0x1p127;
+// outside the chosen groups a lower value yet. A group's score may be the sum of two keys; one without an unmasked
+// expert has at most every such sum (in fp32 the sum of the two lowest, -FLT_MAX; in 64 bits below all).
+constexpr double kMaskedKey = -0x1p127, kDeadGroup = -0x1p129;
+constexpr float kDeadGroup32 = -3.40282346638528859812e+38f;
 __device__ __forceinline__ double finite_key(double key, bool masked) {
   return masked || !(key > kMaskedKey) ? kMaskedKey : fmin(key, -kMaskedKey);
 }
@@ -191,7 +193,8 @@ __device__ void gate_token(const GateArgs& g, int64_t t, double* key) {
       b = fmax(fmin(a, oa), fmax(b, ob));
       a = fmax(a, oa);
     }
-    double left = __shfl(g.top2 && b > kMaskedKey ? a + b : a, (lane * lanes) & 63);
+    const double total = a <= kMaskedKey ? kDeadGroup : g.top2 && b > kMaskedKey ? a + b : a;
+    double left = __shfl(total, (lane * lanes) & 63);
     if (lane >= g.n_group) left = -INFINITY;
     bool kept = false;
     for (int j = 0; j < g.topk_group; ++j) {
@@ -440,7 +443,7 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
     if (lanes > 2) join(dpp32<kFour>(a), dpp32<kFour>(b));
     if (lanes > 4) join(dpp32<kMirror8>(a), dpp32<kMirror8>(b));
     const float ka = from_ordered(a), kb = from_ordered(b);   // (one expert to a group: b is dropped, or NaN)
-    const float gs = g.top2 && kb > kMasked ? ka + kb : ka;
+    const float gs = !(ka > kMasked) ? kDeadGroup32 : g.top2 && kb > kMasked ? ka + kb : ka;
     // off by both keys' errors and the sum's rounding, on both sides
     const float tol = by_logit ? 0.f : 4.f * sigma + 0x1p-21f * (fabsf(ka) + (kb > kMasked ? fabsf(kb) : 0.f));
     int above = 0, near = 0;                // groups surely before this one, groups that may be
@@ -496,7 +499,7 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
         return finite_key(g.bias ? x + static_cast<double>(g.bias[e]) : x, false);
       };
       const double d1 = exact(k1, e1), d2 = exact(k2, e2), most = fmax(d1, d2);
-      const double score = g.top2 && k2 > kMasked ? d1 + d2 : most;
+      const double score = !(k1 > kMasked) ? kDeadGroup : g.top2 && k2 > kMasked ? d1 + d2 : most;
       int before = 0;
       for (int r = lanes; r < 16; r += lanes) {
         const int os = (sub + r) & 15;

@@ -322,3 +322,22 @@ def test_gradient_of_saturated_sigmoids(dtype, renorm):
     want, mag = gate.backward(l64, idx, d_w, "sigmoid", renorm, 2.5)
     half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
     assert np.all(np.abs(got - want) <= half * np.abs(want) + 2.0 ** -18 * mag)
+
+
+@pytest.mark.parametrize("E,n_group", [(64, 4), (256, 8), (60, 4), (96, 6), (640, 8)])
+@pytest.mark.parametrize("kind", ["sigmoid", "softmax"])
+def test_groups_without_a_live_expert_come_last(E, n_group, kind):
+    """Sums of two biased scores may pass -2^127, where no single score counts: they still come before a group whose
+    experts are all masked."""
+    size, k = E // n_group, 4
+    l = torch.zeros((3, E))
+    l[0, :size] = -float("inf")                                    # the first group is masked
+    l[1, :size * (n_group - 1)] = -float("inf")                    # all but the last are
+    l[2, size:] = -float("inf")
+    b = torch.full((E,), -1.5e38)
+    b[1::2] = -1.2e38
+    for topk_group in (1, 2, n_group):
+        g = _gate(E, k, kind, n_group, topk_group, True, bias=b.cuda())
+        idx, _ = _route(g, _device(l, E), 3)
+        want = gate.route(l.double().numpy(), k, kind, n_group, topk_group, True, b.double().numpy())[0]
+        assert np.array_equal(idx, want), topk_group
