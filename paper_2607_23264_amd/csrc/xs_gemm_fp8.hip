@@ -29,9 +29,11 @@ struct GemmArgs {
 
 // Work index t -> (segment, row block, column tile): segments in order; within one, groups of eight row
 // blocks, the row blocks of a group varying fastest (32 consecutive tiles, one XCD's, are then 8 x 4: twelve
-// operand panels for its L2). Every wave scans the segments itself.
+// operand panels for its L2). Every wave scans the segments itself. end: the number of tiles, where the scan has
+// come to the last segments.
 struct Where {
   int seg, m0, rows, nb;
+  int64_t end;
 };
 constexpr int kGroupRows = 8, kRun = 32;
 constexpr int64_t kNoTile = int64_t(1) << 50;
@@ -49,7 +51,7 @@ __device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, 
     if (t >= static_cast<int64_t>(blocks) * nt) return false;
     int mb, nb;
     in_groups(t, blocks, nt, &mb, &nb);
-    at = Where{0, mb * BM, min(BM, p.M - mb * BM), nb};
+    at = Where{0, mb * BM, min(BM, p.M - mb * BM), nb, static_cast<int64_t>(blocks) * nt};
     return true;
   }
   const int lane = threadIdx.x & 63;
@@ -84,6 +86,7 @@ __device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, 
       at.m0 = __builtin_amdgcn_readfirstlane(off + mb * BM);
       at.rows = __builtin_amdgcn_readfirstlane(min(BM, rows - mb * BM));
       at.nb = __builtin_amdgcn_readfirstlane(nb);
+      at.end = s0 + 64 < p.n_seg ? INT64_MAX : base + __shfl(incl, 63);
       return true;
     }
     base += __shfl(incl, 63);
@@ -165,9 +168,11 @@ __global__ __launch_bounds__(T::kThreads, 2) void gemm_kernel(GemmArgs p) {
 // over its four waves, whose scaled fp32 sums meet in LDS once and are added in wave order. Each wave
 // stages its own blocks (one 128-byte line of every row, and the rows' scales) kDepth deep in a slice of
 // LDS of its own, by direct loads, and needs no barrier until the end. SWIGLU: columns y < NJ / 2 are the
-// gate's, the others the same columns of up.
+// gate's, the others the same columns of up. GROUPED: segments that overlap have more row blocks than the grid was
+// sized for, and a workgroup goes on to a second one (the loop in plain products too: 24 x 4096 x 7168 7.82 us
+// where it takes 7.65).
 constexpr uint32_t kNone = 1u << 30;   // an offset past every buffer (the host sees to that); twice it does not wrap
-template <int NB, int NJ, int kDepth, bool ROW, bool SWIGLU, bool F32>
+template <int NB, int NJ, int kDepth, bool ROW, bool SWIGLU, bool F32, bool GROUPED>
 __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
   constexpr int kWaves = 4, kRows = 16 * NB, kCols = 16 * NJ, kPitch = kCols + 4;
   constexpr int kPiece = (kRows + kCols) * 128 + 512;      // B rows, A rows, 64 scales of A, 64 of B
@@ -180,132 +185,135 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
   const int i = lane & 15, g = lane >> 4;
   const int n0 = blockIdx.x * kHalf, n_out = SWIGLU ? p.N / 2 : p.N;
   Where at;
-  if (!find_tile<kRows>(p, blockIdx.y, 1, at)) return;     // the whole workgroup
-  const int rows = at.rows, cols = min(kHalf, n_out - n0);
-  lds_char* const lds = (lds_char*)smem + w * kDepth * kPiece;
-  const uint8_t* const b = p.b + at.seg * p.b_seg;
-  const float* const b_s = p.b_s + at.seg * p.b_s_seg;
-  const int nk = p.K / 128;
-  const auto span = [&](int64_t rows_, int64_t ld, int64_t last) { return static_cast<uint32_t>((rows_ - 1) * ld + last); };
-  const v4i ra = buffer_rsrc(p.a + at.m0 * p.lda, span(rows, p.lda, p.K));
-  const v4i rb = buffer_rsrc(b + n0 * p.ldb, span(cols, p.ldb, p.K));
-  const v4i rb2 = buffer_rsrc(b + (n0 + (SWIGLU ? n_out : 0)) * p.ldb, span(cols, p.ldb, p.K));
-  const v4i rsa = buffer_rsrc(p.a_s + at.m0 * p.lda_s, span(rows, p.lda_s * 4, nk * 4));
-  // scales of B: one per column, or of the workgroup's 128 x 128 block (and of up's)
-  const int sb_rows = ROW ? cols : 1;
-  const v4i rsb = buffer_rsrc(b_s + (ROW ? n0 : n0 / 128) * p.ldb_s,
-                              span(SWIGLU ? n_out / 128 + 1 : sb_rows, p.ldb_s * 4, nk * 4));
-  // load n of an operand fills its rows 8 n .. + 7 of a piece; past the buffers' ends nothing is fetched
-  uint32_t oa[2 * NB], ob[2 * NJ];
-  const int lr = lane >> 3, lp = lane & 7;
-#pragma unroll
-  for (int n = 0; n < 2 * NB; ++n) oa[n] = static_cast<uint32_t>((8 * n + lr) * p.lda + ((lp ^ ((4 * n + (lr >> 1)) & 7)) << 4));
-#pragma unroll
-  for (int n = 0; n < 2 * NJ; ++n) {
-    const int r = SWIGLU && n >= NJ ? 8 * (n - NJ) : 8 * n;
-    ob[n] = static_cast<uint32_t>((r + lr) * p.ldb + ((lp ^ ((4 * n + (lr >> 1)) & 7)) << 4));
-  }
-  const uint32_t osa = lane < kRows ? static_cast<uint32_t>(lane * p.lda_s * 4) : kNone;
-  uint32_t osb = kNone;
-  if (ROW ? lane < kCols : lane < (SWIGLU ? 2 : 1)) osb = static_cast<uint32_t>((SWIGLU ? lane * (n_out / 128) : lane) * p.ldb_s * 4);
-  const int k0 = nk * w / kWaves, k1 = nk * (w + 1) / kWaves;   // this wave's blocks
-  f32x4 acc[NB][NJ];
-#pragma unroll
-  for (int x = 0; x < NB; ++x)
-#pragma unroll
-    for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // block k into slot s; past the wave's range every lane points past the buffers, so the number of loads
-  // in flight stays the same
-  const auto load = [&](int s, int k) {
-    const uint32_t kb = k < k1 ? static_cast<uint32_t>(k) * 128u : kNone, ks = k < k1 ? static_cast<uint32_t>(k) * 4u : kNone;
-    lds_char* const at_ = lds + s * kPiece;
-#pragma unroll
-    for (int n = 0; n < 2 * NJ; ++n) load_lds16(SWIGLU && n >= NJ ? rb2 : rb, ob[n] + kb, at_ + n * 1024);
-#pragma unroll
-    for (int n = 0; n < 2 * NB; ++n) load_lds16(ra, oa[n] + kb, at_ + kCols * 128 + n * 1024);
-    load_lds4(rsa, osa + ks, at_ + (kRows + kCols) * 128);
-    load_lds4(rsb, osb + ks, at_ + (kRows + kCols) * 128 + 256);
-  };
-  const int swz = (i >> 1) & 7;
-  typedef __attribute__((address_space(3))) v4i_ lds_v4i;
-  typedef __attribute__((address_space(3))) float lds_float;
-  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-  const auto frag = [&](const lds_char* row) {
-    const v4i_ lo = *(const lds_v4i*)(row + ((g ^ swz) << 4)), hi = *(const lds_v4i*)(row + (((g + 4) ^ swz) << 4));
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-#pragma unroll
-  for (int s = 0; s < kDepth; ++s) load(s, k0 + s);
-  for (int k = k0; k < k1; k += kDepth) {
-#pragma unroll
-    for (int s = 0; s < kDepth; ++s) {
-      if (k + s >= k1) break;
-      wait_vm<(kDepth - 1) * kLoads>();                    // block k + s has landed
-      const lds_char* const at_ = lds + s * kPiece;
-      const lds_char* const sc = at_ + (kRows + kCols) * 128;
-      v8i bc[NJ], ac[NB];
-      float sa[NB];
-      f32x4 sb[ROW ? NJ : 1];
-#pragma unroll
-      for (int y = 0; y < NJ; ++y) bc[y] = frag(at_ + (16 * y + i) * 128);
-#pragma unroll
-      for (int x = 0; x < NB; ++x) {
-        ac[x] = frag(at_ + (kCols + 16 * x + i) * 128);
-        sa[x] = *(const lds_float*)(sc + (16 * x + i) * 4);
-      }
-      if constexpr (ROW) {
-#pragma unroll
-        for (int y = 0; y < NJ; ++y) sb[y] = *(const lds_f32x4*)(sc + 256 + (16 * y + 4 * g) * 4);
-      } else {
-        sb[0][0] = *(const lds_float*)(sc + 256);
-        sb[0][1] = SWIGLU ? *(const lds_float*)(sc + 260) : 0.f;
-      }
-      __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the slot has been read
-      asm volatile("" ::: "memory");
-      load(s, k + s + kDepth);
-      std::conditional_t<F32, Wide, v8i> bf[NJ], af;
-#pragma unroll
-      for (int y = 0; y < NJ; ++y) as_operand(bc[y], bf[y]);
-#pragma unroll
-      for (int x = 0; x < NB; ++x) {
-        as_operand(ac[x], af);
-#pragma unroll
-        for (int y = 0; y < NJ; ++y) {
-          const f32x4 v = block_sum(bf[y], af);
-          const float f = ROW ? sa[x] : sa[x] * sb[0][SWIGLU && y >= NJ / 2 ? 1 : 0];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[x][y][c] = __builtin_fmaf(ROW ? v[c] * sb[y][c] : v[c], f, acc[x][y][c]);
+  for (int64_t t = blockIdx.y; find_tile<kRows>(p, t, 1, at); t += gridDim.y) {   // (the whole workgroup)
+    const int rows = at.rows, cols = min(kHalf, n_out - n0);
+    lds_char* const lds = (lds_char*)smem + w * kDepth * kPiece;
+    const uint8_t* const b = p.b + at.seg * p.b_seg;
+    const float* const b_s = p.b_s + at.seg * p.b_s_seg;
+    const int nk = p.K / 128;
+    const auto span = [&](int64_t rows_, int64_t ld, int64_t last) { return static_cast<uint32_t>((rows_ - 1) * ld + last); };
+    const v4i ra = buffer_rsrc(p.a + at.m0 * p.lda, span(rows, p.lda, p.K));
+    const v4i rb = buffer_rsrc(b + n0 * p.ldb, span(cols, p.ldb, p.K));
+    const v4i rb2 = buffer_rsrc(b + (n0 + (SWIGLU ? n_out : 0)) * p.ldb, span(cols, p.ldb, p.K));
+    const v4i rsa = buffer_rsrc(p.a_s + at.m0 * p.lda_s, span(rows, p.lda_s * 4, nk * 4));
+    // scales of B: one per column, or of the workgroup's 128 x 128 block (and of up's)
+    const int sb_rows = ROW ? cols : 1;
+    const v4i rsb = buffer_rsrc(b_s + (ROW ? n0 : n0 / 128) * p.ldb_s,
+                                span(SWIGLU ? n_out / 128 + 1 : sb_rows, p.ldb_s * 4, nk * 4));
+    // load n of an operand fills its rows 8 n .. + 7 of a piece; past the buffers' ends nothing is fetched
+    uint32_t oa[2 * NB], ob[2 * NJ];
+    const int lr = lane >> 3, lp = lane & 7;
+  #pragma unroll
+    for (int n = 0; n < 2 * NB; ++n) oa[n] = static_cast<uint32_t>((8 * n + lr) * p.lda + ((lp ^ ((4 * n + (lr >> 1)) & 7)) << 4));
+  #pragma unroll
+    for (int n = 0; n < 2 * NJ; ++n) {
+      const int r = SWIGLU && n >= NJ ? 8 * (n - NJ) : 8 * n;
+      ob[n] = static_cast<uint32_t>((r + lr) * p.ldb + ((lp ^ ((4 * n + (lr >> 1)) & 7)) << 4));
+    }
+    const uint32_t osa = lane < kRows ? static_cast<uint32_t>(lane * p.lda_s * 4) : kNone;
+    uint32_t osb = kNone;
+    if (ROW ? lane < kCols : lane < (SWIGLU ? 2 : 1)) osb = static_cast<uint32_t>((SWIGLU ? lane * (n_out / 128) : lane) * p.ldb_s * 4);
+    const int k0 = nk * w / kWaves, k1 = nk * (w + 1) / kWaves;   // this wave's blocks
+    f32x4 acc[NB][NJ];
+  #pragma unroll
+    for (int x = 0; x < NB; ++x)
+  #pragma unroll
+      for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // block k into slot s; past the wave's range every lane points past the buffers, so the number of loads
+    // in flight stays the same
+    const auto load = [&](int s, int k) {
+      const uint32_t kb = k < k1 ? static_cast<uint32_t>(k) * 128u : kNone, ks = k < k1 ? static_cast<uint32_t>(k) * 4u : kNone;
+      lds_char* const at_ = lds + s * kPiece;
+  #pragma unroll
+      for (int n = 0; n < 2 * NJ; ++n) load_lds16(SWIGLU && n >= NJ ? rb2 : rb, ob[n] + kb, at_ + n * 1024);
+  #pragma unroll
+      for (int n = 0; n < 2 * NB; ++n) load_lds16(ra, oa[n] + kb, at_ + kCols * 128 + n * 1024);
+      load_lds4(rsa, osa + ks, at_ + (kRows + kCols) * 128);
+      load_lds4(rsb, osb + ks, at_ + (kRows + kCols) * 128 + 256);
+    };
+    const int swz = (i >> 1) & 7;
+    typedef __attribute__((address_space(3))) v4i_ lds_v4i;
+    typedef __attribute__((address_space(3))) float lds_float;
+    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+    const auto frag = [&](const lds_char* row) {
+      const v4i_ lo = *(const lds_v4i*)(row + ((g ^ swz) << 4)), hi = *(const lds_v4i*)(row + (((g + 4) ^ swz) << 4));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+  #pragma unroll
+    for (int s = 0; s < kDepth; ++s) load(s, k0 + s);
+    for (int k = k0; k < k1; k += kDepth) {
+  #pragma unroll
+      for (int s = 0; s < kDepth; ++s) {
+        if (k + s >= k1) break;
+        wait_vm<(kDepth - 1) * kLoads>();                    // block k + s has landed
+        const lds_char* const at_ = lds + s * kPiece;
+        const lds_char* const sc = at_ + (kRows + kCols) * 128;
+        v8i bc[NJ], ac[NB];
+        float sa[NB];
+        f32x4 sb[ROW ? NJ : 1];
+  #pragma unroll
+        for (int y = 0; y < NJ; ++y) bc[y] = frag(at_ + (16 * y + i) * 128);
+  #pragma unroll
+        for (int x = 0; x < NB; ++x) {
+          ac[x] = frag(at_ + (kCols + 16 * x + i) * 128);
+          sa[x] = *(const lds_float*)(sc + (16 * x + i) * 4);
+        }
+        if constexpr (ROW) {
+  #pragma unroll
+          for (int y = 0; y < NJ; ++y) sb[y] = *(const lds_f32x4*)(sc + 256 + (16 * y + 4 * g) * 4);
+        } else {
+          sb[0][0] = *(const lds_float*)(sc + 256);
+          sb[0][1] = SWIGLU ? *(const lds_float*)(sc + 260) : 0.f;
+        }
+        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the slot has been read
+        asm volatile("" ::: "memory");
+        load(s, k + s + kDepth);
+        std::conditional_t<F32, Wide, v8i> bf[NJ], af;
+  #pragma unroll
+        for (int y = 0; y < NJ; ++y) as_operand(bc[y], bf[y]);
+  #pragma unroll
+        for (int x = 0; x < NB; ++x) {
+          as_operand(ac[x], af);
+  #pragma unroll
+          for (int y = 0; y < NJ; ++y) {
+            const f32x4 v = block_sum(bf[y], af);
+            const float f = ROW ? sa[x] : sa[x] * sb[0][SWIGLU && y >= NJ / 2 ? 1 : 0];
+  #pragma unroll
+            for (int c = 0; c < 4; ++c) acc[x][y][c] = __builtin_fmaf(ROW ? v[c] * sb[y][c] : v[c], f, acc[x][y][c]);
+          }
         }
       }
     }
-  }
-  wait_vm<0>();
-  __syncthreads();                                         // no load is in flight: the LDS is free
-  float* const red = reinterpret_cast<float*>(smem);
-#pragma unroll
-  for (int x = 0; x < NB; ++x)
-#pragma unroll
-    for (int y = 0; y < NJ; ++y)
-      *reinterpret_cast<f32x4*>(red + (w * kRows + 16 * x + i) * kPitch + 16 * y + 4 * g) = acc[x][y];
-  __syncthreads();
-  const auto sum = [&](int r, int c) {
-    f32x4 v = *reinterpret_cast<const f32x4*>(red + r * kPitch + c);
-#pragma unroll
-    for (int x = 1; x < kWaves; ++x) v += *reinterpret_cast<const f32x4*>(red + (x * kRows + r) * kPitch + c);
-    return v;
-  };
-  for (int u = tid; u < rows * (kHalf / 4); u += 256) {
-    const int r = u / (kHalf / 4), c = 4 * (u % (kHalf / 4));
-    if (n0 + c >= n_out) continue;
-    f32x4 v = sum(r, c);
-    if constexpr (SWIGLU) {
-      const f32x4 up = sum(r, c + kHalf);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = v[q] * __builtin_amdgcn_rcpf(1.f + __expf(-v[q])) * up[q];
+    wait_vm<0>();
+    __syncthreads();                                         // no load is in flight: the LDS is free
+    float* const red = reinterpret_cast<float*>(smem);
+  #pragma unroll
+    for (int x = 0; x < NB; ++x)
+  #pragma unroll
+      for (int y = 0; y < NJ; ++y)
+        *reinterpret_cast<f32x4*>(red + (w * kRows + 16 * x + i) * kPitch + 16 * y + 4 * g) = acc[x][y];
+    __syncthreads();
+    const auto sum = [&](int r, int c) {
+      f32x4 v = *reinterpret_cast<const f32x4*>(red + r * kPitch + c);
+  #pragma unroll
+      for (int x = 1; x < kWaves; ++x) v += *reinterpret_cast<const f32x4*>(red + (x * kRows + r) * kPitch + c);
+      return v;
+    };
+    for (int u = tid; u < rows * (kHalf / 4); u += 256) {
+      const int r = u / (kHalf / 4), c = 4 * (u % (kHalf / 4));
+      if (n0 + c >= n_out) continue;
+      f32x4 v = sum(r, c);
+      if constexpr (SWIGLU) {
+        const f32x4 up = sum(r, c + kHalf);
+  #pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = v[q] * __builtin_amdgcn_rcpf(1.f + __expf(-v[q])) * up[q];
+      }
+      const int64_t to = (at.m0 + r) * p.ldc + n0 + c;
+      if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.c) + to) = v;
+      else *reinterpret_cast<uint2*>(p.c + to * 2) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
-    const int64_t to = (at.m0 + r) * p.ldc + n0 + c;
-    if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.c) + to) = v;
-    else *reinterpret_cast<uint2*>(p.c + to * 2) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    if (!GROUPED || t + gridDim.y >= at.end) return;
+    __syncthreads();                                         // the sums have been read: the LDS is free
   }
 }
 
@@ -333,8 +341,13 @@ template <int NB, int NJ, int kDepth, bool ROW, bool SWIGLU, bool F32>
 int launch_split(const f8::GemmArgs& p, hipStream_t st) {
   const int cols = SWIGLU ? 8 * NJ : 16 * NJ, n_out = SWIGLU ? p.N / 2 : p.N;
   const int64_t blocks = (static_cast<int64_t>(p.M) + 16 * NB - 1) / (16 * NB) + (p.seg_off ? p.n_seg : 0);
-  hipLaunchKernelGGL((f8::split_kernel<NB, NJ, kDepth, ROW, SWIGLU, F32>),
-                     dim3((n_out + cols - 1) / cols, static_cast<unsigned>(blocks)), dim3(256), 0, st, p);
+  const dim3 grid((n_out + cols - 1) / cols, static_cast<unsigned>(blocks));
+  if constexpr (!SWIGLU)
+    if (!p.seg_off) {
+      hipLaunchKernelGGL((f8::split_kernel<NB, NJ, kDepth, ROW, SWIGLU, F32, false>), grid, dim3(256), 0, st, p);
+      return xs_host::launch_status();
+    }
+  if constexpr (!ROW && !F32) hipLaunchKernelGGL((f8::split_kernel<NB, NJ, kDepth, ROW, SWIGLU, F32, true>), grid, dim3(256), 0, st, p);
   return xs_host::launch_status();
 }
 

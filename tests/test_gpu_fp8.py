@@ -450,3 +450,46 @@ def test_more_columns_than_a_grid_of_the_split_form_has():
 def test_gemm_of_about_a_tile_to_a_cu(M, N, blocks, block):
     """Fewer blocks of K than stages, as many, more; whole and ragged last tiles."""
     test_gemm(M, N, blocks * B, block, "bf16")
+
+
+@pytest.mark.parametrize("spans,N,K", [
+    ([(0, 100), (0, 100), (100, 100)], 256, 256),                            # more row blocks than M and n_seg alone ask for
+    ([(0, 700)] * 5 + [(700, 100)], 256, 384),
+    ([(0, 50)] * 70 + [(50, 33), (10, 60), (0, 83)], 264, 256),              # past the 64 segments of one scan
+    ([(0, 3000), (0, 3000), (3000, 500)], 1024, 128),                        # tiles
+    ([(5, 1)] * 40 + [(6, 300)], 512, 1152)])
+@pytest.mark.parametrize("epi", ["store", "swiglu"])
+def test_overlapping_segments_compute_all_their_rows(spans, N, K, epi):
+    """Segments race on their common rows only: an element there is that of one of them, and every other row is its
+    segment's. Small integers and power-of-two scales: the 8-bit products are exact (test_gemm_of_integers_is_exact)."""
+    if epi == "swiglu" and N % 256:
+        pytest.skip("SwiGLU takes N in 256s")
+    X = xs()
+    M, n = max(o + r for o, r in spans) + 3, len(spans)
+    g = np.random.default_rng(M + n)
+    a = Codes(M, K)
+    vals = g.integers(-4, 5, (M, K)).astype(np.float64)
+    a.codes[:M, :K] = torch.from_numpy(mx.encode(vals, mx.E4M3)).cuda()
+    a.scales[:M, :K // B] = 0.125
+    w = g.integers(-2, 3, (n, N, K)).astype(np.float64)
+    bc = torch.from_numpy(mx.encode(w, mx.E4M3)).cuda()
+    bs = torch.full((n, -(-N // B), _up(K // B, 4)), 0.25, device="cuda")
+    n_out = N // 2 if epi == "swiglu" else N
+    c = torch.full((M, n_out), -1, dtype=torch.int16, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    do, dr = (torch.tensor([s[i] for s in spans], dtype=torch.int32, device="cuda") for i in (0, 1))
+    X.check(X.xs_grouped_gemm_fp8(*a.args(), M, do.data_ptr(), dr.data_ptr(), n, bc.data_ptr(), bs.data_ptr(), bs.shape[2], N, K,
+                                  c.data_ptr(), n_out, X.XS_EPI_SWIGLU if epi == "swiglu" else X.XS_EPI_STORE, st.data_ptr(), _stream()))
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    bits = host_bits(c)
+    got, fits, covered = bits_f64(bits), np.zeros((M, n_out), bool), np.zeros(M, bool)
+    for s, (o, r) in enumerate(spans):
+        p = vals[o:o + r] @ w[s].T / 32
+        want = fp8.swiglu(p) if epi == "swiglu" else p
+        tol = 2.0 ** -8 * np.abs(want)
+        if epi == "swiglu":                                        # exponential, reciprocal, products: as in test_grouped_gemm
+            tol = tol + 2.0 ** -19 * (1 + np.abs(p[:, :n_out])) * np.abs(want)
+        fits[o:o + r] |= np.abs(got[o:o + r] - want) <= tol
+        covered[o:o + r] = True
+    assert fits[covered].all() and (bits[~covered] == 0xFFFF).all()
