@@ -244,7 +244,7 @@ typedef struct xs_ep_layer {
   int32_t renormalize;
   int32_t expert_mode;        /* XS_EXPERT_SWIGLU, or XS_EXPERT_IDENTITY (y = x) */
   int32_t cap;                /* capacity_rows of every dispatch window */
-  const float* logits;        /* device fp32 [n_src][T][E] */
+  const float* logits;        /* device fp32 [n_src][T][E]; for xs_fused_ep_layer_gated of the gate's logits_type */
   const void* x;              /* device bf16 [T][H], tokens of source `src` */
   const void* w1;             /* device bf16 [n_experts][2I][H] */
   const void* w2;             /* device bf16 [n_experts][H][I] */
@@ -265,10 +265,14 @@ typedef struct xs_ep_layer {
   void* events[8];            /* optional hipEvent_t per phase boundary (NULL = not recorded),
                                  recorded on `stream`; see XS_EV_* */
   int32_t precision;          /* XS_PREC_BF16 (0), XS_PREC_MXFP8 or XS_PREC_W4A8 */
-  int32_t reserved;           /* 0 */
+  int32_t reserved;           /* 0, or XS_LAYER_BF16_LOGITS */
   const void* w1_scale;       /* MX precisions: device E8M0 [H / 512][n_experts * 2I][16], 16-byte aligned */
   const void* w2_scale;       /* MX precisions: device E8M0 [I / 512][n_experts * H][16], 16-byte aligned */
 } xs_ep_layer;
+
+/* In xs_ep_layer.reserved: the logits are bf16. Calls that would read them as fp32 (xs_fused_ep_layer,
+ * xs_fused_ep_layer_noalloc, a gate of fp32 logits) then return XS_EINVAL; with 0 they cannot know. */
+enum { XS_LAYER_BF16_LOGITS = 2 };
 
 /* Phase boundaries of the EP entry points: events[XS_EV_x] is recorded right before the
  * first launch of phase x (XS_EV_FFN_END right after the expert-FFN kernel(s), XS_EV_END
@@ -394,8 +398,9 @@ int xs_fused_ep_layer(const xs_ep_layer* L, const xs_pacing* pacing, const xs_tr
                       void* stream);
 
 /* The same layer routed by a gate (see "routing gates") instead of top-k softmax: L->logits holds the gate's
- * logits [n_src][T][E] in its logits_type, L->renormalize is not used. gate->E and gate->k are L's (else
- * XS_EINVAL); otherwise as xs_fused_ep_layer and xs_route_gate. */
+ * logits [n_src][T][E] in its logits_type (XS_LAYER_BF16_LOGITS marks a layer of bf16 logits), L->renormalize is
+ * not used. gate->E and gate->k are L's (else XS_EINVAL); otherwise as xs_fused_ep_layer and xs_route_gate. The
+ * other layer calls route by top-k softmax over fp32 logits. */
 int xs_fused_ep_layer_gated(const xs_ep_layer* L, const xs_gate* gate, const xs_pacing* pacing,
                             const xs_trace* trace, void* workspace, int64_t workspace_bytes,
                             int32_t* dev_status, void* stream);

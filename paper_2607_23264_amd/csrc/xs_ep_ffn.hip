@@ -858,7 +858,7 @@ int validate(const xs_ep_layer* L, bool need_out) {
   if (L->expert_mode != XS_EXPERT_SWIGLU && L->expert_mode != XS_EXPERT_IDENTITY) return XS_EINVAL;
   if (L->precision != XS_PREC_BF16 && L->precision != XS_PREC_MXFP8 && L->precision != XS_PREC_W4A8)
     return XS_EINVAL;
-  if (L->reserved != 0) return XS_EINVAL;
+  if (L->reserved != 0 && L->reserved != XS_LAYER_BF16_LOGITS) return XS_EINVAL;
   if (is_mx(L)) {
     if (L->expert_mode != XS_EXPERT_SWIGLU) return XS_EUNSUPPORTED;
     if (!L->w1_scale || !L->w2_scale) return XS_EINVAL;
@@ -1137,6 +1137,7 @@ static int fused_ep_layer(const xs_ep_layer* L, const xs_gate* gate, const xs_pa
                           void* workspace, int64_t workspace_bytes, int32_t* dev_status, void* stream) {
   int rc = validate(L, true);
   if (rc) return rc;
+  if (L->reserved == XS_LAYER_BF16_LOGITS && !(gate && gate->logits_type == XS_TYPE_BF16)) return XS_EINVAL;
   if (pacing && (pacing->policy < XS_POLICY_BURST || pacing->policy > XS_POLICY_AUTO ||
                  pacing->lead_rows < 0 || pacing->chunk_tiles < 0 || pacing->max_producers < 0 ||
                  pacing->gap_ns < 0 || pacing->spin_timeout_us < 0 ||

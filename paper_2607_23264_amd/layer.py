@@ -163,6 +163,7 @@ class EPLayer:
         L.logits = self.logits.data_ptr()
         L.x = self.x_all[s.src].data_ptr()
         L.precision = self.precision
+        L.reserved = X.XS_LAYER_BF16_LOGITS if self.logits.dtype == torch.bfloat16 else 0
         if self.mx:
             L.w1, L.w2 = self.w1q.data_ptr(), self.w2q.data_ptr()
             L.w1_scale, L.w2_scale = self.w1s.data_ptr(), self.w2s.data_ptr()

@@ -35,6 +35,7 @@ XS_SCORE_SOFTMAX, XS_SCORE_SIGMOID = 0, 1
 XS_GROUP_MAX, XS_GROUP_TOP2 = 0, 1
 XS_TYPE_BF16, XS_TYPE_F32 = 0, 1
 XS_BLOCK_ROW, XS_BLOCK_TILE = 0, 1
+XS_LAYER_BF16_LOGITS = 2
 
 vp = C.c_void_p
 i32 = C.c_int32

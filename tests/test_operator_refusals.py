@@ -125,3 +125,25 @@ def test_sizes_past_a_grid():
     assert X.xs_swiglu_fp8_backward(A, 2 * i, A, i, A, i, r, i, A, 2 * i, None, 0, None) == X.XS_EUNSUPPORTED
     assert X.xs_swiglu_fp8(A, 2 * i, r, i, A, i, A, i, None, 0, None, 0, None) == X.XS_EUNSUPPORTED
     assert X.xs_quantize_fp8(A, r, 1 << 30, 1 << 30, A, 1 << 30, A, 1 << 23, None, 0, None, 0, None) == X.XS_EUNSUPPORTED
+
+
+def test_layers_of_bf16_logits_go_to_their_gate_only():
+    """A layer marked as having bf16 logits is refused by every call that would read them as fp32."""
+    X = xs()
+    import ctypes as C
+    win = X.windows([X.xs_window()])
+    L = X.xs_ep_layer(n_src=1, T=4, H=256, E=8, k=2, I=128, W=1, e_begin=0, n_experts=8, src=0, cap=8, h_rows=64)
+    for f in ("logits", "x", "w1", "w2", "topk_idx", "topk_w", "expert_counts", "src_base", "expert_offsets", "dest_counts", "slot_row",
+              "row_src", "h_ws", "out"):
+        setattr(L, f, A)
+    L.dispatch_win = L.combine_win = C.cast(win, C.POINTER(X.xs_window))
+    bf16, f32 = X.gate(8, 2, logits_type=X.XS_TYPE_BF16), X.gate(8, 2)
+    nothing = (None, None, None, 0, None, None)                    # no workspace: past the checks, nothing is launched
+    plain = lambda: X.xs_fused_ep_layer(C.byref(L), *nothing)
+    gated = lambda g: X.xs_fused_ep_layer_gated(C.byref(L), g, *nothing)
+    assert plain() == gated(bf16) == gated(f32) == X.XS_EWORKSPACE
+    L.reserved = X.XS_LAYER_BF16_LOGITS
+    assert gated(bf16) == X.XS_EWORKSPACE
+    assert plain() == gated(f32) == X.XS_EINVAL
+    L.reserved = 1
+    assert gated(bf16) == X.XS_EINVAL
