@@ -95,8 +95,11 @@ int xs_route_topk_softmax(const float* logits, int32_t T, int32_t E, int32_t k,
  *              largest group score (the largest biased score in it, or the sum of its two largest,
  *              one if it has one unmasked expert) are kept, ties to the lower group
  *   selection  the k experts of the kept groups with the largest biased scores in descending order,
- *              ties to the lower index; masked experts come after every other one. Scores are
- *              compared as computed in 64 bits (within 2^127; below that counts as masked)
+ *              ties to the lower index; masked experts come after every other one. Biased scores (with a
+ *              bias, or with groups ranked by sums of two) are compared as computed in 64 bits, within 2^127;
+ *              below that counts as masked. Otherwise experts and groups are compared by their logits, the
+ *              scores' own order, within the same bounds: sigmoid logits 40 and 41 are two scores there, and
+ *              one (1, rounded to 64 bits) under a bias of zeros
  *   weights    w_j = scale s_j, with renormalize != 0 scale s_j / sum_i s_i over the k selected
  * A row that is masked whole selects its lowest indices with weights 0. A NaN logit counts as masked
  * in the selection; weights that depend on it are NaN. */

@@ -341,3 +341,22 @@ def test_groups_without_a_live_expert_come_last(E, n_group, kind):
         idx, _ = _route(g, _device(l, E), 3)
         want = gate.route(l.double().numpy(), k, kind, n_group, topk_group, True, b.double().numpy())[0]
         assert np.array_equal(idx, want), topk_group
+
+
+@pytest.mark.parametrize("E,k,n_group,topk_group", [(16, 4, 1, 1), (256, 8, 1, 1), (256, 8, 8, 3), (60, 5, 4, 2), (700, 9, 1, 1), (96, 6, 6, 2)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_order_of_scores_that_64_bits_cannot_tell_apart(E, k, n_group, topk_group, dtype):
+    """Saturated sigmoids and softmax scores that underflow: by the logits without a bias, with a bias of zeros as
+    computed in 64 bits, where they are equal and go to the lower index."""
+    g = np.random.default_rng(E)
+    for kind, low in (("sigmoid", 38.0), ("softmax", -900.0)):
+        l = low + g.integers(0, 16, (4, E)).astype(np.float64) * (1 if kind == "sigmoid" else 4)
+        if kind == "softmax":
+            l[:, 3] = 0.0                                          # scores of the others: below 2^-1074
+        l[1, ::3] = -float("inf")
+        dev = _device(torch.from_numpy(l).to(torch.bfloat16 if dtype == "bf16" else torch.float32), E)
+        l = dev.cpu().double().numpy()
+        for top2, bias in ((False, None), (False, torch.zeros(E)), (True, torch.zeros(E))):
+            idx, _ = _route(_gate(E, k, kind, n_group, topk_group, top2, bias=None if bias is None else bias.cuda(), dtype=dtype), dev, 4)
+            want = gate.select(l, k, kind, n_group, topk_group, top2, None if bias is None else bias.numpy())
+            assert np.array_equal(idx, want), (kind, top2, bias is None)

@@ -76,3 +76,13 @@ def test_gradient_of_saturated_sigmoids():
     grad, mag = gate.backward(l, np.array([[0, 1, 2, 3]]), np.ones((1, 4)), "sigmoid")
     want = 1 / (2 + np.exp(l) + np.exp(-l))
     assert np.allclose(grad, want, rtol=1e-14, atol=0) and np.allclose(mag, want, rtol=1e-14, atol=0)
+
+
+def test_order_of_scores_that_64_bits_cannot_tell_apart():
+    """Without a bias by the logits; with one, as computed: equal, so to the lower index."""
+    l = np.array([[38.0, 40.0, 39.0, -1.0, 41.0, 40.0]])
+    assert gate.select(l, 4, "sigmoid")[0].tolist() == [4, 1, 5, 2]
+    assert gate.select(l, 4, "sigmoid", bias=np.zeros(6))[0].tolist() == [0, 1, 2, 4]
+    l = np.array([[-800.0, -790.0, 0.0, -799.0]])                  # softmax scores below 64 bits' range
+    assert gate.select(l, 3, "softmax")[0].tolist() == [2, 1, 3]
+    assert gate.select(l, 3, "softmax", bias=np.zeros(4))[0].tolist() == [2, 0, 1]
