@@ -1,8 +1,8 @@
 // GEMM and grouped GEMM on block-scaled E4M3 (xs_gemm_fp8.hpp).
 #include <algorithm>
-#include <cmath>
 
 #include "xs_gemm_fp8.hpp"
+#include "xs_gemm_fp8_form.hpp"
 
 namespace xs {
 namespace f8 {
@@ -171,7 +171,6 @@ __global__ __launch_bounds__(T::kThreads, 2) void gemm_kernel(GemmArgs p) {
 // gate's, the others the same columns of up. GROUPED: segments that overlap have more row blocks than the grid was
 // sized for, and a workgroup goes on to a second one (the loop in plain products too: 24 x 4096 x 7168 7.82 us
 // where it takes 7.65).
-constexpr uint32_t kNone = 1u << 30;   // an offset past every buffer (the host sees to that); twice it does not wrap
 template <int NB, int NJ, int kDepth, bool ROW, bool SWIGLU, bool F32, bool GROUPED>
 __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
   constexpr int kWaves = 4, kRows = 16 * NB, kCols = 16 * NJ, kPitch = kCols + 4;
@@ -203,9 +202,9 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
     // load n of an operand fills its rows 8 n .. + 7 of a piece; past the buffers' ends nothing is fetched
     uint32_t oa[2 * NB], ob[2 * NJ];
     const int lr = lane >> 3, lp = lane & 7;
-  #pragma unroll
+#pragma unroll
     for (int n = 0; n < 2 * NB; ++n) oa[n] = static_cast<uint32_t>((8 * n + lr) * p.lda + ((lp ^ ((4 * n + (lr >> 1)) & 7)) << 4));
-  #pragma unroll
+#pragma unroll
     for (int n = 0; n < 2 * NJ; ++n) {
       const int r = SWIGLU && n >= NJ ? 8 * (n - NJ) : 8 * n;
       ob[n] = static_cast<uint32_t>((r + lr) * p.ldb + ((lp ^ ((4 * n + (lr >> 1)) & 7)) << 4));
@@ -215,18 +214,18 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
     if (ROW ? lane < kCols : lane < (SWIGLU ? 2 : 1)) osb = static_cast<uint32_t>((SWIGLU ? lane * (n_out / 128) : lane) * p.ldb_s * 4);
     const int k0 = nk * w / kWaves, k1 = nk * (w + 1) / kWaves;   // this wave's blocks
     f32x4 acc[NB][NJ];
-  #pragma unroll
+#pragma unroll
     for (int x = 0; x < NB; ++x)
-  #pragma unroll
+#pragma unroll
       for (int y = 0; y < NJ; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
     // block k into slot s; past the wave's range every lane points past the buffers, so the number of loads
     // in flight stays the same
     const auto load = [&](int s, int k) {
       const uint32_t kb = k < k1 ? static_cast<uint32_t>(k) * 128u : kNone, ks = k < k1 ? static_cast<uint32_t>(k) * 4u : kNone;
       lds_char* const at_ = lds + s * kPiece;
-  #pragma unroll
+#pragma unroll
       for (int n = 0; n < 2 * NJ; ++n) load_lds16(SWIGLU && n >= NJ ? rb2 : rb, ob[n] + kb, at_ + n * 1024);
-  #pragma unroll
+#pragma unroll
       for (int n = 0; n < 2 * NB; ++n) load_lds16(ra, oa[n] + kb, at_ + kCols * 128 + n * 1024);
       load_lds4(rsa, osa + ks, at_ + (kRows + kCols) * 128);
       load_lds4(rsb, osb + ks, at_ + (kRows + kCols) * 128 + 256);
@@ -239,10 +238,10 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
       const v4i_ lo = *(const lds_v4i*)(row + ((g ^ swz) << 4)), hi = *(const lds_v4i*)(row + (((g + 4) ^ swz) << 4));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-  #pragma unroll
+#pragma unroll
     for (int s = 0; s < kDepth; ++s) load(s, k0 + s);
     for (int k = k0; k < k1; k += kDepth) {
-  #pragma unroll
+#pragma unroll
       for (int s = 0; s < kDepth; ++s) {
         if (k + s >= k1) break;
         wait_vm<(kDepth - 1) * kLoads>();                    // block k + s has landed
@@ -251,15 +250,15 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
         v8i bc[NJ], ac[NB];
         float sa[NB];
         f32x4 sb[ROW ? NJ : 1];
-  #pragma unroll
+#pragma unroll
         for (int y = 0; y < NJ; ++y) bc[y] = frag(at_ + (16 * y + i) * 128);
-  #pragma unroll
+#pragma unroll
         for (int x = 0; x < NB; ++x) {
           ac[x] = frag(at_ + (kCols + 16 * x + i) * 128);
           sa[x] = *(const lds_float*)(sc + (16 * x + i) * 4);
         }
         if constexpr (ROW) {
-  #pragma unroll
+#pragma unroll
           for (int y = 0; y < NJ; ++y) sb[y] = *(const lds_f32x4*)(sc + 256 + (16 * y + 4 * g) * 4);
         } else {
           sb[0][0] = *(const lds_float*)(sc + 256);
@@ -269,16 +268,16 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
         asm volatile("" ::: "memory");
         load(s, k + s + kDepth);
         std::conditional_t<F32, Wide, v8i> bf[NJ], af;
-  #pragma unroll
+#pragma unroll
         for (int y = 0; y < NJ; ++y) as_operand(bc[y], bf[y]);
-  #pragma unroll
+#pragma unroll
         for (int x = 0; x < NB; ++x) {
           as_operand(ac[x], af);
-  #pragma unroll
+#pragma unroll
           for (int y = 0; y < NJ; ++y) {
             const f32x4 v = block_sum(bf[y], af);
             const float f = ROW ? sa[x] : sa[x] * sb[0][SWIGLU && y >= NJ / 2 ? 1 : 0];
-  #pragma unroll
+#pragma unroll
             for (int c = 0; c < 4; ++c) acc[x][y][c] = __builtin_fmaf(ROW ? v[c] * sb[y][c] : v[c], f, acc[x][y][c]);
           }
         }
@@ -287,15 +286,15 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
     wait_vm<0>();
     __syncthreads();                                         // no load is in flight: the LDS is free
     float* const red = reinterpret_cast<float*>(smem);
-  #pragma unroll
+#pragma unroll
     for (int x = 0; x < NB; ++x)
-  #pragma unroll
+#pragma unroll
       for (int y = 0; y < NJ; ++y)
         *reinterpret_cast<f32x4*>(red + (w * kRows + 16 * x + i) * kPitch + 16 * y + 4 * g) = acc[x][y];
     __syncthreads();
     const auto sum = [&](int r, int c) {
       f32x4 v = *reinterpret_cast<const f32x4*>(red + r * kPitch + c);
-  #pragma unroll
+#pragma unroll
       for (int x = 1; x < kWaves; ++x) v += *reinterpret_cast<const f32x4*>(red + (x * kRows + r) * kPitch + c);
       return v;
     };
@@ -305,7 +304,7 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
       f32x4 v = sum(r, c);
       if constexpr (SWIGLU) {
         const f32x4 up = sum(r, c + kHalf);
-  #pragma unroll
+#pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = v[q] * __builtin_amdgcn_rcpf(1.f + __expf(-v[q])) * up[q];
       }
       const int64_t to = (at.m0 + r) * p.ldc + n0 + c;
@@ -363,77 +362,10 @@ int launch_tiles(f8::GemmArgs p, int per_cu, hipStream_t st) {
   return xs_host::launch_status();
 }
 
-enum Form { kSplit12, kSplit21, kSplit22, kSplit24, kSplit44, kLow, kDeep, kMid, kBig };
-
-// The cheapest form by a model of its time in us, from M, N, K and the CU count (grouped: with exponential
-// segment lengths, n / (1 - exp(-rows n / M)) row blocks of n segments). A split form takes its rounds of
-// workgroups, each a start and a join that grow with its outputs, and its rows of K bytes at the rate of a
-// CU's memory path; tiles take K / 128 blocks a round, of one 256 x 256, up to two 128 x 128 or one tile of four
-// stages a CU. Weights past the caches (grouped products that touch over 100 MB) come more slowly. Measured, us,
-// split 1x2 / 2x4 / 4x4, 64 x 128 and 128 x 128 of four stages, 128- and 256-tiles, N = 4096, K = 7168:
-//   M = 24  8.4 / 12.0 / 16.8 / 25 / 24 / 37 / 71        M = 128  26 / 13.3 / 18.1 / 25.6 / 27.8 / 42 / 71
-//   M = 512  93 / 46 / 35 / 27.2 / 28.3 / 43 / 74        M = 1024  - / 86 / 67 / 52 / 35.7 / 44 / -
-//   M = 2048  - / 171 / 131 / 101 / 71 / 62 / 82         M = 4093  - / - / - / 198 / 146 / 134 / 105
-//   K = 1024: M = 512  - / 16.3 / 12.6 / 8.3 / 9.2 / 11.1 / -
-// 32 segments with SwiGLU: 64 rows in all  137 / 128 / 137 / 127 / 129 / 143 / 178; 1024  342 / 211 / 197 / 170 /
-// 163 / 159 / 189; 8192  - / 909 / 701 / 496 / 371 / 346 / 323.
-Form choose(const f8::GemmArgs& p, bool swiglu, bool f32) {
-  const double cus = xs_host::persistent_grid(0), nk = p.K / 128, n_out = swiglu ? p.N / 2 : p.N;
-  const double segs = p.seg_off ? std::min(p.n_seg, p.M) : 1;
-  const auto blocks = [&](int rows) {
-    return segs > 1 ? std::ceil(segs / (1 - std::exp(-rows * segs / p.M))) : std::ceil(static_cast<double>(p.M) / rows);
-  };
-  const bool far = segs * p.N * p.K > 100e6 && p.seg_off;
-  double best = 1e300;
-  Form form = kMid;
-  const auto offer = [&](Form f, double us) {
-    if (us < best) {
-      best = us;
-      form = f;
-    }
-  };
-  // offsets of the split form's buffers stay below f8::kNone, its column blocks (of 16 or more, 256 threads) in a
-  // grid's first dimension of 2^32 - 1 threads, its row blocks in the second
-  if ((n_out / 128 + 1) * p.ldb_s * 4 < f8::kNone && p.N < (1 << 28)) {
-    constexpr int forms[5][2] = {{1, 2}, {2, 1}, {2, 2}, {2, 4}, {4, 4}};
-    const double rate = f32 ? 55e3 : far ? 47e3 : 70e3;
-    for (int f = 0; f < 5; ++f) {
-      const int rows = 16 * forms[f][0], cols = 16 * forms[f][1];
-      if ((swiglu && f == kSplit21) || static_cast<double>(p.M) / rows + p.n_seg > 65535) continue;   // gate and up take two blocks
-      const double wgs = blocks(rows) * std::ceil(p.N / static_cast<double>(cols));
-      const double idle = (static_cast<double>(p.M) / rows + p.n_seg) * std::ceil(p.N / static_cast<double>(cols)) - wgs;
-      offer(static_cast<Form>(f), 2 + (p.seg_off ? 0.5 * std::max(0.0, idle) / cus : 0) + std::ceil(wgs / cus) * (1.45 + 5.5e-4 * rows * cols + (rows + cols) * static_cast<double>(p.K) / rate));
-    }
-  }
-  const auto tiles = [&](int bm, int bn) { return blocks(bm) * std::ceil(p.N / static_cast<double>(bn)); };
-  const double mid = tiles(128, 128), rest = std::fmod(mid, 2 * cus) / cus;
-  const double part = rest == 0 ? 0 : rest <= 1 ? 0.62 : 0.62 + 0.48 * (rest - 1);
-  offer(kMid, 6 + nk * (std::floor(mid / (2 * cus)) * 1.1 + part) * (f32 ? 1.75 : far ? 1.2 : 1));
-  if (!f32) {                                            // exact sums do not fit its registers
-    // one tile a CU at a time; grouped, a round's end is not the same for all, half a round lost on the average
-    const auto lone = [&](Form f, int rows, double start, double per, double full, double far_per) {
-      const double nt = std::ceil(p.N / 128.);
-      double us = 0;
-      if (segs > 1) {
-        const double x = segs / (1 - std::exp(-rows * segs / p.M)) * nt / cus, rounds = x <= 1.05 ? 1 : x + 0.5;
-        us = start + nk * (far ? far_per : full) * rounds + 5 * (rounds - 1);
-      } else {
-        const double x = blocks(rows) * nt / cus, whole = std::floor(x), rest = x - whole;
-        us = start + nk * (whole * full + (rest == 0 ? 0 : per + (full - per) * std::max(0., 2 * rest - 1))) + 5 * (std::ceil(x) - 1);
-      }
-      offer(f, us);
-    };
-    lone(kLow, 64, 5.2, 0.37, 0.395, 0.56);
-    lone(kDeep, 128, 6.3, 0.38, 0.51, 0.62);
-    const double big = tiles(256, 256), left = std::fmod(big, cus) / cus;
-    offer(kBig, 6 + nk * (std::floor(big / cus) * 1.85 + (left == 0 ? 0 : 1.25 + 0.6 * left)));
-  }
-  return form;
-}
-
 template <bool ROW, bool SWIGLU, bool F32>
 int launch(const f8::GemmArgs& p, hipStream_t st) {
-  switch (choose(p, SWIGLU, F32)) {
+  using namespace f8;
+  switch (choose_form(xs_host::persistent_grid(0), p.M, p.N, p.K, p.ldb_s, p.seg_off ? p.n_seg : 0, SWIGLU, F32)) {
     case kSplit12: return launch_split<1, 2, 4, ROW, SWIGLU, F32>(p, st);
     case kSplit21:
       if constexpr (!SWIGLU) return launch_split<2, 1, 4, ROW, SWIGLU, F32>(p, st);

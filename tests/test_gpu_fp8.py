@@ -455,15 +455,14 @@ def test_gemm_of_about_a_tile_to_a_cu(M, N, blocks, block):
 @pytest.mark.parametrize("spans,N,K", [
     ([(0, 100), (0, 100), (100, 100)], 256, 256),                            # more row blocks than M and n_seg alone ask for
     ([(0, 700)] * 5 + [(700, 100)], 256, 384),
-    ([(0, 50)] * 70 + [(50, 33), (10, 60), (0, 83)], 264, 256),              # past the 64 segments of one scan
+    ([(0, 50)] * 70 + [(50, 33), (10, 60), (0, 83)], 512, 256),              # past the 64 segments of one scan, tiles
     ([(0, 3000), (0, 3000), (3000, 500)], 1024, 128),                        # tiles
-    ([(5, 1)] * 40 + [(6, 300)], 512, 1152)])
+    ([(5, 1)] * 40 + [(6, 300)], 512, 1152),
+    ([(0, 20)] * 100 + [(20, 30)], 256, 128)])                               # past one scan in a split form, two tiles a workgroup
 @pytest.mark.parametrize("epi", ["store", "swiglu"])
 def test_overlapping_segments_compute_all_their_rows(spans, N, K, epi):
     """Segments race on their common rows only: an element there is that of one of them, and every other row is its
     segment's. Small integers and power-of-two scales: the 8-bit products are exact (test_gemm_of_integers_is_exact)."""
-    if epi == "swiglu" and N % 256:
-        pytest.skip("SwiGLU takes N in 256s")
     X = xs()
     M, n = max(o + r for o, r in spans) + 3, len(spans)
     g = np.random.default_rng(M + n)
@@ -493,3 +492,93 @@ def test_overlapping_segments_compute_all_their_rows(spans, N, K, epi):
         fits[o:o + r] |= np.abs(got[o:o + r] - want) <= tol
         covered[o:o + r] = True
     assert fits[covered].all() and (bits[~covered] == 0xFFFF).all()
+
+
+# Sizes for the forms that the tables above do not reach; which form takes each is checked in test_fp8_forms.py.
+FORM_GEMMS = [(96, 1360, 384), (88, 1352, 1280), (33, 4096, 256), (60, 4088, 640), (100, 4096, 256), (190, 4096, 512), (120, 4104, 896)]
+LARGE_GEMMS = [(4093, 4096, 128), (4093, 4096, 256), (4093, 4096, 384), (2300, 4104, 640), (8200, 4096, 256), (8300, 1032, 1152)]
+LARGE_GROUPS = [([3000, 0, 1, 257, 2500, 700, 129, 5], 4096, 128), ([3000, 0, 1, 257, 2500, 700, 129, 5], 4096, 384),
+                ([2600, 1, 255, 256, 3100], 4096, 640), ([0, 3000, 0], 4096, 1152), ([900, 30, 512, 1], 2048, 512),
+                ([700, 300, 0, 129, 400], 2048, 640), ([1200, 7, 300], 2048, 1152), ([0, 2100, 1100], 1280, 256),
+                ([350, 1, 260, 90], 2048, 1408), ([30, 32, 28], 256, 1024), ([60, 40, 30], 1280, 768), ([35, 20, 14], 3584, 512)]
+
+
+@pytest.mark.parametrize("M,N,K", FORM_GEMMS)
+@pytest.mark.parametrize("block", ["tile", "row"])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_gemm_of_every_split_form(M, N, K, block, out):
+    test_gemm(M, N, K, block, out)
+
+
+def _integers(rows, K, seed, down, top, low):
+    """Integer codes up to `top` under scales 2^low .. 2^(low + 2): every sum of products with its like below 2^24 units, so
+    exact in fp32 in any order; products of at most 2^5 lose nothing in the 8-bit unit. Returns device operand, fp32 values."""
+    g = np.random.default_rng(seed)
+    c = Codes(rows, K, down)
+    codes = mx.encode(g.integers(-top, top + 1, (rows, K)).astype(np.float64), mx.E4M3)
+    scales = (2.0 ** g.integers(low, low + 3, (c.srows, K // B))).astype(np.float32)
+    c.codes[:rows, :K] = torch.from_numpy(codes).cuda()
+    c.scales[:c.srows, :K // B] = torch.from_numpy(scales).cuda()
+    return c, fp8.values(codes, scales, down).astype(np.float32)
+
+
+@pytest.mark.parametrize("M,N,K", LARGE_GEMMS)
+@pytest.mark.parametrize("block", ["tile", "row"])
+def test_gemm_in_large_tiles(M, N, K, block):
+    """Every element of exact products, and rows at tiles' edges and elsewhere of random ones, where a persistent
+    workgroup takes one tile or several."""
+    X = xs()
+    down, kind = (1, X.XS_BLOCK_ROW) if block == "row" else (B, X.XS_BLOCK_TILE)
+    a, A = _integers(M, K, M, 1, 8, -4)
+    b, W = _integers(N, K, N + 1, down, 4, -2)
+    c = torch.full((M + 1, N + 8), -1, dtype=torch.int16, device="cuda")
+    _gemm(a, b, kind, c, M, N, K)
+    bits = host_bits(c)
+    assert (bits[M] == 0xFFFF).all() and (bits[:, N:] == 0xFFFF).all()
+    got = (bits[:M, :N].astype(np.uint32) << 16).view(np.float32)
+    assert np.array_equal(got, (synth.to_bf16_bits(A @ W.T).astype(np.uint32) << 16).view(np.float32))
+    del a, b, A, W
+    a, A = _operand(M, K, M + N, 1, pad=16, std=0.01)
+    b, W = _operand(N, K, N + K, down, pad=32, spad=4, std=0.02)
+    _gemm(a, b, kind, c, M, N, K)
+    rows = np.unique(np.r_[0:2, 126:130, 254:258, 2046:2050, M - 258:M - 254, M - 2:M, np.random.default_rng(1).integers(0, M, 48)])
+    _check_product(bits_f64(host_bits(c)[rows, :N]), A[rows], W, 2.0 ** -8, f"{M}x{N}x{K} {block}")
+
+
+def large_layout(rows):
+    """Segments with a row between and behind each: offsets and the rows in all."""
+    return np.cumsum([0] + [r + 1 for r in rows[:-1]]), sum(rows) + len(rows)
+
+
+@pytest.mark.parametrize("rows,N,K", LARGE_GROUPS, ids=lambda v: f"{len(v)}x{sum(v)}" if isinstance(v, list) else str(v))
+@pytest.mark.parametrize("epi", ["store", "swiglu"])
+def test_grouped_gemm_of_thousands_of_rows(rows, N, K, epi):
+    """Every element: exact products (SwiGLU: of exact gate and up values), empty segments, more tiles than workgroups."""
+    X = xs()
+    offs, M = large_layout(rows)
+    n = len(rows)
+    a, A = _integers(M, K, M, 1, 4, -4)
+    bs_, W = zip(*(_integers(N, K, 50 + s, B, 2, -2) for s in range(n)))
+    bc, bs = torch.stack([b.codes[:N] for b in bs_]), torch.stack([b.scales[:-(-N // B)] for b in bs_])
+    n_out = N // 2 if epi == "swiglu" else N
+    c = torch.full((M, n_out + 8), -1, dtype=torch.int16, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    do, dr = (torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda") for v in (offs, rows))
+    X.check(X.xs_grouped_gemm_fp8(*a.args(), M, do.data_ptr(), dr.data_ptr(), n, bc.data_ptr(), bs.data_ptr(), bs.shape[2], N, K,
+                                  c.data_ptr(), n_out + 8, X.XS_EPI_SWIGLU if epi == "swiglu" else X.XS_EPI_STORE, st.data_ptr(), _stream()))
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    bits, outside = host_bits(c), np.ones(M, bool)
+    for s, (o, r) in enumerate(zip(offs, rows)):
+        outside[o:o + r] = False
+        got, gu = (np.ascontiguousarray(bits[o:o + r, :n_out]).astype(np.uint32) << 16).view(np.float32), A[o:o + r] @ W[s].T
+        if epi == "store":
+            assert np.array_equal(got, (synth.to_bf16_bits(gu).astype(np.uint32) << 16).view(np.float32)), s
+        else:
+            # the activation's exponential, reciprocal and products, 2^-20 (1 + |gate|), and one rounding. A sigmoid below
+            # 2^-126 (gates below -87.3, -126 log 2, and here they go to -125) is no normal fp32 number: the reciprocal of
+            # more than 2^126, or of an exponential past fp32's range, is 0, off by at most 2^-126 times |gate up|
+            want, (gate, up) = fp8.swiglu(gu), np.abs(gu.astype(np.float64)).reshape(r, 2, n_out).transpose(1, 0, 2)
+            tol = 2.0 ** -20 * (1 + gate) * np.abs(want) + 2.0 ** -126 * gate * up
+            assert np.all(np.abs(got - want) <= 2.0 ** -8 * (np.abs(want) + tol) + tol + 2.0 ** -126), s
+    assert (bits[outside] == 0xFFFF).all() and (bits[:, n_out:] == 0xFFFF).all()
