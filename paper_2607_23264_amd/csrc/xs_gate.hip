@@ -100,7 +100,16 @@ __device__ __forceinline__ float lanes_max(float v) {
   return v;
 }
 
-// A slot's renormalized weight r_j among its token's lanes (0 without a live slot); l: its logit.
+// n / d, |n| <= d and d within 2^+-64, in one rounding but for 2^-23 of one: the product with the reciprocal unit's 1 / d
+// (within an fp32 unit), and its remainder's. The mean square error of renormalized weights is that of divisions; with
+// the product alone 1.18 times it, in the same time (32,768 tokens: 15.4 us).
+__device__ __forceinline__ float quotient(float n, float d) {
+  const float r = __builtin_amdgcn_rcpf(d), q = n * r;
+  return __builtin_fmaf(__builtin_fmaf(-q, d, n), r, q);
+}
+
+// A slot's renormalized weight r_j among its token's lanes (0 without a live slot); l: its logit. Both divisors are
+// between 1/2 and 32 (the largest s is 1 or, of sigmoids, at least 1/2).
 template <int LPT>
 __device__ __forceinline__ float renormalized(bool softmax, bool slot, float l) {
   slot = slot && l != -INFINITY;
@@ -112,10 +121,10 @@ __device__ __forceinline__ float renormalized(bool softmax, bool slot, float l) 
     // e^-|l| once; below all of the k, e^(l - c) comes with c = 0 from it too
     c = fminf(c, 0.f);
     const float t = expf(-fabsf(l));
-    if (slot) s = (l > 0.f ? 1.f : c == 0.f ? t : expf(l - c)) * __builtin_amdgcn_rcpf(1.f + t);
+    if (slot) s = quotient(l > 0.f ? 1.f : c == 0.f ? t : expf(l - c), 1.f + t);
   }
   const float total = lanes_sum<LPT>(s);
-  return total == 0.f ? 0.f : s * __builtin_amdgcn_rcpf(total);
+  return total == 0.f ? 0.f : quotient(s, total);
 }
 // Its score; m and inv: the row's largest logit and the reciprocal of its softmax sum.
 __device__ __forceinline__ float slot_score(bool softmax, bool slot, float l, float m, float inv) {

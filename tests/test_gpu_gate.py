@@ -360,3 +360,17 @@ def test_order_of_scores_that_64_bits_cannot_tell_apart(E, k, n_group, topk_grou
             idx, _ = _route(_gate(E, k, kind, n_group, topk_group, top2, bias=None if bias is None else bias.cuda(), dtype=dtype), dev, 4)
             want = gate.select(l, k, kind, n_group, topk_group, top2, None if bias is None else bias.numpy())
             assert np.array_equal(idx, want), (kind, top2, bias is None)
+
+
+def test_renormalized_weights_are_as_exact_as_the_formula_in_fp32():
+    """The mean square error against 64 bits is that of sigmoid, sum, division and scale each rounded to fp32 (a product
+    with a rounded reciprocal in place of each division has 1.18 times it): within 5 %, thirty times the
+    sampling error of 262,144 weights."""
+    T, E, k = 32768, 256, 8
+    l, l64 = _logits(T, E, "f32", 21)
+    idx, w = _route(_gate(E, k, "sigmoid", renorm=True, scale=2.5), _device(l, E), T)
+    s = torch.sigmoid(l.cuda()).gather(1, torch.from_numpy(idx).long().cuda())
+    plain = (s / s.sum(1, keepdim=True) * 2.5).cpu().double().numpy()
+    exact = gate.weights(l64, idx, "sigmoid", True, 2.5)
+    rms = lambda v: np.sqrt(np.mean(((v - exact) / exact) ** 2))
+    assert rms(w) <= 1.05 * rms(plain)
