@@ -3,8 +3,9 @@
 //
 //   s = max(amax, 2^-60) / 448        code = E4M3(x / s), ties to even
 //
-// both quotients rounded to fp32, so that every implementation of the same two lines has the same
-// bits. x / s comes without a division: with r = fl(1 / s) and q = fl(x r), q is within an fp32 unit of
+// both quotients rounded to fp32, so that every implementation with these divisions has the same bits (a
+// product with a rounded 1 / 448, as some take for a division by a constant, has other scales, and other codes
+// where x / s is a tie). x / s comes without a division: with r = fl(1 / s) and q = fl(x r), q is within an fp32 unit of
 // x / s, q s - x is exact in one fused multiply-add, and fl(q - (q s - x) r) is the rounded quotient
 // (Markstein's theorem; it asks for r correctly rounded and for a remainder that does not
 // underflow: at a code that is not zero q >= 2^-10 and s >= 2^-69, so its last bit is 2^-125 or more).
@@ -83,36 +84,21 @@ __device__ __forceinline__ uint32_t max16(uint32_t v) {
 constexpr u32x4 kZero4 = {0, 0, 0, 0};
 
 // ------------------------------------------------------------------------------ 1 x 128 along rows
-// Sixteen lanes per block, one 16-byte piece of eight values each; U blocks a lane group at once.
-template <int U>
+// Sixteen lanes per block, one 16-byte piece of eight values each.
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const uint16_t* __restrict__ x, int64_t ldx, int64_t rows,
                                                             int cols, uint8_t* __restrict__ codes, int64_t ldc,
                                                             float* __restrict__ scales, int64_t lds) {
-  const int blocks = (cols + 127) / 128;
-  const int64_t total = rows * blocks;
-  const int sub = threadIdx.x & 15;
-  const int64_t first = (block_number() * 16 + (threadIdx.x >> 4)) * U;
-  u32x4 raw[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    raw[u] = kZero4;
-    const int64_t i = first + u;
-    if (i < total) {
-      const int64_t r = i / blocks;
-      const int col = static_cast<int>(i - r * blocks) * 128 + sub * 8;
-      if (col < cols) raw[u] = *reinterpret_cast<const u32x4*>(x + r * ldx + col);
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t i = first + u;
-    const Scale s = scale_of(amax_f32(max16_packed(amax8(raw[u]))));
-    if (i < total) {
-      const int64_t r = i / blocks;
-      const int b = static_cast<int>(i - r * blocks);
-      *reinterpret_cast<uint2*>(codes + r * ldc + b * 128 + sub * 8) = codes8(raw[u], s);
-      if (sub == 0) scales[r * lds + b] = s.s;
-    }
+  const int blocks = (cols + 127) / 128, sub = threadIdx.x & 15;
+  const int64_t i = block_number() * 16 + (threadIdx.x >> 4);
+  const bool live = i < rows * blocks;
+  const int64_t r = i / blocks;
+  const int b = static_cast<int>(i - r * blocks), col = b * 128 + sub * 8;
+  u32x4 raw = kZero4;
+  if (live && col < cols) raw = *reinterpret_cast<const u32x4*>(x + r * ldx + col);
+  const Scale s = scale_of(amax_f32(max16_packed(amax8(raw))));
+  if (live) {
+    *reinterpret_cast<uint2*>(codes + r * ldc + col) = codes8(raw, s);
+    if (sub == 0) scales[r * lds + b] = s.s;
   }
 }
 
@@ -434,7 +420,7 @@ extern "C" int xs_quantize_fp8(const void* x, int64_t rows, int32_t cols, int64_
   if (!codes_t) {
     const int64_t groups = (rows * ((cols + 127) / 128) + 15) / 16;
     if (groups > xs_host::kMaxBlocks) return XS_EUNSUPPORTED;
-    hipLaunchKernelGGL((f8::quantize_rows_kernel<1>), xs_host::grid_of(groups), dim3(256), 0, st,
+    hipLaunchKernelGGL(f8::quantize_rows_kernel, xs_host::grid_of(groups), dim3(256), 0, st,
                        static_cast<const uint16_t*>(x), ldx, rows, cols, static_cast<uint8_t*>(codes), ld_codes, scales, ld_scales);
     return xs_host::launch_status();
   }
