@@ -367,8 +367,6 @@ int launch(const f8::GemmArgs& p, hipStream_t st) {
   using namespace f8;
   switch (choose_form(xs_host::persistent_grid(0), p.M, p.N, p.K, p.ldb_s, p.seg_off ? p.n_seg : 0, SWIGLU, F32)) {
     case kSplit12: return launch_split<1, 2, 4, ROW, SWIGLU, F32>(p, st);
-    case kSplit21:
-      if constexpr (!SWIGLU) return launch_split<2, 1, 4, ROW, SWIGLU, F32>(p, st);
     case kSplit22: return launch_split<2, 2, 3, ROW, SWIGLU, F32>(p, st);
     case kSplit24: return launch_split<2, 4, 2, ROW, SWIGLU, F32>(p, st);
     case kSplit44: return launch_split<4, 4, 2, ROW, SWIGLU, F32>(p, st);

@@ -11,20 +11,29 @@ namespace f8 {
 
 constexpr uint32_t kNone = 1u << 30;   // an offset past every buffer of the split form; twice it does not wrap
 
-enum Form { kSplit12, kSplit21, kSplit22, kSplit24, kSplit44, kLow, kDeep, kMid, kBig };
+enum Form { kSplit12, kSplit22, kSplit24, kSplit44, kLow, kDeep, kMid, kBig };
 
 // The cheapest form by a model of its time in us, from M, N, K and the CU count (n_seg > 0: grouped, with
 // exponential segment lengths, n / (1 - exp(-rows n / M)) row blocks of n segments). A split form takes its rounds of
 // workgroups, each a start and a join that grow with its outputs, and its rows of K bytes at the rate of a
 // CU's memory path; tiles take K / 128 blocks a round, of one 256 x 256, up to two 128 x 128 or one tile of four
 // stages a CU. Weights past the caches (grouped products that touch over 100 MB) come more slowly. Measured, us,
-// split 1x2 / 2x4 / 4x4, 64 x 128 and 128 x 128 of four stages, 128- and 256-tiles, N = 4096, K = 7168:
-//   M = 24  8.4 / 12.0 / 16.8 / 25 / 24 / 37 / 71        M = 128  26 / 13.3 / 18.1 / 25.6 / 27.8 / 42 / 71
-//   M = 512  93 / 46 / 35 / 27.2 / 28.3 / 43 / 74        M = 1024  - / 86 / 67 / 52 / 35.7 / 44 / -
-//   M = 2048  - / 171 / 131 / 101 / 71 / 62 / 82         M = 4093  - / - / - / 198 / 146 / 134 / 105
-//   K = 1024: M = 512  - / 16.3 / 12.6 / 8.3 / 9.2 / 11.1 / -
-// 32 segments with SwiGLU: 64 rows in all  137 / 128 / 137 / 127 / 129 / 143 / 178; 1024  342 / 211 / 197 / 170 /
-// 163 / 159 / 189; 8192  - / 909 / 701 / 496 / 371 / 346 / 323.
+// split 1x2 / 2x2 / 2x4 / 4x4, 64 x 128 and 128 x 128 of four stages, 128- and 256-tiles, N = 4096, K = 7168:
+//   M = 24  8.0 / 8.9 / 11.6 / 16.2 / 23 / 22 / 36 / 52      M = 64  13.8 / 9.8 / 12.3 / 18.0 / 25 / 23 / 37 / 53
+//   M = 128  25.5 / 17.7 / 12.7 / 17.5 / 25 / 27 / 48 / 55   M = 256  48 / 32 / 23 / 18.0 / 25 / 27 / 45 / 76
+//   M = 512  92 / 62 / 44 / 34 / 26.6 / 27.7 / 43 / 75       M = 1024  180 / 122 / 85 / 66 / 49 / 33.8 / 44 / 76
+//   M = 2048  - / - / - / 134 / 100 / 64 / 62 / 82           M = 4093  - / - / - / 259 / 195 / 131 / 123 / 102
+//   K = 1024: M = 512  - / - / 16.3 / 12.6 / 8.3 / 9.2 / 11.1 / -
+// Scales by rows on both sides cost more in each form and leave the order nearly as it is, so the model has no term
+// for them (the worst choice seen: 2048 rows 80 for 72):
+//   M = 24  9.0 / 10.4 / 15.0 / 18.0 / 27 / 26 / 40 / 66     M = 128  29.7 / 20.1 / 15.4 / 20.3 / 32 / 38 / 50 / 68
+//   M = 512  110 / 72 / 54 / 39.5 / 32.6 / 37.1 / 46 / 98    M = 1024  216 / 142 / 106 / 77 / 62 / 41.7 / 46 / 98
+//   M = 2048  - / - / - / 157 / 122 / 80 / 72 / 102          M = 4093  - / - / - / 309 / 245 / 163 / 143 / 122
+//   fp32 results (split forms, 128-tiles)  M = 128  30.7 / 21.4 / 16.1 / 22.4 / 68   M = 512  115 / 77 / 58 / 44.5 / 67
+//   M = 1024  224 / 150 / 112 / 87 / 68
+// 32 segments with SwiGLU: 64 rows in all  142 / 147 / 130 / 141 / 127 / 129 / 142 / 177; 1024  370 / 281 / 214 / 202 / 169 /
+// 162 / 158 / 188; 8192  - / - / 909 / 701 / 492 / 362 / 337 / 315. Where the
+// model took a 2x1 form (96 x 1360 x 1024 6.7, 160 x 816 x 4096 6.8) 2x2 takes the same: there is none.
 inline Form choose_form(double cus, int M, int N, int K, int64_t ldb_s, int n_seg, bool swiglu, bool f32) {
   const bool grouped = n_seg > 0;
   if (!grouped) n_seg = 1;
@@ -45,11 +54,11 @@ inline Form choose_form(double cus, int M, int N, int K, int64_t ldb_s, int n_se
   // offsets of the split form's buffers stay below kNone, its column blocks (of 16 or more, 256 threads) in a
   // grid's first dimension of 2^32 - 1 threads, its row blocks in the second
   if ((n_out / 128 + 1) * ldb_s * 4 < kNone && N < (1 << 28)) {
-    constexpr int forms[5][2] = {{1, 2}, {2, 1}, {2, 2}, {2, 4}, {4, 4}};
+    constexpr int forms[4][2] = {{1, 2}, {2, 2}, {2, 4}, {4, 4}};
     const double rate = f32 ? 55e3 : far ? 47e3 : 70e3;
-    for (int f = 0; f < 5; ++f) {
+    for (int f = 0; f < 4; ++f) {
       const int rows = 16 * forms[f][0], cols = 16 * forms[f][1];
-      if ((swiglu && f == kSplit21) || static_cast<double>(M) / rows + n_seg > 65535) continue;   // gate and up take two blocks
+      if (static_cast<double>(M) / rows + n_seg > 65535) continue;
       const double wgs = blocks(rows) * std::ceil(N / static_cast<double>(cols));
       const double idle = (static_cast<double>(M) / rows + n_seg) * std::ceil(N / static_cast<double>(cols)) - wgs;
       offer(static_cast<Form>(f), 2 + (grouped ? 0.5 * std::max(0.0, idle) / cus : 0) + std::ceil(wgs / cus) * (1.45 + 5.5e-4 * rows * cols + (rows + cols) * static_cast<double>(K) / rate));
