@@ -29,11 +29,10 @@ struct GemmArgs {
 
 // Work index t -> (segment, row block, column tile): segments in order; within one, groups of eight row
 // blocks, the row blocks of a group varying fastest (32 consecutive tiles, one XCD's, are then 8 x 4: twelve
-// operand panels for its L2). Every wave scans the segments itself. end: the number of tiles, where the scan has
-// come to the last segments.
+// operand panels for its L2). Every wave scans the segments itself. more: there is, or may be, a tile t + step.
 struct Where {
   int seg, m0, rows, nb;
-  int64_t end;
+  bool more;
 };
 constexpr int kGroupRows = 8, kRun = 32;
 constexpr int64_t kNoTile = int64_t(1) << 50;
@@ -45,13 +44,13 @@ __device__ __forceinline__ void in_groups(int64_t t, int blocks, int nt, int* mb
   *nb = local / gm;
 }
 template <int BM>
-__device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, Where& at) {
+__device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int64_t step, int nt, Where& at) {
   if (!p.seg_off) {
     const int blocks = static_cast<int>((static_cast<int64_t>(p.M) + BM - 1) / BM);
     if (t >= static_cast<int64_t>(blocks) * nt) return false;
     int mb, nb;
     in_groups(t, blocks, nt, &mb, &nb);
-    at = Where{0, mb * BM, min(BM, p.M - mb * BM), nb, static_cast<int64_t>(blocks) * nt};
+    at = Where{0, mb * BM, min(BM, p.M - mb * BM), nb, t + step < static_cast<int64_t>(blocks) * nt};
     return true;
   }
   const int lane = threadIdx.x & 63;
@@ -86,7 +85,7 @@ __device__ __forceinline__ bool find_tile(const GemmArgs& p, int64_t t, int nt, 
       at.m0 = __builtin_amdgcn_readfirstlane(off + mb * BM);
       at.rows = __builtin_amdgcn_readfirstlane(min(BM, rows - mb * BM));
       at.nb = __builtin_amdgcn_readfirstlane(nb);
-      at.end = s0 + 64 < p.n_seg ? INT64_MAX : base + __shfl(incl, 63);
+      at.more = s0 + 64 < p.n_seg || __ballot(t + step < base + incl);
       return true;
     }
     base += __shfl(incl, 63);
@@ -110,7 +109,8 @@ __global__ __launch_bounds__(T::kThreads, 2) void gemm_kernel(GemmArgs p) {
   const int G = gridDim.x, b = blockIdx.x;
   int64_t t = G % 8 ? b : (b % 8) * (G / 8) + b / 8;
   if (p.one_each) t = (static_cast<int64_t>(b / 8 / kRun) * 8 + b % 8) * kRun + b / 8 % kRun;
-  for (; find_tile<T::kBM>(p, t, nt, at); t += p.one_each ? kNoTile : G) {
+  const int64_t step = p.one_each ? kNoTile : G;
+  for (; find_tile<T::kBM>(p, t, step, nt, at); t += step) {
     const int n0 = at.nb * kCols;
     const Product q{p.a + at.m0 * p.lda, p.lda, p.a_s + at.m0 * p.lda_s, p.lda_s, at.rows,
                     p.b + at.seg * p.b_seg, p.ldb, p.b_s + at.seg * p.b_s_seg, p.ldb_s, n0, p.N, p.N / 2, p.K};
@@ -164,27 +164,46 @@ __global__ __launch_bounds__(T::kThreads, 2) void gemm_kernel(GemmArgs p) {
   }
 }
 
+// The kernel's only argument, read where this stands from where the launch put it.
+template <class A>
+__device__ __forceinline__ A kernel_args() {
+  typedef const uint32_t __attribute__((address_space(4))) Constant;
+  int zero;
+  asm volatile("s_mov_b32 %0, 0" : "=s"(zero));
+  Constant* const p = (Constant*)__builtin_amdgcn_kernarg_segment_ptr() + zero;
+  struct Words {
+    uint32_t w[sizeof(A) / 4];
+  } words;
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(A) / 4; ++i) words.w[i] = p[i];
+  return __builtin_bit_cast(A, words);
+}
+
 // Products with few output tiles: a workgroup takes 16 NB rows and 16 NJ columns and splits the K blocks
 // over its four waves, whose scaled fp32 sums meet in LDS once and are added in wave order. Each wave
 // stages its own blocks (one 128-byte line of every row, and the rows' scales) kDepth deep in a slice of
 // LDS of its own, by direct loads, and needs no barrier until the end. SWIGLU: columns y < NJ / 2 are the
 // gate's, the others the same columns of up. GROUPED: segments that overlap have more row blocks than the grid was
-// sized for, and a workgroup goes on to a second one (the loop in plain products too: 24 x 4096 x 7168 7.82 us
-// where it takes 7.65).
+// sized for, and a workgroup goes on to a second one. Arguments and lanes' offsets are made anew for each: held over the
+// loop they spill, 137 us for 134 (32 segments, 128 rows of 4096 x 7168) and 4.8 for 4.5 (4 segments of 768 x 1792).
 template <int NB, int NJ, int kDepth, bool ROW, bool SWIGLU, bool F32, bool GROUPED>
-__global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
+__global__ __launch_bounds__(256) void split_kernel(GemmArgs args) {
   constexpr int kWaves = 4, kRows = 16 * NB, kCols = 16 * NJ, kPitch = kCols + 4;
   constexpr int kPiece = (kRows + kCols) * 128 + 512;      // B rows, A rows, 64 scales of A, 64 of B
   constexpr int kLoads = 2 * (NB + NJ) + 2;
   constexpr int kStage = kWaves * kDepth * kPiece, kRed = kWaves * kRows * kPitch * 4;
   constexpr int kHalf = SWIGLU ? kCols / 2 : kCols;        // output columns of the workgroup
   __shared__ __attribute__((aligned(16))) char smem[kStage > kRed ? kStage : kRed];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x * kHalf, n_out = SWIGLU ? p.N / 2 : p.N;
-  Where at;
-  for (int64_t t = blockIdx.y; find_tile<kRows>(p, t, 1, at); t += gridDim.y) {   // (the whole workgroup)
+  for (int64_t t = blockIdx.y;; t += gridDim.y) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const GemmArgs p = GROUPED ? kernel_args<GemmArgs>() : args;
+    Where at;
+    if (!find_tile<kRows>(p, t, gridDim.y, 1, at)) return;  // the whole workgroup
+    const int lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int i = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * kHalf, n_out = SWIGLU ? p.N / 2 : p.N;
     const int rows = at.rows, cols = min(kHalf, n_out - n0);
     lds_char* const lds = (lds_char*)smem + w * kDepth * kPiece;
     const uint8_t* const b = p.b + at.seg * p.b_seg;
@@ -311,7 +330,7 @@ __global__ __launch_bounds__(256) void split_kernel(GemmArgs p) {
       if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.c) + to) = v;
       else *reinterpret_cast<uint2*>(p.c + to * 2) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
-    if (!GROUPED || t + gridDim.y >= at.end) return;
+    if (!GROUPED || !at.more) return;
     __syncthreads();                                         // the sums have been read: the LDS is free
   }
 }
