@@ -359,9 +359,10 @@ __device__ __forceinline__ void load_run(const void* base, int first, int VP, in
 // by the token's whole wave (gate_token).
 // Without a bias the logits are the keys, exactly (bf16 ones also when cut).
 //
-// Bound by vector instructions (32,768 tokens, top-8 of 256 biased sigmoid scores in groups: 850 for four
-// tokens, 12 us at full rate; 17.8 us, 2.0 TB/s): so what a token needs is fixed when the kernel is compiled
-// (the kind of key, whole rows), the lanes exchange by DPP, and the keys are integers throughout.
+// 32,768 tokens, top-8 of 256 biased sigmoid scores in groups: 15.5 us, 2.3 TB/s, vector instructions issuing for 10.3
+// of them (780 for four tokens, at 2.4 GHz). What a token needs is fixed when the kernel is compiled (the kind
+// of key, whole rows), the lanes exchange by DPP, and the keys are integers throughout. Not at a bound: `r % lanes`
+// below is some ten dependent scalar instructions fourteen times, and keys are mapped to integers one by one.
 //   sigmoid: exp(-l) is off by 2^-23 and, from its argument, |l| 2^-23; times s (1 - s), with s (1 - s) |l|
 //     <= 0.224; the sum and the reciprocal 2^-24 + 2^-23 of s: together below 2^-22 (s <= 1).
 //   softmax: e^-d is off by d 2^-22 + 2^-23 (d e^-d <= 0.37), the sum of up to 512 terms (32 in a
@@ -522,7 +523,7 @@ __global__ __launch_bounds__(256) void gate_rows_kernel(GateArgs g, int VP, int 
     }
   }
   // The KL largest of a lane's keys in order; then the sixteen lanes' largest first keys one by one, each taken
-  // from its lane's list (merging the lists in a network over the lanes instead: 19.5 us where this takes 17.8).
+  // from its lane's list (merging the lists in a network over the lanes instead took a tenth longer).
   int top[KL];
 #pragma unroll
   for (int i = 0; i < KL; ++i) top[i] = i < VPL ? pack_key(o[i < VPL ? i : 0], first + i) : kNoKey;
@@ -634,7 +635,9 @@ struct GateGradArgs {
 // or for a plain softmax -s_e sum_i g_i s_i) and goes to LDS; the slots' lanes then write their experts' whole
 // elements over it (LDS operations of one wave are in order; an expert's duplicate slots write the same
 // value, summed in ascending j), and the row is stored from there. Adding the k slots to all of a lane's
-// elements in registers instead took 17.7 us where this takes 11.4 (32,765 tokens of 256 bf16 logits).
+// elements in registers instead took 1.55 times as long (32,765 tokens of 256 bf16 logits: 10.3 us, of sigmoid or
+// renormalized gates, which read no whole row, 7.7; fp32 logits 11.7 and 9.8). Not at a bound: the index, then the slot's
+// logit, then the row's pieces are waited for one after the other.
 template <typename LT, int LPT, int NQ, bool VEC>
 __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs g) {
   constexpr int P = 16 / sizeof(LT), kRow = NQ * LPT * P;      // elements of a row in LDS
@@ -843,7 +846,7 @@ extern "C" int xs_route_gate(const xs_gate* g, const void* logits, int64_t ld, i
   hipStream_t st = static_cast<hipStream_t>(stream);
   const size_t lds = 4 * sizeof(double) * g->E;
   // Sixteen lanes per token where each lane has at most 32 consecutive experts and groups are whole lanes;
-  // one wave per token otherwise (32,768 tokens, top-8 of 256 in groups: 18 us against 120; 16,384, top-4 of 60 in
+  // one wave per token otherwise (32,768 tokens, top-8 of 256 in groups: 15.5 us against 120; 16,384, top-4 of 60 in
   // 4 groups: 8.4 against 18).
   if (a.E <= 512 && a.k <= 16 && 16 % a.n_group == 0) {
     if (g->logits_type == XS_TYPE_BF16) launch_rows<uint16_t>(a, lds, st);
