@@ -1,12 +1,15 @@
 """The GPU parity tests of the E4M3 products reach every kernel form that the library's choice gives to a call: the choice
-(host code) is compiled alone and asked for each of the tests' sizes, with the 256 CUs of the device."""
+(host code) is compiled alone and asked for each of the tests' sizes, with the 256 CUs of the device. And the kernels of
+these forms, like the gates', keep their state in registers."""
 import os
+import re
 import shutil
 import subprocess
 
 import pytest
 
 import test_gpu_fp8 as t
+from test_built_code import READELF, objects  # noqa: F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 NAMES = ["split12", "split22", "split24", "split44", "low", "deep", "mid", "big"]
@@ -69,3 +72,20 @@ def test_overlapping_segments_in_split_forms_and_tiles(forms):
     got = forms([(max(o + r for o, r in spans) + 3, N, K, len(spans), 0, 0) for spans, N, K in cases])
     assert {f[:5] for f in got} >= {"split"} and set(got) & {"low", "deep", "mid", "big"}
     assert any(f.startswith("split") and len(c[0]) > 64 for f, c in zip(got, cases))
+
+
+def test_the_kernels_stay_in_registers(objects):  # noqa: F811
+    """Spilled vector registers: only the 256-tile's, where 256 registers hold the sums and scales by rows or SwiGLU's halves
+    come on top, and no more of them than what the forms' measured times contain."""
+    spills = {}
+    for path in objects:
+        r = subprocess.run([READELF, "--notes", str(path)], capture_output=True, text=True, check=True)
+        names = re.findall(r"^\s+\.name:\s+(_Z\w+)$", r.stdout, flags=re.M)
+        counts = re.findall(r"^\s+\.vgpr_spill_count:\s+(\d+)$", r.stdout, flags=re.M)
+        assert len(names) == len(counts)
+        spills.update((n, int(c)) for n, c in zip(names, counts) if "N2xs2f8" in n or "gate_" in n)
+    assert len(spills) > 100
+    big = "4TileILi256ELi256ELi2ELi4ELi2EEE"
+    allowed = {big + "Lb1ELb0ELb0E": 9, big + "Lb0ELb1ELb0E": 2}
+    for name, n in spills.items():
+        assert n <= max([v for k, v in allowed.items() if k in name], default=0), name
