@@ -267,7 +267,7 @@ struct SwigluArgs {
 };
 
 // h = silu(g) u in fp32, its blocks of 128 columns quantized; with KEEP the gate and up values too, each
-// in its own blocks. Sixteen lanes per block of h, eight columns each. 32,768 x 2048 with KEEP: 94-97 us, memory (a copy's
+// in its own blocks. Sixteen lanes per block of h, eight columns each. 32,768 x 2048 with KEEP: 93-97 us, memory (a copy's
 // rate) and vector issue (90 % of slots) at once. The sigmoid by the reciprocal unit is off by up to an fp32 unit more than a
 // division; the codes' error against 64 bits is that of fp32 divisions all the same (2.4e-4; 2.2e-4 with silu as a
 // quotient of one rounding, which took 4.6 % longer).
