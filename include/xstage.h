@@ -10,6 +10,8 @@
  *     per-destination windows as tiles complete;
  *   - Ulysses sequence parallelism (Sec. 5.4, GEMM-All-to-All): QKV projection whose
  *     epilogue stores head groups into per-destination windows;
+ *   - what surrounds these in a training step and in serving: causal attention of packed sequences and
+ *     over a cache with its gradients, the RMS norm into E4M3, a router's balance loss;
  *   - store pacing: the tile order of the persistent EP kernel (Expert-Wave, cross-wave
  *     interleaving of Alg. 1, chunked bursts) and the Burst-Gap model of Sec. 3
  *     (Eqs. 1-6) with its calibration microbenchmark (Sec. 3.1).
@@ -49,7 +51,8 @@ enum {
   XS_EWORKSPACE = 4,    /* workspace missing or too small */
   XS_ECAPACITY = 5,     /* device: a window received more rows than capacity_rows */
   XS_ETIMEOUT = 6,      /* device: a bounded dependency wait expired */
-  XS_EBADINPUT = 7      /* device: an expert id outside [0, E), or listed twice by one token */
+  XS_EBADINPUT = 7      /* device: an expert id outside [0, E), or listed twice by one token; a segment or
+                           sequence that does not lie in its tensor */
 };
 
 /* Text for a status code (static storage; never NULL). */
@@ -134,6 +137,33 @@ int xs_route_gate(const xs_gate* g, const void* logits, int64_t ld, int32_t T, i
 int xs_route_gate_backward(const xs_gate* g, const void* logits, int64_t ld, int32_t T,
                            const int32_t* topk_idx, const float* d_topk_w, void* d_logits,
                            int64_t ld_d, int32_t* dev_status, void* stream);
+
+/* Counts and balance loss of a router over packed sequences: sequence s is the tokens [seq_start[s],
+ * seq_start[s + 1]), T_s of them (seq_start device int32 [n_seq + 1], or NULL with n_seq = 1: all T tokens).
+ *   counts      device int32 [n_seq][E] out: slots of its tokens routed to expert e; an index outside [0, E) sets
+ *               XS_EBADINPUT in dev_status and its slot counts as absent
+ *   mean_share  device fp32 [n_seq][E] out: P_se, the mean over its tokens of p_te, a token's scores divided by
+ *               their sum (softmax scores as they are; a token masked whole has none)
+ *   loss        device fp32 [n_seq] out: alpha sum_e f_se P_se with f_se = E counts_se / (k T_s), alpha for a balanced
+ *               router; 0 for an empty sequence
+ * Of g, E, k, score and logits_type are read. logits [T][E] rows ld elements apart, topk_idx device int32 [T][k]
+ * (of xs_route_gate). workspace: device, 16-byte aligned, xs_balance_loss_workspace_bytes() bytes. Starts that are not in
+ * [0, T] or descend set XS_EBADINPUT; such sequences count as empty, and with sequences that overlap for it the outputs
+ * are not specified. Sums are fp32, their order follows from the lengths and the device's CU count alone. Requires E <=
+ * 1024, 1 <= k <= min(E, 32), 1 <= n_seq <= 65536, a finite alpha: otherwise XS_EINVAL and nothing is launched. */
+int xs_balance_loss_workspace_bytes(int32_t T, int32_t E, int32_t n_seq, int64_t* bytes);
+int xs_balance_loss(const xs_gate* g, const void* logits, int64_t ld, int32_t T, const int32_t* topk_idx,
+                    const int32_t* seq_start, int32_t n_seq, float alpha, int32_t* counts, float* mean_share,
+                    float* loss, void* workspace, int64_t workspace_bytes, int32_t* dev_status, void* stream);
+
+/* Gradient of sum_s d_loss[s] loss[s] in the logits, counts held fixed, added to d_add (the gradient of
+ * xs_route_gate_backward, say; of logits_type, rows ld_add apart; NULL: nothing is added):
+ *   d_logits[t][e] = d_add[t][e] + p_te (c_e - sum_f c_f p_tf) [(1 - s_te) for sigmoid scores], c_e = alpha d_loss_s f_se / T_s
+ * d_loss device fp32 [n_seq], counts of xs_balance_loss; d_logits device [T][E] of logits_type (rows ld_d apart), d_add or logits
+ * itself (with its row distance) or apart from both; rows of tokens outside every sequence are not written. Argument errors as above. */
+int xs_balance_loss_backward(const xs_gate* g, const void* logits, int64_t ld, int32_t T, const int32_t* seq_start,
+                             int32_t n_seq, float alpha, const int32_t* counts, const float* d_loss, const void* d_add,
+                             int64_t ld_add, void* d_logits, int64_t ld_d, int32_t* dev_status, void* stream);
 
 /* ----------------------------------------------------------------------------- layout
  * Destination-window layout of every (source, token, slot) (the Dispatch exchange,
@@ -560,6 +590,74 @@ int xs_attention(const xs_attn* a, int32_t mode, const xs_trace* trace, void* st
 int xs_ulysses_copy(const void* o, int32_t heads, int32_t M, int32_t head_dim,
                     const xs_window* win, int32_t W, void* stream);
 
+/* ----------------------------------------------------------------------------- packed attention
+ * Attention of packed sequences of different lengths with grouped heads: prompts (keys and queries of the
+ * same tokens), and new tokens over a cache of keys and values. Sequence s has the n = q_start[s + 1] -
+ * q_start[s] queries from row q_start[s] of q and o, and m keys from row k_start[s] of k and v: m = k_start[s + 1] -
+ * k_start[s], or, with k_rows, k_rows[s] (a cache with room behind each sequence; ranges may then overlap, as shared
+ * prefixes do). With causal != 0 query i sees the keys j <= i + m - n (the last query sees every key), else all m:
+ *   O_i = sum_j softmax_j(scale Q_i . K_j) V_j          lse_i = log sum_j exp(scale Q_i . K_j)
+ * over the keys it sees; a query that sees none (i + m < n, or m = 0) has O = 0 and lse = -infinity.
+ * Query head h reads key head h / (heads / kv_heads).
+ *   q, o     device bf16, row t of head h at q + t q_row + h q_head elements (any layout with contiguous head_dim); o apart from
+ *            the rest
+ *   k, v     device bf16, likewise with kv_heads heads
+ *   lse      device fp32 [heads][Tq] out, or NULL
+ *   q_start  device int32 [n_seq + 1]; k_start device int32 [n_seq + 1], with k_rows [n_seq]; k_rows device int32 [n_seq] or NULL
+ *   Tq, Tk   rows of q and o, of k and v
+ *   max_k    the most keys of a sequence (0: Tk)
+ *   scale    0 = 1 / sqrt(head_dim)
+ *   workspace  device, 16-byte aligned, xs_attention_packed_workspace_bytes() bytes (0 for calls with many rows)
+ * A sequence whose queries do not lie in [0, Tq), whose keys do not lie in [0, Tk) or are more than max_k sets
+ * XS_EBADINPUT in dev_status and is skipped. Rows of o and lse outside every sequence are not written, keys and values
+ * outside every sequence (also behind k_rows) are not read. A sequence's keys and values have to be finite: a query
+ * may take 0 times one that causality hides from it.
+ * Scores, softmax and sums are fp32; probabilities are rounded to bf16 for the second product. How keys are
+ * split over workgroups follows from the lengths, the descriptor and the device's CU count alone.
+ * Requires head_dim 64 or 128, row strides of at most 2^23 elements, Tq heads / kv_heads < 2^30, Tk <= 2^30 (else XS_EUNSUPPORTED), heads a multiple of
+ * kv_heads, strides multiples of 8 and at least head_dim, 16-byte aligned pointers, n_seq in [1, 65536], max_k <= Tk,
+ * reserved 0 (else XS_EINVAL); nothing is launched on an error. */
+typedef struct xs_attn_packed {
+  int32_t n_seq, heads, kv_heads, head_dim;
+  int32_t Tq, Tk;
+  int32_t causal;
+  int32_t max_k;
+  float scale;
+  int32_t reserved;           /* 0 */
+  const int32_t* q_start;
+  const int32_t* k_start;
+  const int32_t* k_rows;
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+} xs_attn_packed;
+
+int xs_attention_packed_workspace_bytes(const xs_attn_packed* a, int64_t* bytes);
+int xs_attention_packed(const xs_attn_packed* a, void* workspace, int64_t workspace_bytes, int32_t* dev_status,
+                        void* stream);
+
+/* Its gradients, from the forward call's descriptor with its o and lse and from d_o (rows and heads do_row and do_head
+ * elements apart): dq, dk and dv in bf16 (dk and dv summed over the query heads of a key head in fp32), each apart from
+ * every other tensor. With D = d_o . o per query, P the probabilities:
+ *   dS = P (d_o V^T - D)     dq = scale dS K     dk = scale dS^T Q     dv = P^T d_o
+ * Keys that no query sees have zero gradients; rows outside every sequence are not written. Sums have a fixed
+ * order (nothing is added atomically). k_rows must be NULL (XS_EUNSUPPORTED: gradients of overlapping ranges), a->lse is
+ * required. d_o has to be finite. Otherwise as above. */
+typedef struct xs_attn_grads {
+  const void* d_o;
+  void* dq;
+  void* dk;
+  void* dv;
+  int64_t do_row, do_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
+} xs_attn_grads;
+
+int xs_attention_packed_backward_workspace_bytes(const xs_attn_packed* a, int64_t* bytes);
+int xs_attention_packed_backward(const xs_attn_packed* a, const xs_attn_grads* g, void* workspace,
+                                 int64_t workspace_bytes, int32_t* dev_status, void* stream);
+
 /* ----------------------------------------------------------------------------- MX formats
  * Quantized EP precisions (W8A8, W4A8: Sec. 5.2, the MegaMoE sweep; the paper does not fix the
  * formats). Reading: OCP microscaling as the gfx950 matrix cores take it. A block of 32
@@ -669,6 +767,35 @@ int xs_swiglu_fp8(const void* gu, int64_t ld_gu, int64_t rows, int32_t I, void* 
 int xs_swiglu_fp8_backward(const void* ck_codes, int64_t ld_ck, const float* ck_scales, int64_t ld_cks,
                            const void* dh, int64_t ld_dh, int64_t rows, int32_t I, void* d_gu, int64_t ld_dgu,
                            void* h, int64_t ld_h, void* stream);
+
+/* ----------------------------------------------------------------------------- RMS norm
+ * The norm between a residual stream and the products that read it:
+ *   h = bf16(x + residual)        y = h w / sqrt(mean(h^2) + eps)       (means over a row's cols)
+ *   x, residual  device bf16 [rows][cols] (ldx, ld_res elements per row); residual NULL: h = x
+ *   weight       device [cols], XS_TYPE_BF16 or XS_TYPE_F32 (weight_type)
+ *   h            bf16 [rows][cols] or NULL; x or residual itself (with its row distance) or apart from both
+ *   y            bf16 [rows][cols] or NULL; as h, and not h
+ *   codes, scales  y in E4M3 with 1 x 128 blocks, laid out as by xs_quantize_fp8 (from y's fp32 values, not from the
+ *                bf16 ones), or both NULL. One of y and codes is wanted.
+ * h is rounded first and the rest is fp32, rounded once. Every matrix has 16-byte aligned rows; eps >= 0 (a
+ * row of zeros under eps = 0 gives NaN). cols a multiple of 8, at most 32768, rows below 2^31, else XS_EUNSUPPORTED; XS_EINVAL
+ * on other bad arguments; nothing is launched on an error. */
+int xs_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld_res, const void* weight,
+               int32_t weight_type, float eps, int64_t rows, int32_t cols, void* h, int64_t ld_h, void* y,
+               int64_t ld_y, void* codes, int64_t ld_codes, float* scales, int64_t ld_scales, void* stream);
+
+/* Its gradients from the h that was kept: with i = 1 / sqrt(mean(h^2) + eps), u = h i, g = dy w
+ *   dx       bf16 [rows][cols] out: i (g - u mean(g u)) + dh, the gradient of x and of residual; dy, dh or h itself
+ *            (with its row distance) or apart from them
+ *   d_weight device fp32 [cols] out, 16-byte aligned, or NULL: the sum of dy u over the rows, in an order that follows from
+ *            rows, cols and the device's CU count alone
+ *   dy       bf16 [rows][cols]; dh: bf16 [rows][cols] or NULL, the gradient that h has besides (of the residual stream)
+ *   workspace  device, 16-byte aligned, xs_rmsnorm_backward_workspace_bytes() bytes; not read where d_weight is NULL
+ * Otherwise as xs_rmsnorm. */
+int xs_rmsnorm_backward_workspace_bytes(int64_t rows, int32_t cols, int64_t* bytes);
+int xs_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* dh, int64_t ld_dh, const void* h, int64_t ld_h,
+                        const void* weight, int32_t weight_type, float eps, int64_t rows, int32_t cols, void* dx,
+                        int64_t ld_dx, float* d_weight, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* ----------------------------------------------------------------------------- X-Stage
  * Burst-Gap model (Sec. 3.3-3.5). Units: bytes and microseconds.

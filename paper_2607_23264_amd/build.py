@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libxstage.so")
 BUILD = os.path.join(ROOT, "_build")
 
 SOURCES = ["xs_runtime.hip", "xs_ep.hip", "xs_gemm.hip", "xs_ep_ffn.hip", "xs_attn.hip", "xs_mx.hip", "xs_ring.hip", "xs_gate.hip", "xs_fp8.hip",
-           "xs_gemm_fp8.hip", "xs_microbench.hip",
+           "xs_gemm_fp8.hip", "xs_norm.hip", "xs_balance.hip", "xs_attn_packed.hip", "xs_microbench.hip",
            "xs_model.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -88,6 +88,19 @@ class xs_gate(C.Structure):
                 ("renormalize", i32), ("logits_type", i32), ("scale", C.c_float), ("reserved", i32), ("bias", vp)]
 
 
+class xs_attn_packed(C.Structure):
+    _fields_ = [("n_seq", i32), ("heads", i32), ("kv_heads", i32), ("head_dim", i32), ("Tq", i32), ("Tk", i32), ("causal", i32),
+                ("max_k", i32), ("scale", C.c_float), ("reserved", i32), ("q_start", vp), ("k_start", vp), ("k_rows", vp),
+                ("q", vp), ("k", vp), ("v", vp), ("o", vp), ("lse", vp),
+                ("q_row", i64), ("q_head", i64), ("k_row", i64), ("k_head", i64), ("v_row", i64), ("v_head", i64),
+                ("o_row", i64), ("o_head", i64)]
+
+
+class xs_attn_grads(C.Structure):
+    _fields_ = [("d_o", vp), ("dq", vp), ("dk", vp), ("dv", vp), ("do_row", i64), ("do_head", i64), ("dq_row", i64), ("dq_head", i64),
+                ("dk_row", i64), ("dk_head", i64), ("dv_row", i64), ("dv_head", i64)]
+
+
 class xs_scatter_desc(C.Structure):
     _fields_ = [("kind", i32), ("rows_per_dest", i32), ("n_proj", i32), ("n_heads", i32),
                 ("head_dim", i32), ("heads_per_group", i32)]
@@ -199,8 +212,22 @@ xs_grouped_gemm_fp8 = _sig("xs_grouped_gemm_fp8", C.c_int, vp, i64, vp, i64, i32
                            i64, i32, vp, vp)
 xs_swiglu_fp8 = _sig("xs_swiglu_fp8", C.c_int, vp, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp)
 xs_swiglu_fp8_backward = _sig("xs_swiglu_fp8_backward", C.c_int, vp, i64, vp, i64, vp, i64, i64, i32, vp, i64, vp, i64, vp)
+xs_rmsnorm = _sig("xs_rmsnorm", C.c_int, vp, i64, vp, i64, vp, i32, C.c_float, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp)
+xs_rmsnorm_backward_workspace_bytes = _sig("xs_rmsnorm_backward_workspace_bytes", C.c_int, i64, i32, P(i64))
+xs_rmsnorm_backward = _sig("xs_rmsnorm_backward", C.c_int, vp, i64, vp, i64, vp, i64, vp, i32, C.c_float, i64, i32, vp, i64, vp, vp, i64, vp)
+xs_balance_loss_workspace_bytes = _sig("xs_balance_loss_workspace_bytes", C.c_int, i32, i32, i32, P(i64))
+xs_balance_loss = _sig("xs_balance_loss", C.c_int, P(xs_gate), vp, i64, i32, vp, vp, i32, C.c_float, vp, vp, vp, vp, i64, vp, vp)
+xs_balance_loss_backward = _sig("xs_balance_loss_backward", C.c_int, P(xs_gate), vp, i64, i32, vp, i32, C.c_float, vp, vp, vp, i64,
+                                vp, i64, vp, vp)
+xs_attention_packed_workspace_bytes = _sig("xs_attention_packed_workspace_bytes", C.c_int, P(xs_attn_packed), P(i64))
+xs_attention_packed = _sig("xs_attention_packed", C.c_int, P(xs_attn_packed), vp, i64, vp, vp)
+xs_attention_packed_backward_workspace_bytes = _sig("xs_attention_packed_backward_workspace_bytes", C.c_int, P(xs_attn_packed), P(i64))
+xs_attention_packed_backward = _sig("xs_attention_packed_backward", C.c_int, P(xs_attn_packed), P(xs_attn_grads), vp, i64, vp, vp)
 
-EXPORTED = ["xs_fused_ep_layer_gated", "xs_route_gate", "xs_route_gate_backward", "xs_quantize_fp8", "xs_quantize_fp8_tile", "xs_gemm_fp8",
+EXPORTED = ["xs_rmsnorm", "xs_rmsnorm_backward_workspace_bytes", "xs_rmsnorm_backward", "xs_balance_loss_workspace_bytes",
+            "xs_balance_loss", "xs_balance_loss_backward", "xs_attention_packed_workspace_bytes", "xs_attention_packed",
+            "xs_attention_packed_backward_workspace_bytes", "xs_attention_packed_backward",
+            "xs_fused_ep_layer_gated", "xs_route_gate", "xs_route_gate_backward", "xs_quantize_fp8", "xs_quantize_fp8_tile", "xs_gemm_fp8",
             "xs_grouped_gemm_fp8", "xs_swiglu_fp8", "xs_swiglu_fp8_backward",
             "xs_strerror", "xs_version", "xs_route_topk_softmax", "xs_dispatch_layout_workspace_bytes",
             "xs_dispatch_layout", "xs_dispatch", "xs_ep_layer_workspace_bytes", "xs_expert_ffn",
@@ -258,6 +285,37 @@ def gate(E, k, score=XS_SCORE_SOFTMAX, n_group=1, topk_group=1, group_score=XS_G
     g = xs_gate(E, k, score, n_group, topk_group, group_score, int(renormalize), logits_type, scale, 0, ptr(bias))
     g._bias_ref = bias
     return g
+
+
+def _placed(t):
+    """A [rows][heads][head_dim] tensor's row and head strides; head_dim is contiguous."""
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError("a [rows][heads][head_dim] tensor with contiguous head_dim is wanted")
+    return t.stride(0), t.stride(1)
+
+
+def attn_packed(q, k, v, o, q_start, k_start, k_rows=None, lse=None, causal=True, max_k=0, scale=0.0) -> xs_attn_packed:
+    """Descriptor of packed attention over [rows][heads][head_dim] tensors of any strides; keeps them alive."""
+    a = xs_attn_packed(q_start.numel() - 1, q.shape[1], k.shape[1], q.shape[2], q.shape[0], k.shape[0], int(causal), max_k, scale, 0,
+                       ptr(q_start), ptr(k_start), ptr(k_rows), ptr(q), ptr(k), ptr(v), ptr(o), ptr(lse),
+                       *_placed(q), *_placed(k), *_placed(v), *_placed(o))
+    a._refs = (q, k, v, o, q_start, k_start, k_rows, lse)
+    return a
+
+
+def attn_packed_grads(d_o, dq, dk, dv) -> xs_attn_grads:
+    """The gradient tensors of packed attention, [rows][heads][head_dim] of any strides; keeps them alive."""
+    g = xs_attn_grads(ptr(d_o), ptr(dq), ptr(dk), ptr(dv), *_placed(d_o), *_placed(dq), *_placed(dk), *_placed(dv))
+    g._refs = (d_o, dq, dk, dv)
+    return g
+
+
+def workspace(query, *args, device=None):
+    """A workspace tensor of the size that a `*_workspace_bytes` call names, on the current device unless given."""
+    import torch
+    n = i64()
+    check(query(*args, C.byref(n)), "workspace")
+    return torch.empty((n.value,), dtype=torch.uint8, device="cuda" if device is None else device)
 
 
 def trace(buf, count) -> xs_trace:
