@@ -16,10 +16,11 @@
 //
 // LDS tiles are rows of 2 D bytes in pieces of 16; row r keeps its piece p at p ^ swz(r). A read by rows takes one
 // piece of 16 consecutive rows at a time, a read by columns four pieces of four consecutive rows; swz
-// spreads both over all banks, so that the gradients read one tile both ways.
+// spreads a tile's reads over all banks, also where the gradients read one tile both ways.
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "xs_common.hpp"
 #include "xs_packed.hpp"
@@ -74,30 +75,40 @@ __device__ __forceinline__ int sees(const Args& a, int r, int nq, int nk) {
   return a.causal ? min(max(nk - nq + r / a.G + 1, 0), nk) : nk;
 }
 
+// A lane's value, taken where it stands: what follows from it does not hold registers over a loop before.
+__device__ __forceinline__ int here(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// How a tile is read.
+enum Way { kRows, kCols, kBoth };
+
 template <int D>
 struct Geo {
   static constexpr int kRow = 2 * D, kPieces = D / 8, kRowsPerLoad = 1024 / kRow, kSteps = D / 16, kBlocks = D / 32;
-  // D = 128: a row is all banks; rows of 16 consecutive have distinct swz, rows of four distinct upper bits.
-  // D = 64: two rows are all banks; the same for rows with the same low bit.
-  static __device__ __forceinline__ int swz(int r) {
+  // D = 128: a row is all banks; by rows, 16 consecutive rows need distinct values, by columns four consecutive
+  // rows distinct upper bits. D = 64: two rows are all banks; the same for rows with the same low bit.
+  static __device__ __forceinline__ int swz(Way way, int r) {
+    if (way == kRows) return D == 128 ? r & 15 : r >> 1 & 7;
+    if (way == kCols) return D == 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2;
     return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
   }
 };
 
 // A tile of NR rows into LDS by NW waves (wave w of them), straight from memory; rows past `left` are zeros.
-template <int D, int NR, int NW>
+template <int D, int NR, int NW, Way WAY>
 struct Loader {
   using G = Geo<D>;
   static constexpr int kLoads = NR / (G::kRowsPerLoad * NW), kStep = G::kRowsPerLoad * NW;
   static constexpr int kVar = kStep >= 16 ? 1 : 16 / kStep;     // loads until the swizzles repeat
   uint32_t off[kVar];
   uint32_t row_bytes;
-  __device__ __forceinline__ Loader(int w, int64_t row) : row_bytes(static_cast<uint32_t>(row)) {
-    const int lane = threadIdx.x & 63;
+  __device__ __forceinline__ Loader(int w, int lane, int64_t row) : row_bytes(static_cast<uint32_t>(row)) {
 #pragma unroll
     for (int i = 0; i < kVar; ++i) {
       const int r = G::kRowsPerLoad * (NW * i + w) + lane / G::kPieces;
-      off[i] = static_cast<uint32_t>(r) * row_bytes + (((lane % G::kPieces) ^ G::swz(r)) << 4);
+      off[i] = static_cast<uint32_t>(r) * row_bytes + (((lane % G::kPieces) ^ G::swz(WAY, r)) << 4);
     }
   }
   __device__ __forceinline__ void issue(const char* base, int left, lds_char* dst, int w) const {
@@ -109,48 +120,56 @@ struct Loader {
   }
 };
 
-// A lane's addresses of its fragments in a tile.
-template <int D>
-struct Reads {
-  using G = Geo<D>;
-  uint32_t row[G::kSteps];                 // by rows: row lane % 32 (+ 32 b), piece 2 kk + lane / 32
-  uint32_t col[2][G::kBlocks];             // by columns: key or row 16 s (+ 4 hf), column block db
-  __device__ __forceinline__ Reads() {
-    const int lane = threadIdx.x & 63, r = lane & 31, up = lane >> 5;
-#pragma unroll
-    for (int kk = 0; kk < G::kSteps; ++kk) row[kk] = r * G::kRow + (((2 * kk + up) ^ G::swz(r)) << 4);
+// A lane's addresses of its fragments in a tile, by rows: row lane % 32 (+ 32 b), piece 2 kk + lane / 32; the pieces'
+// upper bits are toggled over the first's.
+template <int D, Way WAY>
+struct RowReads {
+  int first;
+  __device__ __forceinline__ explicit RowReads(int lane) {
+    const int r = lane & 31, up = lane >> 5;
+    first = r * Geo<D>::kRow + ((up ^ Geo<D>::swz(WAY, r)) << 4);
+  }
+  __device__ __forceinline__ int at(int kk) const { return first ^ kk << 5; }
+};
+// By columns: key or row 16 s (+ 4 hf), column block db. Where the swizzle does not change over four rows the second
+// address is the first and a constant.
+template <int D, Way WAY>
+struct ColReads {
+  static constexpr int kHalves = WAY == kBoth ? 2 : 1;
+  int first[kHalves];
+  __device__ __forceinline__ explicit ColReads(int lane) {
     const int grp = lane >> 4, j = lane & 15, d = 16 * (grp & 1) + 4 * (j & 3);
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
+    for (int hf = 0; hf < kHalves; ++hf) {
       const int k = 8 * (grp >> 1) + (j >> 2) + 4 * hf;
-#pragma unroll
-      for (int db = 0; db < G::kBlocks; ++db)
-        col[hf][db] = k * G::kRow + (((4 * db + (d >> 3)) ^ G::swz(k)) << 4) + (d >> 2 & 1) * 8;
+      first[hf] = k * Geo<D>::kRow + (((d >> 3) ^ Geo<D>::swz(WAY, k)) << 4) + (d >> 2 & 1) * 8;
     }
   }
+  __device__ __forceinline__ int at(int hf, int db) const { return first[hf] ^ db << 6; }
 };
 
 // acc[row of the tile][lane's column] = tile rows 32 b .. + 31 times the held fragments
-template <int D>
-__device__ __forceinline__ f32x16 rows_product(const lds_char* tile, int b, const Reads<D>& rd, const bf16x8 (&frag)[D / 16]) {
+template <int D, Way WAY>
+__device__ __forceinline__ f32x16 rows_product(const lds_char* tile, int b, const RowReads<D, WAY>& rd, const bf16x8 (&frag)[D / 16]) {
   f32x16 acc;
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
-    const bf16x8 a = *(const lds_bf16x8*)(tile + b * 32 * Geo<D>::kRow + rd.row[kk]);
+    const bf16x8 a = *(const lds_bf16x8*)(tile + b * 32 * Geo<D>::kRow + rd.at(kk));
     acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, frag[kk], acc, 0, 0, 0);
   }
   return acc;
 }
 
 // acc[column of the tile][lane's column] += sum over 16 rows of the tile, from row 16 s
-template <int D>
-__device__ __forceinline__ void cols_product(const lds_char* tile, int s, const Reads<D>& rd, bf16x8 b, f32x16 (&acc)[D / 32]) {
+template <int D, Way WAY>
+__device__ __forceinline__ void cols_product(const lds_char* tile, int s, const ColReads<D, WAY>& rd, bf16x8 b, f32x16 (&acc)[D / 32]) {
+  constexpr int kLast = ColReads<D, WAY>::kHalves - 1, kNext = kLast ? 0 : 4 * Geo<D>::kRow;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) {
-    const s16x4 r0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + 16 * s * Geo<D>::kRow + rd.col[0][db]));
-    const s16x4 r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + 16 * s * Geo<D>::kRow + rd.col[1][db]));
+    const s16x4 r0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + 16 * s * Geo<D>::kRow + rd.at(0, db)));
+    const s16x4 r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + 16 * s * Geo<D>::kRow + kNext + rd.at(kLast, db)));
     const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(r0, r1, 0, 1, 2, 3, 4, 5, 6, 7));
     acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc[db], 0, 0, 0);
   }
@@ -267,9 +286,9 @@ __device__ __forceinline__ void hide(f32x16& s, int key0, int lim, int up) {
 // and one V slot. Per tile j: S from K slot j % 2, a barrier, K tile j + 2 into that slot; the softmax; V tile
 // j waited for and a barrier; O from the V slot; K tile j + 1 waited for, a barrier, V tile j + 1 into the V slot.
 template <int D>
-__global__ __launch_bounds__(256, 3) void rows_kernel(Args a) {
+__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void rows_kernel(Args a) {
   using G = Geo<D>;
-  constexpr int kBKV = 64, kTile = kBKV * G::kRow, kLoads = Loader<D, kBKV, 4>::kLoads;
+  constexpr int kBKV = 64, kTile = kBKV * G::kRow, kLoads = Loader<D, kBKV, 4, kRows>::kLoads;
   __shared__ __attribute__((aligned(16))) char lds_raw[3 * kTile];
   lds_char* const lds = (lds_char*)lds_raw;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), up = lane >> 5;
@@ -284,17 +303,21 @@ __global__ __launch_bounds__(256, 3) void rows_kernel(Args a) {
   const int r0 = ((R + 127) / 128 - 1 - s.tile) * 128;       // the longest rows first
   const int nkv = (sees(a, min(r0 + 127, R - 1), nq, nk) + kBKV - 1) / kBKV;
   const int w0 = r0 + 32 * w;
-  const int all = w0 < R ? sees(a, w0, nq, nk) : 0, any = w0 < R ? sees(a, min(w0 + 31, R - 1), nq, nk) : 0;   // keys that all, any of the wave's rows see
-  const int r = min(w0 + (lane & 31), R - 1), qi = r / a.G, h = kvh * a.G + (r - qi * a.G), lim = sees(a, r, nq, nk);
+  const int whole = min(sees(a, r0, nq, nk) / kBKV, nkv);   // tiles that every row sees whole
+  const int r = min(w0 + (lane & 31), R - 1), lim = sees(a, r, nq, nk);
   bf16x8 qf[D / 16];
-  load_frags<D>(at(a.q, s.start + qi, h), qf);
-  const Reads<D> rd;
-  const Loader<D, kBKV, 4> lk(w, a.k.row), lv(w, a.v.row);
+  load_frags<D>(at(a.q, s.start + r / a.G, kvh * a.G + r % a.G), qf);
   const char* const kp = at(a.k, k0, kvh);
   const char* const vp = at(a.v, k0, kvh);
   lds_char* const vs = lds + 2 * kTile;
-  auto issue_k = [&](int j) { lk.issue(kp + static_cast<int64_t>(j) * kBKV * a.k.row, nk - j * kBKV, lds + (j & 1) * kTile, w); };
-  auto issue_v = [&](int j) { lv.issue(vp + static_cast<int64_t>(j) * kBKV * a.v.row, nk - j * kBKV, vs, w); };
+  // Every lane's addresses are made anew where they are used: kept over the loop they spill, and a reload waits for all
+  // the tiles in flight.
+  auto issue_k = [&](int j) {
+    Loader<D, kBKV, 4, kRows>(w, here(lane), a.k.row).issue(kp + static_cast<int64_t>(j) * kBKV * a.k.row, nk - j * kBKV, lds + (j & 1) * kTile, w);
+  };
+  auto issue_v = [&](int j) {
+    Loader<D, kBKV, 4, kCols>(w, here(lane), a.v.row).issue(vp + static_cast<int64_t>(j) * kBKV * a.v.row, nk - j * kBKV, vs, w);
+  };
   Soft<D> f;
   f.clear();
   if (nkv > 0) {
@@ -304,41 +327,38 @@ __global__ __launch_bounds__(256, 3) void rows_kernel(Args a) {
     wait_vm<0>();
     asm volatile("s_barrier" ::: "memory");
   }
-  for (int j = 0; j < nkv; ++j) {
+  auto step = [&](int j, auto masked) {
     lds_char* const ks = lds + (j & 1) * kTile;
-    const bool work = j * kBKV < any;                        // wave-uniform
-    f32x16 sc[2];
-    if (work) {
-      sc[0] = rows_product<D>(ks, 0, rd, qf);
-      sc[1] = rows_product<D>(ks, 1, rd, qf);
-    }
+    const RowReads<D, kRows> rr(here(lane));
+    f32x16 sc[2] = {rows_product<D>(ks, 0, rr, qf), rows_product<D>(ks, 1, rr, qf)};
     // every wave is done with K slot j % 2: K tile j + 2 goes there
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const bool k2 = j + 2 < nkv;
     if (k2) issue_k(j + 2);
-    uint32_t pk[2][8];
-    if (work) {
-      if (j * kBKV + kBKV > all) {
-        hide(sc[0], j * kBKV, lim, up);
-        hide(sc[1], j * kBKV + 32, lim, up);
-      }
-      f.take(sc, a.scale_log2e, pk);
+    if constexpr (masked) {
+      hide(sc[0], j * kBKV, lim, here(lane) >> 5);
+      hide(sc[1], j * kBKV + 32, lim, here(lane) >> 5);
     }
+    uint32_t pk[2][8];
+    f.take(sc, a.scale_log2e, pk);
     // V tile j has landed in every wave's share (only K tile j + 2 may still be in flight)
     if (k2) wait_vm<kLoads>(); else wait_vm<0>();
     asm volatile("s_barrier" ::: "memory");
-    if (work) {
+    const ColReads<D, kCols> rc(here(lane));
 #pragma unroll
-      for (int st = 0; st < 4; ++st) cols_product<D>(vs, st, rd, operand(pk[st >> 1], st & 1), f.o);
-    }
+    for (int st = 0; st < 4; ++st) cols_product<D>(vs, st, rc, operand(pk[st >> 1], st & 1), f.o);
     if (j + 1 < nkv) {
       // K tile j + 1 has landed in every wave's share, and no wave reads the V slot any more
       if (k2) wait_vm<kLoads>(); else wait_vm<0>();
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       issue_v(j + 1);
     }
-  }
-  if (w0 + (lane & 31) >= R) return;
+  };
+  for (int j = 0; j < whole; ++j) step(j, std::false_type());
+  for (int j = whole; j < nkv; ++j) step(j, std::true_type());
+  const int rl = w0 + here(lane & 31);
+  if (rl >= R) return;
+  const int qi = rl / a.G, h = kvh * a.G + (rl - qi * a.G);
   store_row<D>(at(a.o, s.start + qi, h), f.o, f.inverse());
   if (a.lse && up == 0) a.lse[static_cast<int64_t>(h) * a.Tq + s.start + qi] = f.lse();
 }
@@ -429,8 +449,10 @@ __global__ __launch_bounds__(256) void split_kernel(Args a) {
   lds_char* const mine = (lds_char*)lds_raw + wv * 4 * kTile;       // K 0, K 1, V 0, V 1
   const int64_t W = static_cast<int64_t>(blockIdx.x) * 4 + wv, NW = static_cast<int64_t>(gridDim.x) * 4;
   const int64_t total = all_tiles(a), per = (total + NW - 1) / NW, end = min(W * per + per, total);
-  const Reads<D> rd;
-  const Loader<D, 32, 1> lk(0, a.k.row), lv(0, a.v.row);
+  const RowReads<D, kRows> rr(lane);
+  const ColReads<D, kCols> rc(lane);
+  const Loader<D, 32, 1, kRows> lk(0, lane, a.k.row);
+  const Loader<D, 32, 1, kCols> lv(0, lane, a.v.row);
   Soft<D> f;
   for (int64_t u = W * per; u < end;) {
     Unit x;
@@ -455,12 +477,12 @@ __global__ __launch_bounds__(256) void split_kernel(Args a) {
       wait_vm<0>();
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // tile j - 1 has been read
       if (j + 1 < stop) issue(j + 1);
-      f32x16 sc[1] = {rows_product<D>(mine + (j & 1) * kTile, 0, rd, qf)};
+      f32x16 sc[1] = {rows_product<D>(mine + (j & 1) * kTile, 0, rr, qf)};
       if (j * 32 + 32 > all) hide(sc[0], j * 32, lim, up);
       uint32_t pk[1][8];
       f.take(sc, a.scale_log2e, pk);
-      cols_product<D>(mine + (2 + (j & 1)) * kTile, 0, rd, operand(pk[0], 0), f.o);
-      cols_product<D>(mine + (2 + (j & 1)) * kTile, 1, rd, operand(pk[0], 1), f.o);
+      cols_product<D>(mine + (2 + (j & 1)) * kTile, 0, rc, operand(pk[0], 0), f.o);
+      cols_product<D>(mine + (2 + (j & 1)) * kTile, 1, rc, operand(pk[0], 1), f.o);
     }
     if (rl < R) {
       if (x.first == 0 && last == x.L) {
@@ -533,6 +555,12 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, int64_t NW) {
 // ------------------------------------------------------------------------------ gradients
 // dq: as rows_kernel, with a second product (V times the row's do) and dS in place of the probabilities. It
 // computes delta for its rows and leaves it for the kernel below.
+//
+// delta = do . o takes o's roundings (of the probabilities and of o itself) to every dS of the row alike, a
+// relative error of dq and dk of about 0.0023 / sqrt(keys that share the weight): nothing beside the 0.0017 that dS's own
+// rounding gives where a row sees many keys, and the larger part where it sees ten. Tiles that see at most
+// kExactTiles tiles of keys therefore take delta = sum_j P_ij (do_i . v_j) in a pass before.
+constexpr int kExactTiles = 4;
 template <int D>
 __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   using G = Geo<D>;
@@ -553,47 +581,68 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   const int w0 = r0 + 32 * w;
   const int all = w0 < R ? sees(a, w0, nq, nk) : 0, any = w0 < R ? sees(a, min(w0 + 31, R - 1), nq, nk) : 0;
   const int r = min(w0 + (lane & 31), R - 1), qi = r / a.G, h = kvh * a.G + (r - qi * a.G), lim = sees(a, r, nq, nk);
-  const Reads<D> rd;
-  const Loader<D, kBKV, 4> lk(w, a.k.row), lv(w, a.v.row);
+  const RowReads<D, kBoth> rk(lane);
+  const ColReads<D, kBoth> ck(lane);
+  const RowReads<D, kRows> rv(lane);
+  const Loader<D, kBKV, 4, kBoth> lk(w, lane, a.k.row);
+  const Loader<D, kBKV, 4, kRows> lv(w, lane, a.v.row);
   const char* const kp = at(a.k, k0, kvh);
   const char* const vp = at(a.v, k0, kvh);
-  auto issue = [&](int j) {
-    lk.issue(kp + static_cast<int64_t>(j) * kBKV * a.k.row, nk - j * kBKV, lds + (j & 1) * kTile, w);
-    lv.issue(vp + static_cast<int64_t>(j) * kBKV * a.v.row, nk - j * kBKV, lds + (2 + (j & 1)) * kTile, w);
+  auto issue = [&](int j, int slot) {
+    lk.issue(kp + static_cast<int64_t>(j) * kBKV * a.k.row, nk - j * kBKV, lds + slot * kTile, w);
+    lv.issue(vp + static_cast<int64_t>(j) * kBKV * a.v.row, nk - j * kBKV, lds + (2 + slot) * kTile, w);
   };
-  if (nkv > 0) issue(0);
+  if (nkv > 0) issue(0, 0);
   bf16x8 qf[D / 16], df[D / 16];
   load_frags<D>(at(a.q, s.start + qi, h), qf);
   load_frags<D>(at(a.d_o, s.start + qi, h), df);
+  const int64_t stat = static_cast<int64_t>(h) * a.Tq + s.start + qi;
+  const float lse2 = lim > 0 ? a.lse[stat] * kLog2e : 0.f;
+  int slot = 0;
+  // tile j has landed in every wave's share, and no wave reads the tile before it any more; then `next` is loaded
+  auto turn = [&](int next) {
+    wait_vm<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    slot ^= 1;
+    if (next < nkv) issue(next, slot);
+  };
   float delta = 0.f;
-  {
+  if (nkv <= kExactTiles) {
+    for (int j = 0; j < nkv; ++j) {
+      turn(j + 1 < nkv ? j + 1 : 0);
+#pragma unroll 1
+      for (int b = 0; b < 2 && j * kBKV + 32 * b < any; ++b) {
+        f32x16 sc = rows_product<D>(lds + (slot ^ 1) * kTile, b, rk, qf);
+        const f32x16 dp = rows_product<D>(lds + (2 + (slot ^ 1)) * kTile, b, rv, df);
+        hide(sc, j * kBKV + 32 * b, lim, up);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          delta = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], a.scale_log2e, -lse2)), dp[e], delta);
+      }
+    }
+  } else {
     bf16x8 of[D / 16];
     load_frags<D>(at(a.o, s.start + qi, h), of);
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(static_cast<float>(df[kk][e]), static_cast<float>(of[kk][e]), delta);
-    delta = add_halves(delta);
   }
-  const int64_t stat = static_cast<int64_t>(h) * a.Tq + s.start + qi;
-  if (up == 0 && w0 + (lane & 31) < R) a.delta[stat] = delta;
-  const float lse2 = lim > 0 ? a.lse[stat] * kLog2e : 0.f;
+  delta = add_halves(delta);
   f32x16 acc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
   for (int j = 0; j < nkv; ++j) {
-    // tile j has landed in every wave's share, and no wave reads tile j - 1's slots any more
-    wait_vm<0>();
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (j + 1 < nkv) issue(j + 1);
+    turn(j + 1);
     if (j * kBKV >= any) continue;                           // wave-uniform
-    lds_char* const ks = lds + (j & 1) * kTile;
-    lds_char* const vs = lds + (2 + (j & 1)) * kTile;
+    lds_char* const ks = lds + (slot ^ 1) * kTile;
+    lds_char* const vs = lds + (2 + (slot ^ 1)) * kTile;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      f32x16 sc = rows_product<D>(ks, b, rd, qf), dp = rows_product<D>(vs, b, rd, df);
+      f32x16 sc = rows_product<D>(ks, b, rk, qf);
+      const f32x16 dp = rows_product<D>(vs, b, rv, df);
       if (j * kBKV + 32 * b + 32 > all) hide(sc, j * kBKV + 32 * b, lim, up);
       uint32_t pk[8];
 #pragma unroll
@@ -602,11 +651,13 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, -lse2));
         pk[e] = pack_bf16x2(p0 * (dp[2 * e] - delta), p1 * (dp[2 * e + 1] - delta));
       }
-      cols_product<D>(ks, 2 * b, rd, operand(pk, 0), acc);
-      cols_product<D>(ks, 2 * b + 1, rd, operand(pk, 1), acc);
+      cols_product<D>(ks, 2 * b, ck, operand(pk, 0), acc);
+      cols_product<D>(ks, 2 * b + 1, ck, operand(pk, 1), acc);
     }
   }
-  if (w0 + (lane & 31) < R) store_row<D>(at(a.dq, s.start + qi, h), acc, a.scale);
+  if (w0 + (lane & 31) >= R) return;
+  if (up == 0) a.delta[stat] = delta;
+  store_row<D>(at(a.dq, s.start + qi, h), acc, a.scale);
 }
 
 // dk and dv: a workgroup takes 128 keys of a key head (four waves of 32), their K and V fragments in registers, and
@@ -633,8 +684,9 @@ __global__ __launch_bounds__(256, 1) void dkv_kernel(Args a) {
   const int key0 = s.tile * 128, kw = key0 + 32 * w, key = kw + (lane & 31), off = nk - nq;
   const int first = a.causal ? max(0, key0 - off) : 0;         // the first query that sees one of these keys
   const int per_head = first < nq ? (nq - first + kBQ - 1) / kBQ : 0, n = per_head * a.G;
-  const Reads<D> rd;
-  const Loader<D, kBQ, 4> lq(w, a.q.row), ld(w, a.d_o.row);
+  const RowReads<D, kBoth> rr(lane);
+  const ColReads<D, kBoth> rc(lane);
+  const Loader<D, kBQ, 4, kBoth> lq(w, lane, a.q.row), ld(w, lane, a.d_o.row);
   auto issue = [&](int i) {
     const int g = i / per_head, t = first + (i - g * per_head) * kBQ, h = kvh * a.G + g, b = i & 1;
     lq.issue(at(a.q, q0 + t, h), nq - t, lds + b * kTile, w);
@@ -665,7 +717,7 @@ __global__ __launch_bounds__(256, 1) void dkv_kernel(Args a) {
     for (int x = 0; x < 2; ++x) {
       const int t0 = t + 32 * x;
       if (t0 >= nq || (a.causal && t0 + 31 + off < kw)) continue;        // wave-uniform
-      f32x16 sc = rows_product<D>(qs, x, rd, kf), dp = rows_product<D>(ds, x, rd, vf);
+      f32x16 sc = rows_product<D>(qs, x, rr, kf), dp = rows_product<D>(ds, x, rr, vf);
       if (a.causal && t0 + off < kw + 31) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -690,8 +742,8 @@ __global__ __launch_bounds__(256, 1) void dkv_kernel(Args a) {
       }
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        cols_product<D>(ds, 2 * x + hf, rd, operand(pp, hf), dv);
-        cols_product<D>(qs, 2 * x + hf, rd, operand(pd, hf), dk);
+        cols_product<D>(ds, 2 * x + hf, rc, operand(pp, hf), dv);
+        cols_product<D>(qs, 2 * x + hf, rc, operand(pd, hf), dk);
       }
     }
   }
