@@ -52,7 +52,7 @@ struct Args {
   float scale, scale_log2e;
   float* lse;            // [H][Tq]
   float* delta;          // [H][Tq] (gradients)
-  float* part_o;         // [waves][2][32][D] (split)
+  float* part_o;         // [waves][2][32][D] (split); dkv_kernel's parts
   float* part_ml;        // [waves][2][32][2]
   int32_t* status;
 };
@@ -660,96 +660,266 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   store_row<D>(at(a.dq, s.start + qi, h), acc, a.scale);
 }
 
-// dk and dv: a workgroup takes 128 keys of a key head (four waves of 32), their K and V fragments in registers, and
-// streams the rows that see them, 64 queries of one head at a time, with do, lse and delta. Queries past the end of
-// the sequence are zeros with lse 0: P = 1, but do = 0 and dS = 1 (0 - 0).
-template <int D>
-__global__ __launch_bounds__(256, 1) void dkv_kernel(Args a) {
-  using G = Geo<D>;
-  constexpr int kBQ = 64, kTile = kBQ * G::kRow;
-  __shared__ __attribute__((aligned(16))) char lds_raw[4 * kTile + 4 * kBQ * 4];
-  lds_char* const lds = (lds_char*)lds_raw;
-  lds_char* const stats = lds + 4 * kTile;                     // lse 0, lse 1, delta 0, delta 1
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), up = lane >> 5;
-  const int64_t id = block_number();
-  const int kvh = static_cast<int>(id % a.Hkv);
-  PackedTile s;
-  if (!packed_tile(a.k_start, a.n_seq, a.Tk, 1, 128, static_cast<int>(id / a.Hkv), &s, a.status)) return;
-  const int nk = s.rows, q0 = __builtin_amdgcn_readfirstlane(a.q_start[s.seq]);
-  const int nq = __builtin_amdgcn_readfirstlane(a.q_start[s.seq + 1]) - q0;
-  if (nk > a.max_k || q0 < 0 || nq < 0 || q0 > a.Tq - nq) {
+// dk and dv: a workgroup holds 128 keys of a key head (four waves of 32), their K and V fragments beside both
+// results' accumulators in registers, and streams the rows that see them, 32 queries of one head at a time with do,
+// lse and delta, two blocks ahead in three LDS slots. Two waves share a SIMD's registers: kStash of V's fragments lie in
+// LDS. Queries past the end of the sequence are zeros with lse 0: P = 1, but do = 0 and dS = 1 (0 - 0).
+//
+// The first keys of a sequence have G times as many rows as it has queries, the last ones hardly any, and there are few key
+// heads: key tiles dealt one to a workgroup leave the chip waiting for the longest (8192 tokens in 4 sequences, 32 heads
+// over 8: 904 us). So the blocks of all key tiles, laid end to end, are dealt out evenly: workgroup W takes the blocks [W per,
+// (W + 1) per), per = ceil(total / workgroups) but at least kLeast. A key tile that lies in one range is finished there, of
+// the others each workgroup leaves a part, in its slot 0 for the tile that its range begins in or with, in slot 1 for one that
+// begins later; dkv_join_kernel adds them up in order.
+constexpr int kLeast = 16;
+
+struct KeySeq {
+  int q0, nq, k0, nk;
+};
+struct KeyTile {
+  KeySeq s;
+  int kvh, tile, per_head;      // key tile; blocks of 32 queries that see it
+  int64_t first, blocks;        // the block searched for, of the tile's
+};
+
+// Blocks of one query head in a sequence's key tiles before tile j: those whose first key every query sees have all
+// ceil(nq / 32) (one where there is none: such keys' zeros are still written), from there on every tile has four less.
+__device__ __forceinline__ int64_t blocks_before(const Args& a, const KeySeq& s, int64_t j) {
+  const int64_t f = max(1, (s.nq + 31) / 32), c = (s.nk + 31) / 32, off = s.nk - s.nq;
+  if (!a.causal) return j * f;
+  const int64_t full = off > 0 ? (off + 127) / 128 : 0;
+  return j <= full ? j * f : full * f + (j - full) * c - 2 * (j * (j - 1) - full * (full - 1));
+}
+
+__device__ __forceinline__ KeySeq key_seq(const Args& a, int s) {
+  KeySeq x{0, 0, 0, 0};
+  if (s >= a.n_seq) return x;
+  const int q0 = a.q_start[s], q1 = a.q_start[s + 1], k0 = a.k_start[s], k1 = a.k_start[s + 1];
+  if (q0 < 0 || q1 < q0 || q1 > a.Tq || k0 < 0 || k1 < k0 || k1 > a.Tk || k1 - k0 > a.max_k) {
     set_status(a.status, XS_EBADINPUT);
-    return;
+    return x;
   }
-  const int key0 = s.tile * 128, kw = key0 + 32 * w, key = kw + (lane & 31), off = nk - nq;
-  const int first = a.causal ? max(0, key0 - off) : 0;         // the first query that sees one of these keys
-  const int per_head = first < nq ? (nq - first + kBQ - 1) / kBQ : 0, n = per_head * a.G;
-  const RowReads<D, kBoth> rr(lane);
-  const ColReads<D, kBoth> rc(lane);
-  const Loader<D, kBQ, 4, kBoth> lq(w, lane, a.q.row), ld(w, lane, a.d_o.row);
-  auto issue = [&](int i) {
-    const int g = i / per_head, t = first + (i - g * per_head) * kBQ, h = kvh * a.G + g, b = i & 1;
-    lq.issue(at(a.q, q0 + t, h), nq - t, lds + b * kTile, w);
-    ld.issue(at(a.d_o, q0 + t, h), nq - t, lds + (2 + b) * kTile, w);
-    if (w < 2) {
-      const float* const src = (w ? a.delta : a.lse) + static_cast<int64_t>(h) * a.Tq + q0 + t;
-      load_lds4(buffer_rsrc(src, min(nq - t, kBQ) * 4), lane * 4, stats + (2 * w + b) * kBQ * 4);
-    }
-  };
-  if (n > 0) issue(0);
-  bf16x8 kf[D / 16], vf[D / 16];
-  const int kc = min(key, nk - 1);
-  load_frags<D>(at(a.k, s.start + kc, kvh), kf);
-  load_frags<D>(at(a.v, s.start + kc, kvh), vf);
-  f32x16 dk[D / 32], dv[D / 32];
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) dk[db][e] = dv[db][e] = 0.f;
-  for (int i = 0; i < n; ++i) {
-    wait_vm<0>();
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (i + 1 < n) issue(i + 1);
-    const int t = first + (i % per_head) * kBQ, b = i & 1;
-    lds_char* const qs = lds + b * kTile;
-    lds_char* const ds = lds + (2 + b) * kTile;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int t0 = t + 32 * x;
-      if (t0 >= nq || (a.causal && t0 + 31 + off < kw)) continue;        // wave-uniform
-      f32x16 sc = rows_product<D>(qs, x, rr, kf), dp = rows_product<D>(ds, x, rr, vf);
-      if (a.causal && t0 + off < kw + 31) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (t0 + entry_row(e, up) + off < key) sc[e] = -INFINITY;
+  return KeySeq{q0, q1 - q0, k0, k1 - k0};
+}
+__device__ __forceinline__ int64_t blocks_of(const Args& a, const KeySeq& s) { return blocks_before(a, s, (s.nk + 127) / 128) * a.H; }
+
+__device__ __forceinline__ int64_t all_blocks(const Args& a) {
+  int64_t total = 0;
+  for (int s0 = 0; s0 < a.n_seq; s0 += 64) total += lane64(scan64(blocks_of(a, key_seq(a, s0 + (threadIdx.x & 63)))), 63);
+  return total;
+}
+
+__device__ __forceinline__ KeySeq lane_seq(const KeySeq& s, int l) {
+  return KeySeq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l), __builtin_amdgcn_readlane(s.k0, l),
+                __builtin_amdgcn_readlane(s.nk, l)};
+}
+
+// The key tile that block u of all lies in; u is less than their number.
+__device__ __forceinline__ void key_tile_at(const Args& a, int64_t u, KeyTile* out) {
+  int64_t before = 0;
+  for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+    const KeySeq mine = key_seq(a, s0 + (threadIdx.x & 63));
+    const int64_t n = blocks_of(a, mine), upto = scan64(n);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(before + upto > u);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      out->s = lane_seq(mine, l);
+      const int tiles = (out->s.nk + 127) / 128;
+      const int64_t head = blocks_before(a, out->s, tiles) * a.G, in = u - before - lane64(upto - n, l);
+      out->kvh = static_cast<int>(in / head);
+      const int64_t x = in - out->kvh * head;
+      int lo = 0, hi = tiles - 1;                               // the tile with before(tile) G <= x < before(tile + 1) G
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (blocks_before(a, out->s, mid + 1) * a.G > x) hi = mid;
+        else lo = mid + 1;
       }
-      uint32_t pp[8], pd[8];
+      const int64_t b0 = blocks_before(a, out->s, lo);
+      out->tile = lo;
+      out->per_head = static_cast<int>(blocks_before(a, out->s, lo + 1) - b0);
+      out->blocks = static_cast<int64_t>(out->per_head) * a.G;
+      out->first = x - b0 * a.G;
+      return;
+    }
+    before += lane64(upto, 63);
+  }
+}
+
+// Workgroups that have blocks to do lie side by side on one XCD, whose L2 then holds their rows.
+__device__ __forceinline__ int64_t range_of_block(int b, int n) { return n % 8 ? b : static_cast<int64_t>(b % 8) * (n / 8) + b / 8; }
+
+template <int D>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dkv_kernel(Args a) {
+  using G = Geo<D>;
+  constexpr int kBQ = 32, kTile = kBQ * G::kRow, kStages = 3, kStash = D == 128 ? 5 : 0;
+  constexpr int kLoads = 2 * Loader<D, kBQ, 4, kBoth>::kLoads;                 // of a stage, a wave's (without lse and delta)
+  __shared__ __attribute__((aligned(16))) char lds_raw[2 * kStages * kTile + 2 * kStages * kBQ * 4 + 4 * kStash * 1024];
+  lds_char* const lds = (lds_char*)lds_raw;
+  lds_char* const stats = lds + 2 * kStages * kTile;                           // lse and delta of each stage
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  lds_char* const stash = stats + 2 * kStages * kBQ * 4 + w * kStash * 1024;
+  const int64_t total = all_blocks(a), per = max(static_cast<int64_t>(kLeast), (total + gridDim.x - 1) / gridDim.x);
+  const int64_t W = range_of_block(blockIdx.x, gridDim.x), begin = W * per, end = min(begin + per, total);
+  for (int64_t u = begin; u < end;) {
+    KeyTile x;
+    key_tile_at(a, u, &x);
+    const int n = static_cast<int>(min(x.blocks - x.first, end - u));
+    const int nq = x.s.nq, nk = x.s.nk, key0 = x.tile * 128, kw = key0 + 32 * w, off = nk - nq;
+    const int first = a.causal ? max(0, key0 - off) : 0;       // the first query that sees one of these keys
+    // the next block to load: its head in the group, first query and stage
+    int lg = static_cast<int>(x.first / x.per_head), lt = first + static_cast<int>(x.first - static_cast<int64_t>(lg) * x.per_head) * kBQ, lst = 0;
+    int t = lt, st = 0;
+    auto issue = [&] {
+      const int h = x.kvh * a.G + lg;
+      const Loader<D, kBQ, 4, kBoth> lq(w, here(lane), a.q.row), ld(w, here(lane), a.d_o.row);
+      lq.issue(at(a.q, x.s.q0 + lt, h), nq - lt, lds + 2 * lst * kTile, w);
+      ld.issue(at(a.d_o, x.s.q0 + lt, h), nq - lt, lds + (2 * lst + 1) * kTile, w);
+      if (w < 2) {                                             // the lower half's lanes fetch the 32 rows' numbers
+        const float* const src = (w ? a.delta : a.lse) + static_cast<int64_t>(h) * a.Tq + x.s.q0 + lt;
+        if ((here(lane) & 32) == 0) load_lds4(buffer_rsrc(src, min(nq - lt, kBQ) * 4), here(lane) * 4, stats + (2 * lst + w) * kBQ * 4);
+      }
+      lt += kBQ;
+      if (lt >= nq) {
+        lt = first;
+        ++lg;
+      }
+      lst = lst + 1 == kStages ? 0 : lst + 1;
+    };
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the slots of the tile before have been read
+    const bool some = nq > 0;
+    if (some) issue();
+    if (some && n > 1) issue();
+    bf16x8 kf[D / 16], vf[D / 16];
+    {
+      const int kc = min(kw + (lane & 31), nk - 1);
+      load_frags<D>(at(a.k, x.s.k0 + kc, x.kvh), kf);
+      load_frags<D>(at(a.v, x.s.k0 + kc, x.kvh), vf);
+    }
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-        const f32x4 ls = *(const lds_f32x4*)(stats + b * kBQ * 4 + (32 * x + 8 * g + 4 * up) * 4);
-        const f32x4 de = *(const lds_f32x4*)(stats + (2 + b) * kBQ * 4 + (32 * x + 8 * g + 4 * up) * 4);
-        float p[4], d[4];
+    for (int kk = 0; kk < kStash; ++kk) *(lds_bf16x8*)(stash + kk * 1024 + lane * 16) = vf[kk];
+    f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * g + e], a.scale_log2e, -ls[e] * kLog2e));
-          d[e] = p[e] * (dp[4 * g + e] - de[e]);
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dk[db][e] = dv[db][e] = 0.f;
+    for (int i = 0; some && i < n; ++i) {
+      // block i has landed in every wave's share (of block i + 1 nothing need have), and no wave reads block i - 1 any more
+      if (i + 1 < n) wait_vm<kLoads>(); else wait_vm<0>();
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (i + 2 < n) issue();
+      if (!a.causal || t + 31 + off >= kw) {                   // wave-uniform
+        lds_char* const qs = lds + 2 * st * kTile;
+        lds_char* const ds = qs + kTile;
+        const int ln = here(lane);
+        const RowReads<D, kBoth> rr(ln);
+        f32x16 sc = rows_product<D>(qs, 0, rr, kf), dp;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dp[e] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const bf16x8 b = kk < kStash ? *(const lds_bf16x8*)(stash + kk * 1024 + ln * 16) : vf[kk];
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds_bf16x8*)(ds + rr.at(kk)), b, dp, 0, 0, 0);
         }
-        pp[2 * g] = pack_bf16x2(p[0], p[1]);
-        pp[2 * g + 1] = pack_bf16x2(p[2], p[3]);
-        pd[2 * g] = pack_bf16x2(d[0], d[1]);
-        pd[2 * g + 1] = pack_bf16x2(d[2], d[3]);
-      }
+        if (a.causal && t + off < kw + 31) {
+          const int key = kw + (ln & 31);
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        cols_product<D>(ds, 2 * x + hf, rc, operand(pp, hf), dv);
-        cols_product<D>(qs, 2 * x + hf, rc, operand(pd, hf), dk);
+          for (int e = 0; e < 16; ++e)
+            if (t + entry_row(e, ln >> 5) + off < key) sc[e] = -INFINITY;
+        }
+        uint32_t pp[8], pd[8];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+          const lds_char* const at4 = stats + 2 * st * kBQ * 4 + (8 * g + 4 * (ln >> 5)) * 4;
+          const f32x4 ls = *(const lds_f32x4*)at4, de = *(const lds_f32x4*)(at4 + kBQ * 4);
+          float p[4], d[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * g + e], a.scale_log2e, -ls[e] * kLog2e));
+            d[e] = p[e] * (dp[4 * g + e] - de[e]);
+          }
+          pp[2 * g] = pack_bf16x2(p[0], p[1]);
+          pp[2 * g + 1] = pack_bf16x2(p[2], p[3]);
+          pd[2 * g] = pack_bf16x2(d[0], d[1]);
+          pd[2 * g + 1] = pack_bf16x2(d[2], d[3]);
+        }
+        const ColReads<D, kBoth> rc(ln);
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          cols_product<D>(ds, hf, rc, operand(pp, hf), dv);
+          cols_product<D>(qs, hf, rc, operand(pd, hf), dk);
+        }
       }
+      t += kBQ;
+      if (t >= nq) t = first;
+      st = st + 1 == kStages ? 0 : st + 1;
     }
+    const int key = kw + here(lane & 31);
+    if (n == x.blocks) {
+      if (key < nk) {
+        store_row<D>(at(a.dk, x.s.k0 + key, x.kvh), dk, a.scale);
+        store_row<D>(at(a.dv, x.s.k0 + key, x.kvh), dv, 1.f);
+      }
+    } else {
+      f32x4* const part = reinterpret_cast<f32x4*>(a.part_o) + ((W * 2 + (u > begin)) * 4 + w) * (D * 16) + here(lane);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          part[(db * 4 + g) * 64] = f32x4{dk[db][4 * g], dk[db][4 * g + 1], dk[db][4 * g + 2], dk[db][4 * g + 3]};
+          part[(D / 8 + db * 4 + g) * 64] = f32x4{dv[db][4 * g], dv[db][4 * g + 1], dv[db][4 * g + 2], dv[db][4 * g + 3]};
+        }
+    }
+    u += n;
   }
-  if (key < nk) {
-    store_row<D>(at(a.dk, s.start + key, kvh), dk, a.scale);
-    store_row<D>(at(a.dv, s.start + key, kvh), dv, 1.f);
+}
+
+// One workgroup a key tile: its parts, each wave its 32 keys', in the order of the ranges.
+template <int D>
+__global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t id = block_number(), total = all_blocks(a), per = max(static_cast<int64_t>(kLeast), (total + n_ranges - 1) / n_ranges);
+  const int kvh = static_cast<int>(id % a.Hkv);
+  int64_t t = id / a.Hkv, blocks = 0;                 // the tile's number, counted over the sequences
+  for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+    const KeySeq mine = key_seq(a, s0 + lane);
+    const int64_t tiles = (mine.nk + 127) / 128, upto = scan64(tiles), n = blocks_of(a, mine), n_upto = scan64(n);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > t);
+    if (!hit) {
+      t -= lane64(upto, 63);
+      blocks += lane64(n_upto, 63);
+      continue;
+    }
+    const int l = __builtin_ctzll(hit);
+    const KeySeq s = lane_seq(mine, l);
+    const int64_t tile = t - lane64(upto - tiles, l), b0 = blocks_before(a, s, tile), b1 = blocks_before(a, s, tile + 1);
+    const int64_t head = blocks + lane64(n_upto - n, l) + kvh * blocks_before(a, s, (s.nk + 127) / 128) * a.G;
+    const int64_t u0 = head + b0 * a.G, u1 = head + b1 * a.G, w0 = u0 / per, w1 = (u1 - 1) / per;
+    if (w0 == w1) return;                             // finished by its workgroup
+    f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dk[db][e] = dv[db][e] = 0.f;
+    for (int64_t W = w0; W <= w1; ++W) {
+      const f32x4* const part = reinterpret_cast<const f32x4*>(a.part_o) + ((W * 2 + (W == w0 && u0 > w0 * per)) * 4 + w) * (D * 16) + lane;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 k4 = part[(db * 4 + g) * 64], v4 = part[(D / 8 + db * 4 + g) * 64];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            dk[db][4 * g + e] += k4[e];
+            dv[db][4 * g + e] += v4[e];
+          }
+        }
+    }
+    const int key = static_cast<int>(tile) * 128 + 32 * w + (lane & 31);
+    if (key >= s.nk) return;
+    store_row<D>(at(a.dk, s.k0 + key, kvh), dk, a.scale);
+    store_row<D>(at(a.dv, s.k0 + key, kvh), dv, 1.f);
+    return;
   }
 }
 
@@ -833,14 +1003,32 @@ int forward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
   return xs_host::launch_status();
 }
 
+// Workgroups of dkv_kernel: as many as the chip holds, fewer where there cannot be kLeast blocks for each.
 template <int D>
-int backward(const pattn::Args& a, hipStream_t st) {
+int dkv_ranges(const pattn::Args& a) {
+  const int64_t most = (packed_tiles_bound(a.Tk, a.n_seq, 1, 128) * a.H * (a.Tq / 32 + 1) + pattn::kLeast - 1) / pattn::kLeast;
+  return static_cast<int>(std::min<int64_t>(most, (D == 128 ? 2 : 3) * int64_t(xs_host::num_cus())));
+}
+int64_t delta_bytes(const pattn::Args& a) { return (static_cast<int64_t>(a.H) * a.Tq * 4 + 255) / 256 * 256; }
+template <int D>
+int64_t grad_bytes(const pattn::Args& a) { return delta_bytes(a) + dkv_ranges<D>(a) * int64_t(2 * 2 * 128 * D * 4); }
+
+template <int D>
+int backward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
+  const int64_t need = grad_bytes<D>(a);
+  if (need && (!ws || !aligned16(ws) || bytes < need)) return XS_EWORKSPACE;
+  a.delta = static_cast<float*>(ws);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + delta_bytes(a));
   if (a.Tq) {
     hipLaunchKernelGGL((pattn::dq_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv), dim3(256), 0, st, a);
     if (xs_host::launch_status()) return XS_EHIP;
   }
-  if (a.Tk) {
-    hipLaunchKernelGGL((pattn::dkv_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tk, a.n_seq, 1, 128) * a.Hkv), dim3(256), 0, st, a);
+  const int ranges = dkv_ranges<D>(a);
+  if (ranges) {
+    hipLaunchKernelGGL((pattn::dkv_kernel<D>), dim3(ranges), dim3(256), 0, st, a);
+    if (xs_host::launch_status()) return XS_EHIP;
+    hipLaunchKernelGGL((pattn::dkv_join_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tk, a.n_seq, 1, 128) * a.Hkv), dim3(256), 0, st, a,
+                       ranges);
     if (xs_host::launch_status()) return XS_EHIP;
   }
   return XS_OK;
@@ -869,7 +1057,7 @@ extern "C" int xs_attention_packed_backward_workspace_bytes(const xs_attn_packed
   pattn::Args a{};
   if (!bytes) return XS_EINVAL;
   if (int rc = check(A, &a)) return rc;
-  *bytes = static_cast<int64_t>(a.H) * a.Tq * 4;
+  *bytes = A->head_dim == 128 ? grad_bytes<128>(a) : grad_bytes<64>(a);
   return XS_OK;
 }
 
@@ -886,13 +1074,11 @@ extern "C" int xs_attention_packed_backward(const xs_attn_packed* A, const xs_at
     unsupported |= r != XS_OK;
   }
   if (unsupported) return XS_EUNSUPPORTED;
-  if (a.Tq && (!workspace || !aligned16(workspace) || workspace_bytes < static_cast<int64_t>(a.H) * a.Tq * 4)) return XS_EWORKSPACE;
   a.d_o = mat(g->d_o, g->do_row, g->do_head);
   a.dq = mat(g->dq, g->dq_row, g->dq_head);
   a.dk = mat(g->dk, g->dk_row, g->dk_head);
   a.dv = mat(g->dv, g->dv_row, g->dv_head);
-  a.delta = static_cast<float*>(workspace);
   a.status = dev_status;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  return D == 128 ? backward<128>(a, st) : backward<64>(a, st);
+  return D == 128 ? backward<128>(a, workspace, workspace_bytes, st) : backward<64>(a, workspace, workspace_bytes, st);
 }
