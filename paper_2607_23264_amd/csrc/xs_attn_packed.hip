@@ -101,6 +101,7 @@ template <int D, int NR, int NW, Way WAY>
 struct Loader {
   using G = Geo<D>;
   static constexpr int kLoads = NR / (G::kRowsPerLoad * NW), kStep = G::kRowsPerLoad * NW;
+  static_assert(kLoads * kStep == NR);
   static constexpr int kVar = kStep >= 16 ? 1 : 16 / kStep;     // loads until the swizzles repeat
   uint32_t off[kVar];
   uint32_t row_bytes;
@@ -148,31 +149,54 @@ struct ColReads {
   __device__ __forceinline__ int at(int hf, int db) const { return first[hf] ^ db << 6; }
 };
 
+// N matrix instructions, mul(i, operand), whose LDS reads are issued AHEAD instructions before them. Left to itself the
+// compiler reads one operand, waits for it and multiplies.
+template <int N, int AHEAD, class Read, class Mul>
+__device__ __forceinline__ void fed(const Read& read, const Mul& mul) {
+  decltype(read(0)) buf[AHEAD + 1];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) buf[i] = read(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i + AHEAD < N) buf[(i + AHEAD) % (AHEAD + 1)] = read(i + AHEAD);
+    __builtin_amdgcn_sched_barrier(0);
+    mul(i, buf[i % (AHEAD + 1)]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <int D, Way WAY>
+__device__ __forceinline__ bf16x8 row_operand(const lds_char* tile, int b, const RowReads<D, WAY>& rd, int kk) {
+  return *(const lds_bf16x8*)(tile + b * 32 * Geo<D>::kRow + rd.at(kk));
+}
+template <int D, Way WAY>
+__device__ __forceinline__ bf16x8 col_operand(const lds_char* tile, int s, const ColReads<D, WAY>& rd, int db) {
+  constexpr int kLast = ColReads<D, WAY>::kHalves - 1, kNext = kLast ? 0 : 4 * Geo<D>::kRow;
+  const s16x4 r0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + 16 * s * Geo<D>::kRow + rd.at(0, db)));
+  const s16x4 r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + 16 * s * Geo<D>::kRow + kNext + rd.at(kLast, db)));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(r0, r1, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ __forceinline__ void zero(f32x16& v) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = 0.f;
+}
+__device__ __forceinline__ void mma(f32x16& acc, bf16x8 a, bf16x8 b) { acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0); }
+
 // acc[row of the tile][lane's column] = tile rows 32 b .. + 31 times the held fragments
 template <int D, Way WAY>
 __device__ __forceinline__ f32x16 rows_product(const lds_char* tile, int b, const RowReads<D, WAY>& rd, const bf16x8 (&frag)[D / 16]) {
   f32x16 acc;
+  zero(acc);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) {
-    const bf16x8 a = *(const lds_bf16x8*)(tile + b * 32 * Geo<D>::kRow + rd.at(kk));
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, frag[kk], acc, 0, 0, 0);
-  }
+  for (int kk = 0; kk < D / 16; ++kk) mma(acc, row_operand<D>(tile, b, rd, kk), frag[kk]);
   return acc;
 }
 
 // acc[column of the tile][lane's column] += sum over 16 rows of the tile, from row 16 s
 template <int D, Way WAY>
 __device__ __forceinline__ void cols_product(const lds_char* tile, int s, const ColReads<D, WAY>& rd, bf16x8 b, f32x16 (&acc)[D / 32]) {
-  constexpr int kLast = ColReads<D, WAY>::kHalves - 1, kNext = kLast ? 0 : 4 * Geo<D>::kRow;
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db) {
-    const s16x4 r0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + 16 * s * Geo<D>::kRow + rd.at(0, db)));
-    const s16x4 r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + 16 * s * Geo<D>::kRow + kNext + rd.at(kLast, db)));
-    const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(r0, r1, 0, 1, 2, 3, 4, 5, 6, 7));
-    acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc[db], 0, 0, 0);
-  }
+  for (int db = 0; db < D / 32; ++db) mma(acc[db], col_operand<D>(tile, s, rd, db), b);
 }
 
 // Accumulator entry e of a 32-row block is row 8 (e / 4) + 4 (lane / 32) + e % 4.
@@ -660,7 +684,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   store_row<D>(at(a.dq, s.start + qi, h), acc, a.scale);
 }
 
-// dk and dv: a workgroup holds 128 keys of a key head (four waves of 32), their K and V fragments beside both
+// dk and dv: a workgroup holds 32 NW keys of a key head (NW waves of 32), their K and V fragments beside both
 // results' accumulators in registers, and streams the rows that see them, 32 queries of one head at a time with do,
 // lse and delta, two blocks ahead in three LDS slots. Two waves share a SIMD's registers: kStash of V's fragments lie in
 // LDS. Queries past the end of the sequence are zeros with lse 0: P = 1, but do = 0 and dS = 1 (0 - 0).
@@ -682,13 +706,14 @@ struct KeyTile {
   int64_t first, blocks;        // the block searched for, of the tile's
 };
 
-// Blocks of one query head in a sequence's key tiles before tile j: those whose first key every query sees have all
-// ceil(nq / 32) (one where there is none: such keys' zeros are still written), from there on every tile has four less.
+// Blocks of one query head in a sequence's tiles of 32 NW keys before tile j: those whose first key every query sees have all
+// ceil(nq / 32) (one where there is none: such keys' zeros are still written), from there on every tile has NW less.
+template <int NW>
 __device__ __forceinline__ int64_t blocks_before(const Args& a, const KeySeq& s, int64_t j) {
   const int64_t f = max(1, (s.nq + 31) / 32), c = (s.nk + 31) / 32, off = s.nk - s.nq;
   if (!a.causal) return j * f;
-  const int64_t full = off > 0 ? (off + 127) / 128 : 0;
-  return j <= full ? j * f : full * f + (j - full) * c - 2 * (j * (j - 1) - full * (full - 1));
+  const int64_t full = off > 0 ? (off + 32 * NW - 1) / (32 * NW) : 0;
+  return j <= full ? j * f : full * f + (j - full) * c - NW / 2 * (j * (j - 1) - full * (full - 1));
 }
 
 __device__ __forceinline__ KeySeq key_seq(const Args& a, int s) {
@@ -701,11 +726,15 @@ __device__ __forceinline__ KeySeq key_seq(const Args& a, int s) {
   }
   return KeySeq{q0, q1 - q0, k0, k1 - k0};
 }
-__device__ __forceinline__ int64_t blocks_of(const Args& a, const KeySeq& s) { return blocks_before(a, s, (s.nk + 127) / 128) * a.H; }
+template <int NW>
+__device__ __forceinline__ int key_tiles(const KeySeq& s) { return (s.nk + 32 * NW - 1) / (32 * NW); }
+template <int NW>
+__device__ __forceinline__ int64_t blocks_of(const Args& a, const KeySeq& s) { return blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.H; }
 
+template <int NW>
 __device__ __forceinline__ int64_t all_blocks(const Args& a) {
   int64_t total = 0;
-  for (int s0 = 0; s0 < a.n_seq; s0 += 64) total += lane64(scan64(blocks_of(a, key_seq(a, s0 + (threadIdx.x & 63)))), 63);
+  for (int s0 = 0; s0 < a.n_seq; s0 += 64) total += lane64(scan64(blocks_of<NW>(a, key_seq(a, s0 + (threadIdx.x & 63)))), 63);
   return total;
 }
 
@@ -715,28 +744,29 @@ __device__ __forceinline__ KeySeq lane_seq(const KeySeq& s, int l) {
 }
 
 // The key tile that block u of all lies in; u is less than their number.
+template <int NW>
 __device__ __forceinline__ void key_tile_at(const Args& a, int64_t u, KeyTile* out) {
   int64_t before = 0;
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
     const KeySeq mine = key_seq(a, s0 + (threadIdx.x & 63));
-    const int64_t n = blocks_of(a, mine), upto = scan64(n);
+    const int64_t n = blocks_of<NW>(a, mine), upto = scan64(n);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(before + upto > u);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       out->s = lane_seq(mine, l);
-      const int tiles = (out->s.nk + 127) / 128;
-      const int64_t head = blocks_before(a, out->s, tiles) * a.G, in = u - before - lane64(upto - n, l);
+      const int tiles = key_tiles<NW>(out->s);
+      const int64_t head = blocks_before<NW>(a, out->s, tiles) * a.G, in = u - before - lane64(upto - n, l);
       out->kvh = static_cast<int>(in / head);
       const int64_t x = in - out->kvh * head;
       int lo = 0, hi = tiles - 1;                               // the tile with before(tile) G <= x < before(tile + 1) G
       while (lo < hi) {
         const int mid = (lo + hi) / 2;
-        if (blocks_before(a, out->s, mid + 1) * a.G > x) hi = mid;
+        if (blocks_before<NW>(a, out->s, mid + 1) * a.G > x) hi = mid;
         else lo = mid + 1;
       }
-      const int64_t b0 = blocks_before(a, out->s, lo);
+      const int64_t b0 = blocks_before<NW>(a, out->s, lo);
       out->tile = lo;
-      out->per_head = static_cast<int>(blocks_before(a, out->s, lo + 1) - b0);
+      out->per_head = static_cast<int>(blocks_before<NW>(a, out->s, lo + 1) - b0);
       out->blocks = static_cast<int64_t>(out->per_head) * a.G;
       out->first = x - b0 * a.G;
       return;
@@ -748,30 +778,30 @@ __device__ __forceinline__ void key_tile_at(const Args& a, int64_t u, KeyTile* o
 // Workgroups that have blocks to do lie side by side on one XCD, whose L2 then holds their rows.
 __device__ __forceinline__ int64_t range_of_block(int b, int n) { return n % 8 ? b : static_cast<int64_t>(b % 8) * (n / 8) + b / 8; }
 
-template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dkv_kernel(Args a) {
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kernel(Args a) {
   using G = Geo<D>;
-  constexpr int kBQ = 32, kTile = kBQ * G::kRow, kStages = 3, kStash = D == 128 ? 5 : 0;
-  constexpr int kLoads = 2 * Loader<D, kBQ, 4, kBoth>::kLoads;                 // of a stage, a wave's (without lse and delta)
-  __shared__ __attribute__((aligned(16))) char lds_raw[2 * kStages * kTile + 2 * kStages * kBQ * 4 + 4 * kStash * 1024];
+  constexpr int kBQ = 32, kTile = kBQ * G::kRow, kStages = 3, kStash = D == 128 ? 6 : 0;
+  constexpr int kLoads = 2 * Loader<D, kBQ, NW, kBoth>::kLoads;                 // of a stage, a wave's (without lse and delta)
+  __shared__ __attribute__((aligned(16))) char lds_raw[2 * kStages * kTile + 2 * kStages * kBQ * 4 + NW * kStash * 1024];
   lds_char* const lds = (lds_char*)lds_raw;
   lds_char* const stats = lds + 2 * kStages * kTile;                           // lse and delta of each stage
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   lds_char* const stash = stats + 2 * kStages * kBQ * 4 + w * kStash * 1024;
-  const int64_t total = all_blocks(a), per = max(static_cast<int64_t>(kLeast), (total + gridDim.x - 1) / gridDim.x);
+  const int64_t total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), (total + gridDim.x - 1) / gridDim.x);
   const int64_t W = range_of_block(blockIdx.x, gridDim.x), begin = W * per, end = min(begin + per, total);
   for (int64_t u = begin; u < end;) {
     KeyTile x;
-    key_tile_at(a, u, &x);
+    key_tile_at<NW>(a, u, &x);
     const int n = static_cast<int>(min(x.blocks - x.first, end - u));
-    const int nq = x.s.nq, nk = x.s.nk, key0 = x.tile * 128, kw = key0 + 32 * w, off = nk - nq;
+    const int nq = x.s.nq, nk = x.s.nk, key0 = x.tile * 32 * NW, kw = key0 + 32 * w, off = nk - nq;
     const int first = a.causal ? max(0, key0 - off) : 0;       // the first query that sees one of these keys
     // the next block to load: its head in the group, first query and stage
     int lg = static_cast<int>(x.first / x.per_head), lt = first + static_cast<int>(x.first - static_cast<int64_t>(lg) * x.per_head) * kBQ, lst = 0;
     int t = lt, st = 0;
     auto issue = [&] {
       const int h = x.kvh * a.G + lg;
-      const Loader<D, kBQ, 4, kBoth> lq(w, here(lane), a.q.row), ld(w, here(lane), a.d_o.row);
+      const Loader<D, kBQ, NW, kBoth> lq(w, here(lane), a.q.row), ld(w, here(lane), a.d_o.row);
       lq.issue(at(a.q, x.s.q0 + lt, h), nq - lt, lds + 2 * lst * kTile, w);
       ld.issue(at(a.d_o, x.s.q0 + lt, h), nq - lt, lds + (2 * lst + 1) * kTile, w);
       if (w < 2) {                                             // the lower half's lanes fetch the 32 rows' numbers
@@ -794,6 +824,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dkv_kernel(Args a) {
       const int kc = min(kw + (lane & 31), nk - 1);
       load_frags<D>(at(a.k, x.s.k0 + kc, x.kvh), kf);
       load_frags<D>(at(a.v, x.s.k0 + kc, x.kvh), vf);
+      wait_vm<0>();                                            // here, or the loop waits for them, and so for the blocks in flight
     }
 #pragma unroll
     for (int kk = 0; kk < kStash; ++kk) *(lds_bf16x8*)(stash + kk * 1024 + lane * 16) = vf[kk];
@@ -812,14 +843,20 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dkv_kernel(Args a) {
         lds_char* const ds = qs + kTile;
         const int ln = here(lane);
         const RowReads<D, kBoth> rr(ln);
-        f32x16 sc = rows_product<D>(qs, 0, rr, kf), dp;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) dp[e] = 0.f;
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const bf16x8 b = kk < kStash ? *(const lds_bf16x8*)(stash + kk * 1024 + ln * 16) : vf[kk];
-          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds_bf16x8*)(ds + rr.at(kk)), b, dp, 0, 0, 0);
-        }
+        f32x16 sc, dp;
+        zero(sc);
+        zero(dp);
+        struct Pair {
+          bf16x8 a, b;
+        };
+        fed<D / 8, 2>([&](int i) {
+                        Pair p;
+                        p.a = row_operand<D>(i < D / 16 ? qs : ds, 0, rr, i % (D / 16));
+                        const int kk = i - D / 16;
+                        p.b = kk < 0 ? kf[i] : kk < kStash ? *(const lds_bf16x8*)(stash + kk * 1024 + ln * 16) : vf[kk];
+                        return p;
+                      },
+                      [&](int i, const Pair& p) { mma(i < D / 16 ? sc : dp, p.a, p.b); });
         if (a.causal && t + off < kw + 31) {
           const int key = kw + (ln & 31);
 #pragma unroll
@@ -844,11 +881,13 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dkv_kernel(Args a) {
           pd[2 * g + 1] = pack_bf16x2(d[2], d[3]);
         }
         const ColReads<D, kBoth> rc(ln);
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          cols_product<D>(ds, hf, rc, operand(pp, hf), dv);
-          cols_product<D>(qs, hf, rc, operand(pd, hf), dk);
-        }
+        const bf16x8 po[2] = {operand(pp, 0), operand(pp, 1)}, so[2] = {operand(pd, 0), operand(pd, 1)};
+        constexpr int kB = D / 32;                             // instruction i: 16 rows i / (2 kB), of dv, then dk, its block
+        fed<4 * kB, 2>([&](int i) { return col_operand<D>(i / kB % 2 ? qs : ds, i / (2 * kB), rc, i % kB); },
+                       [&](int i, bf16x8 v) {
+                         if (i / kB % 2) mma(dk[i % kB], v, so[i / (2 * kB)]);
+                         else mma(dv[i % kB], v, po[i / (2 * kB)]);
+                       });
       }
       t += kBQ;
       if (t >= nq) t = first;
@@ -861,7 +900,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dkv_kernel(Args a) {
         store_row<D>(at(a.dv, x.s.k0 + key, x.kvh), dv, 1.f);
       }
     } else {
-      f32x4* const part = reinterpret_cast<f32x4*>(a.part_o) + ((W * 2 + (u > begin)) * 4 + w) * (D * 16) + here(lane);
+      f32x4* const part = reinterpret_cast<f32x4*>(a.part_o) + ((W * 2 + (u > begin)) * NW + w) * (D * 16) + here(lane);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -875,15 +914,15 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dkv_kernel(Args a) {
 }
 
 // One workgroup a key tile: its parts, each wave its 32 keys', in the order of the ranges.
-template <int D>
-__global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void dkv_join_kernel(Args a, int n_ranges) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t id = block_number(), total = all_blocks(a), per = max(static_cast<int64_t>(kLeast), (total + n_ranges - 1) / n_ranges);
+  const int64_t id = block_number(), total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), (total + n_ranges - 1) / n_ranges);
   const int kvh = static_cast<int>(id % a.Hkv);
   int64_t t = id / a.Hkv, blocks = 0;                 // the tile's number, counted over the sequences
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
     const KeySeq mine = key_seq(a, s0 + lane);
-    const int64_t tiles = (mine.nk + 127) / 128, upto = scan64(tiles), n = blocks_of(a, mine), n_upto = scan64(n);
+    const int64_t tiles = key_tiles<NW>(mine), upto = scan64(tiles), n = blocks_of<NW>(a, mine), n_upto = scan64(n);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > t);
     if (!hit) {
       t -= lane64(upto, 63);
@@ -892,8 +931,8 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
     }
     const int l = __builtin_ctzll(hit);
     const KeySeq s = lane_seq(mine, l);
-    const int64_t tile = t - lane64(upto - tiles, l), b0 = blocks_before(a, s, tile), b1 = blocks_before(a, s, tile + 1);
-    const int64_t head = blocks + lane64(n_upto - n, l) + kvh * blocks_before(a, s, (s.nk + 127) / 128) * a.G;
+    const int64_t tile = t - lane64(upto - tiles, l), b0 = blocks_before<NW>(a, s, tile), b1 = blocks_before<NW>(a, s, tile + 1);
+    const int64_t head = blocks + lane64(n_upto - n, l) + kvh * blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.G;
     const int64_t u0 = head + b0 * a.G, u1 = head + b1 * a.G, w0 = u0 / per, w1 = (u1 - 1) / per;
     if (w0 == w1) return;                             // finished by its workgroup
     f32x16 dk[D / 32], dv[D / 32];
@@ -902,7 +941,7 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) dk[db][e] = dv[db][e] = 0.f;
     for (int64_t W = w0; W <= w1; ++W) {
-      const f32x4* const part = reinterpret_cast<const f32x4*>(a.part_o) + ((W * 2 + (W == w0 && u0 > w0 * per)) * 4 + w) * (D * 16) + lane;
+      const f32x4* const part = reinterpret_cast<const f32x4*>(a.part_o) + ((W * 2 + (W == w0 && u0 > w0 * per)) * NW + w) * (D * 16) + lane;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -915,7 +954,7 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
           }
         }
     }
-    const int key = static_cast<int>(tile) * 128 + 32 * w + (lane & 31);
+    const int key = static_cast<int>(tile) * 32 * NW + 32 * w + (lane & 31);
     if (key >= s.nk) return;
     store_row<D>(at(a.dk, s.k0 + key, kvh), dk, a.scale);
     store_row<D>(at(a.dv, s.k0 + key, kvh), dv, 1.f);
@@ -1003,15 +1042,29 @@ int forward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
   return xs_host::launch_status();
 }
 
-// Workgroups of dkv_kernel: as many as the chip holds, fewer where there cannot be kLeast blocks for each.
+// Waves of a dkv_kernel workgroup: eight (256 keys, half the rows' traffic) for sequences of 512 keys and more on average, four
+// for shorter ones and for heads of 64, where a block of 32 rows is four waves' loads.
+template <int D>
+int dkv_waves(const pattn::Args& a) { return D == 128 && a.Tk / a.n_seq >= 512 ? 8 : 4; }
+template <int D>
+int64_t key_tiles_bound(const pattn::Args& a) { return packed_tiles_bound(a.Tk, a.n_seq, 1, 32 * dkv_waves<D>(a)) * a.Hkv; }
+// Its workgroups: as many as the chip holds, fewer where there cannot be kLeast blocks for each.
 template <int D>
 int dkv_ranges(const pattn::Args& a) {
-  const int64_t most = (packed_tiles_bound(a.Tk, a.n_seq, 1, 128) * a.H * (a.Tq / 32 + 1) + pattn::kLeast - 1) / pattn::kLeast;
-  return static_cast<int>(std::min<int64_t>(most, (D == 128 ? 2 : 3) * int64_t(xs_host::num_cus())));
+  const int64_t most = (key_tiles_bound<D>(a) * a.G * (a.Tq / 32 + 1) + pattn::kLeast - 1) / pattn::kLeast;
+  return static_cast<int>(std::min<int64_t>(most, (D == 128 ? 8 : 12) / dkv_waves<D>(a) * int64_t(xs_host::num_cus())));
 }
 int64_t delta_bytes(const pattn::Args& a) { return (static_cast<int64_t>(a.H) * a.Tq * 4 + 255) / 256 * 256; }
 template <int D>
-int64_t grad_bytes(const pattn::Args& a) { return delta_bytes(a) + dkv_ranges<D>(a) * int64_t(2 * 2 * 128 * D * 4); }
+int64_t grad_bytes(const pattn::Args& a) { return delta_bytes(a) + dkv_ranges<D>(a) * int64_t(2 * 2 * 32 * D * 4) * dkv_waves<D>(a); }
+
+template <int D, int NW>
+int dkv(const pattn::Args& a, int ranges, hipStream_t st) {
+  hipLaunchKernelGGL((pattn::dkv_kernel<D, NW>), dim3(ranges), dim3(64 * NW), 0, st, a);
+  if (xs_host::launch_status()) return XS_EHIP;
+  hipLaunchKernelGGL((pattn::dkv_join_kernel<D, NW>), xs_host::grid_of(key_tiles_bound<D>(a)), dim3(64 * NW), 0, st, a, ranges);
+  return xs_host::launch_status();
+}
 
 template <int D>
 int backward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
@@ -1024,14 +1077,10 @@ int backward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
     if (xs_host::launch_status()) return XS_EHIP;
   }
   const int ranges = dkv_ranges<D>(a);
-  if (ranges) {
-    hipLaunchKernelGGL((pattn::dkv_kernel<D>), dim3(ranges), dim3(256), 0, st, a);
-    if (xs_host::launch_status()) return XS_EHIP;
-    hipLaunchKernelGGL((pattn::dkv_join_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tk, a.n_seq, 1, 128) * a.Hkv), dim3(256), 0, st, a,
-                       ranges);
-    if (xs_host::launch_status()) return XS_EHIP;
-  }
-  return XS_OK;
+  if (!ranges) return XS_OK;
+  if constexpr (D == 128)
+    if (dkv_waves<D>(a) == 8) return dkv<D, 8>(a, ranges, st);
+  return dkv<D, 4>(a, ranges, st);
 }
 
 }  // namespace

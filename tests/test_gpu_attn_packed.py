@@ -195,6 +195,30 @@ def test_gradients_of_more_keys_than_queries_and_fewer():
             c.check_backward()
 
 
+# 512 keys and more a sequence take key tiles of 256; 70, 3 and 1 heads leave tiles inside one workgroup's share and over several
+@pytest.mark.parametrize("lens,H,Hkv", [([1025], 4, 1), ([511, 1, 1030], 6, 2), ([700, 900], 70, 35), ([513], 1, 1)])
+@pytest.mark.parametrize("D,layout", [(128, "token"), (64, "room")])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_sequences(lens, H, Hkv, D, layout, causal):
+    spans, T = _packed(lens)
+    assert T // len(lens) >= 512
+    c = Case(spans, T, T, H, Hkv, D, layout, causal, seed=H)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+
+
+def test_gradients_of_a_long_prefix_and_of_queries_that_see_nothing():
+    spans = [(0, 33, 0, 1500), (33, 600, 1500, 90), (633, 0, 1590, 257), (633, 700, 1847, 513)]
+    for causal in (True, False):
+        c = Case(spans, 1333, 2360, 4, 2, 128, causal=causal)
+        c.forward()
+        c.check_forward()
+        c.backward()
+        c.check_backward()
+
+
 def test_large_scores_and_a_given_scale():
     spans, T = _packed([150, 40])
     for std, scale in ((3.0, 0.0), (1.0, 0.5), (2.0, 1e-3)):
