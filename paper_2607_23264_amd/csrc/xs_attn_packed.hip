@@ -31,6 +31,7 @@ namespace pattn {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -49,6 +50,7 @@ struct Args {
   Mat q, k, v, o, d_o, dq, dk, dv;
   const int32_t *q_start, *k_start, *k_rows;
   int n_seq, H, Hkv, G, Tq, Tk, causal, max_k;
+  int shift;             // log2 G, or -1
   float scale, scale_log2e;
   float* lse;            // [H][Tq]
   float* delta;          // [H][Tq] (gradients)
@@ -57,22 +59,26 @@ struct Args {
   int32_t* status;
 };
 
-// The keys of a sequence; false (with the error noted) if they do not lie in k.
-__device__ __forceinline__ bool keys_of(const Args& a, int seq, int* k0, int* m) {
-  const int s = a.k_start[seq];
-  const int n = a.k_rows ? a.k_rows[seq] : a.k_start[seq + 1] - s;
-  if (s < 0 || n < 0 || n > a.max_k || s > a.Tk - n) {
-    set_status(a.status, XS_EBADINPUT);
-    return false;
-  }
-  *k0 = s;
-  *m = n;
-  return true;
+// a / b of what is not negative and the same in all lanes: mostly it fits 32 bits, and a division of 64 takes four times as long.
+__device__ __forceinline__ int64_t quot(int64_t a, int64_t b) {
+  if ((a | b) >> 32) return a / b;
+  return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
 }
 
+struct Seq {
+  int q0, nq, k0, nk;       // its first query and their number, its first key and theirs
+};
+
+// The query of row r.
+__device__ __forceinline__ int query_of(const Args& a, int r) { return a.shift >= 0 ? r >> a.shift : r / a.G; }
 // How many keys row r of a sequence sees.
 __device__ __forceinline__ int sees(const Args& a, int r, int nq, int nk) {
-  return a.causal ? min(max(nk - nq + r / a.G + 1, 0), nk) : nk;
+  return a.causal ? min(max(nk - nq + query_of(a, r) + 1, 0), nk) : nk;
+}
+// Where row r of a sequence and key head lies in q, o, ...
+__device__ __forceinline__ char* row_at(const Args& a, const Mat& m, const Seq& s, int kvh, int r) {
+  const int qi = query_of(a, r);
+  return at(m, s.q0 + qi, kvh * a.G + (r - qi * a.G));
 }
 
 // A lane's value, taken where it stands: what follows from it does not hold registers over a loop before.
@@ -236,17 +242,48 @@ __device__ __forceinline__ void load_frags(const char* row, bf16x8 (&f)[D / 16])
   for (int kk = 0; kk < D / 16; ++kk) f[kk] = *reinterpret_cast<const bf16x8*>(row + 32 * kk + 16 * up);
 }
 
-// A lane's row (or key) of accumulators, times c, as bf16 to `row`.
+// 8 consecutive columns of a lane's row from the pieces of four that the two halves of a wave hold: the lower half gets the
+// first 8, the upper half the next.
+__device__ __forceinline__ u32x4 columns8(u32x2 first, u32x2 next) {
+  const auto x = __builtin_amdgcn_permlane32_swap(first[0], next[0], false, false);
+  const auto y = __builtin_amdgcn_permlane32_swap(first[1], next[1], false, false);
+  return u32x4{x[0], y[0], x[1], y[1]};
+}
+__device__ __forceinline__ u32x2 four(const f32x16& v, int g, float c) {
+  return u32x2{pack_bf16x2(v[4 * g] * c, v[4 * g + 1] * c), pack_bf16x2(v[4 * g + 2] * c, v[4 * g + 3] * c)};
+}
+
+// Accumulators, times c, as bf16: each lane its row (or key), all lanes together; where `live`.
 template <int D>
-__device__ __forceinline__ void store_row(char* row, const f32x16 (&acc)[D / 32], float c) {
+__device__ __forceinline__ void store_row(char* row, const f32x16 (&acc)[D / 32], float c, bool live) {
   const int up = (threadIdx.x & 63) >> 5;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const u32x2 v = {pack_bf16x2(acc[db][4 * g] * c, acc[db][4 * g + 1] * c), pack_bf16x2(acc[db][4 * g + 2] * c, acc[db][4 * g + 3] * c)};
-      *reinterpret_cast<u32x2*>(row + (32 * db + 8 * g + 4 * up) * 2) = v;
+    for (int g = 0; g < 4; g += 2) {
+      const u32x4 v = columns8(four(acc[db], g, c), four(acc[db], g + 1, c));
+      if (live) *reinterpret_cast<u32x4*>(row + (32 * db + 8 * (g + up)) * 2) = v;
     }
+}
+
+// The same through LDS (32 rows of 2 D bytes, the wave's own), whole rows at a time: row(i) says where row i goes, NULL: nowhere.
+// A store by lanes' rows touches 32 cache lines, 16 of them for a wave took as long as one and a half tiles of 64 keys.
+template <int D, class Row>
+__device__ __forceinline__ void store_rows(lds_char* mine, const f32x16 (&acc)[D / 32], float c, const Row& row) {
+  using G = Geo<D>;
+  const int lane = here(threadIdx.x & 63), i = lane & 31, up = lane >> 5;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *(lds_u32x2*)(mine + i * G::kRow + (((4 * db + g) ^ G::swz(kRows, i)) << 4) + up * 8) = four(acc[db], g, c);
+#pragma unroll
+  for (int t = 0; t < 32 / G::kRowsPerLoad; ++t) {
+    const int r = t * G::kRowsPerLoad + lane / G::kPieces, p = lane % G::kPieces;
+    const bf16x8 v = *(const lds_bf16x8*)(mine + r * G::kRow + ((p ^ G::swz(kRows, r)) << 4));
+    char* const dst = row(r);
+    if (dst) *reinterpret_cast<bf16x8*>(dst + 16 * p) = v;
+  }
 }
 
 // A row's softmax so far: maximum (in powers of two, scaled) and sum. The maximum starts at the lowest finite
@@ -305,63 +342,100 @@ __device__ __forceinline__ void hide(f32x16& s, int key0, int lim, int up) {
     if (key0 + entry_row(e, up) >= lim) s[e] = -INFINITY;
 }
 
+__device__ __forceinline__ int64_t lane64(int64_t v, int l) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), l), hi = __builtin_amdgcn_readlane(static_cast<int>(v >> 32), l);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ Seq lane_seq(const Seq& s, int l) {
+  return Seq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l), __builtin_amdgcn_readlane(s.k0, l), __builtin_amdgcn_readlane(s.nk, l)};
+}
+
+// Sequence i; without queries and keys (and with the error noted) if they do not lie in q and k, and where there is none.
+__device__ __forceinline__ Seq seq_of(const Args& a, int i) {
+  if (i >= a.n_seq) return Seq{0, 0, 0, 0};
+  const int q0 = a.q_start[i], q1 = a.q_start[i + 1], k0 = a.k_start[i], nk = a.k_rows ? a.k_rows[i] : a.k_start[i + 1] - k0;
+  if (q0 < 0 || q1 < q0 || q1 > a.Tq || k0 < 0 || nk < 0 || nk > a.max_k || k0 > a.Tk - nk) {
+    set_status(a.status, XS_EBADINPUT);
+    return Seq{0, 0, 0, 0};
+  }
+  return Seq{q0, q1 - q0, k0, nk};
+}
+
+// The workgroup's tile of PER rows of a sequence and key head, key heads side by side; false past the last. Every wave finds it
+// by itself, 64 sequences a step, all that it has to know of one in a lane and on its way at once.
+template <int PER>
+__device__ __forceinline__ bool tile_of(const Args& a, Seq* s, int* kvh, int* tile) {
+  const int64_t id = block_number(), t = quot(id, a.Hkv);
+  *kvh = static_cast<int>(id - t * a.Hkv);
+  int left = static_cast<int>(t);
+  for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
+    const Seq mine = seq_of(a, s0 + (threadIdx.x & 63));
+    const int n = static_cast<int>((static_cast<int64_t>(mine.nq) * a.G + PER - 1) / PER), upto = wave_scan(n);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > left);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      *s = lane_seq(mine, l);
+      *tile = left - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
+      return true;
+    }
+    left -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
 // ------------------------------------------------------------------------------ many rows
-// A workgroup takes 128 rows (four waves of 32) and streams the keys they see in tiles of 64. LDS: two K slots
-// and one V slot. Per tile j: S from K slot j % 2, a barrier, K tile j + 2 into that slot; the softmax; V tile
+// The rows [r0, end) of a sequence and key head (128 at most, four waves of 32) over the key tiles [jb, je) of 64. LDS: two K
+// slots and one V slot. Per tile j: S from K slot j % 2, a barrier, K tile j + 2 into that slot; the softmax; V tile
 // j waited for and a barrier; O from the V slot; K tile j + 1 waited for, a barrier, V tile j + 1 into the V slot.
-template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void rows_kernel(Args a) {
-  using G = Geo<D>;
-  constexpr int kBKV = 64, kTile = kBKV * G::kRow, kLoads = Loader<D, kBKV, 4, kRows>::kLoads;
-  __shared__ __attribute__((aligned(16))) char lds_raw[3 * kTile];
-  lds_char* const lds = (lds_char*)lds_raw;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), up = lane >> 5;
-  const int64_t id = block_number();
-  const int kvh = static_cast<int>(id % a.Hkv);
-  PackedTile s;
-  int k0, nk;
-  if (!packed_tile(a.q_start, a.n_seq, a.Tq, a.G, 128, static_cast<int>(id / a.Hkv), &s, a.status) || !keys_of(a, s.seq, &k0, &nk)) return;
-  k0 = __builtin_amdgcn_readfirstlane(k0);
-  nk = __builtin_amdgcn_readfirstlane(nk);
-  const int nq = s.rows, R = nq * a.G;
-  const int r0 = ((R + 127) / 128 - 1 - s.tile) * 128;       // the longest rows first
-  const int nkv = (sees(a, min(r0 + 127, R - 1), nq, nk) + kBKV - 1) / kBKV;
-  const int w0 = r0 + 32 * w;
-  const int whole = min(sees(a, r0, nq, nk) / kBKV, nkv);   // tiles that every row sees whole
-  const int r = min(w0 + (lane & 31), R - 1), lim = sees(a, r, nq, nk);
-  bf16x8 qf[D / 16];
-  load_frags<D>(at(a.q, s.start + r / a.G, kvh * a.G + r % a.G), qf);
-  const char* const kp = at(a.k, k0, kvh);
-  const char* const vp = at(a.v, k0, kvh);
+#ifndef RA
+#define RA 2
+#endif
+#ifndef NA
+#define NA 4
+#endif
+constexpr int kKeys = 64;      // of a tile
+template <int D, int AHEAD>
+__device__ __forceinline__ void rows_unit(const Args& a, lds_char* lds, const Seq& s, int kvh, int r0, int end, int jb, int je, Soft<D>& f) {
+  constexpr int kTile = kKeys * Geo<D>::kRow, kLoads = Loader<D, kKeys, 4, kRows>::kLoads;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int whole = min(sees(a, r0, s.nq, s.nk) / kKeys, je);   // tiles that every row sees whole
+  const int r = min(r0 + 32 * w + (lane & 31), end - 1), lim = sees(a, r, s.nq, s.nk);
+  const char* const kp = at(a.k, s.k0, kvh);
+  const char* const vp = at(a.v, s.k0, kvh);
   lds_char* const vs = lds + 2 * kTile;
   // Every lane's addresses are made anew where they are used: kept over the loop they spill, and a reload waits for all
   // the tiles in flight.
   auto issue_k = [&](int j) {
-    Loader<D, kBKV, 4, kRows>(w, here(lane), a.k.row).issue(kp + static_cast<int64_t>(j) * kBKV * a.k.row, nk - j * kBKV, lds + (j & 1) * kTile, w);
+    Loader<D, kKeys, 4, kRows>(w, here(lane), a.k.row).issue(kp + static_cast<int64_t>(j) * kKeys * a.k.row, s.nk - j * kKeys, lds + (j & 1) * kTile, w);
   };
   auto issue_v = [&](int j) {
-    Loader<D, kBKV, 4, kCols>(w, here(lane), a.v.row).issue(vp + static_cast<int64_t>(j) * kBKV * a.v.row, nk - j * kBKV, vs, w);
+    Loader<D, kKeys, 4, kCols>(w, here(lane), a.v.row).issue(vp + static_cast<int64_t>(j) * kKeys * a.v.row, s.nk - j * kKeys, vs, w);
   };
-  Soft<D> f;
+  bf16x8 qf[D / 16];
   f.clear();
-  if (nkv > 0) {
-    issue_k(0);
-    issue_v(0);
-    if (nkv > 1) issue_k(1);
+  if (jb < je) {
+    issue_k(jb);
+    issue_v(jb);
+    if (jb + 1 < je) issue_k(jb + 1);
+    // behind the tiles: 32 rows' pieces are 32 cache lines an instruction
+    load_frags<D>(row_at(a, a.q, s, kvh, r), qf);
     wait_vm<0>();
     asm volatile("s_barrier" ::: "memory");
   }
   auto step = [&](int j, auto masked) {
     lds_char* const ks = lds + (j & 1) * kTile;
     const RowReads<D, kRows> rr(here(lane));
-    f32x16 sc[2] = {rows_product<D>(ks, 0, rr, qf), rows_product<D>(ks, 1, rr, qf)};
+    f32x16 sc[2];
+    zero(sc[0]);
+    zero(sc[1]);
+    fed<D / 8, AHEAD>([&](int i) { return row_operand<D>(ks, i & 1, rr, i >> 1); }, [&](int i, bf16x8 v) { mma(sc[i & 1], v, qf[i >> 1]); });
     // every wave is done with K slot j % 2: K tile j + 2 goes there
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const bool k2 = j + 2 < nkv;
+    const bool k2 = j + 2 < je;
     if (k2) issue_k(j + 2);
     if constexpr (masked) {
-      hide(sc[0], j * kBKV, lim, here(lane) >> 5);
-      hide(sc[1], j * kBKV + 32, lim, here(lane) >> 5);
+      hide(sc[0], j * kKeys, lim, here(lane) >> 5);
+      hide(sc[1], j * kKeys + 32, lim, here(lane) >> 5);
     }
     uint32_t pk[2][8];
     f.take(sc, a.scale_log2e, pk);
@@ -369,210 +443,438 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void rows_kernel(Args a) {
     if (k2) wait_vm<kLoads>(); else wait_vm<0>();
     asm volatile("s_barrier" ::: "memory");
     const ColReads<D, kCols> rc(here(lane));
-#pragma unroll
-    for (int st = 0; st < 4; ++st) cols_product<D>(vs, st, rc, operand(pk[st >> 1], st & 1), f.o);
-    if (j + 1 < nkv) {
+    const bf16x8 p[4] = {operand(pk[0], 0), operand(pk[0], 1), operand(pk[1], 0), operand(pk[1], 1)};
+    fed<D / 8, AHEAD>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
+                      [&](int i, bf16x8 v) { mma(f.o[i % (D / 32)], v, p[i / (D / 32)]); });
+    if (j + 1 < je) {
       // K tile j + 1 has landed in every wave's share, and no wave reads the V slot any more
       if (k2) wait_vm<kLoads>(); else wait_vm<0>();
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       issue_v(j + 1);
     }
   };
-  for (int j = 0; j < whole; ++j) step(j, std::false_type());
-  for (int j = whole; j < nkv; ++j) step(j, std::true_type());
-  const int rl = w0 + here(lane & 31);
-  if (rl >= R) return;
-  const int qi = rl / a.G, h = kvh * a.G + (rl - qi * a.G);
-  store_row<D>(at(a.o, s.start + qi, h), f.o, f.inverse());
-  if (a.lse && up == 0) a.lse[static_cast<int64_t>(h) * a.Tq + s.start + qi] = f.lse();
+  int j = jb;
+  for (; j < whole; ++j) step(j, std::false_type());
+  for (; j < je; ++j) step(j, std::true_type());
 }
 
-// ------------------------------------------------------------------------------ few rows
-// Few rows over many keys: what counts is how fast the chip reads K and V, so the keys are dealt out evenly
-// over all waves. The work is units (sequence, 32 rows, key head) of L = ceil(m / 32) key tiles each, laid end
-// to end; wave W of NW takes the tiles [W per, (W + 1) per), per = ceil(total / NW), wherever units
-// begin and end. A unit that lies in one wave's range is finished there; of the others each wave leaves a
-// part (sums relative to its maximum): in its slot 0 for the unit that its range begins in or with, in slot 1 for
-// one that begins later. join_kernel adds them up in order. A wave has its own two slots of K and V and waits for
-// nobody.
-struct Unit {
-  int seq, q0, nq, k0, nk, L, first, kvh, r0;
+// 32 rows of a sequence and key head from r0 are done, those before `end` of them; `mine`: LDS of the wave's own for whole rows, or NULL.
+template <int D>
+__device__ __forceinline__ void finish(const Args& a, const Seq& s, int kvh, int r0, int end, const Soft<D>& f, lds_char* mine = nullptr) {
+  const int lane = here(threadIdx.x & 63), r = r0 + (lane & 31), qi = query_of(a, min(r, end - 1)), h = kvh * a.G + (min(r, end - 1) - qi * a.G);
+  if (mine) store_rows<D>(mine, f.o, f.inverse(), [&](int i) { return r0 + i < end ? row_at(a, a.o, s, kvh, r0 + i) : nullptr; });
+  else store_row<D>(at(a.o, s.q0 + qi, h), f.o, f.inverse(), r < end);
+  if (a.lse && lane < 32 && r < end) a.lse[static_cast<int64_t>(h) * a.Tq + s.q0 + qi] = f.lse();
+}
+
+// A row's part over some of its keys: its sums relative to its maximum, and that with the sum of the weights.
+template <int D>
+__device__ __forceinline__ void leave_part(const Args& a, int64_t at, const Soft<D>& f) {
+  const int up = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<f32x4*>(a.part_o + at * D + 32 * db + 8 * g + 4 * up) =
+          f32x4{f.o[db][4 * g], f.o[db][4 * g + 1], f.o[db][4 * g + 2], f.o[db][4 * g + 3]};
+  if (up == 0) *reinterpret_cast<f32x2_t*>(a.part_ml + at * 2) = f32x2_t{f.m, f.l};
+}
+
+// The same of all 128 rows of a workgroup's slot, each lane's accumulators in its own pieces: whole lines.
+template <int D>
+__device__ __forceinline__ void leave_whole(const Args& a, int64_t slot, const Soft<D>& f) {
+  const int lane = here(threadIdx.x & 63), w = threadIdx.x >> 6;
+  f32x4* const part = reinterpret_cast<f32x4*>(a.part_o) + (slot * 4 + w) * (D * 8) + lane;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) part[(db * 4 + g) * 64] = f32x4{f.o[db][4 * g], f.o[db][4 * g + 1], f.o[db][4 * g + 2], f.o[db][4 * g + 3]};
+  if (lane < 32) *reinterpret_cast<f32x2_t*>(a.part_ml + (slot * 128 + 32 * w + lane) * 2) = f32x2_t{f.m, f.l};
+}
+
+template <int D>
+__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void rows_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[3 * kKeys * Geo<D>::kRow];
+  Seq s;
+  int kvh, tile;
+  if (!tile_of<128>(a, &s, &kvh, &tile)) return;
+  const int R = s.nq * a.G, r0 = ((R + 127) / 128 - 1 - tile) * 128, end = min(r0 + 128, R);       // the longest rows first
+  Soft<D> f;
+  rows_unit<D, RA>(a, (lds_char*)lds, s, kvh, r0, end, 0, (sees(a, end - 1, s.nq, s.nk) + kKeys - 1) / kKeys, f);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // no wave reads the K slots any more
+  if (r0 + 32 * w < end) finish<D>(a, s, kvh, r0 + 32 * w, end, f, (lds_char*)lds + w * 32 * Geo<D>::kRow);
+}
+
+// ------------------------------------------------------------------------------ keys dealt out
+// Where the rows alone do not fill the chip their keys are dealt out too: all work is laid end to end, as units of rows
+// of one key head times the keys these see, and cut into ranges of the same length, wherever units begin and
+// end. A unit that lies in one range is finished there; of the others each range leaves a part: in its slot 0 of
+// the unit that it begins in or with, in slot 1 of one that begins later. the join adds them in order.
+//
+// Wide units, for sequences of many rows: as many queries as make 128 rows at most, in keys; a workgroup
+// a range. It takes the tiles of 64 that begin in it.
+struct Wide {
+  static constexpr int kRows = 128;
+  static constexpr int kLeast = 512;          // keys of a range: a part's way to memory and back costs about as much as these
+  static __device__ __forceinline__ int queries(const Args& a) { return a.G < 128 ? a.shift >= 0 ? 128 >> a.shift : 128 / a.G : 1; }
+  static __device__ __forceinline__ int units(const Args& a, const Seq& s) { return (s.nq + queries(a) - 1) / queries(a); }
+  // keys of the units before unit b: those its last query sees, one where that sees none
+  static __device__ __forceinline__ int64_t before(const Args& a, const Seq& s, int b) {
+    if (!a.causal) return static_cast<int64_t>(b) * max(1, s.nk);
+    const int n = queries(a), off = s.nk - s.nq, full = min(b, units(a, s) - 1);
+    const int none = off < 0 ? min(full, -off / n) : 0;
+    int64_t v = none + static_cast<int64_t>(full - none) * off + n * ((static_cast<int64_t>(full) * (full + 1) - static_cast<int64_t>(none) * (none + 1)) / 2);
+    if (b > full) v += max(1, s.nk);
+    return v;
+  }
+  static __device__ __forceinline__ int64_t of_head(const Args& a, const Seq& s) { return before(a, s, units(a, s)); }
+  static __device__ __forceinline__ int64_t work(const Args& a, const Seq& s) { return s.nq > 0 ? of_head(a, s) * a.Hkv : 0; }
+  static __device__ __forceinline__ int64_t length(int64_t total, int64_t n) { return max(static_cast<int64_t>(kLeast), quot(total + n - 1, n)); }
 };
 
-// What a sequence has to do: false if it is skipped.
-__device__ __forceinline__ int64_t units_of(const Args& a, int s, int* q0, int* nq, int* k0, int* nk) {
-  *q0 = *nq = *k0 = *nk = 0;
-  if (s >= a.n_seq) return 0;
-  const int lo = a.q_start[s], hi = a.q_start[s + 1];
-  if (lo < 0 || hi < lo || hi > a.Tq) {
-    set_status(a.status, XS_EBADINPUT);
-    return 0;
+// Narrow units, for a few rows: 32 of them, in tiles of 32 keys, a wave a range. Up to four key heads are side by side: waves of
+// one workgroup take the same tiles of theirs, which lie side by side in memory too where a token's heads do.
+struct Narrow {
+  static constexpr int kRows = 32;
+  static __device__ __forceinline__ int tiles(const Seq& s) { return max(1, (s.nk + 31) >> 5); }
+  static __device__ __forceinline__ int side(const Args& a) { return a.Hkv % 4 == 0 ? 4 : a.Hkv % 2 == 0 ? 2 : 1; }
+  static __device__ __forceinline__ int64_t work(const Args& a, const Seq& s) {
+    return static_cast<int64_t>((s.nq * a.G + 31) / 32) * (a.Hkv / side(a)) * tiles(s);
   }
-  if (hi == lo || !keys_of(a, s, k0, nk)) return 0;
-  *q0 = lo;
-  *nq = hi - lo;
-  return static_cast<int64_t>((static_cast<int64_t>(*nq) * a.G + 31) / 32) * a.Hkv;
-}
-__device__ __forceinline__ int tiles_of(int nk) { return nk > 0 ? static_cast<int>((static_cast<int64_t>(nk) + 31) / 32) : 1; }
-
-__device__ __forceinline__ int64_t scan64(int64_t v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t u = __shfl_up(v, d);
-    if (lane >= d) v += u;
+  static __device__ __forceinline__ int64_t length(int64_t total, int64_t n) { return max(static_cast<int64_t>(1), quot(total + n - 1, n)); }
+  static __device__ __forceinline__ void row(const Args& a, const Seq& s, int64_t x, int* kvh, int* r, int* i, int64_t* u0) {
+    const int b = static_cast<int>(quot(x, 32 * static_cast<int64_t>(a.Hkv))), n = min(32, s.nq * a.G - 32 * b);
+    const int in = static_cast<int>(x - static_cast<int64_t>(b) * 32 * a.Hkv);
+    *kvh = in / n;
+    *i = in - *kvh * n;
+    *r = 32 * b + *i;
+    *u0 = (static_cast<int64_t>(b) * (a.Hkv / side(a)) + *kvh / side(a)) * tiles(s);
   }
-  return v;
-}
-__device__ __forceinline__ int64_t lane64(int64_t v, int l) {
-  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), l), hi = __builtin_amdgcn_readlane(static_cast<int>(v >> 32), l);
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
+};
 
-__device__ __forceinline__ int64_t all_tiles(const Args& a) {
-  int64_t total = 0;
-  for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-    int q0, nq, k0, nk;
-    const int64_t u = units_of(a, s0 + (threadIdx.x & 63), &q0, &nq, &k0, &nk);
-    total += lane64(scan64(u * tiles_of(nk)), 63);
+// The sequences laid end to end, one a lane, 64 at a time; the first 64 are kept.
+template <class U>
+struct Line {
+  Seq mine;
+  int64_t n, upto, total;
+  __device__ __forceinline__ explicit Line(const Args& a) {
+    const int lane = threadIdx.x & 63;
+    mine = seq_of(a, lane);
+    n = U::work(a, mine);
+    upto = wave_scan(n);
+    total = lane64(upto, 63);
+    for (int s0 = 64; s0 < a.n_seq; s0 += 64) total += lane64(wave_scan(U::work(a, seq_of(a, s0 + lane))), 63);
   }
-  return total;
-}
-
-// The unit that tile u of all lies in; u is less than their number.
-__device__ __forceinline__ void unit_at(const Args& a, int64_t u, Unit* out) {
-  int64_t before = 0;
-  for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-    int q0, nq, k0, nk;
-    const int64_t tiles = units_of(a, s0 + (threadIdx.x & 63), &q0, &nq, &k0, &nk) * tiles_of(nk), upto = scan64(tiles);
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(before + upto > u);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      out->seq = s0 + l;
-      out->q0 = __builtin_amdgcn_readlane(q0, l);
-      out->nq = __builtin_amdgcn_readlane(nq, l);
-      out->k0 = __builtin_amdgcn_readlane(k0, l);
-      out->nk = __builtin_amdgcn_readlane(nk, l);
-      out->L = tiles_of(out->nk);
-      const int64_t in = u - before - lane64(upto - tiles, l), unit = in / out->L;
-      out->first = static_cast<int>(in - unit * out->L);
-      out->kvh = static_cast<int>(unit % a.Hkv);
-      out->r0 = static_cast<int>(unit / a.Hkv) * 32;
-      return;
+  // The sequence in which u (less than total) lies, and u's place in it.
+  __device__ __forceinline__ Seq find(const Args& a, int64_t u, int64_t* in) const {
+    Seq m = mine;
+    int64_t nn = n, up = upto;
+    for (int s0 = 0;;) {
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(up > u);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        *in = u - lane64(up - nn, l);
+        return lane_seq(m, l);
+      }
+      u -= lane64(up, 63);
+      s0 += 64;
+      m = seq_of(a, s0 + (threadIdx.x & 63));
+      nn = U::work(a, m);
+      up = wave_scan(nn);
     }
-    before += lane64(upto, 63);
   }
+};
+
+// The range of workgroup b of n, of `used` ranges that are not empty: those side by side lie on one XCD, whose L2 then holds what they
+// share, and every XCD has as many.
+__device__ __forceinline__ int64_t range_of_block(int b, int n, int64_t used) {
+  if (n % 8) return b;
+  const int64_t each = (used + 7) / 8;
+  return b / 8 < each ? b % 8 * each + b / 8 : used;
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void split_kernel(Args a) {
-  using G = Geo<D>;
-  constexpr int kTile = 32 * G::kRow;
-  __shared__ __attribute__((aligned(16))) char lds_raw[16 * kTile];
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), up = lane >> 5;
-  lds_char* const mine = (lds_char*)lds_raw + wv * 4 * kTile;       // K 0, K 1, V 0, V 1
-  const int64_t W = static_cast<int64_t>(blockIdx.x) * 4 + wv, NW = static_cast<int64_t>(gridDim.x) * 4;
-  const int64_t total = all_tiles(a), per = (total + NW - 1) / NW, end = min(W * per + per, total);
+__global__ __launch_bounds__(256, 2) void wide_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[3 * kKeys * Geo<D>::kRow];
+  const Line<Wide> line(a);
+  const int64_t per = Wide::length(line.total, gridDim.x), W = range_of_block(blockIdx.x, gridDim.x, quot(line.total + per - 1, per));
+  const int64_t begin = W * per, end = min(begin + per, line.total);
+  for (int64_t u = begin; u < end;) {
+    int64_t in;
+    const Seq s = line.find(a, u, &in);
+    const int64_t head = Wide::of_head(a, s);
+    const int kvh = static_cast<int>(quot(in, head));
+    in -= kvh * head;
+    int lo = 0, hi = Wide::units(a, s) - 1;                     // the unit with before(unit) <= in < before(unit + 1)
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (Wide::before(a, s, mid + 1) > in) hi = mid;
+      else lo = mid + 1;
+    }
+    const int64_t b0 = Wide::before(a, s, lo), b1 = Wide::before(a, s, lo + 1);
+    const int first = static_cast<int>(in - b0), last = static_cast<int>(min(b1 - b0, first + (end - u)));
+    const int rows = Wide::queries(a) * a.G, r0 = lo * rows, r_end = min(r0 + rows, s.nq * a.G);
+    Soft<D> f;
+    // the last unit's reads of these slots are done
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    rows_unit<D, 4>(a, (lds_char*)lds, s, kvh, r0, r_end, (first + kKeys - 1) / kKeys,
+                 (min(last, sees(a, r_end - 1, s.nq, s.nk)) + kKeys - 1) / kKeys, f);
+    const int rw = r0 + 32 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (first != 0 || last != b1 - b0) leave_whole<D>(a, W * 2 + (u > begin), f);
+    else if (rw < r_end) finish<D>(a, s, kvh, rw, r_end, f, (lds_char*)lds + (rw - r0) * Geo<D>::kRow);
+    u += last - first;
+  }
+}
+
+// A wave's key tiles [first, stop), every step-th, of 32 rows. It has a slot of K and one of V to itself and waits for
+// nobody: K tile j + 1 is on its way from the time the scores are there, V tile j + 1 from the end of the second product.
+template <int D>
+__device__ __forceinline__ void narrow_unit(const Args& a, lds_char* mine, const Seq& s, int kvh, int r0, int first, int stop, int step, Soft<D>& f) {
+  using Lk = Loader<D, 32, 1, kRows>;
+  using Lv = Loader<D, 32, 1, kCols>;
+  constexpr int kTile = 32 * Geo<D>::kRow;
+  const int lane = threadIdx.x & 63, R = s.nq * a.G, r = min(r0 + (lane & 31), R - 1);
+  const int lim = sees(a, r, s.nq, s.nk), all = sees(a, r0, s.nq, s.nk);
+  const char* const kp = at(a.k, s.k0, kvh);
+  const char* const vp = at(a.v, s.k0, kvh);
+  lds_char* const vs = mine + kTile;
+  const Lk lk(0, lane, a.k.row);
+  const Lv lv(0, lane, a.v.row);
+  auto issue_k = [&](int j) { lk.issue(kp + static_cast<int64_t>(j) * 32 * a.k.row, s.nk - j * 32, mine, 0); };
+  auto issue_v = [&](int j) { lv.issue(vp + static_cast<int64_t>(j) * 32 * a.v.row, s.nk - j * 32, vs, 0); };
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // the last unit's reads of these slots are done
+  if (first < stop) {
+    issue_k(first);
+    issue_v(first);
+  }
+  bf16x8 qf[D / 16];
+  load_frags<D>(row_at(a, a.q, s, kvh, r), qf);
   const RowReads<D, kRows> rr(lane);
   const ColReads<D, kCols> rc(lane);
-  const Loader<D, 32, 1, kRows> lk(0, lane, a.k.row);
-  const Loader<D, 32, 1, kCols> lv(0, lane, a.v.row);
-  Soft<D> f;
-  for (int64_t u = W * per; u < end;) {
-    Unit x;
-    unit_at(a, u, &x);
-    const int last = static_cast<int>(min(static_cast<int64_t>(x.L), x.first + (end - u)));
-    const int R = x.nq * a.G, rl = x.r0 + (lane & 31), r = min(rl, R - 1), qi = r / a.G, h = x.kvh * a.G + (r - qi * a.G);
-    const int lim = sees(a, r, x.nq, x.nk), all = sees(a, x.r0, x.nq, x.nk), any = sees(a, min(x.r0 + 31, R - 1), x.nq, x.nk);
-    const int stop = min(last, (any + 31) / 32);
-    const char* const kp = at(a.k, x.k0, x.kvh);
-    const char* const vp = at(a.v, x.k0, x.kvh);
-    auto issue = [&](int j) {
-      lk.issue(kp + static_cast<int64_t>(j) * 32 * a.k.row, x.nk - j * 32, mine + (j & 1) * kTile, 0);
-      lv.issue(vp + static_cast<int64_t>(j) * 32 * a.v.row, x.nk - j * 32, mine + (2 + (j & 1)) * kTile, 0);
-    };
-    // the last unit's reads of these slots are done
+  f.clear();
+  for (int j = first; j < stop; j += step) {
+    const bool more = j + step < stop;
+    wait_vm<Lv::kLoads>();                                       // K tile j (V tile j may still be in flight)
+    f32x16 sc[1];
+    zero(sc[0]);
+    fed<D / 16, NA>([&](int i) { return row_operand<D>(mine, 0, rr, i); }, [&](int i, bf16x8 v) { mma(sc[0], v, qf[i]); });
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (x.first < stop) issue(x.first);
-    bf16x8 qf[D / 16];
-    load_frags<D>(at(a.q, x.q0 + qi, h), qf);
-    f.clear();
-    for (int j = x.first; j < stop; ++j) {
-      wait_vm<0>();
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // tile j - 1 has been read
-      if (j + 1 < stop) issue(j + 1);
-      f32x16 sc[1] = {rows_product<D>(mine + (j & 1) * kTile, 0, rr, qf)};
-      if (j * 32 + 32 > all) hide(sc[0], j * 32, lim, up);
-      uint32_t pk[1][8];
-      f.take(sc, a.scale_log2e, pk);
-      cols_product<D>(mine + (2 + (j & 1)) * kTile, 0, rc, operand(pk[0], 0), f.o);
-      cols_product<D>(mine + (2 + (j & 1)) * kTile, 1, rc, operand(pk[0], 1), f.o);
-    }
-    if (rl < R) {
-      if (x.first == 0 && last == x.L) {
-        store_row<D>(at(a.o, x.q0 + qi, h), f.o, f.inverse());
-        if (a.lse && up == 0) a.lse[static_cast<int64_t>(h) * a.Tq + x.q0 + qi] = f.lse();
-      } else {
-        const int64_t slot = (W * 2 + (u > W * per)) * 32 + (lane & 31);
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-          for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<f32x4*>(a.part_o + slot * D + 32 * db + 8 * g + 4 * up) =
-                f32x4{f.o[db][4 * g], f.o[db][4 * g + 1], f.o[db][4 * g + 2], f.o[db][4 * g + 3]};
-        if (up == 0) *reinterpret_cast<f32x2_t*>(a.part_ml + slot * 2) = f32x2_t{f.m, f.l};
-      }
-    }
-    u += last - x.first;
+    if (more) issue_k(j + step);
+    if (j * 32 + 32 > all) hide(sc[0], j * 32, lim, lane >> 5);
+    uint32_t pk[1][8];
+    f.take(sc, a.scale_log2e, pk);
+    if (more) wait_vm<Lk::kLoads>(); else wait_vm<0>();          // V tile j
+    const bf16x8 p[2] = {operand(pk[0], 0), operand(pk[0], 1)};
+    fed<D / 16, NA>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
+                    [&](int i, bf16x8 v) { mma(f.o[i % (D / 32)], v, p[i / (D / 32)]); });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) issue_v(j + step);
   }
 }
 
-// One workgroup a unit, a wave a row at a time.
 template <int D>
-__global__ __launch_bounds__(256) void join_kernel(Args a, int64_t NW) {
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int64_t id = block_number(), total = all_tiles(a), per = (total + NW - 1) / NW;
-  // the id-th unit and its first tile
-  int64_t units = 0, tiles = 0;
+__global__ __launch_bounds__(256, 2) void narrow_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[4 * 2 * 32 * Geo<D>::kRow];
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), side = Narrow::side(a), sub = wv % side;
+  lds_char* const mine = (lds_char*)lds + wv * 2 * 32 * Geo<D>::kRow;
+  const Line<Narrow> line(a);
+  const int64_t W = static_cast<int64_t>(blockIdx.x) * (4 / side) + wv / side;
+  const int64_t per = Narrow::length(line.total, static_cast<int64_t>(gridDim.x) * (4 / side)), begin = W * per, end = min(begin + per, line.total);
+  for (int64_t u = begin; u < end;) {
+    int64_t in;
+    const Seq s = line.find(a, u, &in);
+    const int L = Narrow::tiles(s);
+    const int64_t unit = quot(in, L);
+    const int64_t block = quot(unit, a.Hkv / side);
+    const int first = static_cast<int>(in - unit * L), last = static_cast<int>(min(static_cast<int64_t>(L), first + (end - u)));
+    const int kvh = static_cast<int>(unit - block * (a.Hkv / side)) * side + sub, r0 = static_cast<int>(block) * 32, R = s.nq * a.G;
+    Soft<D> f;
+    narrow_unit<D>(a, mine, s, kvh, r0, first, min(last, (sees(a, min(r0 + 31, R - 1), s.nq, s.nk) + 31) / 32), 1, f);
+    const int i = here(threadIdx.x & 31);
+    if (first == 0 && last == L) finish<D>(a, s, kvh, r0, R, f);
+    else if (r0 + i < R) leave_part<D>(a, ((W * side + sub) * 2 + (u > begin)) * Narrow::kRows + i, f);
+    u += last - first;
+  }
+}
+
+// The b-th of all things, `things(s)` in sequence s: its sequence, its number there, and U's work before the sequence and in all.
+// False past the last.
+template <class U, class Things>
+__device__ __forceinline__ bool locate(const Args& a, const Things& things, int64_t b, Seq* s, int64_t* in, int64_t* before, int64_t* total) {
+  bool found = false;
+  *total = 0;
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-    int q0, nq, k0, nk;
-    const int64_t n = units_of(a, s0 + lane, &q0, &nq, &k0, &nk), upto = scan64(n), t = n * tiles_of(nk), t_upto = scan64(t);
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(units + upto > id);
-    if (!hit) {
-      units += lane64(upto, 63);
-      tiles += lane64(t_upto, 63);
-      continue;
+    const Seq mine = seq_of(a, s0 + (threadIdx.x & 63));
+    const int64_t work = U::work(a, mine), w_upto = wave_scan(work), n = things(mine), upto = wave_scan(n);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > b);
+    if (!found && hit) {
+      const int l = __builtin_ctzll(hit);
+      found = true;
+      *in = b - lane64(upto - n, l);
+      *before = *total + lane64(w_upto - work, l);
+      *s = lane_seq(mine, l);
+    } else if (!found) {
+      b -= lane64(upto, 63);
     }
-    const int l = __builtin_ctzll(hit);
-    q0 = __builtin_amdgcn_readlane(q0, l);
-    nq = __builtin_amdgcn_readlane(nq, l);
-    const int L = tiles_of(__builtin_amdgcn_readlane(nk, l));
-    const int64_t in = id - units - lane64(upto - n, l), u0 = tiles + lane64(t_upto - t, l) + in * L;
-    const int64_t w0 = u0 / per, w1 = (u0 + L - 1) / per;
-    if (w0 == w1) return;                                   // finished by its wave
-    const int kvh = static_cast<int>(in % a.Hkv), r0 = static_cast<int>(in / a.Hkv) * 32;
-    const int n_rows = min(32, nq * a.G - r0);
-    for (int i = wv; i < n_rows; i += 4) {
-      const auto slot = [&](int64_t w) { return (w * 2 + (w == w0 && u0 > w0 * per)) * 32 + i; };
-      float top = -FLT_MAX;
-      for (int64_t w = w0; w <= w1; ++w) top = fmaxf(top, a.part_ml[slot(w) * 2]);
-      float sum = 0.f, o[D / 64] = {};
-      for (int64_t w = w0; w <= w1; ++w) {
-        const f32x2_t ml = *reinterpret_cast<const f32x2_t*>(a.part_ml + slot(w) * 2);
-        const float c = __builtin_amdgcn_exp2f(ml.x - top);
-        sum = __builtin_fmaf(ml.y, c, sum);
+    *total += lane64(w_upto, 63);
+  }
+  return found;
+}
+
+__device__ __forceinline__ void store_joined(const Args& a, const Seq& s, int kvh, int r, int col, const f32x4& o, float top, float sum) {
+  const int qi = query_of(a, r), h = kvh * a.G + (r - qi * a.G);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  *reinterpret_cast<u32x2*>(at(a.o, s.q0 + qi, h) + col * 2) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+  if (a.lse && col == 0) a.lse[static_cast<int64_t>(h) * a.Tq + s.q0 + qi] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// Wide units: a wave takes 32 rows' 32 columns over the parts in turn, its lanes as they left them.
+template <int D>
+__global__ __launch_bounds__(256) void join_wide_kernel(Args a, int64_t ranges) {
+  const int lane = threadIdx.x & 63, up = lane >> 5;
+  const int64_t id = block_number() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = static_cast<int>(id % (D / 8)), w = part / (D / 32), db = part % (D / 32);
+  Seq s;
+  int64_t in, before, total;
+  if (!locate<Wide>(a, [&](const Seq& x) { return static_cast<int64_t>(Wide::units(a, x)) * a.Hkv; }, id / (D / 8), &s, &in, &before, &total)) return;
+  const int units = Wide::units(a, s), kvh = static_cast<int>(quot(in, units)), b = static_cast<int>(in - static_cast<int64_t>(kvh) * units);
+  const int per_unit = Wide::queries(a) * a.G, r0 = b * per_unit + 32 * w, end = min(b * per_unit + per_unit, s.nq * a.G);
+  if (r0 >= end) return;
+  before += kvh * Wide::of_head(a, s);
+  const int64_t u0 = before + Wide::before(a, s, b), u1 = before + Wide::before(a, s, b + 1);
+  const int64_t per = Wide::length(total, ranges), w0 = quot(u0, per), w1 = quot(u1 - 1, per);
+  if (w0 == w1) return;                                       // finished by its range
+  float top = -FLT_MAX, sum = 0.f;
+  f32x4 o[4];
 #pragma unroll
-        for (int d = 0; d < D / 64; ++d) o[d] = __builtin_fmaf(a.part_o[slot(w) * D + lane * (D / 64) + d], c, o[d]);
-      }
-      const int r = r0 + i, qi = r / a.G, h = kvh * a.G + (r - qi * a.G);
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      char* const out = at(a.o, q0 + qi, h);
-      if constexpr (D == 128) reinterpret_cast<uint32_t*>(out)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
-      else reinterpret_cast<uint16_t*>(out)[lane] = static_cast<uint16_t>(f2bf(o[0] * inv));
-      if (a.lse && lane == 0)
-        a.lse[static_cast<int64_t>(h) * a.Tq + q0 + qi] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
-    }
+  for (int g = 0; g < 4; ++g) o[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+  for (int64_t x = w0; x <= w1; ++x) {
+    const int64_t slot = x * 2 + (x == w0 && u0 > w0 * per);
+    const f32x4* const from = reinterpret_cast<const f32x4*>(a.part_o) + ((slot * 4 + w) * (D / 32) + db) * 256 + lane;
+    const f32x2_t ml = *reinterpret_cast<const f32x2_t*>(a.part_ml + (slot * 128 + 32 * w + (lane & 31)) * 2);
+    f32x4 v[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) v[g] = from[g * 64];
+    const float m = fmaxf(top, ml.x), was = __builtin_amdgcn_exp2f(top - m), is = __builtin_amdgcn_exp2f(ml.x - m);
+    top = m;
+    sum = __builtin_fmaf(ml.y, is, sum * was);
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[g][e] = __builtin_fmaf(v[g][e], is, o[g][e] * was);
+  }
+  const int r = min(r0 + (lane & 31), end - 1), qi = query_of(a, r), h = kvh * a.G + (r - qi * a.G);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  char* const to = at(a.o, s.q0 + qi, h) + 64 * db;
+#pragma unroll
+  for (int g = 0; g < 4; g += 2) {
+    const auto pack = [&](const f32x4& v) { return u32x2{pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv)}; };
+    const u32x4 v = columns8(pack(o[g]), pack(o[g + 1]));
+    if (r0 + (lane & 31) < end) *reinterpret_cast<u32x4*>(to + 16 * (g + up)) = v;
+  }
+  if (a.lse && db == 0 && lane < 32 && r0 + lane < end)
+    a.lse[static_cast<int64_t>(h) * a.Tq + s.q0 + qi] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// Narrow units: a wave a row, D / 4 lanes a part, 16 parts at once (a request's next token has a few rows, and their parts are many).
+template <int D>
+__global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges) {
+  constexpr int kLanes = D / 4, kParts = 64 / kLanes, kOnce = 16 / kParts;
+  const int lane = threadIdx.x & 63, side = Narrow::side(a);
+  Seq s;
+  int64_t in, before, total;
+  if (!locate<Narrow>(a, [&](const Seq& x) { return static_cast<int64_t>(x.nq) * a.H; },
+                      block_number() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), &s, &in, &before, &total))
     return;
+  int kvh, r, i;
+  int64_t u0;
+  Narrow::row(a, s, in, &kvh, &r, &i, &u0);
+  u0 += before;
+  const int64_t per = Narrow::length(total, ranges), w0 = quot(u0, per), w1 = quot(u0 + Narrow::tiles(s) - 1, per);
+  if (w0 == w1) return;                                       // finished by its range
+  const auto part = [&](int64_t w) { return ((w * side + kvh % side) * 2 + (w == w0 && u0 > w0 * per)) * Narrow::kRows + i; };
+  const auto weight = [&](int64_t w) {                        // maximum and sum of part w, none past the last
+    return w <= w1 ? *reinterpret_cast<const f32x2_t*>(a.part_ml + part(w) * 2) : f32x2_t{-FLT_MAX, 0.f};
+  };
+  float top = -FLT_MAX;
+  for (int64_t w = w0; w <= w1; w += 64) top = fmaxf(top, weight(w + lane).x);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  float sum = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const int grp = lane / kLanes, col = lane % kLanes * 4;
+  for (int64_t w = w0; w <= w1; w += 64) {
+    const f32x2_t ml = weight(w + lane);
+    const float c = w + lane <= w1 ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+    sum = __builtin_fmaf(ml.y, c, sum);
+    const int n = static_cast<int>(min(w1 - w + 1, static_cast<int64_t>(64)));
+    for (int p = 0; p < n; p += 16) {
+      f32x4 v[kOnce];
+#pragma unroll
+      for (int q = 0; q < kOnce; ++q) v[q] = *reinterpret_cast<const f32x4*>(a.part_o + part(w + min(p + q * kParts + grp, n - 1)) * D + col);
+#pragma unroll
+      for (int q = 0; q < kOnce; ++q) {
+        const float cq = __shfl(c, p + q * kParts + grp);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(v[q][e], cq, o[e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+#pragma unroll
+  for (int d = kLanes; d < 64; d <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
+  if (grp == 0) store_joined(a, s, kvh, r, col, o, top, sum);
+}
+
+// Short caches: a workgroup a narrow unit, its eight waves each an eighth of the key tiles, added up in LDS: no second launch.
+template <int D>
+__global__ __launch_bounds__(512, 2) void short_kernel(Args a) {
+  constexpr int kMine = 2 * 32 * Geo<D>::kRow;                  // a wave's slots: also 32 rows of D sums
+  __shared__ __attribute__((aligned(16))) char lds[8 * kMine];
+  __shared__ f32x2_t ml[8][32];
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, up = lane >> 5;
+  Seq s;
+  int kvh, tile;
+  if (!tile_of<32>(a, &s, &kvh, &tile)) return;
+  const int R = s.nq * a.G, r0 = tile * 32, tiles = (sees(a, min(r0 + 31, R - 1), s.nq, s.nk) + 31) / 32;
+  Soft<D> f;
+  narrow_unit<D>(a, (lds_char*)lds + wv * kMine, s, kvh, r0, wv, tiles, 8, f);
+  const int waves = min(8, max(1, tiles)), rows = min(32, R - r0);
+  if (waves == 1) {
+    if (wv == 0) finish<D>(a, s, kvh, r0, R, f);
+    return;
+  }
+  // row i of a wave's sums: pieces of four columns, piece p at p ^ i
+  if (wv < waves) {
+    const int i = lane & 31;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(lds + wv * kMine + i * D * 4 + (((8 * db + 2 * g + up) ^ i % (D / 4)) << 4)) =
+            f32x4{f.o[db][4 * g], f.o[db][4 * g + 1], f.o[db][4 * g + 2], f.o[db][4 * g + 3]};
+    if (up == 0) ml[wv][i] = f32x2_t{f.m, f.l};
+  }
+  __syncthreads();
+  constexpr int kLanes = D / 4;
+  const int col = threadIdx.x % kLanes;
+  for (int i = threadIdx.x / kLanes; i < rows; i += 512 / kLanes) {
+    float top = -FLT_MAX, sum = 0.f;
+    for (int w = 0; w < waves; ++w) top = fmaxf(top, ml[w][i].x);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < waves; ++w) {
+      const float c = __builtin_amdgcn_exp2f(ml[w][i].x - top);
+      sum = __builtin_fmaf(ml[w][i].y, c, sum);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(lds + w * kMine + i * D * 4 + ((col ^ i % kLanes) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(v[e], c, o[e]);
+    }
+    store_joined(a, s, kvh, r0 + i, 4 * col, o, top, sum);
   }
 }
 
@@ -592,35 +894,30 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   __shared__ __attribute__((aligned(16))) char lds_raw[4 * kTile];
   lds_char* const lds = (lds_char*)lds_raw;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), up = lane >> 5;
-  const int64_t id = block_number();
-  const int kvh = static_cast<int>(id % a.Hkv);
-  PackedTile s;
-  int k0, nk;
-  if (!packed_tile(a.q_start, a.n_seq, a.Tq, a.G, 128, static_cast<int>(id / a.Hkv), &s, a.status) || !keys_of(a, s.seq, &k0, &nk)) return;
-  k0 = __builtin_amdgcn_readfirstlane(k0);
-  nk = __builtin_amdgcn_readfirstlane(nk);
-  const int nq = s.rows, R = nq * a.G;
-  const int r0 = ((R + 127) / 128 - 1 - s.tile) * 128;
-  const int nkv = (sees(a, min(r0 + 127, R - 1), nq, nk) + kBKV - 1) / kBKV;
+  Seq s;
+  int kvh, tile;
+  if (!tile_of<128>(a, &s, &kvh, &tile)) return;
+  const int nq = s.nq, nk = s.nk, R = nq * a.G, r0 = ((R + 127) / 128 - 1 - tile) * 128, end = min(r0 + 128, R);
+  const int nkv = (sees(a, end - 1, nq, nk) + kBKV - 1) / kBKV;
   const int w0 = r0 + 32 * w;
   const int all = w0 < R ? sees(a, w0, nq, nk) : 0, any = w0 < R ? sees(a, min(w0 + 31, R - 1), nq, nk) : 0;
-  const int r = min(w0 + (lane & 31), R - 1), qi = r / a.G, h = kvh * a.G + (r - qi * a.G), lim = sees(a, r, nq, nk);
+  const int r = min(w0 + (lane & 31), R - 1), qi = query_of(a, r), h = kvh * a.G + (r - qi * a.G), lim = sees(a, r, nq, nk);
   const RowReads<D, kBoth> rk(lane);
   const ColReads<D, kBoth> ck(lane);
   const RowReads<D, kRows> rv(lane);
   const Loader<D, kBKV, 4, kBoth> lk(w, lane, a.k.row);
   const Loader<D, kBKV, 4, kRows> lv(w, lane, a.v.row);
-  const char* const kp = at(a.k, k0, kvh);
-  const char* const vp = at(a.v, k0, kvh);
+  const char* const kp = at(a.k, s.k0, kvh);
+  const char* const vp = at(a.v, s.k0, kvh);
   auto issue = [&](int j, int slot) {
     lk.issue(kp + static_cast<int64_t>(j) * kBKV * a.k.row, nk - j * kBKV, lds + slot * kTile, w);
     lv.issue(vp + static_cast<int64_t>(j) * kBKV * a.v.row, nk - j * kBKV, lds + (2 + slot) * kTile, w);
   };
   if (nkv > 0) issue(0, 0);
   bf16x8 qf[D / 16], df[D / 16];
-  load_frags<D>(at(a.q, s.start + qi, h), qf);
-  load_frags<D>(at(a.d_o, s.start + qi, h), df);
-  const int64_t stat = static_cast<int64_t>(h) * a.Tq + s.start + qi;
+  load_frags<D>(at(a.q, s.q0 + qi, h), qf);
+  load_frags<D>(at(a.d_o, s.q0 + qi, h), df);
+  const int64_t stat = static_cast<int64_t>(h) * a.Tq + s.q0 + qi;
   const float lse2 = lim > 0 ? a.lse[stat] * kLog2e : 0.f;
   int slot = 0;
   // tile j has landed in every wave's share, and no wave reads the tile before it any more; then `next` is loaded
@@ -646,7 +943,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     }
   } else {
     bf16x8 of[D / 16];
-    load_frags<D>(at(a.o, s.start + qi, h), of);
+    load_frags<D>(at(a.o, s.q0 + qi, h), of);
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
@@ -679,9 +976,9 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       cols_product<D>(ks, 2 * b + 1, ck, operand(pk, 1), acc);
     }
   }
-  if (w0 + (lane & 31) >= R) return;
-  if (up == 0) a.delta[stat] = delta;
-  store_row<D>(at(a.dq, s.start + qi, h), acc, a.scale);
+  if (up == 0 && w0 + lane < R) a.delta[stat] = delta;
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // no wave reads the tiles any more
+  if (w0 < end) store_rows<D>(lds + w * 32 * G::kRow, acc, a.scale, [&](int i) { return w0 + i < end ? row_at(a, a.dq, s, kvh, w0 + i) : nullptr; });
 }
 
 // dk and dv: a workgroup holds 32 NW keys of a key head (NW waves of 32), their K and V fragments beside both
@@ -697,11 +994,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
 // begins later; dkv_join_kernel adds them up in order.
 constexpr int kLeast = 16;
 
-struct KeySeq {
-  int q0, nq, k0, nk;
-};
 struct KeyTile {
-  KeySeq s;
+  Seq s;
   int kvh, tile, per_head;      // key tile; blocks of 32 queries that see it
   int64_t first, blocks;        // the block searched for, of the tile's
 };
@@ -709,54 +1003,50 @@ struct KeyTile {
 // Blocks of one query head in a sequence's tiles of 32 NW keys before tile j: those whose first key every query sees have all
 // ceil(nq / 32) (one where there is none: such keys' zeros are still written), from there on every tile has NW less.
 template <int NW>
-__device__ __forceinline__ int64_t blocks_before(const Args& a, const KeySeq& s, int64_t j) {
+__device__ __forceinline__ int64_t blocks_before(const Args& a, const Seq& s, int64_t j) {
   const int64_t f = max(1, (s.nq + 31) / 32), c = (s.nk + 31) / 32, off = s.nk - s.nq;
   if (!a.causal) return j * f;
   const int64_t full = off > 0 ? (off + 32 * NW - 1) / (32 * NW) : 0;
   return j <= full ? j * f : full * f + (j - full) * c - NW / 2 * (j * (j - 1) - full * (full - 1));
 }
 
-__device__ __forceinline__ KeySeq key_seq(const Args& a, int s) {
-  KeySeq x{0, 0, 0, 0};
+__device__ __forceinline__ Seq key_seq(const Args& a, int s) {
+  Seq x{0, 0, 0, 0};
   if (s >= a.n_seq) return x;
   const int q0 = a.q_start[s], q1 = a.q_start[s + 1], k0 = a.k_start[s], k1 = a.k_start[s + 1];
   if (q0 < 0 || q1 < q0 || q1 > a.Tq || k0 < 0 || k1 < k0 || k1 > a.Tk || k1 - k0 > a.max_k) {
     set_status(a.status, XS_EBADINPUT);
     return x;
   }
-  return KeySeq{q0, q1 - q0, k0, k1 - k0};
+  return Seq{q0, q1 - q0, k0, k1 - k0};
 }
 template <int NW>
-__device__ __forceinline__ int key_tiles(const KeySeq& s) { return (s.nk + 32 * NW - 1) / (32 * NW); }
+__device__ __forceinline__ int key_tiles(const Seq& s) { return (s.nk + 32 * NW - 1) / (32 * NW); }
 template <int NW>
-__device__ __forceinline__ int64_t blocks_of(const Args& a, const KeySeq& s) { return blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.H; }
+__device__ __forceinline__ int64_t blocks_of(const Args& a, const Seq& s) { return blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.H; }
 
 template <int NW>
 __device__ __forceinline__ int64_t all_blocks(const Args& a) {
   int64_t total = 0;
-  for (int s0 = 0; s0 < a.n_seq; s0 += 64) total += lane64(scan64(blocks_of<NW>(a, key_seq(a, s0 + (threadIdx.x & 63)))), 63);
+  for (int s0 = 0; s0 < a.n_seq; s0 += 64) total += lane64(wave_scan(blocks_of<NW>(a, key_seq(a, s0 + (threadIdx.x & 63)))), 63);
   return total;
 }
 
-__device__ __forceinline__ KeySeq lane_seq(const KeySeq& s, int l) {
-  return KeySeq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l), __builtin_amdgcn_readlane(s.k0, l),
-                __builtin_amdgcn_readlane(s.nk, l)};
-}
 
 // The key tile that block u of all lies in; u is less than their number.
 template <int NW>
 __device__ __forceinline__ void key_tile_at(const Args& a, int64_t u, KeyTile* out) {
   int64_t before = 0;
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-    const KeySeq mine = key_seq(a, s0 + (threadIdx.x & 63));
-    const int64_t n = blocks_of<NW>(a, mine), upto = scan64(n);
+    const Seq mine = key_seq(a, s0 + (threadIdx.x & 63));
+    const int64_t n = blocks_of<NW>(a, mine), upto = wave_scan(n);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(before + upto > u);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       out->s = lane_seq(mine, l);
       const int tiles = key_tiles<NW>(out->s);
       const int64_t head = blocks_before<NW>(a, out->s, tiles) * a.G, in = u - before - lane64(upto - n, l);
-      out->kvh = static_cast<int>(in / head);
+      out->kvh = static_cast<int>(quot(in, head));
       const int64_t x = in - out->kvh * head;
       int lo = 0, hi = tiles - 1;                               // the tile with before(tile) G <= x < before(tile + 1) G
       while (lo < hi) {
@@ -775,9 +1065,6 @@ __device__ __forceinline__ void key_tile_at(const Args& a, int64_t u, KeyTile* o
   }
 }
 
-// Workgroups that have blocks to do lie side by side on one XCD, whose L2 then holds their rows.
-__device__ __forceinline__ int64_t range_of_block(int b, int n) { return n % 8 ? b : static_cast<int64_t>(b % 8) * (n / 8) + b / 8; }
-
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kernel(Args a) {
   using G = Geo<D>;
@@ -788,8 +1075,8 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
   lds_char* const stats = lds + 2 * kStages * kTile;                           // lse and delta of each stage
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   lds_char* const stash = stats + 2 * kStages * kBQ * 4 + w * kStash * 1024;
-  const int64_t total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), (total + gridDim.x - 1) / gridDim.x);
-  const int64_t W = range_of_block(blockIdx.x, gridDim.x), begin = W * per, end = min(begin + per, total);
+  const int64_t total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), quot(total + gridDim.x - 1, gridDim.x));
+  const int64_t W = range_of_block(blockIdx.x, gridDim.x, quot(total + per - 1, per)), begin = W * per, end = min(begin + per, total);
   for (int64_t u = begin; u < end;) {
     KeyTile x;
     key_tile_at<NW>(a, u, &x);
@@ -895,10 +1182,9 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
     }
     const int key = kw + here(lane & 31);
     if (n == x.blocks) {
-      if (key < nk) {
-        store_row<D>(at(a.dk, x.s.k0 + key, x.kvh), dk, a.scale);
-        store_row<D>(at(a.dv, x.s.k0 + key, x.kvh), dv, 1.f);
-      }
+      const int kc = min(key, nk - 1);
+      store_row<D>(at(a.dk, x.s.k0 + kc, x.kvh), dk, a.scale, key < nk);
+      store_row<D>(at(a.dv, x.s.k0 + kc, x.kvh), dv, 1.f, key < nk);
     } else {
       f32x4* const part = reinterpret_cast<f32x4*>(a.part_o) + ((W * 2 + (u > begin)) * NW + w) * (D * 16) + here(lane);
 #pragma unroll
@@ -917,12 +1203,13 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW) void dkv_join_kernel(Args a, int n_ranges) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t id = block_number(), total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), (total + n_ranges - 1) / n_ranges);
-  const int kvh = static_cast<int>(id % a.Hkv);
+  const int64_t id = block_number(), total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), quot(total + n_ranges - 1, n_ranges));
+  const int64_t tile = quot(id, a.Hkv);
+  const int kvh = static_cast<int>(id - tile * a.Hkv);
   int64_t t = id / a.Hkv, blocks = 0;                 // the tile's number, counted over the sequences
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-    const KeySeq mine = key_seq(a, s0 + lane);
-    const int64_t tiles = key_tiles<NW>(mine), upto = scan64(tiles), n = blocks_of<NW>(a, mine), n_upto = scan64(n);
+    const Seq mine = key_seq(a, s0 + lane);
+    const int64_t tiles = key_tiles<NW>(mine), upto = wave_scan(tiles), n = blocks_of<NW>(a, mine), n_upto = wave_scan(n);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > t);
     if (!hit) {
       t -= lane64(upto, 63);
@@ -930,10 +1217,10 @@ __global__ __launch_bounds__(64 * NW) void dkv_join_kernel(Args a, int n_ranges)
       continue;
     }
     const int l = __builtin_ctzll(hit);
-    const KeySeq s = lane_seq(mine, l);
+    const Seq s = lane_seq(mine, l);
     const int64_t tile = t - lane64(upto - tiles, l), b0 = blocks_before<NW>(a, s, tile), b1 = blocks_before<NW>(a, s, tile + 1);
     const int64_t head = blocks + lane64(n_upto - n, l) + kvh * blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.G;
-    const int64_t u0 = head + b0 * a.G, u1 = head + b1 * a.G, w0 = u0 / per, w1 = (u1 - 1) / per;
+    const int64_t u0 = head + b0 * a.G, u1 = head + b1 * a.G, w0 = quot(u0, per), w1 = quot(u1 - 1, per);
     if (w0 == w1) return;                             // finished by its workgroup
     f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
@@ -955,9 +1242,9 @@ __global__ __launch_bounds__(64 * NW) void dkv_join_kernel(Args a, int n_ranges)
         }
     }
     const int key = static_cast<int>(tile) * 32 * NW + 32 * w + (lane & 31);
-    if (key >= s.nk) return;
-    store_row<D>(at(a.dk, s.k0 + key, kvh), dk, a.scale);
-    store_row<D>(at(a.dv, s.k0 + key, kvh), dv, 1.f);
+    const int kc = min(key, s.nk - 1);
+    store_row<D>(at(a.dk, s.k0 + kc, kvh), dk, a.scale, key < s.nk);
+    store_row<D>(at(a.dv, s.k0 + kc, kvh), dv, 1.f, key < s.nk);
     return;
   }
 }
@@ -992,7 +1279,8 @@ int check(const xs_attn_packed* A, pattn::Args* a) {
                       lies(A->o, A->o_row, A->o_head, A->heads, D)})
     if (rc != XS_EINVAL && r) rc = r;
   if (rc == XS_EINVAL) return rc;
-  if (rc || (D != 64 && D != 128) || static_cast<int64_t>(A->Tq) * (A->heads / A->kv_heads) >= (1 << 30) || A->Tk > (1 << 30))
+  if (rc || (D != 64 && D != 128) || static_cast<int64_t>(A->Tq) * (A->heads / A->kv_heads) >= (1 << 30) || A->Tk > (1 << 30) || A->heads > (1 << 16) ||
+      static_cast<int64_t>(A->Tq) * A->heads >= (int64_t(1) << 34) || static_cast<int64_t>(A->Tk) * A->kv_heads >= (int64_t(1) << 38))
     return XS_EUNSUPPORTED;
   a->q = mat(A->q, A->q_row, A->q_head);
   a->k = mat(A->k, A->k_row, A->k_head);
@@ -1005,6 +1293,7 @@ int check(const xs_attn_packed* A, pattn::Args* a) {
   a->H = A->heads;
   a->Hkv = A->kv_heads;
   a->G = A->heads / A->kv_heads;
+  a->shift = a->G & (a->G - 1) ? -1 : __builtin_ctz(a->G);
   a->Tq = A->Tq;
   a->Tk = A->Tk;
   a->causal = A->causal != 0;
@@ -1015,29 +1304,49 @@ int check(const xs_attn_packed* A, pattn::Args* a) {
   return XS_OK;
 }
 
-// Few rows: on average at most 32 a sequence and key head, or 128-row tiles that leave CUs without one.
-bool few_rows(const pattn::Args& a) {
-  const int64_t rows = static_cast<int64_t>(a.Tq) * a.G;
-  return rows <= 32ll * a.n_seq || packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv <= xs_host::num_cus();
+// Which kernels a forward call takes, from what the host knows.
+enum class Form { kRows, kWide, kNarrow, kShort };
+Form form_of(const pattn::Args& a) {
+  const int cus = xs_host::num_cus();
+  if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq)
+    return a.max_k <= 1024 && packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv <= cus ? Form::kShort : Form::kNarrow;
+  if (packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv > cus) return Form::kRows;
+  return a.G <= 128 ? Form::kWide : Form::kNarrow;
 }
 
-template <int D>
-int64_t split_bytes() { return static_cast<int64_t>(xs_host::num_cus()) * 4 * 2 * 32 * (D + 2) * 4; }
+// Ranges of a call whose keys are dealt out: two workgroups a CU, of narrow units each wave's.
+int64_t ranges_of(const pattn::Args& a, Form f) {
+  return 2 * int64_t(xs_host::num_cus()) * (f == Form::kWide ? 1 : a.Hkv % 4 == 0 ? 1 : a.Hkv % 2 == 0 ? 2 : 4);
+}
+// Rows of parts: two slots of each of its waves' 32 rows.
+int64_t part_rows(Form f) { return f == Form::kWide || f == Form::kNarrow ? 2 * int64_t(xs_host::num_cus()) * 4 * 2 * 32 : 0; }
+int64_t part_bytes(const pattn::Args& a, int D) { return a.Tq ? part_rows(form_of(a)) * (D + 2) * 4 : 0; }
 
 template <int D>
 int forward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
-  if (few_rows(a)) {
-    if (!ws || !aligned16(ws) || bytes < split_bytes<D>()) return XS_EWORKSPACE;
-    const int cus = xs_host::num_cus();
-    a.part_o = static_cast<float*>(ws);
-    a.part_ml = a.part_o + static_cast<int64_t>(cus) * 4 * 2 * 32 * D;
-    hipLaunchKernelGGL((pattn::split_kernel<D>), dim3(cus), dim3(256), 0, st, a);
+  const Form f = form_of(a);
+  if (f == Form::kRows) {
+    hipLaunchKernelGGL((pattn::rows_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv), dim3(256), 0, st, a);
+    return xs_host::launch_status();
+  }
+  if (f == Form::kShort) {
+    hipLaunchKernelGGL((pattn::short_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv), dim3(512), 0, st, a);
+    return xs_host::launch_status();
+  }
+  if (!ws || !aligned16(ws) || bytes < part_bytes(a, D)) return XS_EWORKSPACE;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = a.part_o + part_rows(f) * D;
+  const dim3 grid(2 * xs_host::num_cus());
+  if (f == Form::kWide) {
+    hipLaunchKernelGGL((pattn::wide_kernel<D>), grid, dim3(256), 0, st, a);
     if (xs_host::launch_status()) return XS_EHIP;
-    const int64_t units = packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv;
-    hipLaunchKernelGGL((pattn::join_kernel<D>), xs_host::grid_of(units), dim3(256), 0, st, a, static_cast<int64_t>(cus) * 4);
+    const int64_t units = packed_tiles_bound(a.Tq, a.n_seq, 1, a.G < 128 ? 128 / a.G : 1) * a.Hkv;
+    hipLaunchKernelGGL((pattn::join_wide_kernel<D>), xs_host::grid_of(D / 32 * units), dim3(256), 0, st, a, ranges_of(a, f));
   } else {
-    const int64_t tiles = packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv;
-    hipLaunchKernelGGL((pattn::rows_kernel<D>), xs_host::grid_of(tiles), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((pattn::narrow_kernel<D>), grid, dim3(256), 0, st, a);
+    if (xs_host::launch_status()) return XS_EHIP;
+    const int64_t rows = static_cast<int64_t>(a.Tq) * a.H;
+    hipLaunchKernelGGL((pattn::join_narrow_kernel<D>), xs_host::grid_of((rows + 3) / 4), dim3(256), 0, st, a, ranges_of(a, f));
   }
   return xs_host::launch_status();
 }
@@ -1089,7 +1398,7 @@ extern "C" int xs_attention_packed_workspace_bytes(const xs_attn_packed* A, int6
   pattn::Args a{};
   if (!bytes) return XS_EINVAL;
   if (int rc = check(A, &a)) return rc;
-  *bytes = a.Tq == 0 || !few_rows(a) ? 0 : A->head_dim == 128 ? split_bytes<128>() : split_bytes<64>();
+  *bytes = part_bytes(a, A->head_dim);
   return XS_OK;
 }
 

@@ -11,15 +11,25 @@ struct PackedTile {
   int rows;     // and its number of rows
 };
 
-// Inclusive sum over the wave's lanes.
-__device__ __forceinline__ int wave_scan(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int up = __shfl_up(v, d);
-    if (lane >= d) v += up;
-  }
-  return v;
+// Inclusive sum over the wave's lanes: within rows of 16, then each row's last value to the rows behind it. Lanes without a
+// source add 0. (With __shfl_up, which goes through LDS, a scan is six round trips of about 100 cycles.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp0(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int64_t add_dpp(int64_t v) {
+  const uint32_t lo = dpp0<CTRL, ROWS>(static_cast<int>(v)), hi = dpp0<CTRL, ROWS>(static_cast<int>(v >> 32));
+  return v + static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int add_dpp(int v) { return v + dpp0<CTRL, ROWS>(v); }
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v = add_dpp<0x111>(v);            // row_shr 1, 2, 4, 8
+  v = add_dpp<0x112>(v);
+  v = add_dpp<0x114>(v);
+  v = add_dpp<0x118>(v);
+  v = add_dpp<0x142, 0xa>(v);       // row_bcast 15 to rows 1 and 3
+  return add_dpp<0x143, 0xc>(v);    // row_bcast 31 to rows 2 and 3
 }
 
 // The t-th tile of all sequences, ceil(rows mult / per) of each; false past the last. A sequence that does not

@@ -375,7 +375,7 @@ def test_keys_past_2_gib_and_32_bit_offsets():
 
 def test_a_workspace_that_is_missing_or_small_is_refused():
     X = xs()
-    c = Case([(0, 1, 0, 100)], 1, 100, 4, 1, 128)
+    c = Case([(0, 1, 0, 2000)], 1, 2000, 4, 1, 128)
     assert c.ws.numel() > 0
     f = lambda p, n: X.xs_attention_packed(c.a, p, n, c.status.data_ptr(), _stream())
     assert f(None, c.ws.numel()) == f(c.ws.data_ptr(), c.ws.numel() - 1) == f(c.ws.data_ptr() + 8, c.ws.numel()) == X.XS_EWORKSPACE
