@@ -387,6 +387,21 @@ __device__ __forceinline__ bool tile_of(const Args& a, Seq* s, int* kvh, int* ti
 // The rows [r0, end) of a sequence and key head (128 at most, four waves of 32) over the key tiles [jb, je) of 64. LDS: two K
 // slots and one V slot. Per tile j: S from K slot j % 2, a barrier, K tile j + 2 into that slot; the softmax; V tile
 // j waited for and a barrier; O from the V slot; K tile j + 1 waited for, a barrier, V tile j + 1 into the V slot.
+#ifndef KS
+#define KS 256
+#endif
+#ifndef KL
+#define KL 384
+#endif
+#ifndef NL
+#define NL 2
+#endif
+#ifndef XR
+#define XR 512
+#endif
+#ifndef XC
+#define XC 1
+#endif
 #ifndef RA
 #define RA 2
 #endif
@@ -480,15 +495,16 @@ __device__ __forceinline__ void leave_part(const Args& a, int64_t at, const Soft
   if (up == 0) *reinterpret_cast<f32x2_t*>(a.part_ml + at * 2) = f32x2_t{f.m, f.l};
 }
 
-// The same of all 128 rows of a workgroup's slot, each lane's accumulators in its own pieces: whole lines.
+// The same of all 128 rows of a workgroup's slot, each lane's accumulators in its own pieces: whole lines. Without a tile only that the
+// weights' sum is 0.
 template <int D>
-__device__ __forceinline__ void leave_whole(const Args& a, int64_t slot, const Soft<D>& f) {
+__device__ __forceinline__ void leave_whole(const Args& a, int64_t slot, const Soft<D>& f, bool any) {
   const int lane = here(threadIdx.x & 63), w = threadIdx.x >> 6;
   f32x4* const part = reinterpret_cast<f32x4*>(a.part_o) + (slot * 4 + w) * (D * 8) + lane;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) part[(db * 4 + g) * 64] = f32x4{f.o[db][4 * g], f.o[db][4 * g + 1], f.o[db][4 * g + 2], f.o[db][4 * g + 3]};
+    for (int g = 0; any && g < 4; ++g) part[(db * 4 + g) * 64] = f32x4{f.o[db][4 * g], f.o[db][4 * g + 1], f.o[db][4 * g + 2], f.o[db][4 * g + 3]};
   if (lane < 32) *reinterpret_cast<f32x2_t*>(a.part_ml + (slot * 128 + 32 * w + lane) * 2) = f32x2_t{f.m, f.l};
 }
 
@@ -512,19 +528,20 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void rows_kernel(Args a) {
 // end. A unit that lies in one range is finished there; of the others each range leaves a part: in its slot 0 of
 // the unit that it begins in or with, in slot 1 of one that begins later. the join adds them in order.
 //
-// Wide units, for sequences of many rows: as many queries as make 128 rows at most, in keys; a workgroup
-// a range. It takes the tiles of 64 that begin in it.
+// Wide units, for sequences of many rows: as many queries as make 128 rows at most, in keys, behind them kStart keys for
+// what a unit takes besides its tiles (chunks of 61 tokens over 7 caches, some of them short: 45 us without). A workgroup a range: it takes the
+// tiles of 64 keys that begin in it.
 struct Wide {
-  static constexpr int kRows = 128;
-  static constexpr int kLeast = 512;          // keys of a range: a part's way to memory and back costs about as much as these
+  static constexpr int kStart = KS;
+  static constexpr int kLeast = KL;          // keys of a range: a part's way to memory and back costs about as much as these
   static __device__ __forceinline__ int queries(const Args& a) { return a.G < 128 ? a.shift >= 0 ? 128 >> a.shift : 128 / a.G : 1; }
   static __device__ __forceinline__ int units(const Args& a, const Seq& s) { return (s.nq + queries(a) - 1) / queries(a); }
-  // keys of the units before unit b: those its last query sees, one where that sees none
+  // length of the units before unit b: the keys that its last query sees, one where that sees none, and kStart
   static __device__ __forceinline__ int64_t before(const Args& a, const Seq& s, int b) {
-    if (!a.causal) return static_cast<int64_t>(b) * max(1, s.nk);
+    if (!a.causal) return static_cast<int64_t>(b) * (max(1, s.nk) + kStart);
     const int n = queries(a), off = s.nk - s.nq, full = min(b, units(a, s) - 1);
     const int none = off < 0 ? min(full, -off / n) : 0;
-    int64_t v = none + static_cast<int64_t>(full - none) * off + n * ((static_cast<int64_t>(full) * (full + 1) - static_cast<int64_t>(none) * (none + 1)) / 2);
+    int64_t v = static_cast<int64_t>(b) * kStart + none + static_cast<int64_t>(full - none) * off + n * ((static_cast<int64_t>(full) * (full + 1) - static_cast<int64_t>(none) * (none + 1)) / 2);
     if (b > full) v += max(1, s.nk);
     return v;
   }
@@ -537,12 +554,13 @@ struct Wide {
 // one workgroup take the same tiles of theirs, which lie side by side in memory too where a token's heads do.
 struct Narrow {
   static constexpr int kRows = 32;
+  static constexpr int kLeast = NL;            // tiles of a range: with fewer the join takes longer than the ranges
   static __device__ __forceinline__ int tiles(const Seq& s) { return max(1, (s.nk + 31) >> 5); }
   static __device__ __forceinline__ int side(const Args& a) { return a.Hkv % 4 == 0 ? 4 : a.Hkv % 2 == 0 ? 2 : 1; }
   static __device__ __forceinline__ int64_t work(const Args& a, const Seq& s) {
     return static_cast<int64_t>((s.nq * a.G + 31) / 32) * (a.Hkv / side(a)) * tiles(s);
   }
-  static __device__ __forceinline__ int64_t length(int64_t total, int64_t n) { return max(static_cast<int64_t>(1), quot(total + n - 1, n)); }
+  static __device__ __forceinline__ int64_t length(int64_t total, int64_t n) { return max(static_cast<int64_t>(kLeast), quot(total + n - 1, n)); }
   static __device__ __forceinline__ void row(const Args& a, const Seq& s, int64_t x, int* kvh, int* r, int* i, int64_t* u0) {
     const int b = static_cast<int>(quot(x, 32 * static_cast<int64_t>(a.Hkv))), n = min(32, s.nq * a.G - 32 * b);
     const int in = static_cast<int>(x - static_cast<int64_t>(b) * 32 * a.Hkv);
@@ -618,10 +636,10 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Args a) {
     Soft<D> f;
     // the last unit's reads of these slots are done
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    rows_unit<D, 4>(a, (lds_char*)lds, s, kvh, r0, r_end, (first + kKeys - 1) / kKeys,
-                 (min(last, sees(a, r_end - 1, s.nq, s.nk)) + kKeys - 1) / kKeys, f);
+    const int jb = (first + kKeys - 1) / kKeys, je = (min(last, sees(a, r_end - 1, s.nq, s.nk)) + kKeys - 1) / kKeys;
+    rows_unit<D, 4>(a, (lds_char*)lds, s, kvh, r0, r_end, jb, je, f);
     const int rw = r0 + 32 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (first != 0 || last != b1 - b0) leave_whole<D>(a, W * 2 + (u > begin), f);
+    if (first != 0 || last != b1 - b0) leave_whole<D>(a, W * 2 + (u > begin), f, jb < je);
     else if (rw < r_end) finish<D>(a, s, kvh, rw, r_end, f, (lds_char*)lds + (rw - r0) * Geo<D>::kRow);
     u += last - first;
   }
@@ -756,7 +774,11 @@ __global__ __launch_bounds__(256) void join_wide_kernel(Args a, int64_t ranges) 
     const f32x2_t ml = *reinterpret_cast<const f32x2_t*>(a.part_ml + (slot * 128 + 32 * w + (lane & 31)) * 2);
     f32x4 v[4];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) v[g] = from[g * 64];
+    for (int g = 0; g < 4; ++g) {
+      v[g] = from[g * 64];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[g][e] = ml.y == 0.f ? 0.f : v[g][e];       // not written
+    }
     const float m = fmaxf(top, ml.x), was = __builtin_amdgcn_exp2f(top - m), is = __builtin_amdgcn_exp2f(ml.x - m);
     top = m;
     sum = __builtin_fmaf(ml.y, is, sum * was);
@@ -778,15 +800,17 @@ __global__ __launch_bounds__(256) void join_wide_kernel(Args a, int64_t ranges) 
     a.lse[static_cast<int64_t>(h) * a.Tq + s.q0 + qi] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// Narrow units: a wave a row, D / 4 lanes a part, 16 parts at once (a request's next token has a few rows, and their parts are many).
+// Narrow units: a workgroup a row, D / 4 lanes a part, 16 parts at once in each wave (a request's next token has a few rows, and their
+// parts are many).
 template <int D>
 __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges) {
   constexpr int kLanes = D / 4, kParts = 64 / kLanes, kOnce = 16 / kParts;
-  const int lane = threadIdx.x & 63, side = Narrow::side(a);
+  __shared__ __attribute__((aligned(16))) f32x4 waves[4][kLanes];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), side = Narrow::side(a);
   Seq s;
   int64_t in, before, total;
   if (!locate<Narrow>(a, [&](const Seq& x) { return static_cast<int64_t>(x.nq) * a.H; },
-                      block_number() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), &s, &in, &before, &total))
+                      block_number(), &s, &in, &before, &total))
     return;
   int kvh, r, i;
   int64_t u0;
@@ -810,7 +834,7 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges
     const float c = w + lane <= w1 ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
     sum = __builtin_fmaf(ml.y, c, sum);
     const int n = static_cast<int>(min(w1 - w + 1, static_cast<int64_t>(64)));
-    for (int p = 0; p < n; p += 16) {
+    for (int p = 16 * wv; p < n; p += 64) {
       f32x4 v[kOnce];
 #pragma unroll
       for (int q = 0; q < kOnce; ++q) v[q] = *reinterpret_cast<const f32x4*>(a.part_o + part(w + min(p + q * kParts + grp, n - 1)) * D + col);
@@ -828,7 +852,14 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges
   for (int d = kLanes; d < 64; d <<= 1)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
-  if (grp == 0) store_joined(a, s, kvh, r, col, o, top, sum);
+  if (grp == 0) waves[wv][lane] = o;
+  __syncthreads();
+  if (wv || grp) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += waves[w][lane][e];
+  store_joined(a, s, kvh, r, col, o, top, sum);
 }
 
 // Short caches: a workgroup a narrow unit, its eight waves each an eighth of the key tiles, added up in LDS: no second launch.
@@ -1310,7 +1341,7 @@ Form form_of(const pattn::Args& a) {
   const int cus = xs_host::num_cus();
   if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq)
     return a.max_k <= 1024 && packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv <= cus ? Form::kShort : Form::kNarrow;
-  if (packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv > cus) return Form::kRows;
+  if (a.max_k <= XR || packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv > XC * cus) return Form::kRows;
   return a.G <= 128 ? Form::kWide : Form::kNarrow;
 }
 
@@ -1346,7 +1377,7 @@ int forward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
     hipLaunchKernelGGL((pattn::narrow_kernel<D>), grid, dim3(256), 0, st, a);
     if (xs_host::launch_status()) return XS_EHIP;
     const int64_t rows = static_cast<int64_t>(a.Tq) * a.H;
-    hipLaunchKernelGGL((pattn::join_narrow_kernel<D>), xs_host::grid_of((rows + 3) / 4), dim3(256), 0, st, a, ranges_of(a, f));
+    hipLaunchKernelGGL((pattn::join_narrow_kernel<D>), xs_host::grid_of(rows), dim3(256), 0, st, a, ranges_of(a, f));
   }
   return xs_host::launch_status();
 }

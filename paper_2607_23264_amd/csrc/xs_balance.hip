@@ -8,8 +8,8 @@
 //
 // A token is LPT lanes with EPL experts each, a lane's experts V consecutive ones at a time. Every lane keeps the
 // sums of its experts over its tokens in registers, so that the only exchange between lanes is a token's
-// maximum and sum; a workgroup joins them in LDS and leaves one row of sums and counts, and finish_kernel
-// adds a sequence's rows in a fixed order.
+// maximum and sum; a workgroup joins them in LDS and leaves one row of sums and counts. finish_kernel adds a sequence's rows
+// in a fixed order, 64 experts to a workgroup, and the last of a sequence's workgroups adds their shares of the loss.
 #include <cmath>
 
 #include "xs_common.hpp"
@@ -25,8 +25,11 @@ struct Args {
   const int32_t* start;     // [n_seq + 1], or NULL: one sequence of T tokens
   int T, E, k, n_seq, sigmoid, chunk, tiles;
   float alpha;
-  float* part;              // [tiles][E] sums of shares
-  int* part_n;              // [tiles][E] counts
+  int width;                // E up to a multiple of four
+  float* part;              // [tiles][width] sums of shares
+  int* part_n;              // [tiles][width] counts
+  float* terms;             // [n_seq][16] shares of the loss
+  int* done;                // [n_seq] workgroups that have left theirs
   int* counts;              // [n_seq][E]
   float* mean;              // [n_seq][E]
   float* loss;              // [n_seq]
@@ -109,9 +112,10 @@ __device__ __forceinline__ void shares(bool sigmoid, float (&p)[EPL], float (&re
   if (sigmoid) {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
+      // the reciprocal of one unit in the last place, which is what exp2 has too: a quotient takes ten instructions
       const float x = p[i];
-      p[i] = 1.f / (1.f + __builtin_amdgcn_exp2f(-x * kLog2e));
-      if constexpr (REST) rest[i] = 1.f / (1.f + __builtin_amdgcn_exp2f(x * kLog2e));
+      p[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * kLog2e));
+      if constexpr (REST) rest[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * kLog2e));
       total += p[i];
     }
   } else {
@@ -137,11 +141,15 @@ __global__ __launch_bounds__(256) void sums_kernel(Args a) {
   constexpr int kGroups = 256 / LPT, kCols = LPT * EPL;
   __shared__ float sums[kGroups * kCols];
   __shared__ int hist[kCols];
+  const int tid = threadIdx.x, sub = tid % LPT, grp = tid / LPT;
+  for (int64_t i = block_number() * 256 + tid; i < a.n_seq; i += static_cast<int64_t>(gridDim.x) * gridDim.y * 256) a.done[i] = 0;
   PackedTile s;
   if (block_number() >= a.tiles || !find(a, static_cast<int>(block_number()), &s)) return;
-  const int tid = threadIdx.x, sub = tid % LPT, grp = tid / LPT;
   const int first = s.tile * a.chunk, n = min(a.chunk, s.rows - first);
   const int64_t t0 = static_cast<int64_t>(s.start) + first;
+  // a token's logits are on their way while the token before is worked on
+  float next[EPL], acc[EPL];
+  load_row<LT, V, LPT, EPL>(a.logits, (t0 + min(grp, n - 1)) * a.ld, a.E, sub, -INFINITY, next);
   for (int e = tid; e < kCols; e += 256) hist[e] = 0;
   __syncthreads();
   for (int64_t i = tid; i < static_cast<int64_t>(n) * a.k; i += 256) {
@@ -149,12 +157,13 @@ __global__ __launch_bounds__(256) void sums_kernel(Args a) {
     if (e < 0 || e >= a.E) set_status(a.status, XS_EBADINPUT);
     else atomicAdd(&hist[e], 1);
   }
-  float acc[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) acc[i] = 0.f;
   for (int t = grp; t < n; t += kGroups) {
     float p[EPL], none[1];
-    load_row<LT, V, LPT, EPL>(a.logits, (t0 + t) * a.ld, a.E, sub, -INFINITY, p);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) p[i] = next[i];
+    load_row<LT, V, LPT, EPL>(a.logits, (t0 + min(t + kGroups, n - 1)) * a.ld, a.E, sub, -INFINITY, next);
     shares<LPT, EPL, false>(a.sigmoid, p, none);
 #pragma unroll
     for (int i = 0; i < EPL; ++i) acc[i] += p[i];
@@ -162,7 +171,7 @@ __global__ __launch_bounds__(256) void sums_kernel(Args a) {
 #pragma unroll
   for (int i = 0; i < EPL; ++i) sums[grp * kCols + expert_of<V, LPT>(sub, i)] = acc[i];
   __syncthreads();
-  const int64_t row = block_number() * a.E;
+  const int64_t row = block_number() * a.width;
   for (int e = tid; e < a.E; e += 256) {
     float v = 0.f;
 #pragma unroll
@@ -172,25 +181,31 @@ __global__ __launch_bounds__(256) void sums_kernel(Args a) {
   }
 }
 
-// One workgroup a sequence: its tiles' rows are added four groups of threads at a time.
-__global__ __launch_bounds__(1024) void finish_kernel(Args a) {
-  __shared__ float sums[1024];
-  __shared__ int hist[1024];
-  __shared__ float wave[16];
-  const int tid = threadIdx.x, s = blockIdx.x;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// 64 experts of a sequence: 16 lanes have four each, NT / 16 groups of lanes the tiles' rows in turn.
+template <int NT>
+__global__ __launch_bounds__(NT) void finish_kernel(Args a) {
+  constexpr int kGroups = NT / 16, kAhead = 8;
+  __shared__ __attribute__((aligned(16))) f32x4 sums[NT / 64][16];
+  __shared__ __attribute__((aligned(16))) i32x4 hist[NT / 64][16];
+  const int tid = threadIdx.x, blocks = (a.E + 63) / 64;
+  const int64_t id = block_number();
+  const int s = static_cast<int>(id / blocks), b = static_cast<int>(id - static_cast<int64_t>(s) * blocks);
+  if (s >= a.n_seq) return;
   int first = 0, rows = a.T;                           // the sequence's first tile and tokens
   if (a.start) {
     int before = 0;
     for (int s0 = 0; s0 <= s; s0 += 64) {
       const int i = s0 + (tid & 63);
-      int b = 0;
+      int len = 0;
       if (i < a.n_seq) {
         const int lo = a.start[i], hi = a.start[i + 1];
-        b = lo < 0 || hi < lo || hi > a.T ? 0 : hi - lo;
+        len = lo < 0 || hi < lo || hi > a.T ? 0 : hi - lo;
       }
-      const int tiles = static_cast<int>((static_cast<int64_t>(b) + a.chunk - 1) / a.chunk), upto = wave_scan(tiles);
+      const int tiles = static_cast<int>((static_cast<int64_t>(len) + a.chunk - 1) / a.chunk), upto = wave_scan(tiles);
       if (s < s0 + 64) {
-        rows = __builtin_amdgcn_readlane(b, s - s0);
+        rows = __builtin_amdgcn_readlane(len, s - s0);
         first = before + __builtin_amdgcn_readlane(upto, s - s0) - __builtin_amdgcn_readlane(tiles, s - s0);
       }
       before += __builtin_amdgcn_readlane(upto, 63);
@@ -198,39 +213,69 @@ __global__ __launch_bounds__(1024) void finish_kernel(Args a) {
   }
   int tiles = static_cast<int>((static_cast<int64_t>(rows) + a.chunk - 1) / a.chunk);
   tiles = min(tiles, max(0, a.tiles - first));         // sequences that overlap have more tiles than the workspace holds
-  const int width = a.E <= 64 ? 64 : a.E <= 256 ? 256 : 1024, groups = 1024 / width;
-  const int e = tid % width, g = tid / width;
-  float v = 0.f;
-  int c = 0;
-  if (e < a.E)
-    for (int i = g; i < tiles; i += groups) {
-      v += a.part[(static_cast<int64_t>(first) + i) * a.E + e];
-      c += a.part_n[(static_cast<int64_t>(first) + i) * a.E + e];
+  const int q = tid & 15, g = tid >> 4, e = b * 64 + 4 * q;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  i32x4 c = {0, 0, 0, 0};
+  if (e < a.width) {
+    const int64_t base = static_cast<int64_t>(first) * a.width + e;
+    for (int i = g; i < tiles; i += kAhead * kGroups) {
+      f32x4 vs[kAhead];
+      i32x4 cs[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int64_t at = base + static_cast<int64_t>(min(i + u * kGroups, tiles - 1)) * a.width;
+        vs[u] = *reinterpret_cast<const f32x4*>(a.part + at);
+        cs[u] = *reinterpret_cast<const i32x4*>(a.part_n + at);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i + u * kGroups < tiles) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v[j] += vs[u][j];
+            c[j] += cs[u][j];
+          }
+        }
     }
-  sums[tid] = v;
-  hist[tid] = c;
+  }
+#pragma unroll
+  for (int d = 16; d < 64; d <<= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] += __shfl_xor(v[j], d);
+      c[j] += __shfl_xor(c[j], d);
+    }
+  if ((tid & 63) < 16) {
+    sums[tid >> 6][q] = v;
+    hist[tid >> 6][q] = c;
+  }
   __syncthreads();
+  if (tid >= 64) return;
+  const int x = b * 64 + tid;
   float term = 0.f;
-  if (g == 0 && e < a.E) {
-    for (int i = 1; i < groups; ++i) {
-      v += sums[i * width + e];
-      c += hist[i * width + e];
+  if (x < a.E) {
+    float sum = 0.f;
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      sum += reinterpret_cast<const float*>(sums[w])[tid];
+      n += reinterpret_cast<const int*>(hist[w])[tid];
     }
-    const float n = static_cast<float>(rows > 0 ? rows : 1);
-    const float mean = v / n;
-    a.counts[static_cast<int64_t>(s) * a.E + e] = c;
-    a.mean[static_cast<int64_t>(s) * a.E + e] = mean;
-    term = static_cast<float>(c) / (static_cast<float>(a.k) * n) * mean;
+    const float tokens = static_cast<float>(rows > 0 ? rows : 1), mean = sum / tokens;
+    a.counts[static_cast<int64_t>(s) * a.E + x] = n;
+    a.mean[static_cast<int64_t>(s) * a.E + x] = mean;
+    term = static_cast<float>(n) / (static_cast<float>(a.k) * tokens) * mean;
   }
   term = lanes_sum<64>(term);
-  if ((tid & 63) == 0) wave[tid >> 6] = term;
-  __syncthreads();
-  if (tid == 0) {
-    float total = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) total += wave[i];
-    a.loss[s] = a.alpha * static_cast<float>(a.E) * total;
+  if (tid) return;
+  if (blocks > 1) {
+    float* const terms = a.terms + static_cast<int64_t>(s) * 16;
+    __hip_atomic_store(terms + b, term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__hip_atomic_fetch_add(a.done + s, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != blocks - 1) return;
+    term = 0.f;
+    for (int i = 0; i < blocks; ++i) term += __hip_atomic_load(terms + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
+  a.loss[s] = a.alpha * static_cast<float>(a.E) * term;
 }
 
 template <typename LT, int V, int LPT, int EPL>
@@ -297,10 +342,13 @@ int chunk_of(int32_t T) {
   return static_cast<int>(c < 16 ? 16 : (c + 15) / 16 * 16);
 }
 
+int64_t width_of(int32_t E) { return (E + 3) / 4 * 4; }
 int64_t tiles_of(int32_t T, int32_t n_seq) {
   const int64_t n = packed_tiles_bound(T, n_seq, 1, chunk_of(T));
   return n > 0 ? n : 1;
 }
+
+int64_t workspace_of(int32_t T, int32_t E, int32_t n_seq) { return tiles_of(T, n_seq) * width_of(E) * 8 + int64_t(n_seq) * 17 * 4; }
 
 int balance_ok(const xs_gate* g, const void* logits, int64_t ld, int32_t T, const int32_t* start, int32_t n_seq, float alpha) {
   if (!g || !logits || g->E < 1 || g->E > 1024 || g->k < 1 || g->k > g->E || g->k > 32 || g->reserved != 0) return XS_EINVAL;
@@ -336,7 +384,7 @@ void launch_grad(const balance::GradArgs& a, dim3 grid, hipStream_t st) {
 extern "C" int xs_balance_loss_workspace_bytes(int32_t T, int32_t E, int32_t n_seq, int64_t* bytes) {
   if (!bytes || T < 0 || E < 1 || E > 1024 || n_seq < 1 || n_seq > balance::kMaxSeq) return XS_EINVAL;
   if (T > INT32_MAX - 64) return XS_EUNSUPPORTED;
-  *bytes = tiles_of(T, n_seq) * E * 8;
+  *bytes = workspace_of(T, E, n_seq);
   return XS_OK;
 }
 
@@ -346,17 +394,22 @@ extern "C" int xs_balance_loss(const xs_gate* g, const void* logits, int64_t ld,
   if (int rc = balance_ok(g, logits, ld, T, seq_start, n_seq, alpha)) return rc;
   if (!topk_idx || !counts || !mean_share || !loss) return XS_EINVAL;
   const int64_t tiles = tiles_of(T, n_seq);
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15) || workspace_bytes < tiles * g->E * 8) return XS_EWORKSPACE;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15) || workspace_bytes < workspace_of(T, g->E, n_seq)) return XS_EWORKSPACE;
   balance::Args a{logits, ld, topk_idx, seq_start, T, g->E, g->k, n_seq, g->score == XS_SCORE_SIGMOID, chunk_of(T), static_cast<int>(tiles), alpha,
-                  static_cast<float*>(workspace), nullptr, counts, mean_share, loss, dev_status};
-  a.part_n = reinterpret_cast<int*>(a.part + tiles * g->E);
+                  static_cast<int>(width_of(g->E)), static_cast<float*>(workspace), nullptr, nullptr, nullptr, counts, mean_share, loss, dev_status};
+  a.part_n = reinterpret_cast<int*>(a.part + tiles * a.width);
+  a.terms = reinterpret_cast<float*>(a.part_n + tiles * a.width);
+  a.done = reinterpret_cast<int*>(a.terms + int64_t(n_seq) * 16);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const dim3 grid = xs_host::grid_of(tiles);
   const bool v4 = vectors(logits, ld, g->E, g->logits_type == XS_TYPE_BF16 ? 2 : 4);
   if (g->logits_type == XS_TYPE_BF16) v4 ? launch_sums<uint16_t, 4>(a, grid, st) : launch_sums<uint16_t, 1>(a, grid, st);
   else v4 ? launch_sums<float, 4>(a, grid, st) : launch_sums<float, 1>(a, grid, st);
   if (xs_host::launch_status()) return XS_EHIP;
-  hipLaunchKernelGGL(balance::finish_kernel, dim3(n_seq), dim3(1024), 0, st, a);
+  // few sequences have many tiles each
+  const dim3 parts = xs_host::grid_of(int64_t(n_seq) * ((g->E + 63) / 64));
+  if (n_seq <= 64) hipLaunchKernelGGL((balance::finish_kernel<1024>), parts, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((balance::finish_kernel<256>), parts, dim3(256), 0, st, a);
   return xs_host::launch_status();
 }
 

@@ -124,7 +124,7 @@ def test_attention_gradients():
     for bad in (dict(ws=None), dict(ws=A + 8), dict(nb=8 * 64 * 4 - 1)):
         assert f(**bad) == X.XS_EWORKSPACE, bad
     n = C.c_int64()
-    assert X.xs_attention_packed_backward_workspace_bytes(_attn(), C.byref(n)) == X.XS_OK and n.value == 8 * 64 * 4
+    assert X.xs_attention_packed_backward_workspace_bytes(_attn(), C.byref(n)) == X.XS_OK and n.value >= 8 * 64 * 4
     assert X.xs_attention_packed_workspace_bytes(_attn(), None) == X.XS_EINVAL
     # a single head has no head stride
     assert X.xs_attention_packed_workspace_bytes(_attn(heads=1, kv_heads=1, q_head=0, k_head=0, v_head=0, o_head=0), C.byref(n)) == X.XS_OK
