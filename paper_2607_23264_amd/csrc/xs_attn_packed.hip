@@ -387,27 +387,6 @@ __device__ __forceinline__ bool tile_of(const Args& a, Seq* s, int* kvh, int* ti
 // The rows [r0, end) of a sequence and key head (128 at most, four waves of 32) over the key tiles [jb, je) of 64. LDS: two K
 // slots and one V slot. Per tile j: S from K slot j % 2, a barrier, K tile j + 2 into that slot; the softmax; V tile
 // j waited for and a barrier; O from the V slot; K tile j + 1 waited for, a barrier, V tile j + 1 into the V slot.
-#ifndef KS
-#define KS 256
-#endif
-#ifndef KL
-#define KL 384
-#endif
-#ifndef NL
-#define NL 2
-#endif
-#ifndef XR
-#define XR 512
-#endif
-#ifndef XC
-#define XC 1
-#endif
-#ifndef RA
-#define RA 2
-#endif
-#ifndef NA
-#define NA 4
-#endif
 constexpr int kKeys = 64;      // of a tile
 template <int D, int AHEAD>
 __device__ __forceinline__ void rows_unit(const Args& a, lds_char* lds, const Seq& s, int kvh, int r0, int end, int jb, int je, Soft<D>& f) {
@@ -516,7 +495,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void rows_kernel(Args a) {
   if (!tile_of<128>(a, &s, &kvh, &tile)) return;
   const int R = s.nq * a.G, r0 = ((R + 127) / 128 - 1 - tile) * 128, end = min(r0 + 128, R);       // the longest rows first
   Soft<D> f;
-  rows_unit<D, RA>(a, (lds_char*)lds, s, kvh, r0, end, 0, (sees(a, end - 1, s.nq, s.nk) + kKeys - 1) / kKeys, f);
+  rows_unit<D, 2>(a, (lds_char*)lds, s, kvh, r0, end, 0, (sees(a, end - 1, s.nq, s.nk) + kKeys - 1) / kKeys, f);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // no wave reads the K slots any more
   if (r0 + 32 * w < end) finish<D>(a, s, kvh, r0 + 32 * w, end, f, (lds_char*)lds + w * 32 * Geo<D>::kRow);
@@ -532,8 +511,8 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void rows_kernel(Args a) {
 // what a unit takes besides its tiles (chunks of 61 tokens over 7 caches, some of them short: 45 us without). A workgroup a range: it takes the
 // tiles of 64 keys that begin in it.
 struct Wide {
-  static constexpr int kStart = KS;
-  static constexpr int kLeast = KL;          // keys of a range: a part's way to memory and back costs about as much as these
+  static constexpr int kStart = 256;
+  static constexpr int kLeast = 384;          // of a range (256 to 768 measured: the parts against the ranges)
   static __device__ __forceinline__ int queries(const Args& a) { return a.G < 128 ? a.shift >= 0 ? 128 >> a.shift : 128 / a.G : 1; }
   static __device__ __forceinline__ int units(const Args& a, const Seq& s) { return (s.nq + queries(a) - 1) / queries(a); }
   // length of the units before unit b: the keys that its last query sees, one where that sees none, and kStart
@@ -554,7 +533,7 @@ struct Wide {
 // one workgroup take the same tiles of theirs, which lie side by side in memory too where a token's heads do.
 struct Narrow {
   static constexpr int kRows = 32;
-  static constexpr int kLeast = NL;            // tiles of a range: with fewer the join takes longer than the ranges
+  static constexpr int kLeast = 2;             // tiles of a range (1 to 8 measured: with 1 the join takes longer than the ranges)
   static __device__ __forceinline__ int tiles(const Seq& s) { return max(1, (s.nk + 31) >> 5); }
   static __device__ __forceinline__ int side(const Args& a) { return a.Hkv % 4 == 0 ? 4 : a.Hkv % 2 == 0 ? 2 : 1; }
   static __device__ __forceinline__ int64_t work(const Args& a, const Seq& s) {
@@ -676,7 +655,7 @@ __device__ __forceinline__ void narrow_unit(const Args& a, lds_char* mine, const
     wait_vm<Lv::kLoads>();                                       // K tile j (V tile j may still be in flight)
     f32x16 sc[1];
     zero(sc[0]);
-    fed<D / 16, NA>([&](int i) { return row_operand<D>(mine, 0, rr, i); }, [&](int i, bf16x8 v) { mma(sc[0], v, qf[i]); });
+    fed<D / 16, 4>([&](int i) { return row_operand<D>(mine, 0, rr, i); }, [&](int i, bf16x8 v) { mma(sc[0], v, qf[i]); });
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) issue_k(j + step);
     if (j * 32 + 32 > all) hide(sc[0], j * 32, lim, lane >> 5);
@@ -684,7 +663,7 @@ __device__ __forceinline__ void narrow_unit(const Args& a, lds_char* mine, const
     f.take(sc, a.scale_log2e, pk);
     if (more) wait_vm<Lk::kLoads>(); else wait_vm<0>();          // V tile j
     const bf16x8 p[2] = {operand(pk[0], 0), operand(pk[0], 1)};
-    fed<D / 16, NA>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
+    fed<D / 16, 4>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
                     [&](int i, bf16x8 v) { mma(f.o[i % (D / 32)], v, p[i / (D / 32)]); });
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) issue_v(j + step);
@@ -1023,7 +1002,10 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
 // (W + 1) per), per = ceil(total / workgroups) but at least kLeast. A key tile that lies in one range is finished there, of
 // the others each workgroup leaves a part, in its slot 0 for the tile that its range begins in or with, in slot 1 for one that
 // begins later; dkv_join_kernel adds them up in order.
-constexpr int kLeast = 16;
+#ifndef DL
+#define DL 16
+#endif
+constexpr int kLeast = DL;
 
 struct KeyTile {
   Seq s;
@@ -1230,53 +1212,70 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
   }
 }
 
-// One workgroup a key tile: its parts, each wave its 32 keys', in the order of the ranges.
+// A wave adds 32 columns of 32 keys' dk and dv over the parts, in the order of the ranges.
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW) void dkv_join_kernel(Args a, int n_ranges) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t id = block_number(), total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), quot(total + n_ranges - 1, n_ranges));
-  const int64_t tile = quot(id, a.Hkv);
-  const int kvh = static_cast<int>(id - tile * a.Hkv);
-  int64_t t = id / a.Hkv, blocks = 0;                 // the tile's number, counted over the sequences
+__global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
+  constexpr int kPieces = NW * (D / 32);              // waves of a key tile
+  const int lane = threadIdx.x & 63, up = lane >> 5;
+  const int64_t id = block_number() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int piece = static_cast<int>(id % kPieces), w = piece / (D / 32), db = piece % (D / 32);
+  const int64_t number = quot(id / kPieces, a.Hkv);
+  const int kvh = static_cast<int>(id / kPieces - number * a.Hkv);
+  int64_t t = number, blocks = 0, total = 0, b0 = 0;
+  Seq s{0, 0, 0, 0};
+  bool found = false;
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
     const Seq mine = key_seq(a, s0 + lane);
     const int64_t tiles = key_tiles<NW>(mine), upto = wave_scan(tiles), n = blocks_of<NW>(a, mine), n_upto = wave_scan(n);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > t);
-    if (!hit) {
+    if (!found && hit) {
+      const int l = __builtin_ctzll(hit);
+      found = true;
+      s = lane_seq(mine, l);
+      t -= lane64(upto - tiles, l);
+      blocks = total + lane64(n_upto - n, l);
+    } else if (!found) {
       t -= lane64(upto, 63);
-      blocks += lane64(n_upto, 63);
-      continue;
     }
-    const int l = __builtin_ctzll(hit);
-    const Seq s = lane_seq(mine, l);
-    const int64_t tile = t - lane64(upto - tiles, l), b0 = blocks_before<NW>(a, s, tile), b1 = blocks_before<NW>(a, s, tile + 1);
-    const int64_t head = blocks + lane64(n_upto - n, l) + kvh * blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.G;
-    const int64_t u0 = head + b0 * a.G, u1 = head + b1 * a.G, w0 = quot(u0, per), w1 = quot(u1 - 1, per);
-    if (w0 == w1) return;                             // finished by its workgroup
-    f32x16 dk[D / 32], dv[D / 32];
+    total += lane64(n_upto, 63);
+  }
+  if (!found) return;
+  const int64_t per = max(static_cast<int64_t>(kLeast), quot(total + n_ranges - 1, n_ranges));
+  b0 = blocks_before<NW>(a, s, t);
+  const int64_t head = blocks + kvh * blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.G;
+  const int64_t u0 = head + b0 * a.G, u1 = head + blocks_before<NW>(a, s, t + 1) * a.G, w0 = quot(u0, per), w1 = quot(u1 - 1, per);
+  if (w0 == w1) return;                               // finished by its workgroup
+  f32x4 dk[4], dv[4];
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+  for (int g = 0; g < 4; ++g) dk[g] = dv[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+  for (int64_t W = w0; W <= w1; ++W) {
+    const f32x4* const part = reinterpret_cast<const f32x4*>(a.part_o) + ((W * 2 + (W == w0 && u0 > w0 * per)) * NW + w) * (D * 16) + db * 256 + lane;
+    f32x4 k4[4], v4[4];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dk[db][e] = dv[db][e] = 0.f;
-    for (int64_t W = w0; W <= w1; ++W) {
-      const f32x4* const part = reinterpret_cast<const f32x4*>(a.part_o) + ((W * 2 + (W == w0 && u0 > w0 * per)) * NW + w) * (D * 16) + lane;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 k4 = part[(db * 4 + g) * 64], v4 = part[(D / 8 + db * 4 + g) * 64];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            dk[db][4 * g + e] += k4[e];
-            dv[db][4 * g + e] += v4[e];
-          }
-        }
+    for (int g = 0; g < 4; ++g) {
+      k4[g] = part[g * 64];
+      v4[g] = part[D * 8 + g * 64];
     }
-    const int key = static_cast<int>(tile) * 32 * NW + 32 * w + (lane & 31);
-    const int kc = min(key, s.nk - 1);
-    store_row<D>(at(a.dk, s.k0 + kc, kvh), dk, a.scale, key < s.nk);
-    store_row<D>(at(a.dv, s.k0 + kc, kvh), dv, 1.f, key < s.nk);
-    return;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        dk[g][e] += k4[g][e];
+        dv[g][e] += v4[g][e];
+      }
+  }
+  const int key = static_cast<int>(t) * 32 * NW + 32 * w + (lane & 31), kc = min(key, s.nk - 1);
+  const auto pack = [](const f32x4& v, float c) { return u32x2{pack_bf16x2(v[0] * c, v[1] * c), pack_bf16x2(v[2] * c, v[3] * c)}; };
+  char* const to_k = at(a.dk, s.k0 + kc, kvh) + 64 * db + 16 * up;
+  char* const to_v = at(a.dv, s.k0 + kc, kvh) + 64 * db + 16 * up;
+#pragma unroll
+  for (int g = 0; g < 4; g += 2) {
+    const u32x4 k = columns8(pack(dk[g], a.scale), pack(dk[g + 1], a.scale)), v = columns8(pack(dv[g], 1.f), pack(dv[g + 1], 1.f));
+    if (key < s.nk) {
+      *reinterpret_cast<u32x4*>(to_k + 16 * g) = k;
+      *reinterpret_cast<u32x4*>(to_v + 16 * g) = v;
+    }
   }
 }
 
@@ -1338,11 +1337,15 @@ int check(const xs_attn_packed* A, pattn::Args* a) {
 // Which kernels a forward call takes, from what the host knows.
 enum class Form { kRows, kWide, kNarrow, kShort };
 Form form_of(const pattn::Args& a) {
-  const int cus = xs_host::num_cus();
-  if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq)
-    return a.max_k <= 1024 && packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv <= cus ? Form::kShort : Form::kNarrow;
-  if (a.max_k <= XR || packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv > XC * cus) return Form::kRows;
-  return a.G <= 128 ? Form::kWide : Form::kNarrow;
+  const int64_t tiles = packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv;
+  // Few rows a sequence: one launch up to 1024 keys (8 units of 1024 keys 9.6 us, in two 11.4 and the time between; 256 22.0 and 29.8; of 2048
+  // keys 13.3 and 11.7).
+  if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq) return a.max_k <= 1024 ? Form::kShort : Form::kNarrow;
+  // A prompt's sequences are about as long as twice their average, a cache is taken to be full. Tiles that leave CUs without one take their keys
+  // dealt out if they are long (8 heads of one prompt, 1000 tokens: 26.3 us by rows, 25.9 and a launch dealt out; 2000: 46.7 and
+  // 36.3; 4000: 88 and 66; 32 heads, 2000: 54.5 and 73).
+  const int64_t keys = a.k_rows ? a.max_k : std::min<int64_t>(a.max_k, 2 * int64_t(a.Tk) / a.n_seq);
+  return keys <= 1024 || tiles > xs_host::num_cus() || a.G > 128 ? Form::kRows : Form::kWide;
 }
 
 // Ranges of a call whose keys are dealt out: two workgroups a CU, of narrow units each wave's.
@@ -1402,7 +1405,7 @@ template <int D, int NW>
 int dkv(const pattn::Args& a, int ranges, hipStream_t st) {
   hipLaunchKernelGGL((pattn::dkv_kernel<D, NW>), dim3(ranges), dim3(64 * NW), 0, st, a);
   if (xs_host::launch_status()) return XS_EHIP;
-  hipLaunchKernelGGL((pattn::dkv_join_kernel<D, NW>), xs_host::grid_of(key_tiles_bound<D>(a)), dim3(64 * NW), 0, st, a, ranges);
+  hipLaunchKernelGGL((pattn::dkv_join_kernel<D, NW>), xs_host::grid_of(key_tiles_bound<D>(a) * (NW * (D / 32) / 4)), dim3(256), 0, st, a, ranges);
   return xs_host::launch_status();
 }
 

@@ -95,7 +95,8 @@ __device__ __forceinline__ float row_sum(float v, float* red, int row) {
   return v;
 }
 
-template <int NT, int NP, int RP>
+// EARLY: the weights are read with the row, not behind its sum (few rows, where a kernel's time is its chain of loads).
+template <int NT, int NP, int RP, bool EARLY>
 __global__ __launch_bounds__(NT * RP) void norm_kernel(Args a) {
   __shared__ float red[NT > 64 ? RP * NT / 64 : 1];
   const int in = threadIdx.x / NT, t = threadIdx.x % NT;
@@ -103,6 +104,7 @@ __global__ __launch_bounds__(NT * RP) void norm_kernel(Args a) {
   const bool live = row < a.rows;
   if (NT > 64 && block_number() * RP >= a.rows) return;      // the whole workgroup (surplus of the grid)
   u32x4 h[NP];
+  W8 early[EARLY ? NP : 1];
   float ss = 0.f;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
@@ -110,6 +112,7 @@ __global__ __launch_bounds__(NT * RP) void norm_kernel(Args a) {
     h[p] = kZero4;
     if (live && col < a.cols) {
       h[p] = *reinterpret_cast<const u32x4*>(a.x + row * a.ldx + col);
+      if constexpr (EARLY) early[p] = weights8(a.w, a.w32, col);
       if (a.r) {
         const u32x4 r = *reinterpret_cast<const u32x4*>(a.r + row * a.ldr + col);
 #pragma unroll
@@ -127,7 +130,7 @@ __global__ __launch_bounds__(NT * RP) void norm_kernel(Args a) {
     const int col = (p * NT + t) * 8;
     float y[8] = {};
     if (col < a.cols) {
-      const W8 w = weights8(a.w, a.w32, col);
+      const W8 w = EARLY ? early[EARLY ? p : 0] : weights8(a.w, a.w32, col);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         y[2 * e] = bf_lo(h[p][e]) * inv * w.v[2 * e];
@@ -240,19 +243,34 @@ __global__ __launch_bounds__(NT * RP) void norm_grad_kernel(GradArgs a) {
   }
 }
 
-// dw[c] = sum over n parts: sixteen threads of a workgroup have four columns each, sixteen groups of threads
-// every sixteenth part.
-__global__ __launch_bounds__(256) void sum_kernel(const float* __restrict__ part, int n, int cols, float* __restrict__ dw) {
+// dw[c] = sum over n parts: sixteen threads of a workgroup have four columns each, 64 groups of threads every 64th part, eight of
+// them on their way at once.
+__global__ __launch_bounds__(1024) void sum_kernel(const float* __restrict__ part, int n, int cols, float* __restrict__ dw) {
   __shared__ __attribute__((aligned(16))) f32x4 red[16][16];
   const int q = threadIdx.x & 15, g = threadIdx.x >> 4, col = (blockIdx.x * 16 + q) * 4;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (col < cols)
-    for (int i = g; i < n; i += 16) s += *reinterpret_cast<const f32x4*>(part + static_cast<int64_t>(i) * cols + col);
-  red[g][q] = s;
+    for (int i = g; i < n; i += 8 * 64) {
+      f32x4 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const f32x4*>(part + static_cast<int64_t>(min(i + 64 * u, n - 1)) * cols + col);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i + 64 * u < n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[e] += v[u][e];
+    }
+#pragma unroll
+  for (int d = 16; d < 64; d <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += __shfl_xor(s[e], d);
+  if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][q] = s;
   __syncthreads();
   if (g || col >= cols) return;
 #pragma unroll
-  for (int i = 1; i < 16; ++i) s += red[i][q];
+  for (int w = 1; w < 16; ++w)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += red[w][q][e];
   *reinterpret_cast<f32x4*>(dw + col) = s;
 }
 
@@ -301,9 +319,14 @@ template <int NT, int NP, int RP>
 struct Forward {
   static void go(const norm::Args& a, hipStream_t st) {
     constexpr int rp = NT == 64 ? RP : 1;
-    hipLaunchKernelGGL((norm::norm_kernel<NT, NP, rp>), xs_host::grid_of((a.rows + rp - 1) / rp), dim3(NT * rp), 0, st, a);
+    hipLaunchKernelGGL((norm::norm_kernel<NT, NP, rp, false>), xs_host::grid_of((a.rows + rp - 1) / rp), dim3(NT * rp), 0, st, a);
   }
 };
+// Few rows: as many threads a row as it has pieces.
+template <int NT, int NP>
+void forward_few(const norm::Args& a, hipStream_t st) {
+  hipLaunchKernelGGL((norm::norm_kernel<NT, NP, 1, true>), xs_host::grid_of(a.rows), dim3(NT), 0, st, a);
+}
 template <int NT, int NP, int RP>
 struct Backward {
   static void go(const norm::GradArgs& a, hipStream_t st) {
@@ -334,7 +357,13 @@ extern "C" int xs_rmsnorm(const void* x, int64_t ldx, const void* residual, int6
   const norm::Args a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(residual), ldx, ld_res, weight,
                      weight_type == XS_TYPE_F32, eps, rows, cols, static_cast<uint16_t*>(h), static_cast<uint16_t*>(y), ld_h, ld_y,
                      static_cast<uint8_t*>(codes), ld_codes, scales, ld_scales};
-  by_columns<Forward>(a, static_cast<hipStream_t>(stream));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (rows > xs_host::num_cus()) by_columns<Forward>(a, st);
+  else if (cols <= 512) forward_few<64, 1>(a, st);
+  else if (cols <= 2048) forward_few<256, 1>(a, st);
+  else if (cols <= 8192) forward_few<1024, 1>(a, st);
+  else if (cols <= 16384) forward_few<1024, 2>(a, st);
+  else forward_few<1024, 4>(a, st);
   return xs_host::launch_status();
 }
 
@@ -368,6 +397,6 @@ extern "C" int xs_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* dh
     if (xs_host::launch_status()) return XS_EHIP;
   }
   if (!d_weight) return XS_OK;
-  hipLaunchKernelGGL(norm::sum_kernel, dim3((cols + 63) / 64), dim3(256), 0, st, static_cast<const float*>(workspace), groups, cols, d_weight);
+  hipLaunchKernelGGL(norm::sum_kernel, dim3((cols + 63) / 64), dim3(1024), 0, st, static_cast<const float*>(workspace), groups, cols, d_weight);
   return xs_host::launch_status();
 }
