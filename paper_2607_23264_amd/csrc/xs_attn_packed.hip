@@ -137,6 +137,11 @@ struct RowReads {
     first = r * Geo<D>::kRow + ((up ^ Geo<D>::swz(WAY, r)) << 4);
   }
   __device__ __forceinline__ int at(int kk) const { return first ^ kk << 5; }
+  __device__ __forceinline__ RowReads fresh() const {
+    RowReads r(*this);
+    r.first = here(first);
+    return r;
+  }
 };
 // By columns: key or row 16 s (+ 4 hf), column block db. Where the swizzle does not change over four rows the second
 // address is the first and a constant.
@@ -153,13 +158,21 @@ struct ColReads {
     }
   }
   __device__ __forceinline__ int at(int hf, int db) const { return first[hf] ^ db << 6; }
+  __device__ __forceinline__ ColReads fresh() const {
+    ColReads r(*this);
+#pragma unroll
+    for (int hf = 0; hf < kHalves; ++hf) r.first[hf] = here(first[hf]);
+    return r;
+  }
 };
 
 // N matrix instructions, mul(i, operand), whose LDS reads are issued AHEAD instructions before them. Left to itself the
-// compiler reads one operand, waits for it and multiplies.
-template <int N, int AHEAD, class Read, class Mul>
+// compiler reads one operand, waits for it and multiplies. FIRST: the wave goes before the others of its SIMD, whose softmax fills the
+// matrix unit's time (heads of 128: rows 550 -> 530 us, dq 322 -> 306; of 64 2% slower).
+template <int N, int AHEAD, bool FIRST, class Read, class Mul>
 __device__ __forceinline__ void fed(const Read& read, const Mul& mul) {
   decltype(read(0)) buf[AHEAD + 1];
+  if constexpr (FIRST) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) buf[i] = read(i);
 #pragma unroll
@@ -169,6 +182,7 @@ __device__ __forceinline__ void fed(const Read& read, const Mul& mul) {
     mul(i, buf[i % (AHEAD + 1)]);
     __builtin_amdgcn_sched_barrier(0);
   }
+  if constexpr (FIRST) __builtin_amdgcn_s_setprio(0);
 }
 
 template <int D, Way WAY>
@@ -397,14 +411,14 @@ __device__ __forceinline__ void rows_unit(const Args& a, lds_char* lds, const Se
   const char* const kp = at(a.k, s.k0, kvh);
   const char* const vp = at(a.v, s.k0, kvh);
   lds_char* const vs = lds + 2 * kTile;
-  // Every lane's addresses are made anew where they are used: kept over the loop they spill, and a reload waits for all
-  // the tiles in flight.
-  auto issue_k = [&](int j) {
-    Loader<D, kKeys, 4, kRows>(w, here(lane), a.k.row).issue(kp + static_cast<int64_t>(j) * kKeys * a.k.row, s.nk - j * kKeys, lds + (j & 1) * kTile, w);
-  };
-  auto issue_v = [&](int j) {
-    Loader<D, kKeys, 4, kCols>(w, here(lane), a.v.row).issue(vp + static_cast<int64_t>(j) * kKeys * a.v.row, s.nk - j * kKeys, vs, w);
-  };
+  const Loader<D, kKeys, 4, kRows> lk(w, lane, a.k.row);
+  const Loader<D, kKeys, 4, kCols> lv(w, lane, a.v.row);
+  // What follows from these is made anew where it is used: kept over the loop it spills, and a reload waits for all the tiles
+  // in flight.
+  const RowReads<D, kRows> rows(lane);
+  const ColReads<D, kCols> cols(lane);
+  auto issue_k = [&](int j) { lk.issue(kp + static_cast<int64_t>(j) * kKeys * a.k.row, s.nk - j * kKeys, lds + (j & 1) * kTile, w); };
+  auto issue_v = [&](int j) { lv.issue(vp + static_cast<int64_t>(j) * kKeys * a.v.row, s.nk - j * kKeys, vs, w); };
   bf16x8 qf[D / 16];
   f.clear();
   if (jb < je) {
@@ -418,11 +432,11 @@ __device__ __forceinline__ void rows_unit(const Args& a, lds_char* lds, const Se
   }
   auto step = [&](int j, auto masked) {
     lds_char* const ks = lds + (j & 1) * kTile;
-    const RowReads<D, kRows> rr(here(lane));
+    const RowReads<D, kRows> rr = rows.fresh();
     f32x16 sc[2];
     zero(sc[0]);
     zero(sc[1]);
-    fed<D / 8, AHEAD>([&](int i) { return row_operand<D>(ks, i & 1, rr, i >> 1); }, [&](int i, bf16x8 v) { mma(sc[i & 1], v, qf[i >> 1]); });
+    fed<D / 8, AHEAD, D == 128>([&](int i) { return row_operand<D>(ks, i & 1, rr, i >> 1); }, [&](int i, bf16x8 v) { mma(sc[i & 1], v, qf[i >> 1]); });
     // every wave is done with K slot j % 2: K tile j + 2 goes there
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const bool k2 = j + 2 < je;
@@ -436,9 +450,9 @@ __device__ __forceinline__ void rows_unit(const Args& a, lds_char* lds, const Se
     // V tile j has landed in every wave's share (only K tile j + 2 may still be in flight)
     if (k2) wait_vm<kLoads>(); else wait_vm<0>();
     asm volatile("s_barrier" ::: "memory");
-    const ColReads<D, kCols> rc(here(lane));
+    const ColReads<D, kCols> rc = cols.fresh();
     const bf16x8 p[4] = {operand(pk[0], 0), operand(pk[0], 1), operand(pk[1], 0), operand(pk[1], 1)};
-    fed<D / 8, AHEAD>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
+    fed<D / 8, AHEAD, D == 128>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
                       [&](int i, bf16x8 v) { mma(f.o[i % (D / 32)], v, p[i / (D / 32)]); });
     if (j + 1 < je) {
       // K tile j + 1 has landed in every wave's share, and no wave reads the V slot any more
@@ -655,7 +669,7 @@ __device__ __forceinline__ void narrow_unit(const Args& a, lds_char* mine, const
     wait_vm<Lv::kLoads>();                                       // K tile j (V tile j may still be in flight)
     f32x16 sc[1];
     zero(sc[0]);
-    fed<D / 16, 4>([&](int i) { return row_operand<D>(mine, 0, rr, i); }, [&](int i, bf16x8 v) { mma(sc[0], v, qf[i]); });
+    fed<D / 16, 4, D == 128>([&](int i) { return row_operand<D>(mine, 0, rr, i); }, [&](int i, bf16x8 v) { mma(sc[0], v, qf[i]); });
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) issue_k(j + step);
     if (j * 32 + 32 > all) hide(sc[0], j * 32, lim, lane >> 5);
@@ -663,7 +677,7 @@ __device__ __forceinline__ void narrow_unit(const Args& a, lds_char* mine, const
     f.take(sc, a.scale_log2e, pk);
     if (more) wait_vm<Lk::kLoads>(); else wait_vm<0>();          // V tile j
     const bf16x8 p[2] = {operand(pk[0], 0), operand(pk[0], 1)};
-    fed<D / 16, 4>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
+    fed<D / 16, 4, D == 128>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
                     [&](int i, bf16x8 v) { mma(f.o[i % (D / 32)], v, p[i / (D / 32)]); });
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) issue_v(j + step);
@@ -972,8 +986,11 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     lds_char* const vs = lds + (2 + (slot ^ 1)) * kTile;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      f32x16 sc = rows_product<D>(ks, b, rk, qf);
-      const f32x16 dp = rows_product<D>(vs, b, rv, df);
+      f32x16 sc, dp;
+      zero(sc);
+      zero(dp);
+      fed<D / 8, 2, D == 128>([&](int i) { return i & 1 ? row_operand<D>(vs, b, rv, i >> 1) : row_operand<D>(ks, b, rk, i >> 1); },
+                     [&](int i, bf16x8 v) { mma(i & 1 ? dp : sc, v, i & 1 ? df[i >> 1] : qf[i >> 1]); });
       if (j * kBKV + 32 * b + 32 > all) hide(sc, j * kBKV + 32 * b, lim, up);
       uint32_t pk[8];
 #pragma unroll
@@ -982,8 +999,9 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, -lse2));
         pk[e] = pack_bf16x2(p0 * (dp[2 * e] - delta), p1 * (dp[2 * e + 1] - delta));
       }
-      cols_product<D>(ks, 2 * b, ck, operand(pk, 0), acc);
-      cols_product<D>(ks, 2 * b + 1, ck, operand(pk, 1), acc);
+      const bf16x8 ds[2] = {operand(pk, 0), operand(pk, 1)};
+      fed<D / 16, 2, D == 128>([&](int i) { return col_operand<D>(ks, 2 * b + i / (D / 32), ck, i % (D / 32)); },
+                      [&](int i, bf16x8 v) { mma(acc[i % (D / 32)], v, ds[i / (D / 32)]); });
     }
   }
   if (up == 0 && w0 + lane < R) a.delta[stat] = delta;
@@ -1002,10 +1020,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
 // (W + 1) per), per = ceil(total / workgroups) but at least kLeast. A key tile that lies in one range is finished there, of
 // the others each workgroup leaves a part, in its slot 0 for the tile that its range begins in or with, in slot 1 for one that
 // begins later; dkv_join_kernel adds them up in order.
-#ifndef DL
-#define DL 16
-#endif
-constexpr int kLeast = DL;
+constexpr int kLeast = 8;       // 4 to 32 measured: short sequences wait for a range, long ones do not reach it
 
 struct KeyTile {
   Seq s;
@@ -1149,7 +1164,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
         struct Pair {
           bf16x8 a, b;
         };
-        fed<D / 8, 2>([&](int i) {
+        fed<D / 8, 2, D == 128>([&](int i) {
                         Pair p;
                         p.a = row_operand<D>(i < D / 16 ? qs : ds, 0, rr, i % (D / 16));
                         const int kk = i - D / 16;
@@ -1183,7 +1198,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
         const ColReads<D, kBoth> rc(ln);
         const bf16x8 po[2] = {operand(pp, 0), operand(pp, 1)}, so[2] = {operand(pd, 0), operand(pd, 1)};
         constexpr int kB = D / 32;                             // instruction i: 16 rows i / (2 kB), of dv, then dk, its block
-        fed<4 * kB, 2>([&](int i) { return col_operand<D>(i / kB % 2 ? qs : ds, i / (2 * kB), rc, i % kB); },
+        fed<4 * kB, 2, D == 128>([&](int i) { return col_operand<D>(i / kB % 2 ? qs : ds, i / (2 * kB), rc, i % kB); },
                        [&](int i, bf16x8 v) {
                          if (i / kB % 2) mma(dk[i % kB], v, so[i / (2 * kB)]);
                          else mma(dv[i % kB], v, po[i / (2 * kB)]);
