@@ -287,25 +287,42 @@ def gate(E, k, score=XS_SCORE_SOFTMAX, n_group=1, topk_group=1, group_score=XS_G
     return g
 
 
-def _placed(t):
-    """A [rows][heads][head_dim] tensor's row and head strides; head_dim is contiguous."""
-    if t.dim() != 3 or t.stride(2) != 1:
-        raise ValueError("a [rows][heads][head_dim] tensor with contiguous head_dim is wanted")
-    return t.stride(0), t.stride(1)
+def _placed(*tensors):
+    """Row and head strides of bf16 [rows][heads][head_dim] tensors of one device; head_dim is contiguous."""
+    import torch
+    out = []
+    for t in tensors:
+        if t.dim() != 3 or t.stride(2) != 1 or t.dtype != torch.bfloat16 or t.device != tensors[0].device:
+            raise ValueError("bf16 [rows][heads][head_dim] tensors with contiguous head_dim on one device are wanted")
+        out += t.stride()[:2]
+    return out
 
 
 def attn_packed(q, k, v, o, q_start, k_start, k_rows=None, lse=None, causal=True, max_k=0, scale=0.0) -> xs_attn_packed:
     """Descriptor of packed attention over [rows][heads][head_dim] tensors of any strides; keeps them alive."""
-    a = xs_attn_packed(q_start.numel() - 1, q.shape[1], k.shape[1], q.shape[2], q.shape[0], k.shape[0], int(causal), max_k, scale, 0,
-                       ptr(q_start), ptr(k_start), ptr(k_rows), ptr(q), ptr(k), ptr(v), ptr(o), ptr(lse),
-                       *_placed(q), *_placed(k), *_placed(v), *_placed(o))
+    import torch
+    placed = _placed(q, k, v, o)
+    n_seq = q_start.numel() - 1
+    if q.shape != o.shape or k.shape != v.shape or q.shape[2] != k.shape[2]:
+        raise ValueError("q and o, k and v have to be of one shape each, and of one head_dim")
+    for t, n in ((q_start, n_seq + 1), (k_start, n_seq + (k_rows is None)), (k_rows, n_seq)):
+        # (k_start may hold one more beside k_rows)
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < max(n, 1) or t.device != q.device):
+            raise ValueError("q_start [n_seq + 1], k_start and k_rows have to be contiguous int32 on q's device")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (q.shape[1], q.shape[0]) or not lse.is_contiguous() or lse.device != q.device):
+        raise ValueError("lse has to be contiguous fp32 [heads][rows of q] on q's device")
+    a = xs_attn_packed(n_seq, q.shape[1], k.shape[1], q.shape[2], q.shape[0], k.shape[0], int(causal), max_k, scale, 0,
+                       ptr(q_start), ptr(k_start), ptr(k_rows), ptr(q), ptr(k), ptr(v), ptr(o), ptr(lse), *placed)
     a._refs = (q, k, v, o, q_start, k_start, k_rows, lse)
     return a
 
 
 def attn_packed_grads(d_o, dq, dk, dv) -> xs_attn_grads:
     """The gradient tensors of packed attention, [rows][heads][head_dim] of any strides; keeps them alive."""
-    g = xs_attn_grads(ptr(d_o), ptr(dq), ptr(dk), ptr(dv), *_placed(d_o), *_placed(dq), *_placed(dk), *_placed(dv))
+    placed = _placed(d_o, dq, dk, dv)
+    if d_o.shape != dq.shape or dk.shape != dv.shape or dq.shape[2] != dk.shape[2]:
+        raise ValueError("d_o and dq, dk and dv have to be of one shape each, and of one head_dim")
+    g = xs_attn_grads(ptr(d_o), ptr(dq), ptr(dk), ptr(dv), *placed)
     g._refs = (d_o, dq, dk, dv)
     return g
 

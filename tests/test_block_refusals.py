@@ -134,9 +134,20 @@ def test_attention_gradients():
 def test_binding_refuses_other_layouts():
     import torch
     X = xs()
-    q = torch.zeros((4, 2, 128), dtype=torch.bfloat16)
-    i = torch.zeros(2, dtype=torch.int32)
-    with pytest.raises(ValueError):
-        X.attn_packed(q.transpose(1, 2), q, q, q, i, i)
-    with pytest.raises(ValueError):
-        X.attn_packed_grads(q[0], q, q, q)
+    t = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)
+    i32 = lambda n: t(n, dtype=torch.int32)
+    ok = dict(q=t(4, 2, 128), k=t(6, 1, 128), v=t(6, 1, 128), o=t(4, 2, 128), q_start=i32(3), k_start=i32(3))
+    a = X.attn_packed(**ok)
+    assert (a.n_seq, a.heads, a.kv_heads, a.Tq, a.Tk) == (2, 2, 1, 4, 6)
+    assert X.attn_packed(**{**ok, "k_start": i32(2)}, k_rows=i32(2)).n_seq == 2
+    for bad in (dict(q=t(4, 128, 2).transpose(1, 2)), dict(q=t(4, 2, 128, dtype=torch.float16)), dict(o=t(4, 2, 64)), dict(o=t(3, 2, 128)), dict(v=t(5, 1, 128)),
+                dict(v=t(6, 2, 128)), dict(k=t(6, 1, 64), v=t(6, 1, 64)), dict(q=t(4, 256)), dict(q_start=t(3, dtype=torch.int64)), dict(k_start=i32(2)),
+                dict(k_rows=i32(1)), dict(k_rows=i32(2), k_start=i32(1)), dict(q_start=i32(6)[::2]), dict(lse=t(4, 2, dtype=torch.float32)), dict(lse=t(2, 4)),
+                dict(v=torch.zeros((6, 1, 128), dtype=torch.bfloat16, device="meta"))):
+        with pytest.raises(ValueError):
+            X.attn_packed(**{**ok, **bad})
+    q, k = ok["q"], ok["k"]
+    X.attn_packed_grads(q, q, k, k)
+    for bad in ((q[0], q, k, k), (q, q[:3], k, k), (q, q, k, k[:5]), (q, q, k[..., :64], k[..., :64]), (q.float(), q, k, k)):
+        with pytest.raises(ValueError):
+            X.attn_packed_grads(*bad)

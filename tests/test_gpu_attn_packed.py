@@ -152,12 +152,15 @@ def test_many_rows(lens, H, Hkv, D, layout, causal):
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("new,H,Hkv", [(1, 8, 2), (1, 1, 1), (1, 32, 1), (2, 6, 2), (5, 8, 1), (17, 4, 2), (40, 3, 3), (50, 96, 32)])
-def test_new_tokens_over_a_cache(new, H, Hkv, D):
-    # keys behind each sequence's rows are NaN; lengths around the tiles' ends, fewer keys than queries, none
-    lens = [new, 0, 1, 31, 32, 33, 64, 95, 127, 129, 300, 1000]
-    cap = 1024
+@pytest.mark.parametrize("cap", [1024, 1700])
+def test_new_tokens_over_a_cache(new, H, Hkv, D, cap):
+    # keys behind each sequence's rows are NaN; lengths around the tiles' ends, fewer keys than queries, none. Caches of 1024 keys take one
+    # launch, in longer ones the keys are dealt out.
+    lens = [new, 0, 1, 31, 32, 33, 64, 95, 127, 129, 300, cap - 24]
     spans = [(1 + i * new, new, i * cap, m) for i, m in enumerate(lens)]
     c = Case(spans, 2 + new * len(lens), cap * len(lens), H, Hkv, D, cache=True, max_k=cap, seed=new)
+    many = (new * (H // Hkv) * len(lens) // 128 + len(lens)) * Hkv > 256
+    assert (c.ws.numel() > 0) == (cap > 1024 and not many)
     c.forward()
     c.check_forward()
 
@@ -178,7 +181,36 @@ def test_many_sequences():
         spans.append((at, q, ks, m))
         at += q
         ks += m + 5
-    c = Case(spans, at, ks, 4, 2, 128, cache=True, max_k=70)
+    for max_k in (70, 0):              # in one launch, and dealt out
+        c = Case(spans, at, ks, 4, 2, 128, cache=True, max_k=max_k)
+        assert (c.ws.numel() > 0) == (max_k == 0)
+        c.forward()
+        c.check_forward()
+
+
+def test_many_sequences_of_many_rows():
+    # more than 64 sequences over units of 128 rows, some without queries or keys, one long
+    n = 90
+    rng = np.random.default_rng(1)
+    spans, at, ks = [], 0, 0
+    for i in range(n):
+        q, m = (0 if i % 7 == 0 else int(rng.integers(1, 40))), (1500 if i == 70 else int(rng.integers(0, 90)))
+        spans.append((at, q, ks, m))
+        at += q
+        ks += m
+    for causal in (True, False):
+        c = Case(spans, at, ks, 2, 1, 64, cache=True, causal=causal, max_k=1500)
+        assert c.ws.numel() > 0
+        c.forward()
+        c.check_forward()
+
+
+@pytest.mark.parametrize("G", [3, 8, 48, 128, 130])
+def test_groups_of_any_size_over_long_sequences(G):
+    # units of as many queries as fit 128 rows; groups of more than 128 heads have none
+    spans = [(0, 130, 0, 1300), (130, 1, 1300, 64), (131, 70, 1364, 65)]
+    c = Case(spans, 201, 1429, G, 1, 64, cache=True)
+    assert (c.ws.numel() > 0) == (G <= 128)
     c.forward()
     c.check_forward()
 
@@ -309,7 +341,8 @@ def test_bad_sequences_have_no_gradients():
 
 def test_two_streams_and_replayed_graphs_with_workspaces_of_their_own():
     spans = [(i, 1, i * 700, 650 - 50 * i) for i in range(5)]
-    cases = [Case(spans, 5, 3500, 8, 2, 128, cache=True, max_k=700, seed=s) for s in range(2)]
+    cases = [Case(spans, 5, 3500, 8, 2, 128, cache=True, seed=s) for s in range(2)]
+    assert cases[0].ws.numel() > 0
     streams = [torch.cuda.Stream() for _ in cases]
     torch.cuda.synchronize()
     for c, st in zip(cases, streams):
@@ -359,16 +392,21 @@ def test_a_training_step_in_a_graph_and_equal_bits():
             assert torch.equal(t, w)
 
 
-def test_keys_past_2_gib_and_32_bit_offsets():
-    # one key head of a cache with rows 2^22 elements apart: 700 rows are 5.5 GiB
+@pytest.mark.parametrize("new,max_k", [(3, 0), (3, 1100), (60, 0), (60, 1100)])
+def test_keys_past_2_gib_and_32_bit_offsets(new, max_k):
+    # one key head of a cache with rows 2^22 elements apart: 700 rows are 5.5 GiB; all four forms
     m, D, row = 700, 128, 1 << 22
     big = torch.empty((m, row), dtype=torch.bfloat16, device="cuda")
     k, v = big[:, :D].unflatten(1, (1, D)), big[:, D:2 * D].unflatten(1, (1, D))
-    c = Case([(0, 3, 0, m)], 3, m, 4, 1, D, cache=True)
+    c = Case([(0, new, 0, m)], new, m, 4, 1, D, cache=True)
     k.copy_(c.k)
     v.copy_(c.v)
     X = xs()
     c.a = X.attn_packed(c.q, k, v, c.o, c.q_start, c.k_start, c.k_rows, c.lse)
+    if max_k:                              # Tk and max_k only choose the form: no row behind the 700 is read
+        c.a.Tk = c.a.max_k = max_k
+    c.ws = X.workspace(X.xs_attention_packed_workspace_bytes, c.a)
+    assert (c.ws.numel() > 0) == (max_k > 0)
     c.forward()
     c.check_forward()
 

@@ -47,7 +47,9 @@ def _weight(cols, kind, seed=9):
 
 
 SHAPES = [(1, 8), (5, 8), (3, 120), (4, 136), (7, 512), (6, 520), (5, 1024), (9, 1032), (3, 2048), (3, 2056), (2, 4096), (5, 4104), (3, 6144), (2, 6152),
-          (4, 7168), (3, 8192), (2, 8200), (2, 16384), (2, 16392), (1, 32768), (515, 256), (300, 3080)]
+          (4, 7168), (3, 8192), (2, 8200), (2, 16384), (2, 16392), (1, 32768), (515, 256), (300, 3080)] + [
+          # more rows than CUs: the forms of many rows, each width of theirs
+          (257, 1000), (263, 2040), (258, 6000), (257, 8192), (259, 16384), (258, 20000)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
