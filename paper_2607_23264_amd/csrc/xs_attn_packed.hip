@@ -399,17 +399,22 @@ __device__ __forceinline__ bool tile_of(const Args& a, Seq* s, int* kvh, int* ti
 
 // ------------------------------------------------------------------------------ many rows
 // The rows [r0, end) of a sequence and key head (128 at most, four waves of 32) over the key tiles [jb, je) of 64. LDS: two K
-// slots and one V slot. Per tile j: S from K slot j % 2, a barrier, K tile j + 2 into that slot; the softmax; V tile
-// j waited for and a barrier; O from the V slot; K tile j + 1 waited for, a barrier, V tile j + 1 into the V slot.
+// slots and one V slot. Per tile t: S from K slot t % 2, a barrier, K tile t + 2 into that slot; the softmax; V tile
+// t waited for and a barrier; O from the V slot; K tile t + 1 waited for, a barrier, V tile t + 1 into the V slot.
+//
+// NG = 2: eight waves, each four of them every second tile in slots of their own; join_groups adds the second's sums to the first's. A tile takes
+// a wave alone on its SIMD 1.9 us, with eight waves two of them take about 3.
 constexpr int kKeys = 64;      // of a tile
-template <int D, int AHEAD>
+template <int D, int AHEAD, int NG>
 __device__ __forceinline__ void rows_unit(const Args& a, lds_char* lds, const Seq& s, int kvh, int r0, int end, int jb, int je, Soft<D>& f) {
   constexpr int kTile = kKeys * Geo<D>::kRow, kLoads = Loader<D, kKeys, 4, kRows>::kLoads;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int whole = min(sees(a, r0, s.nq, s.nk) / kKeys, je);   // tiles that every row sees whole
-  const int r = min(r0 + 32 * w + (lane & 31), end - 1), lim = sees(a, r, s.nq, s.nk);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, first = jb + (wave >> 2);
+  const int n = (je - jb + NG - 1) / NG;                                           // tiles first + NG t; the second group's last may be tile je
+  const int whole = min(max((sees(a, r0, s.nq, s.nk) / kKeys - first + NG - 1) / NG, 0), NG == 1 ? n : (je - first + 1) / 2);   // those that every row sees whole
+  const int r = min(r0 + 32 * w + (lane & 31), end - 1), lim = NG == 1 ? sees(a, r, s.nq, s.nk) : min(sees(a, r, s.nq, s.nk), je * kKeys);
   const char* const kp = at(a.k, s.k0, kvh);
   const char* const vp = at(a.v, s.k0, kvh);
+  lds += (wave >> 2) * 3 * kTile;
   lds_char* const vs = lds + 2 * kTile;
   const Loader<D, kKeys, 4, kRows> lk(w, lane, a.k.row);
   const Loader<D, kKeys, 4, kCols> lv(w, lane, a.v.row);
@@ -417,53 +422,96 @@ __device__ __forceinline__ void rows_unit(const Args& a, lds_char* lds, const Se
   // in flight.
   const RowReads<D, kRows> rows(lane);
   const ColReads<D, kCols> cols(lane);
-  auto issue_k = [&](int j) { lk.issue(kp + static_cast<int64_t>(j) * kKeys * a.k.row, s.nk - j * kKeys, lds + (j & 1) * kTile, w); };
-  auto issue_v = [&](int j) { lv.issue(vp + static_cast<int64_t>(j) * kKeys * a.v.row, s.nk - j * kKeys, vs, w); };
+  auto issue_k = [&](int t) {
+    const int key = (first + NG * t) * kKeys;
+    lk.issue(kp + key * a.k.row, s.nk - key, lds + (t & 1) * kTile, w);
+  };
+  auto issue_v = [&](int t) {
+    const int key = (first + NG * t) * kKeys;
+    lv.issue(vp + key * a.v.row, s.nk - key, vs, w);
+  };
   bf16x8 qf[D / 16];
   f.clear();
-  if (jb < je) {
-    issue_k(jb);
-    issue_v(jb);
-    if (jb + 1 < je) issue_k(jb + 1);
+  if (n > 0) {
+    issue_k(0);
+    issue_v(0);
+    if (n > 1) issue_k(1);
     // behind the tiles: 32 rows' pieces are 32 cache lines an instruction
     load_frags<D>(row_at(a, a.q, s, kvh, r), qf);
     wait_vm<0>();
     asm volatile("s_barrier" ::: "memory");
   }
-  auto step = [&](int j, auto masked) {
-    lds_char* const ks = lds + (j & 1) * kTile;
+  auto step = [&](int t, auto masked) {
+    lds_char* const ks = lds + (t & 1) * kTile;
     const RowReads<D, kRows> rr = rows.fresh();
     f32x16 sc[2];
     zero(sc[0]);
     zero(sc[1]);
     fed<D / 8, AHEAD, D == 128>([&](int i) { return row_operand<D>(ks, i & 1, rr, i >> 1); }, [&](int i, bf16x8 v) { mma(sc[i & 1], v, qf[i >> 1]); });
-    // every wave is done with K slot j % 2: K tile j + 2 goes there
+    // every wave is done with K slot t % 2: K tile t + 2 goes there
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const bool k2 = j + 2 < je;
-    if (k2) issue_k(j + 2);
+    const bool k2 = t + 2 < n;
+    if (k2) issue_k(t + 2);
     if constexpr (masked) {
-      hide(sc[0], j * kKeys, lim, here(lane) >> 5);
-      hide(sc[1], j * kKeys + 32, lim, here(lane) >> 5);
+      const int key = (first + NG * t) * kKeys;
+      hide(sc[0], key, lim, here(lane) >> 5);
+      hide(sc[1], key + 32, lim, here(lane) >> 5);
     }
     uint32_t pk[2][8];
     f.take(sc, a.scale_log2e, pk);
-    // V tile j has landed in every wave's share (only K tile j + 2 may still be in flight)
+    // V tile t has landed in every wave's share (only K tile t + 2 may still be in flight)
     if (k2) wait_vm<kLoads>(); else wait_vm<0>();
     asm volatile("s_barrier" ::: "memory");
     const ColReads<D, kCols> rc = cols.fresh();
     const bf16x8 p[4] = {operand(pk[0], 0), operand(pk[0], 1), operand(pk[1], 0), operand(pk[1], 1)};
     fed<D / 8, AHEAD, D == 128>([&](int i) { return col_operand<D>(vs, i / (D / 32), rc, i % (D / 32)); },
-                      [&](int i, bf16x8 v) { mma(f.o[i % (D / 32)], v, p[i / (D / 32)]); });
-    if (j + 1 < je) {
-      // K tile j + 1 has landed in every wave's share, and no wave reads the V slot any more
+                                [&](int i, bf16x8 v) { mma(f.o[i % (D / 32)], v, p[i / (D / 32)]); });
+    if (t + 1 < n) {
+      // K tile t + 1 has landed in every wave's share, and no wave reads the V slot any more
       if (k2) wait_vm<kLoads>(); else wait_vm<0>();
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      issue_v(j + 1);
+      issue_v(t + 1);
     }
   };
-  int j = jb;
-  for (; j < whole; ++j) step(j, std::false_type());
-  for (; j < je; ++j) step(j, std::true_type());
+  // The groups are one barrier apart: one's softmax goes with the other's products.
+  if (NG == 2 && n > 0 && wave >= 4) asm volatile("s_barrier" ::: "memory");
+  int t = 0;
+  for (; t < whole; ++t) step(t, std::false_type());
+  for (; t < n; ++t) step(t, std::true_type());
+  if (NG == 2 && n > 0 && wave < 4) asm volatile("s_barrier" ::: "memory");
+}
+
+// The sums of waves 4 to 7 into those of waves 0 to 3, through LDS that nobody reads any more behind the barrier (4 D 128 bytes and 2048).
+template <int D>
+__device__ __forceinline__ void join_groups(lds_char* lds, Soft<D>& f) {
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+  typedef __attribute__((address_space(3))) f32x2_t lds_f32x2;
+  const int lane = here(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3;
+  lds_char* const o = lds + w * D * 128 + lane * 16;
+  lds_char* const ml = lds + 4 * D * 128 + (w * 64 + lane) * 8;
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  if (wave >= 4) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(lds_f32x4*)(o + (db * 4 + g) * 1024) = f32x4{f.o[db][4 * g], f.o[db][4 * g + 1], f.o[db][4 * g + 2], f.o[db][4 * g + 3]};
+    *(lds_f32x2*)ml = f32x2_t{f.m, f.l};
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  if (wave >= 4) return;
+  const f32x2_t other = *(const lds_f32x2*)ml;
+  const float m = fmaxf(f.m, other.x), was = __builtin_amdgcn_exp2f(f.m - m), is = __builtin_amdgcn_exp2f(other.x - m);
+  f.m = m;
+  f.l = __builtin_fmaf(other.y, is, f.l * was);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 v = *(const lds_f32x4*)(o + (db * 4 + g) * 1024);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f.o[db][4 * g + e] = __builtin_fmaf(v[e], is, f.o[db][4 * g + e] * was);
+    }
 }
 
 // 32 rows of a sequence and key head from r0 are done, those before `end` of them; `mine`: LDS of the wave's own for whole rows, or NULL.
@@ -501,18 +549,19 @@ __device__ __forceinline__ void leave_whole(const Args& a, int64_t slot, const S
   if (lane < 32) *reinterpret_cast<f32x2_t*>(a.part_ml + (slot * 128 + 32 * w + lane) * 2) = f32x2_t{f.m, f.l};
 }
 
-template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void rows_kernel(Args a) {
-  __shared__ __attribute__((aligned(16))) char lds[3 * kKeys * Geo<D>::kRow];
+template <int D, int NG>
+__global__ __launch_bounds__(256 * NG, NG == 2 ? (D == 128 ? 2 : 4) : (D == 128 ? 3 : 4)) void rows_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) char lds[NG * 3 * kKeys * Geo<D>::kRow];
   Seq s;
   int kvh, tile;
   if (!tile_of<128>(a, &s, &kvh, &tile)) return;
   const int R = s.nq * a.G, r0 = ((R + 127) / 128 - 1 - tile) * 128, end = min(r0 + 128, R);       // the longest rows first
   Soft<D> f;
-  rows_unit<D, 2>(a, (lds_char*)lds, s, kvh, r0, end, 0, (sees(a, end - 1, s.nq, s.nk) + kKeys - 1) / kKeys, f);
+  rows_unit<D, 2, NG>(a, (lds_char*)lds, s, kvh, r0, end, 0, (sees(a, end - 1, s.nq, s.nk) + kKeys - 1) / kKeys, f);
+  if constexpr (NG == 2) join_groups<D>((lds_char*)lds, f);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // no wave reads the K slots any more
-  if (r0 + 32 * w < end) finish<D>(a, s, kvh, r0 + 32 * w, end, f, (lds_char*)lds + w * 32 * Geo<D>::kRow);
+  // no wave reads the K slots any more, or what the others have left of this one's sums
+  if (w < 4 && r0 + 32 * w < end) finish<D>(a, s, kvh, r0 + 32 * w, end, f, (lds_char*)lds + w * (NG == 2 ? D * 128 : 32 * Geo<D>::kRow));
 }
 
 // ------------------------------------------------------------------------------ keys dealt out
@@ -630,10 +679,10 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Args a) {
     // the last unit's reads of these slots are done
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const int jb = (first + kKeys - 1) / kKeys, je = (min(last, sees(a, r_end - 1, s.nq, s.nk)) + kKeys - 1) / kKeys;
-    rows_unit<D, 4>(a, (lds_char*)lds, s, kvh, r0, r_end, jb, je, f);
-    const int rw = r0 + 32 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    rows_unit<D, 4, 1>(a, (lds_char*)lds, s, kvh, r0, r_end, jb, je, f);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (first != 0 || last != b1 - b0) leave_whole<D>(a, W * 2 + (u > begin), f, jb < je);
-    else if (rw < r_end) finish<D>(a, s, kvh, rw, r_end, f, (lds_char*)lds + (rw - r0) * Geo<D>::kRow);
+    else if (r0 + 32 * w < r_end) finish<D>(a, s, kvh, r0 + 32 * w, r_end, f, (lds_char*)lds + w * 32 * Geo<D>::kRow);
     u += last - first;
   }
 }
@@ -911,18 +960,19 @@ __global__ __launch_bounds__(512, 2) void short_kernel(Args a) {
 // rounding gives where a row sees many keys, and the larger part where it sees ten. Tiles that see at most
 // kExactTiles tiles of keys therefore take delta = sum_j P_ij (do_i . v_j) in a pass before.
 constexpr int kExactTiles = 4;
-template <int D>
-__global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
+template <int D, int NG>
+__global__ __launch_bounds__(256 * NG, 2) void dq_kernel(Args a) {
   using G = Geo<D>;
   constexpr int kBKV = 64, kTile = kBKV * G::kRow;
-  __shared__ __attribute__((aligned(16))) char lds_raw[4 * kTile];
-  lds_char* const lds = (lds_char*)lds_raw;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), up = lane >> 5;
+  __shared__ __attribute__((aligned(16))) char lds_raw[NG * 4 * kTile];
+  __shared__ float deltas[NG][128];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, group = wave >> 2, up = lane >> 5;
+  lds_char* const lds = (lds_char*)lds_raw + group * 4 * kTile;
   Seq s;
   int kvh, tile;
   if (!tile_of<128>(a, &s, &kvh, &tile)) return;
   const int nq = s.nq, nk = s.nk, R = nq * a.G, r0 = ((R + 127) / 128 - 1 - tile) * 128, end = min(r0 + 128, R);
-  const int nkv = (sees(a, end - 1, nq, nk) + kBKV - 1) / kBKV;
+  const int nkv = (sees(a, end - 1, nq, nk) + kBKV - 1) / kBKV, n = (nkv + NG - 1) / NG;      // the group's tiles are group + NG t
   const int w0 = r0 + 32 * w;
   const int all = w0 < R ? sees(a, w0, nq, nk) : 0, any = w0 < R ? sees(a, min(w0 + 31, R - 1), nq, nk) : 0;
   const int r = min(w0 + (lane & 31), R - 1), qi = query_of(a, r), h = kvh * a.G + (r - qi * a.G), lim = sees(a, r, nq, nk);
@@ -933,37 +983,45 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   const Loader<D, kBKV, 4, kRows> lv(w, lane, a.v.row);
   const char* const kp = at(a.k, s.k0, kvh);
   const char* const vp = at(a.v, s.k0, kvh);
-  auto issue = [&](int j, int slot) {
-    lk.issue(kp + static_cast<int64_t>(j) * kBKV * a.k.row, nk - j * kBKV, lds + slot * kTile, w);
-    lv.issue(vp + static_cast<int64_t>(j) * kBKV * a.v.row, nk - j * kBKV, lds + (2 + slot) * kTile, w);
+  auto issue = [&](int t, int slot) {
+    const int key = (group + NG * t) * kBKV;
+    lk.issue(kp + key * a.k.row, nk - key, lds + slot * kTile, w);
+    lv.issue(vp + key * a.v.row, nk - key, lds + (2 + slot) * kTile, w);
   };
-  if (nkv > 0) issue(0, 0);
+  if (n > 0) issue(0, 0);
   bf16x8 qf[D / 16], df[D / 16];
   load_frags<D>(at(a.q, s.q0 + qi, h), qf);
   load_frags<D>(at(a.d_o, s.q0 + qi, h), df);
   const int64_t stat = static_cast<int64_t>(h) * a.Tq + s.q0 + qi;
   const float lse2 = lim > 0 ? a.lse[stat] * kLog2e : 0.f;
   int slot = 0;
-  // tile j has landed in every wave's share, and no wave reads the tile before it any more; then `next` is loaded
+  // a tile has landed in every wave's share, and no wave reads the tile before it any more; then `next` is loaded
   auto turn = [&](int next) {
     wait_vm<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     slot ^= 1;
-    if (next < nkv) issue(next, slot);
+    if (next < n) issue(next, slot);
   };
   float delta = 0.f;
   if (nkv <= kExactTiles) {
-    for (int j = 0; j < nkv; ++j) {
-      turn(j + 1 < nkv ? j + 1 : 0);
+    for (int t = 0; t < n; ++t) {
+      turn(t + 1 < n ? t + 1 : 0);
+      const int key = (group + NG * t) * kBKV;
 #pragma unroll 1
-      for (int b = 0; b < 2 && j * kBKV + 32 * b < any; ++b) {
+      for (int b = 0; b < 2 && key + 32 * b < any; ++b) {
         f32x16 sc = rows_product<D>(lds + (slot ^ 1) * kTile, b, rk, qf);
         const f32x16 dp = rows_product<D>(lds + (2 + (slot ^ 1)) * kTile, b, rv, df);
-        hide(sc, j * kBKV + 32 * b, lim, up);
+        hide(sc, key + 32 * b, lim, up);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           delta = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], a.scale_log2e, -lse2)), dp[e], delta);
       }
+    }
+    delta = add_halves(delta);
+    if constexpr (NG == 2) {
+      if (up == 0) deltas[group][32 * w + lane] = delta;
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      delta = deltas[0][32 * w + (lane & 31)] + deltas[1][32 * w + (lane & 31)];
     }
   } else {
     bf16x8 of[D / 16];
@@ -972,16 +1030,17 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(static_cast<float>(df[kk][e]), static_cast<float>(of[kk][e]), delta);
+    delta = add_halves(delta);
   }
-  delta = add_halves(delta);
   f32x16 acc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
-  for (int j = 0; j < nkv; ++j) {
-    turn(j + 1);
-    if (j * kBKV >= any) continue;                           // wave-uniform
+  for (int t = 0; t < n; ++t) {
+    turn(t + 1);
+    const int key = (group + NG * t) * kBKV;
+    if (key >= any) continue;                                // wave-uniform
     lds_char* const ks = lds + (slot ^ 1) * kTile;
     lds_char* const vs = lds + (2 + (slot ^ 1)) * kTile;
 #pragma unroll
@@ -991,7 +1050,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       zero(dp);
       fed<D / 8, 2, D == 128>([&](int i) { return i & 1 ? row_operand<D>(vs, b, rv, i >> 1) : row_operand<D>(ks, b, rk, i >> 1); },
                      [&](int i, bf16x8 v) { mma(i & 1 ? dp : sc, v, i & 1 ? df[i >> 1] : qf[i >> 1]); });
-      if (j * kBKV + 32 * b + 32 > all) hide(sc, j * kBKV + 32 * b, lim, up);
+      if (key + 32 * b + 32 > all) hide(sc, key + 32 * b, lim, up);
       uint32_t pk[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -1004,9 +1063,29 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
                       [&](int i, bf16x8 v) { mma(acc[i % (D / 32)], v, ds[i / (D / 32)]); });
     }
   }
-  if (up == 0 && w0 + lane < R) a.delta[stat] = delta;
+  if (group == 0 && up == 0 && w0 + lane < R) a.delta[stat] = delta;
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // no wave reads the tiles any more
-  if (w0 < end) store_rows<D>(lds + w * 32 * G::kRow, acc, a.scale, [&](int i) { return w0 + i < end ? row_at(a, a.dq, s, kvh, w0 + i) : nullptr; });
+  lds_char* const mine = (lds_char*)lds_raw + w * D * 128;
+  if constexpr (NG == 2) {
+    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+    if (group)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *(lds_f32x4*)(mine + ((db * 4 + g) * 64 + lane) * 16) = f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (group) return;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 v = *(const lds_f32x4*)(mine + ((db * 4 + g) * 64 + lane) * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[db][4 * g + e] += v[e];
+      }
+  }
+  if (w0 < end) store_rows<D>(mine, acc, a.scale, [&](int i) { return w0 + i < end ? row_at(a, a.dq, s, kvh, w0 + i) : nullptr; });
 }
 
 // dk and dv: a workgroup holds 32 NW keys of a key head (NW waves of 32), their K and V fragments beside both
@@ -1349,18 +1428,22 @@ int check(const xs_attn_packed* A, pattn::Args* a) {
   return XS_OK;
 }
 
+// How many keys a long sequence has, as far as the host knows: a prompt's about twice their average, a cache is taken to be full.
+int64_t long_keys(const pattn::Args& a) { return a.k_rows ? a.max_k : std::min<int64_t>(a.max_k, 2 * int64_t(a.Tk) / a.n_seq); }
+int64_t row_tiles(const pattn::Args& a) { return packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv; }
+// Eight waves a tile of rows where the tiles are few and long (one prompt of 1000 tokens, 8 heads: rows 25.6 -> 21.5 us, dq 28.9 -> 25.6;
+// 5500 tokens in three, heads of 64: 51 -> 39, 54 -> 41; short ones lose: twenty of 200, 12 -> 16; as do many: 3000 tokens, 32 heads, 86 -> 103).
+bool pairs(const pattn::Args& a) { return long_keys(a) > 768 && 2 * row_tiles(a) <= 3 * int64_t(xs_host::num_cus()); }
+
 // Which kernels a forward call takes, from what the host knows.
 enum class Form { kRows, kWide, kNarrow, kShort };
 Form form_of(const pattn::Args& a) {
-  const int64_t tiles = packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv;
   // Few rows a sequence: one launch up to 1024 keys (8 units of 1024 keys 9.6 us, in two 11.4 and the time between; 256 22.0 and 29.8; of 2048
   // keys 13.3 and 11.7).
   if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq) return a.max_k <= 1024 ? Form::kShort : Form::kNarrow;
-  // A prompt's sequences are about as long as twice their average, a cache is taken to be full. Tiles that leave CUs without one take their keys
-  // dealt out if they are long (8 heads of one prompt, 1000 tokens: 26.3 us by rows, 25.9 and a launch dealt out; 2000: 46.7 and
-  // 36.3; 4000: 88 and 66; 32 heads, 2000: 54.5 and 73).
-  const int64_t keys = a.k_rows ? a.max_k : std::min<int64_t>(a.max_k, 2 * int64_t(a.Tk) / a.n_seq);
-  return keys <= 1024 || tiles > xs_host::num_cus() || a.G > 128 ? Form::kRows : Form::kWide;
+  // Tiles that leave CUs without one take their keys dealt out if they are long (8 heads of one prompt, 1000 tokens: 21.5 us by rows, 25.9 and a
+  // launch dealt out; 2000: 46.7 and 35.5; 4000: 88 and 64; 32 heads, 2000: 54.5 and 73).
+  return long_keys(a) <= 1024 || row_tiles(a) > xs_host::num_cus() || a.G > 128 ? Form::kRows : Form::kWide;
 }
 
 // Ranges of a call whose keys are dealt out: two workgroups a CU, of narrow units each wave's.
@@ -1375,7 +1458,8 @@ template <int D>
 int forward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
   const Form f = form_of(a);
   if (f == Form::kRows) {
-    hipLaunchKernelGGL((pattn::rows_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv), dim3(256), 0, st, a);
+    if (pairs(a)) hipLaunchKernelGGL((pattn::rows_kernel<D, 2>), xs_host::grid_of(row_tiles(a)), dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((pattn::rows_kernel<D, 1>), xs_host::grid_of(row_tiles(a)), dim3(256), 0, st, a);
     return xs_host::launch_status();
   }
   if (f == Form::kShort) {
@@ -1431,7 +1515,8 @@ int backward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
   a.delta = static_cast<float*>(ws);
   a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + delta_bytes(a));
   if (a.Tq) {
-    hipLaunchKernelGGL((pattn::dq_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv), dim3(256), 0, st, a);
+    if (pairs(a)) hipLaunchKernelGGL((pattn::dq_kernel<D, 2>), xs_host::grid_of(row_tiles(a)), dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((pattn::dq_kernel<D, 1>), xs_host::grid_of(row_tiles(a)), dim3(256), 0, st, a);
     if (xs_host::launch_status()) return XS_EHIP;
   }
   const int ranges = dkv_ranges<D>(a);

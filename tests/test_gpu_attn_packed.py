@@ -228,7 +228,7 @@ def test_gradients_of_more_keys_than_queries_and_fewer():
 
 
 # 512 keys and more a sequence take key tiles of 256; 70, 3 and 1 heads leave tiles inside one workgroup's share and over several
-@pytest.mark.parametrize("lens,H,Hkv", [([1025], 4, 1), ([511, 1, 1030], 6, 2), ([700, 900], 70, 35), ([513], 1, 1)])
+@pytest.mark.parametrize("lens,H,Hkv", [([1025], 4, 1), ([511, 1, 1030], 6, 2), ([700, 900], 70, 35), ([513], 1, 1), ([900], 6, 2), ([521, 503], 3, 3)])
 @pytest.mark.parametrize("D,layout", [(128, "token"), (64, "room")])
 @pytest.mark.parametrize("causal", [True, False])
 def test_long_sequences(lens, H, Hkv, D, layout, causal):
