@@ -53,7 +53,7 @@ struct Args {
   int shift;             // log2 G, or -1
   float scale, scale_log2e;
   float* lse;            // [H][Tq]
-  float* delta;          // [H][Tq] (gradients)
+  float *delta, *lse2;   // [H][Tq] (gradients): do . o, lse in powers of two
   float* part_o;         // [waves][2][32][D] (split); dkv_kernel's parts
   float* part_ml;        // [waves][2][32][2]
   int32_t* status;
@@ -1063,7 +1063,10 @@ __global__ __launch_bounds__(256 * NG, 2) void dq_kernel(Args a) {
                       [&](int i, bf16x8 v) { mma(acc[i % (D / 32)], v, ds[i / (D / 32)]); });
     }
   }
-  if (group == 0 && up == 0 && w0 + lane < R) a.delta[stat] = delta;
+  if (group == 0 && up == 0 && w0 + lane < R) {
+    a.delta[stat] = delta;
+    a.lse2[stat] = lse2;
+  }
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // no wave reads the tiles any more
   lds_char* const mine = (lds_char*)lds_raw + w * D * 128;
   if constexpr (NG == 2) {
@@ -1181,6 +1184,8 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
   lds_char* const lds = (lds_char*)lds_raw;
   lds_char* const stats = lds + 2 * kStages * kTile;                           // lse and delta of each stage
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const RowReads<D, kBoth> rows(lane);
+  const ColReads<D, kBoth> cols(lane);
   lds_char* const stash = stats + 2 * kStages * kBQ * 4 + w * kStash * 1024;
   const int64_t total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), quot(total + gridDim.x - 1, gridDim.x));
   const int64_t W = range_of_block(blockIdx.x, gridDim.x, quot(total + per - 1, per)), begin = W * per, end = min(begin + per, total);
@@ -1199,7 +1204,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
       lq.issue(at(a.q, x.s.q0 + lt, h), nq - lt, lds + 2 * lst * kTile, w);
       ld.issue(at(a.d_o, x.s.q0 + lt, h), nq - lt, lds + (2 * lst + 1) * kTile, w);
       if (w < 2) {                                             // the lower half's lanes fetch the 32 rows' numbers
-        const float* const src = (w ? a.delta : a.lse) + static_cast<int64_t>(h) * a.Tq + x.s.q0 + lt;
+        const float* const src = (w ? a.delta : a.lse2) + static_cast<int64_t>(h) * a.Tq + x.s.q0 + lt;
         if ((here(lane) & 32) == 0) load_lds4(buffer_rsrc(src, min(nq - lt, kBQ) * 4), here(lane) * 4, stats + (2 * lst + w) * kBQ * 4);
       }
       lt += kBQ;
@@ -1236,7 +1241,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
         lds_char* const qs = lds + 2 * st * kTile;
         lds_char* const ds = qs + kTile;
         const int ln = here(lane);
-        const RowReads<D, kBoth> rr(ln);
+        const RowReads<D, kBoth> rr = rows.fresh();
         f32x16 sc, dp;
         zero(sc);
         zero(dp);
@@ -1266,7 +1271,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
           float p[4], d[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * g + e], a.scale_log2e, -ls[e] * kLog2e));
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * g + e], a.scale_log2e, -ls[e]));
             d[e] = p[e] * (dp[4 * g + e] - de[e]);
           }
           pp[2 * g] = pack_bf16x2(p[0], p[1]);
@@ -1274,7 +1279,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
           pd[2 * g] = pack_bf16x2(d[0], d[1]);
           pd[2 * g + 1] = pack_bf16x2(d[2], d[3]);
         }
-        const ColReads<D, kBoth> rc(ln);
+        const ColReads<D, kBoth> rc = cols.fresh();
         const bf16x8 po[2] = {operand(pp, 0), operand(pp, 1)}, so[2] = {operand(pd, 0), operand(pd, 1)};
         constexpr int kB = D / 32;                             // instruction i: 16 rows i / (2 kB), of dv, then dk, its block
         fed<4 * kB, 2, D == 128>([&](int i) { return col_operand<D>(i / kB % 2 ? qs : ds, i / (2 * kB), rc, i % kB); },
@@ -1496,9 +1501,10 @@ int dkv_ranges(const pattn::Args& a) {
   const int64_t most = (key_tiles_bound<D>(a) * a.G * (a.Tq / 32 + 1) + pattn::kLeast - 1) / pattn::kLeast;
   return static_cast<int>(std::min<int64_t>(most, (D == 128 ? 8 : 12) / dkv_waves<D>(a) * int64_t(xs_host::num_cus())));
 }
-int64_t delta_bytes(const pattn::Args& a) { return (static_cast<int64_t>(a.H) * a.Tq * 4 + 255) / 256 * 256; }
+// delta and lse of every row
+int64_t stats_bytes(const pattn::Args& a) { return (static_cast<int64_t>(a.H) * a.Tq * 8 + 255) / 256 * 256; }
 template <int D>
-int64_t grad_bytes(const pattn::Args& a) { return delta_bytes(a) + dkv_ranges<D>(a) * int64_t(2 * 2 * 32 * D * 4) * dkv_waves<D>(a); }
+int64_t grad_bytes(const pattn::Args& a) { return stats_bytes(a) + dkv_ranges<D>(a) * int64_t(2 * 2 * 32 * D * 4) * dkv_waves<D>(a); }
 
 template <int D, int NW>
 int dkv(const pattn::Args& a, int ranges, hipStream_t st) {
@@ -1513,7 +1519,8 @@ int backward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
   const int64_t need = grad_bytes<D>(a);
   if (need && (!ws || !aligned16(ws) || bytes < need)) return XS_EWORKSPACE;
   a.delta = static_cast<float*>(ws);
-  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + delta_bytes(a));
+  a.lse2 = a.delta + static_cast<int64_t>(a.H) * a.Tq;
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + stats_bytes(a));
   if (a.Tq) {
     if (pairs(a)) hipLaunchKernelGGL((pattn::dq_kernel<D, 2>), xs_host::grid_of(row_tiles(a)), dim3(512), 0, st, a);
     else hipLaunchKernelGGL((pattn::dq_kernel<D, 1>), xs_host::grid_of(row_tiles(a)), dim3(256), 0, st, a);
