@@ -1186,6 +1186,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const RowReads<D, kBoth> rows(lane);
   const ColReads<D, kBoth> cols(lane);
+  const Loader<D, kBQ, NW, kBoth> lq(w, lane, a.q.row), ld(w, lane, a.d_o.row);
   lds_char* const stash = stats + 2 * kStages * kBQ * 4 + w * kStash * 1024;
   const int64_t total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), quot(total + gridDim.x - 1, gridDim.x));
   const int64_t W = range_of_block(blockIdx.x, gridDim.x, quot(total + per - 1, per)), begin = W * per, end = min(begin + per, total);
@@ -1196,21 +1197,26 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
     const int nq = x.s.nq, nk = x.s.nk, key0 = x.tile * 32 * NW, kw = key0 + 32 * w, off = nk - nq;
     const int first = a.causal ? max(0, key0 - off) : 0;       // the first query that sees one of these keys
     // the next block to load: its head in the group, first query and stage
-    int lg = static_cast<int>(x.first / x.per_head), lt = first + static_cast<int>(x.first - static_cast<int64_t>(lg) * x.per_head) * kBQ, lst = 0;
+    const int lg = static_cast<int>(quot(x.first, x.per_head));
+    int lt = first + static_cast<int>(x.first - static_cast<int64_t>(lg) * x.per_head) * kBQ, lst = 0;
     int t = lt, st = 0;
+    const char *pq = at(a.q, x.s.q0 + lt, x.kvh * a.G + lg), *pd = at(a.d_o, x.s.q0 + lt, x.kvh * a.G + lg);
+    const float* ps = (w ? a.delta : a.lse2) + static_cast<int64_t>(x.kvh * a.G + lg) * a.Tq + x.s.q0 + lt;
     auto issue = [&] {
-      const int h = x.kvh * a.G + lg;
-      const Loader<D, kBQ, NW, kBoth> lq(w, here(lane), a.q.row), ld(w, here(lane), a.d_o.row);
-      lq.issue(at(a.q, x.s.q0 + lt, h), nq - lt, lds + 2 * lst * kTile, w);
-      ld.issue(at(a.d_o, x.s.q0 + lt, h), nq - lt, lds + (2 * lst + 1) * kTile, w);
-      if (w < 2) {                                             // the lower half's lanes fetch the 32 rows' numbers
-        const float* const src = (w ? a.delta : a.lse2) + static_cast<int64_t>(h) * a.Tq + x.s.q0 + lt;
-        if ((here(lane) & 32) == 0) load_lds4(buffer_rsrc(src, min(nq - lt, kBQ) * 4), here(lane) * 4, stats + (2 * lst + w) * kBQ * 4);
-      }
+      lq.issue(pq, nq - lt, lds + 2 * lst * kTile, w);
+      ld.issue(pd, nq - lt, lds + (2 * lst + 1) * kTile, w);
+      // waves 0 and 1: the lower half's lanes fetch the 32 rows' numbers
+      if (w < 2 && (here(lane) & 32) == 0) load_lds4(buffer_rsrc(ps, min(nq - lt, kBQ) * 4), here(lane) * 4, stats + (2 * lst + w) * kBQ * 4);
       lt += kBQ;
-      if (lt >= nq) {
+      if (lt < nq) {
+        pq += kBQ * a.q.row;
+        pd += kBQ * a.d_o.row;
+        ps += kBQ;
+      } else {                                                 // the next head's first query
+        pq += a.q.head - (lt - kBQ - first) * a.q.row;
+        pd += a.d_o.head - (lt - kBQ - first) * a.d_o.row;
+        ps += a.Tq - (lt - kBQ - first);
         lt = first;
-        ++lg;
       }
       lst = lst + 1 == kStages ? 0 : lst + 1;
     };
