@@ -1452,9 +1452,11 @@ Form form_of(const pattn::Args& a) {
   // Few rows a sequence: one launch up to 1024 keys (8 units of 1024 keys 9.6 us, in two 11.4 and the time between; 256 22.0 and 29.8; of 2048
   // keys 13.3 and 11.7).
   if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq) return a.max_k <= 1024 ? Form::kShort : Form::kNarrow;
-  // Tiles that leave CUs without one take their keys dealt out if they are long (8 heads of one prompt, 1000 tokens: 21.5 us by rows, 25.9 and a
-  // launch dealt out; 2000: 46.7 and 35.5; 4000: 88 and 64; 32 heads, 2000: 54.5 and 73).
-  return long_keys(a) <= 1024 || row_tiles(a) > xs_host::num_cus() || a.G > 128 ? Form::kRows : Form::kWide;
+  // Where the tiles of rows are too few for their length the keys are dealt out too. One prompt, us by rows and dealt out (two launches): 8 heads of 1100
+  // tokens 23.1 and 25.8, 2000: 35.7 and 35.5, 4000: 65.5 and 64.3, 8000: 184 and 164, 16384: 509 and 598; one head of 5000: 83 and 32; 16 heads of 2000: 39 and
+  // 47, 4000: 95 and 101; 7 chunks of 61 tokens, 32 heads, caches of 1100: 23.8 and 32.6.
+  const int64_t tiles = row_tiles(a), cus = xs_host::num_cus(), keys = long_keys(a);
+  return keys <= 1024 || tiles > 2 * cus || tiles * 4000 > cus * keys || a.G > 128 ? Form::kRows : Form::kWide;
 }
 
 // Ranges of a call whose keys are dealt out: two workgroups a CU, of narrow units each wave's.
