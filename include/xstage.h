@@ -607,16 +607,18 @@ int xs_ulysses_copy(const void* o, int32_t heads, int32_t M, int32_t head_dim,
  *   Tq, Tk   rows of q and o, of k and v
  *   max_k    the most keys of a sequence (0: Tk)
  *   scale    0 = 1 / sqrt(head_dim)
- *   workspace  device, 16-byte aligned, xs_attention_packed_workspace_bytes() bytes (0 for calls with many rows)
+ *   workspace  device, 16-byte aligned, xs_attention_packed_workspace_bytes() bytes (0 for calls with many rows and for short
+ *            caches: NULL then)
  * A sequence whose queries do not lie in [0, Tq), whose keys do not lie in [0, Tk) or are more than max_k sets
  * XS_EBADINPUT in dev_status and is skipped. Rows of o and lse outside every sequence are not written, keys and values
  * outside every sequence (also behind k_rows) are not read. A sequence's keys and values have to be finite: a query
  * may take 0 times one that causality hides from it.
  * Scores, softmax and sums are fp32; probabilities are rounded to bf16 for the second product. How keys are
  * split over workgroups follows from the lengths, the descriptor and the device's CU count alone.
- * Requires head_dim 64 or 128, row strides of at most 2^23 elements, Tq heads / kv_heads < 2^30, Tk <= 2^30 (else XS_EUNSUPPORTED), heads a multiple of
- * kv_heads, strides multiples of 8 and at least head_dim, 16-byte aligned pointers, n_seq in [1, 65536], max_k <= Tk,
- * reserved 0 (else XS_EINVAL); nothing is launched on an error. */
+ * Requires head_dim 64 or 128, row strides of at most 2^23 elements, heads <= 65536, Tq heads / kv_heads < 2^30, Tq heads < 2^34, Tk <= 2^30, Tk kv_heads <
+ * 2^38 (else XS_EUNSUPPORTED), heads a multiple of kv_heads, strides multiples of 8 and at least head_dim, 16-byte aligned pointers, n_seq in
+ * [1, 65536], max_k <= Tk, reserved 0 (else XS_EINVAL); nothing is launched on an error. Calls that may run at the same time, replayed graphs
+ * among them, need a workspace each. */
 typedef struct xs_attn_packed {
   int32_t n_seq, heads, kv_heads, head_dim;
   int32_t Tq, Tk;

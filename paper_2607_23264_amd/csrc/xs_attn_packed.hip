@@ -14,6 +14,10 @@
 // read), and a result in registers becomes the next product's B operand with two half swaps for
 // 16 keys or rows.
 //
+// Forward, four forms (form_of chooses): rows_kernel, a workgroup 128 rows over all keys that they see; wide_kernel, the same with the
+// keys dealt out evenly where such tiles do not fill the chip; narrow_kernel, a few rows a sequence, each wave its share of all keys; short_kernel,
+// a few rows over short caches in one launch. Gradients: dq_kernel by rows, dkv_kernel by keys, each recomputing P.
+//
 // LDS tiles are rows of 2 D bytes in pieces of 16; row r keeps its piece p at p ^ swz(r). A read by rows takes one
 // piece of 16 consecutive rows at a time, a read by columns four pieces of four consecutive rows; swz
 // spreads a tile's reads over all banks, also where the gradients read one tile both ways.
@@ -568,7 +572,7 @@ __global__ __launch_bounds__(256 * NG, NG == 2 ? (D == 128 ? 2 : 4) : (D == 128 
 // Where the rows alone do not fill the chip their keys are dealt out too: all work is laid end to end, as units of rows
 // of one key head times the keys these see, and cut into ranges of the same length, wherever units begin and
 // end. A unit that lies in one range is finished there; of the others each range leaves a part: in its slot 0 of
-// the unit that it begins in or with, in slot 1 of one that begins later. the join adds them in order.
+// the unit that it begins in or with, in slot 1 of one that begins later. A second launch adds them in order.
 //
 // Wide units, for sequences of many rows: as many queries as make 128 rows at most, in keys, behind them kStart keys for
 // what a unit takes besides its tiles (chunks of 61 tokens over 7 caches, some of them short: 45 us without). A workgroup a range: it takes the

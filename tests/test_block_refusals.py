@@ -93,7 +93,8 @@ BAD = [dict(n_seq=0), dict(n_seq=65537), dict(heads=0), dict(kv_heads=0), dict(k
        dict(max_k=129), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(reserved=1), dict(q_start=None), dict(k_start=None), dict(q=None),
        dict(k=None), dict(v=None), dict(o=None), dict(q=A + 8), dict(k=A + 2), dict(v=A + 8), dict(o=A + 4), dict(q_row=120), dict(q_row=1028), dict(q_head=64),
        dict(k_row=100), dict(k_head=0), dict(k_head=132), dict(v_row=0), dict(v_head=120), dict(o_row=-1024), dict(o_head=1 << 40)]
-UNSUPPORTED = [dict(head_dim=96, q_head=128), dict(head_dim=32), dict(q_row=(1 << 23) + 8), dict(k_row=1 << 24), dict(Tq=1 << 28), dict(Tk=(1 << 30) + 1)]
+UNSUPPORTED = [dict(head_dim=96, q_head=128), dict(head_dim=32), dict(q_row=(1 << 23) + 8), dict(k_row=1 << 24), dict(Tq=1 << 28), dict(Tk=(1 << 30) + 1),
+               dict(heads=1 << 17, kv_heads=1 << 17), dict(heads=1 << 16, kv_heads=1 << 16, Tq=1 << 18), dict(heads=1 << 16, kv_heads=1 << 16, Tk=1 << 22)]
 
 
 @pytest.mark.parametrize("kw,code", [(b, "XS_EINVAL") for b in BAD] + [(u, "XS_EUNSUPPORTED") for u in UNSUPPORTED])
