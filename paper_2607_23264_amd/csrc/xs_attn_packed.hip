@@ -55,6 +55,7 @@ struct Args {
   const int32_t *q_start, *k_start, *k_rows;
   int n_seq, H, Hkv, G, Tq, Tk, causal, max_k;
   int shift;             // log2 G, or -1
+  int cus;
   float scale, scale_log2e;
   float* lse;            // [H][Tq]
   float *delta, *lse2;   // [H][Tq] (gradients): do . o, lse in powers of two
@@ -1103,10 +1104,15 @@ __global__ __launch_bounds__(256 * NG, 2) void dq_kernel(Args a) {
 // The first keys of a sequence have G times as many rows as it has queries, the last ones hardly any, and there are few key
 // heads: key tiles dealt one to a workgroup leave the chip waiting for the longest (8192 tokens in 4 sequences, 32 heads
 // over 8: 904 us). So the blocks of all key tiles, laid end to end, are dealt out evenly: workgroup W takes the blocks [W per,
-// (W + 1) per), per = ceil(total / workgroups) but at least kLeast. A key tile that lies in one range is finished there, of
+// (W + 1) per). A key tile that lies in one range is finished there, of
 // the others each workgroup leaves a part, in its slot 0 for the tile that its range begins in or with, in slot 1 for one that
 // begins later; dkv_join_kernel adds them up in order.
-constexpr int kLeast = 8;       // 4 to 32 measured: short sequences wait for a range, long ones do not reach it
+constexpr int kLeast = 4;
+// Blocks of a range: all dealt out over n workgroups, but 8 at least (with fewer the parts take longer than the ranges are shorter), or as many as
+// give every CU one, 4 at least (two documents of 300 and 200 tokens, 4 heads: 8 blocks 27.6 us, 4 18.4; 32: 78).
+__device__ __forceinline__ int64_t range_length(const Args& a, int64_t total, int64_t n) {
+  return max(min(max(quot(total + a.cus - 1, a.cus), static_cast<int64_t>(kLeast)), static_cast<int64_t>(8)), quot(total + n - 1, n));
+}
 
 struct KeyTile {
   Seq s;
@@ -1192,7 +1198,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
   const ColReads<D, kBoth> cols(lane);
   const Loader<D, kBQ, NW, kBoth> lq(w, lane, a.q.row), ld(w, lane, a.d_o.row);
   lds_char* const stash = stats + 2 * kStages * kBQ * 4 + w * kStash * 1024;
-  const int64_t total = all_blocks<NW>(a), per = max(static_cast<int64_t>(kLeast), quot(total + gridDim.x - 1, gridDim.x));
+  const int64_t total = all_blocks<NW>(a), per = range_length(a, total, gridDim.x);
   const int64_t W = range_of_block(blockIdx.x, gridDim.x, quot(total + per - 1, per)), begin = W * per, end = min(begin + per, total);
   for (int64_t u = begin; u < end;) {
     KeyTile x;
@@ -1349,7 +1355,7 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
     total += lane64(n_upto, 63);
   }
   if (!found) return;
-  const int64_t per = max(static_cast<int64_t>(kLeast), quot(total + n_ranges - 1, n_ranges));
+  const int64_t per = range_length(a, total, n_ranges);
   b0 = blocks_before<NW>(a, s, t);
   const int64_t head = blocks + kvh * blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.G;
   const int64_t u0 = head + b0 * a.G, u1 = head + blocks_before<NW>(a, s, t + 1) * a.G, w0 = quot(u0, per), w1 = quot(u1 - 1, per);
@@ -1433,6 +1439,7 @@ int check(const xs_attn_packed* A, pattn::Args* a) {
   a->Hkv = A->kv_heads;
   a->G = A->heads / A->kv_heads;
   a->shift = a->G & (a->G - 1) ? -1 : __builtin_ctz(a->G);
+  a->cus = xs_host::num_cus();
   a->Tq = A->Tq;
   a->Tk = A->Tk;
   a->causal = A->causal != 0;
