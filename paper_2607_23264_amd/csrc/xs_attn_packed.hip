@@ -1107,17 +1107,19 @@ __global__ __launch_bounds__(256 * NG, 2) void dq_kernel(Args a) {
 // (W + 1) per). A key tile that lies in one range is finished there, of
 // the others each workgroup leaves a part, in its slot 0 for the tile that its range begins in or with, in slot 1 for one that
 // begins later; dkv_join_kernel adds them up in order.
-constexpr int kLeast = 4;
-// Blocks of a range: all dealt out over n workgroups, but 8 at least (with fewer the parts take longer than the ranges are shorter), or as many as
-// give every CU one, 4 at least (two documents of 300 and 200 tokens, 4 heads: 8 blocks 27.6 us, 4 18.4; 32: 78).
+constexpr int kTileStart = 3;    // what a key tile takes besides its blocks, in blocks: its length is theirs and these, which come first
+constexpr int kLeast = 5;
+// Length of a range: all dealt out over n workgroups, but kLeast + 4 at least (with less the parts take longer than the ranges are shorter), or as
+// much as gives every CU one, kLeast at least (two documents of 300 and 200 tokens, 4 heads: 32 blocks 78 us, 8 27.6, 4 18; one of 17
+// tokens: a tile each of 4 key heads in one range 20.5, in four 8).
 __device__ __forceinline__ int64_t range_length(const Args& a, int64_t total, int64_t n) {
-  return max(min(max(quot(total + a.cus - 1, a.cus), static_cast<int64_t>(kLeast)), static_cast<int64_t>(8)), quot(total + n - 1, n));
+  return max(min(max(quot(total + a.cus - 1, a.cus), static_cast<int64_t>(kLeast)), static_cast<int64_t>(kLeast + 4)), quot(total + n - 1, n));
 }
 
 struct KeyTile {
   Seq s;
   int kvh, tile, per_head;      // key tile; blocks of 32 queries that see it
-  int64_t first, blocks;        // the block searched for, of the tile's
+  int64_t place, blocks;        // the place searched for in the tile; its blocks of all heads of the group, behind kTileStart
 };
 
 // Blocks of one query head in a sequence's tiles of 32 NW keys before tile j: those whose first key every query sees have all
@@ -1142,43 +1144,45 @@ __device__ __forceinline__ Seq key_seq(const Args& a, int s) {
 }
 template <int NW>
 __device__ __forceinline__ int key_tiles(const Seq& s) { return (s.nk + 32 * NW - 1) / (32 * NW); }
+// Length of a key head's tiles before tile j: their blocks of all heads of the group, and kTileStart for each.
 template <int NW>
-__device__ __forceinline__ int64_t blocks_of(const Args& a, const Seq& s) { return blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.H; }
+__device__ __forceinline__ int64_t length_before(const Args& a, const Seq& s, int64_t j) { return blocks_before<NW>(a, s, j) * a.G + j * kTileStart; }
+template <int NW>
+__device__ __forceinline__ int64_t length_of(const Args& a, const Seq& s) { return length_before<NW>(a, s, key_tiles<NW>(s)) * a.Hkv; }
 
 template <int NW>
-__device__ __forceinline__ int64_t all_blocks(const Args& a) {
+__device__ __forceinline__ int64_t whole_length(const Args& a) {
   int64_t total = 0;
-  for (int s0 = 0; s0 < a.n_seq; s0 += 64) total += lane64(wave_scan(blocks_of<NW>(a, key_seq(a, s0 + (threadIdx.x & 63)))), 63);
+  for (int s0 = 0; s0 < a.n_seq; s0 += 64) total += lane64(wave_scan(length_of<NW>(a, key_seq(a, s0 + (threadIdx.x & 63)))), 63);
   return total;
 }
 
 
-// The key tile that block u of all lies in; u is less than their number.
+// The key tile that place u of all lies in; u is less than the whole length.
 template <int NW>
 __device__ __forceinline__ void key_tile_at(const Args& a, int64_t u, KeyTile* out) {
   int64_t before = 0;
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
     const Seq mine = key_seq(a, s0 + (threadIdx.x & 63));
-    const int64_t n = blocks_of<NW>(a, mine), upto = wave_scan(n);
+    const int64_t n = length_of<NW>(a, mine), upto = wave_scan(n);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(before + upto > u);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       out->s = lane_seq(mine, l);
       const int tiles = key_tiles<NW>(out->s);
-      const int64_t head = blocks_before<NW>(a, out->s, tiles) * a.G, in = u - before - lane64(upto - n, l);
+      const int64_t head = length_before<NW>(a, out->s, tiles), in = u - before - lane64(upto - n, l);
       out->kvh = static_cast<int>(quot(in, head));
       const int64_t x = in - out->kvh * head;
-      int lo = 0, hi = tiles - 1;                               // the tile with before(tile) G <= x < before(tile + 1) G
+      int lo = 0, hi = tiles - 1;                               // the tile with before(tile) <= x < before(tile + 1)
       while (lo < hi) {
         const int mid = (lo + hi) / 2;
-        if (blocks_before<NW>(a, out->s, mid + 1) * a.G > x) hi = mid;
+        if (length_before<NW>(a, out->s, mid + 1) > x) hi = mid;
         else lo = mid + 1;
       }
-      const int64_t b0 = blocks_before<NW>(a, out->s, lo);
       out->tile = lo;
-      out->per_head = static_cast<int>(blocks_before<NW>(a, out->s, lo + 1) - b0);
+      out->per_head = static_cast<int>(blocks_before<NW>(a, out->s, lo + 1) - blocks_before<NW>(a, out->s, lo));
       out->blocks = static_cast<int64_t>(out->per_head) * a.G;
-      out->first = x - b0 * a.G;
+      out->place = x - length_before<NW>(a, out->s, lo);
       return;
     }
     before += lane64(upto, 63);
@@ -1198,17 +1202,22 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
   const ColReads<D, kBoth> cols(lane);
   const Loader<D, kBQ, NW, kBoth> lq(w, lane, a.q.row), ld(w, lane, a.d_o.row);
   lds_char* const stash = stats + 2 * kStages * kBQ * 4 + w * kStash * 1024;
-  const int64_t total = all_blocks<NW>(a), per = range_length(a, total, gridDim.x);
+  const int64_t total = whole_length<NW>(a), per = range_length(a, total, gridDim.x);
   const int64_t W = range_of_block(blockIdx.x, gridDim.x, quot(total + per - 1, per)), begin = W * per, end = min(begin + per, total);
   for (int64_t u = begin; u < end;) {
     KeyTile x;
     key_tile_at<NW>(a, u, &x);
-    const int n = static_cast<int>(min(x.blocks - x.first, end - u));
+    const int64_t from = max(x.place - kTileStart, static_cast<int64_t>(0)), step = min(x.blocks + kTileStart - x.place, end - u);
+    const int n = static_cast<int>(x.place + step - kTileStart - from);       // blocks [from, from + n) of the tile
+    if (n <= 0) {
+      u += step;
+      continue;
+    }
     const int nq = x.s.nq, nk = x.s.nk, key0 = x.tile * 32 * NW, kw = key0 + 32 * w, off = nk - nq;
     const int first = a.causal ? max(0, key0 - off) : 0;       // the first query that sees one of these keys
     // the next block to load: its head in the group, first query and stage
-    const int lg = static_cast<int>(quot(x.first, x.per_head));
-    int lt = first + static_cast<int>(x.first - static_cast<int64_t>(lg) * x.per_head) * kBQ, lst = 0;
+    const int lg = static_cast<int>(quot(from, x.per_head));
+    int lt = first + static_cast<int>(from - static_cast<int64_t>(lg) * x.per_head) * kBQ, lst = 0;
     int t = lt, st = 0;
     const char *pq = at(a.q, x.s.q0 + lt, x.kvh * a.G + lg), *pd = at(a.d_o, x.s.q0 + lt, x.kvh * a.G + lg);
     const float* ps = (w ? a.delta : a.lse2) + static_cast<int64_t>(x.kvh * a.G + lg) * a.Tq + x.s.q0 + lt;
@@ -1323,7 +1332,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 8 / NW : 12 / NW) void dkv_kern
           part[(D / 8 + db * 4 + g) * 64] = f32x4{dv[db][4 * g], dv[db][4 * g + 1], dv[db][4 * g + 2], dv[db][4 * g + 3]};
         }
     }
-    u += n;
+    u += step;
   }
 }
 
@@ -1336,12 +1345,12 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
   const int piece = static_cast<int>(id % kPieces), w = piece / (D / 32), db = piece % (D / 32);
   const int64_t number = quot(id / kPieces, a.Hkv);
   const int kvh = static_cast<int>(id / kPieces - number * a.Hkv);
-  int64_t t = number, blocks = 0, total = 0, b0 = 0;
+  int64_t t = number, blocks = 0, total = 0;
   Seq s{0, 0, 0, 0};
   bool found = false;
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
     const Seq mine = key_seq(a, s0 + lane);
-    const int64_t tiles = key_tiles<NW>(mine), upto = wave_scan(tiles), n = blocks_of<NW>(a, mine), n_upto = wave_scan(n);
+    const int64_t tiles = key_tiles<NW>(mine), upto = wave_scan(tiles), n = length_of<NW>(a, mine), n_upto = wave_scan(n);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > t);
     if (!found && hit) {
       const int l = __builtin_ctzll(hit);
@@ -1356,15 +1365,15 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
   }
   if (!found) return;
   const int64_t per = range_length(a, total, n_ranges);
-  b0 = blocks_before<NW>(a, s, t);
-  const int64_t head = blocks + kvh * blocks_before<NW>(a, s, key_tiles<NW>(s)) * a.G;
-  const int64_t u0 = head + b0 * a.G, u1 = head + blocks_before<NW>(a, s, t + 1) * a.G, w0 = quot(u0, per), w1 = quot(u1 - 1, per);
-  if (w0 == w1) return;                               // finished by its workgroup
+  const int64_t u0 = blocks + kvh * length_before<NW>(a, s, key_tiles<NW>(s)) + length_before<NW>(a, s, t);
+  const int64_t u1 = u0 + length_before<NW>(a, s, t + 1) - length_before<NW>(a, s, t);
+  const int64_t w0 = quot(u0, per), w_first = quot(u0 + kTileStart, per), w1 = quot(u1 - 1, per);     // the first with blocks of it: w_first
+  if (w_first == w1) return;                          // finished by its workgroup
   f32x4 dk[4], dv[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) dk[g] = dv[g] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 2
-  for (int64_t W = w0; W <= w1; ++W) {
+  for (int64_t W = w_first; W <= w1; ++W) {
     const f32x4* const part = reinterpret_cast<const f32x4*>(a.part_o) + ((W * 2 + (W == w0 && u0 > w0 * per)) * NW + w) * (D * 16) + db * 256 + lane;
     f32x4 k4[4], v4[4];
 #pragma unroll
@@ -1514,10 +1523,10 @@ template <int D>
 int dkv_waves(const pattn::Args& a) { return D == 128 && a.Tk / a.n_seq >= 512 ? 8 : 4; }
 template <int D>
 int64_t key_tiles_bound(const pattn::Args& a) { return packed_tiles_bound(a.Tk, a.n_seq, 1, 32 * dkv_waves<D>(a)) * a.Hkv; }
-// Its workgroups: as many as the chip holds, fewer where there cannot be kLeast blocks for each.
+// Its workgroups: as many as the chip holds, fewer where the shortest ranges need fewer.
 template <int D>
 int dkv_ranges(const pattn::Args& a) {
-  const int64_t most = (key_tiles_bound<D>(a) * a.G * (a.Tq / 32 + 1) + pattn::kLeast - 1) / pattn::kLeast;
+  const int64_t most = (key_tiles_bound<D>(a) * (static_cast<int64_t>(a.G) * (a.Tq / 32 + 1) + pattn::kTileStart) + pattn::kLeast - 1) / pattn::kLeast;
   return static_cast<int>(std::min<int64_t>(most, (D == 128 ? 8 : 12) / dkv_waves<D>(a) * int64_t(xs_host::num_cus())));
 }
 // delta and lse of every row
