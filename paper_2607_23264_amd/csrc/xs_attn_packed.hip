@@ -407,8 +407,13 @@ __device__ __forceinline__ bool tile_of(const Args& a, Seq* s, int* kvh, int* ti
 // slots and one V slot. Per tile t: S from K slot t % 2, a barrier, K tile t + 2 into that slot; the softmax; V tile
 // t waited for and a barrier; O from the V slot; K tile t + 1 waited for, a barrier, V tile t + 1 into the V slot.
 //
-// NG = 2: eight waves, each four of them every second tile in slots of their own; join_groups adds the second's sums to the first's. A tile takes
-// a wave alone on its SIMD 1.9 us, with eight waves two of them take about 3.
+// Measured: 16384 tokens, 8 heads of 128: 497 us, 1105 TFLOP/s; 16381 in 12 prompts, 32 heads over 8: 443 us, 1058. Three waves share a SIMD; matrix units are busy
+// 59% of cycles at the 1.75 GHz that the power limit leaves, vector units 61% (exp takes 40% of that), LDS 30%: no unit is full, what is missing is
+// overlap within a SIMD (a library's plain product of 8192^3 runs at 1430 TFLOP/s here). 168 registers hold three waves without spills only
+// with addresses made anew in the loop.
+//
+// NG = 2: eight waves, each four of them every second tile in slots of their own; join_groups adds the second's sums to the first's: for few long tiles,
+// where a wave is alone on its SIMD (one prompt of 2000 tokens, 8 heads: 46.7 -> 35.7 us).
 constexpr int kKeys = 64;      // of a tile
 template <int D, int AHEAD, int NG>
 __device__ __forceinline__ void rows_unit(const Args& a, lds_char* lds, const Seq& s, int kvh, int r0, int end, int jb, int je, Soft<D>& f) {
@@ -577,7 +582,8 @@ __global__ __launch_bounds__(256 * NG, NG == 2 ? (D == 128 ? 2 : 4) : (D == 128 
 //
 // Wide units, for sequences of many rows: as many queries as make 128 rows at most, in keys, behind them kStart keys for
 // what a unit takes besides its tiles (chunks of 61 tokens over 7 caches, some of them short: 45 us without). A workgroup a range: it takes the
-// tiles of 64 keys that begin in it.
+// tiles of 64 keys that begin in it. Measured: those chunks, 32 heads over 8, 7900 keys: 23 to 24 us, 10 of them a workgroup's start and end, and 10 to join; the
+// parts are 28 MB written and read, as much as the caches.
 struct Wide {
   static constexpr int kStart = 256;
   static constexpr int kLeast = 384;          // of a range (256 to 768 measured: the parts against the ranges)
@@ -598,7 +604,8 @@ struct Wide {
 };
 
 // Narrow units, for a few rows: 32 of them, in tiles of 32 keys, a wave a range. Up to four key heads are side by side: waves of
-// one workgroup take the same tiles of theirs, which lie side by side in memory too where a token's heads do.
+// one workgroup take the same tiles of theirs, which lie side by side in memory too where a token's heads do. Bound by memory: 32 requests, 39,400
+// keys of 8 heads, 162 MB: 31 to 35 us, 4.6 to 5.3 TB/s (a large copy: 4.9), and 6.5 to join.
 struct Narrow {
   static constexpr int kRows = 32;
   static constexpr int kLeast = 2;             // tiles of a range (1 to 8 measured: with 1 the join takes longer than the ranges)
@@ -814,7 +821,7 @@ __global__ __launch_bounds__(256) void join_wide_kernel(Args a, int64_t ranges) 
   f32x4 o[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) o[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
+#pragma unroll 4
   for (int64_t x = w0; x <= w1; ++x) {
     const int64_t slot = x * 2 + (x == w0 && u0 > w0 * per);
     const f32x4* const from = reinterpret_cast<const f32x4*>(a.part_o) + ((slot * 4 + w) * (D / 32) + db) * 256 + lane;
@@ -909,7 +916,8 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges
   store_joined(a, s, kvh, r, col, o, top, sum);
 }
 
-// Short caches: a workgroup a narrow unit, its eight waves each an eighth of the key tiles, added up in LDS: no second launch.
+// Short caches: a workgroup a narrow unit, its eight waves each an eighth of the key tiles, added up in LDS: no second launch. One request's next token
+// over 80 keys: 4 us, a chain of dependent loads (starts, keys, result); 1024 keys 9.6.
 template <int D>
 __global__ __launch_bounds__(512, 2) void short_kernel(Args a) {
   constexpr int kMine = 2 * 32 * Geo<D>::kRow;                  // a wave's slots: also 32 rows of D sums
@@ -957,8 +965,9 @@ __global__ __launch_bounds__(512, 2) void short_kernel(Args a) {
 }
 
 // ------------------------------------------------------------------------------ gradients
-// dq: as rows_kernel, with a second product (V times the row's do) and dS in place of the probabilities. It
-// computes delta for its rows and leaves it for the kernel below.
+// dq: as rows_kernel, with a second product (V times the row's do) and dS in place of the probabilities, K and V tiles in two slots each, one
+// barrier a tile. It computes delta for its rows and leaves it, and lse in powers of two, for the kernel below. 8192 tokens in 4 documents, 32 heads over 8: 285 to
+// 301 us, 1010 to 1060 TFLOP/s; matrix units busy 55% of cycles at 1.8 GHz, vector units 43%.
 //
 // delta = do . o takes o's roundings (of the probabilities and of o itself) to every dS of the row alike, a
 // relative error of dq and dk of about 0.0023 / sqrt(keys that share the weight): nothing beside the 0.0017 that dS's own
@@ -1100,6 +1109,10 @@ __global__ __launch_bounds__(256 * NG, 2) void dq_kernel(Args a) {
 // results' accumulators in registers, and streams the rows that see them, 32 queries of one head at a time with do,
 // lse and delta, two blocks ahead in three LDS slots. Two waves share a SIMD's registers: kStash of V's fragments lie in
 // LDS. Queries past the end of the sequence are zeros with lse 0: P = 1, but do = 0 and dS = 1 (0 - 0).
+//
+// The same 8192 tokens: 395 to 417 us, 970 to 1020 TFLOP/s, and 28 to join (60 to 130 MB of parts). Matrix units are busy 48% of cycles, vector units 36%, LDS 34%: both waves of
+// a SIMD wait at the same barrier. One wave a SIMD with all its registers, a block's products between the next one's softmax: 684 us, some 630 instructions a
+// block at five cycles each; the softmax put between this kernel's own products: 495 us against 447 then.
 //
 // The first keys of a sequence have G times as many rows as it has queries, the last ones hardly any, and there are few key
 // heads: key tiles dealt one to a workgroup leave the chip waiting for the longest (8192 tokens in 4 sequences, 32 heads
@@ -1372,22 +1385,28 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
   f32x4 dk[4], dv[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) dk[g] = dv[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-  for (int64_t W = w_first; W <= w1; ++W) {
-    const f32x4* const part = reinterpret_cast<const f32x4*>(a.part_o) + ((W * 2 + (W == w0 && u0 > w0 * per)) * NW + w) * (D * 16) + db * 256 + lane;
-    f32x4 k4[4], v4[4];
+  for (int64_t W = w_first; W <= w1; W += 4) {         // four parts on their way at once
+    f32x4 k4[4][4], v4[4][4];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      k4[g] = part[g * 64];
-      v4[g] = part[D * 8 + g * 64];
+    for (int q = 0; q < 4; ++q) {
+      const int64_t x = min(W + q, w1);
+      const f32x4* const part = reinterpret_cast<const f32x4*>(a.part_o) + ((x * 2 + (x == w0 && u0 > w0 * per)) * NW + w) * (D * 16) + db * 256 + lane;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        k4[q][g] = part[g * 64];
+        v4[q][g] = part[D * 8 + g * 64];
+      }
     }
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
+    for (int q = 0; q < 4; ++q)
+      if (W + q <= w1)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        dk[g][e] += k4[g][e];
-        dv[g][e] += v4[g][e];
-      }
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            dk[g][e] += k4[q][g][e];
+            dv[g][e] += v4[q][g][e];
+          }
   }
   const int key = static_cast<int>(t) * 32 * NW + 32 * w + (lane & 31), kc = min(key, s.nk - 1);
   const auto pack = [](const f32x4& v, float c) { return u32x2{pack_bf16x2(v[0] * c, v[1] * c), pack_bf16x2(v[2] * c, v[3] * c)}; };
