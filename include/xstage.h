@@ -147,7 +147,7 @@ int xs_route_gate_backward(const xs_gate* g, const void* logits, int64_t ld, int
  *   loss        device fp32 [n_seq] out: alpha sum_e f_se P_se with f_se = E counts_se / (k T_s), alpha for a balanced
  *               router; 0 for an empty sequence
  * Of g, E, k, score and logits_type are read. logits [T][E] rows ld elements apart, topk_idx device int32 [T][k]
- * (of xs_route_gate). workspace: device, 16-byte aligned, xs_balance_loss_workspace_bytes() bytes. Starts that are not in
+ * (of xs_route_gate); with T = 0 they may be NULL. workspace: device, 16-byte aligned, xs_balance_loss_workspace_bytes() bytes. Starts that are not in
  * [0, T] or descend set XS_EBADINPUT; such sequences count as empty, and with sequences that overlap for it the outputs
  * are not specified. Sums are fp32, their order follows from the lengths and the device's CU count alone. Requires E <=
  * 1024, 1 <= k <= min(E, 32), 1 <= n_seq <= 65536, a finite alpha: otherwise XS_EINVAL and nothing is launched. */
@@ -609,6 +609,7 @@ int xs_ulysses_copy(const void* o, int32_t heads, int32_t M, int32_t head_dim,
  *   scale    0 = 1 / sqrt(head_dim)
  *   workspace  device, 16-byte aligned, xs_attention_packed_workspace_bytes() bytes (0 for calls with many rows and for short
  *            caches: NULL then)
+ * Tensors without rows (Tq or Tk 0) may be NULL.
  * A sequence whose queries do not lie in [0, Tq), whose keys do not lie in [0, Tk) or are more than max_k sets
  * XS_EBADINPUT in dev_status and is skipped. Rows of o and lse outside every sequence are not written, keys and values
  * outside every sequence (also behind k_rows) are not read. A sequence's keys and values have to be finite: a query
@@ -778,7 +779,7 @@ int xs_swiglu_fp8_backward(const void* ck_codes, int64_t ld_ck, const float* ck_
  *   h            bf16 [rows][cols] or NULL; x or residual itself (with its row distance) or apart from both
  *   y            bf16 [rows][cols] or NULL; as h, and not h
  *   codes, scales  y in E4M3 with 1 x 128 blocks, laid out as by xs_quantize_fp8 (from y's fp32 values, not from the
- *                bf16 ones), or both NULL. One of y and codes is wanted.
+ *                bf16 ones), or both NULL. One of y and codes is wanted. With no rows all of them may be NULL.
  * h is rounded first and the rest is fp32, rounded once. Every matrix has 16-byte aligned rows; eps >= 0 (a
  * row of zeros under eps = 0 gives NaN). cols a multiple of 8, at most 32768, rows below 2^31, else XS_EUNSUPPORTED; XS_EINVAL
  * on other bad arguments; nothing is launched on an error. */

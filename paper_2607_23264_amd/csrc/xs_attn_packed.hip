@@ -1433,9 +1433,9 @@ namespace {
 
 bool aligned16(const void* p) { return !(reinterpret_cast<uintptr_t>(p) & 15); }
 
-// A tensor of `heads` heads of D values, strides in elements.
-int lies(const void* p, int64_t row, int64_t head, int heads, int D) {
-  if (!p || !aligned16(p) || row < D || row % 8 || (heads > 1 && (head < D || head % 8 || head >= (int64_t(1) << 40)))) return XS_EINVAL;
+// A tensor of `heads` heads of D values, strides in elements; it may be NULL if it has no rows.
+int lies(const void* p, int64_t row, int64_t head, int heads, int D, int rows) {
+  if ((!p && rows) || !aligned16(p) || row < D || row % 8 || (heads > 1 && (head < D || head % 8 || head >= (int64_t(1) << 40)))) return XS_EINVAL;
   return row > (1 << 23) ? XS_EUNSUPPORTED : XS_OK;
 }
 
@@ -1447,9 +1447,9 @@ int check(const xs_attn_packed* A, pattn::Args* a) {
       !A->q_start || !A->k_start)
     return XS_EINVAL;
   const int D = A->head_dim;
-  int rc = lies(A->q, A->q_row, A->q_head, A->heads, D);
-  for (const int r : {lies(A->k, A->k_row, A->k_head, A->kv_heads, D), lies(A->v, A->v_row, A->v_head, A->kv_heads, D),
-                      lies(A->o, A->o_row, A->o_head, A->heads, D)})
+  int rc = lies(A->q, A->q_row, A->q_head, A->heads, D, A->Tq);
+  for (const int r : {lies(A->k, A->k_row, A->k_head, A->kv_heads, D, A->Tk), lies(A->v, A->v_row, A->v_head, A->kv_heads, D, A->Tk),
+                      lies(A->o, A->o_row, A->o_head, A->heads, D, A->Tq)})
     if (rc != XS_EINVAL && r) rc = r;
   if (rc == XS_EINVAL) return rc;
   if (rc || (D != 64 && D != 128) || static_cast<int64_t>(A->Tq) * (A->heads / A->kv_heads) >= (1 << 30) || A->Tk > (1 << 30) || A->heads > (1 << 16) ||
@@ -1611,11 +1611,11 @@ extern "C" int xs_attention_packed_backward(const xs_attn_packed* A, const xs_at
                                             int32_t* dev_status, void* stream) {
   pattn::Args a{};
   if (int rc = check(A, &a)) return rc;
-  if (!g || !a.lse) return XS_EINVAL;
+  if (!g || (!a.lse && a.Tq)) return XS_EINVAL;
   const int D = A->head_dim;
   bool unsupported = a.k_rows != nullptr;
-  for (const int r : {lies(g->d_o, g->do_row, g->do_head, a.H, D), lies(g->dq, g->dq_row, g->dq_head, a.H, D),
-                      lies(g->dk, g->dk_row, g->dk_head, a.Hkv, D), lies(g->dv, g->dv_row, g->dv_head, a.Hkv, D)}) {
+  for (const int r : {lies(g->d_o, g->do_row, g->do_head, a.H, D, a.Tq), lies(g->dq, g->dq_row, g->dq_head, a.H, D, a.Tq),
+                      lies(g->dk, g->dk_row, g->dk_head, a.Hkv, D, a.Tk), lies(g->dv, g->dv_row, g->dv_head, a.Hkv, D, a.Tk)}) {
     if (r == XS_EINVAL) return r;
     unsupported |= r != XS_OK;
   }

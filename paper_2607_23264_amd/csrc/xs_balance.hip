@@ -358,7 +358,7 @@ int64_t tiles_of(int32_t T, int32_t n_seq, int chunk) {
 int64_t workspace_of(int32_t T, int32_t E, int32_t n_seq) { return tiles_of(T, n_seq, chunk_of(T)) * width_of(E) * 8 + int64_t(n_seq) * 17 * 4; }
 
 int balance_ok(const xs_gate* g, const void* logits, int64_t ld, int32_t T, const int32_t* start, int32_t n_seq, float alpha) {
-  if (!g || !logits || g->E < 1 || g->E > 1024 || g->k < 1 || g->k > g->E || g->k > 32 || g->reserved != 0) return XS_EINVAL;
+  if (!g || (!logits && T) || g->E < 1 || g->E > 1024 || g->k < 1 || g->k > g->E || g->k > 32 || g->reserved != 0) return XS_EINVAL;
   if (g->score != XS_SCORE_SOFTMAX && g->score != XS_SCORE_SIGMOID) return XS_EINVAL;
   if (g->logits_type != XS_TYPE_BF16 && g->logits_type != XS_TYPE_F32) return XS_EINVAL;
   if (T < 0 || ld < g->E || ld > (int64_t(1) << 40) || !std::isfinite(alpha)) return XS_EINVAL;
@@ -399,7 +399,7 @@ extern "C" int xs_balance_loss(const xs_gate* g, const void* logits, int64_t ld,
                                const int32_t* seq_start, int32_t n_seq, float alpha, int32_t* counts, float* mean_share, float* loss,
                                void* workspace, int64_t workspace_bytes, int32_t* dev_status, void* stream) {
   if (int rc = balance_ok(g, logits, ld, T, seq_start, n_seq, alpha)) return rc;
-  if (!topk_idx || !counts || !mean_share || !loss) return XS_EINVAL;
+  if ((!topk_idx && T) || !counts || !mean_share || !loss) return XS_EINVAL;
   const int64_t tiles = tiles_of(T, n_seq, chunk_of(T));
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15) || workspace_bytes < workspace_of(T, g->E, n_seq)) return XS_EWORKSPACE;
   balance::Args a{logits, ld, topk_idx, seq_start, T, g->E, g->k, n_seq, g->score == XS_SCORE_SIGMOID, chunk_of(T), static_cast<int>(tiles), alpha,
@@ -427,9 +427,9 @@ extern "C" int xs_balance_loss_backward(const xs_gate* g, const void* logits, in
   const auto lies = [=](const void* p, int64_t l) {
     return l >= g->E && l <= (int64_t(1) << 40) && !(reinterpret_cast<uintptr_t>(p) & (size - 1));
   };
-  if (!counts || !d_loss || !d_logits || !lies(d_logits, ld_d) || (d_add && !lies(d_add, ld_add))) return XS_EINVAL;
-  if ((d_logits == logits && ld_d != ld) || (d_logits == d_add && ld_d != ld_add)) return XS_EINVAL;
+  if (!counts || !d_loss || (!d_logits && T) || !lies(d_logits, ld_d) || (d_add && !lies(d_add, ld_add))) return XS_EINVAL;
   if (T == 0) return XS_OK;
+  if ((d_logits == logits && ld_d != ld) || (d_logits == d_add && ld_d != ld_add)) return XS_EINVAL;
   const balance::GradArgs a{logits, ld, seq_start, T, g->E, g->k, n_seq, g->score == XS_SCORE_SIGMOID, chunk_of(T, 4), alpha, counts,
                             d_loss, d_add, ld_add, d_logits, ld_d, dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -286,8 +286,8 @@ using namespace xs;
 
 namespace {
 
-bool lies_at(const void* p, int64_t ld, int32_t cols) {     // a bf16 matrix of 16-byte pieces
-  return p && !(reinterpret_cast<uintptr_t>(p) & 15) && ld >= cols && ld % 8 == 0 && ld < (int64_t(1) << 40);
+bool lies_at(const void* p, int64_t ld, int32_t cols, int64_t rows) {     // a bf16 matrix of 16-byte pieces; NULL if it has no rows
+  return (p || rows == 0) && !(reinterpret_cast<uintptr_t>(p) & 15) && ld >= cols && ld % 8 == 0 && ld < (int64_t(1) << 40);
 }
 
 int norm_ok(const void* w, int32_t wt, float eps, int64_t rows, int32_t cols) {
@@ -343,8 +343,8 @@ extern "C" int xs_rmsnorm(const void* x, int64_t ldx, const void* residual, int6
                           int32_t weight_type, float eps, int64_t rows, int32_t cols, void* h, int64_t ld_h, void* y,
                           int64_t ld_y, void* codes, int64_t ld_codes, float* scales, int64_t ld_scales, void* stream) {
   if (int rc = norm_ok(weight, weight_type, eps, rows, cols)) return rc;
-  if (!lies_at(x, ldx, cols) || (residual && !lies_at(residual, ld_res, cols)) || (h && !lies_at(h, ld_h, cols)) ||
-      (y && !lies_at(y, ld_y, cols)) || (!y && !codes) || (!codes != !scales))
+  if (!lies_at(x, ldx, cols, rows) || (residual && !lies_at(residual, ld_res, cols, rows)) || (h && !lies_at(h, ld_h, cols, rows)) ||
+      (y && !lies_at(y, ld_y, cols, rows)) || (!y && !codes && rows) || (!codes != !scales))
     return XS_EINVAL;
   if (codes) {
     const int blocks = (cols + 127) / 128;
@@ -381,10 +381,10 @@ extern "C" int xs_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* dh
                                    const void* weight, int32_t weight_type, float eps, int64_t rows, int32_t cols, void* dx,
                                    int64_t ld_dx, float* d_weight, void* workspace, int64_t workspace_bytes, void* stream) {
   if (int rc = norm_ok(weight, weight_type, eps, rows, cols)) return rc;
-  if (!lies_at(dy, ld_dy, cols) || (dh && !lies_at(dh, ld_dh, cols)) || !lies_at(h, ld_h, cols) || !lies_at(dx, ld_dx, cols) ||
+  if (!lies_at(dy, ld_dy, cols, rows) || (dh && !lies_at(dh, ld_dh, cols, rows)) || !lies_at(h, ld_h, cols, rows) || !lies_at(dx, ld_dx, cols, rows) ||
       (reinterpret_cast<uintptr_t>(d_weight) & 15))
     return XS_EINVAL;
-  const auto shifted = [=](const void* i, int64_t ldi) { return dx == i && ld_dx != ldi; };
+  const auto shifted = [=](const void* i, int64_t ldi) { return dx && dx == i && ld_dx != ldi; };
   if (shifted(dy, ld_dy) || shifted(dh, ld_dh) || shifted(h, ld_h)) return XS_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int groups = grad_groups(rows, cols);

@@ -26,7 +26,7 @@ def test_rmsnorm():
         assert f(**bad) == X.XS_EINVAL, bad
     for bad in (dict(cols=252), dict(cols=32776, ldx=40000, ldr=40000, ldh=40000, ldy=40000), dict(rows=1 << 31)):
         assert f(**bad) == X.XS_EUNSUPPORTED, bad
-    assert f(rows=0) == X.XS_OK
+    assert f(rows=0) == f(rows=0, x=None, r=None, h=None, y=None, c=None, s=None) == X.XS_OK
 
 
 def test_rmsnorm_backward():
@@ -40,7 +40,7 @@ def test_rmsnorm_backward():
         assert f(**bad) == X.XS_EINVAL, bad
     for bad in (dict(cols=12), dict(rows=1 << 31)):
         assert f(**bad) == X.XS_EUNSUPPORTED, bad
-    assert f(rows=0) == X.XS_OK
+    assert f(rows=0) == f(rows=0, dy=None, dh=None, h=None, dx=None) == X.XS_OK
     n = C.c_int64()
     q = lambda r, c, p=C.byref(n): X.xs_rmsnorm_backward_workspace_bytes(r, c, p)
     assert q(-1, 8) == q(1, 0) == q(1, 8, None) == X.XS_EINVAL
@@ -71,7 +71,7 @@ def test_balance_loss():
         assert f(**bad) == X.XS_EWORKSPACE, bad
     for bad in (dict(dl=None), dict(add=A + 2), dict(lda=63), dict(d=None), dict(d=A + 2), dict(ldd=63), dict(d=2 * A, ldd=72), dict(d=A, ldd=72)):
         assert b(**bad) == X.XS_EINVAL, bad
-    assert b(T=0) == X.XS_OK and b(T=0, st=None, n=1) == X.XS_OK
+    assert b(T=0) == b(T=0, st=None, n=1) == b(T=0, l=None, add=None, d=None) == X.XS_OK
     assert f(T=2 ** 31 - 10) == X.XS_EUNSUPPORTED
     n = C.c_int64()
     q = lambda T, E, s, p=C.byref(n): X.xs_balance_loss_workspace_bytes(T, E, s, p)
@@ -130,6 +130,7 @@ def test_attention_gradients():
     # a single head has no head stride
     assert X.xs_attention_packed_workspace_bytes(_attn(heads=1, kv_heads=1, q_head=0, k_head=0, v_head=0, o_head=0), C.byref(n)) == X.XS_OK
     assert X.xs_attention_packed(_attn(Tq=0), None, 0, None, None) == X.XS_OK
+    assert X.xs_attention_packed(_attn(Tq=0, q=None, o=None, lse=None), None, 0, None, None) == X.XS_OK
 
 
 def test_binding_refuses_other_layouts():

@@ -165,9 +165,10 @@ def test_new_tokens_over_a_cache(new, H, Hkv, D, cap):
     c.check_forward()
 
 
-def test_a_shared_prefix_and_sequences_in_any_order():
+@pytest.mark.parametrize("Tk", [800, 1600])
+def test_a_shared_prefix_and_sequences_in_any_order(Tk):
     spans = [(0, 1, 500, 300), (1, 1, 0, 700), (2, 1, 500, 299), (3, 1, 10, 1)]
-    c = Case(spans, 4, 800, 8, 2, 128, cache=True)
+    c = Case(spans, 4, Tk, 8, 2, 128, cache=True)
     c.forward()
     c.check_forward()
 
@@ -245,6 +246,41 @@ def test_gradients_of_a_long_prefix_and_of_queries_that_see_nothing():
     spans = [(0, 33, 0, 1500), (33, 600, 1500, 90), (633, 0, 1590, 257), (633, 700, 1847, 513)]
     for causal in (True, False):
         c = Case(spans, 1333, 2360, 4, 2, 128, causal=causal)
+        c.forward()
+        c.check_forward()
+        c.backward()
+        c.check_backward()
+
+
+def test_no_queries_or_no_keys_at_all():
+    X = xs()
+    for D in (64, 128):
+        k = torch.randn(300, 2, D, device="cuda").bfloat16()
+        q = torch.randn(70, 4, D, device="cuda").bfloat16()
+        none = torch.empty(0, 4, D, device="cuda", dtype=torch.bfloat16), torch.empty(0, 2, D, device="cuda", dtype=torch.bfloat16)
+        i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        status = i32(0)
+        for qq, kk in ((none[0], k), (q, none[1]), (none[0], none[1])):
+            o, lse = torch.full_like(qq, SENTINEL), torch.full((4, qq.shape[0]), SENTINEL, device="cuda")
+            a = X.attn_packed(qq, kk, kk.clone(), o, i32(0, 0, qq.shape[0]), i32(0, kk.shape[0], kk.shape[0]), lse=lse)
+            ws = X.workspace(X.xs_attention_packed_workspace_bytes, a)
+            X.check(X.xs_attention_packed(a, X.ptr(ws), ws.numel(), status.data_ptr(), _stream()))
+            dq, dk, dv = torch.full_like(qq, SENTINEL), torch.full_like(kk, SENTINEL), torch.full_like(kk, SENTINEL)
+            ws = X.workspace(X.xs_attention_packed_backward_workspace_bytes, a)
+            X.check(X.xs_attention_packed_backward(a, X.attn_packed_grads(qq.clone(), dq, dk, dv), X.ptr(ws), ws.numel(), status.data_ptr(), _stream()))
+            torch.cuda.synchronize()
+            assert int(status.item()) == 0
+            assert all((t == 0).all() for t in (o, dq, dk, dv)) and (lse == -np.inf).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_thousands_of_short_sequences(causal):
+    # queries and keys of 3000 sequences of 0 to 3 tokens, one of 900 among them
+    lens = [int(x) for x in np.random.default_rng(2).integers(0, 4, 3000)]
+    lens[1717] = 900
+    spans, T = _packed(lens)
+    for H, Hkv in ((1, 1), (40, 1)):
+        c = Case(spans, T, T, H, Hkv, 64, causal=causal)
         c.forward()
         c.check_forward()
         c.backward()

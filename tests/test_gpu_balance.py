@@ -194,3 +194,31 @@ def test_equal_bits_in_a_replayed_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(c, counts) and torch.equal(m, mean) and torch.equal(lo, loss) and torch.equal(d, first)
+
+
+def test_no_tokens():
+    X = xs()
+    g = _gate(64, 4, "sigmoid", "f32")
+    counts, mean, loss = torch.full((2, 64), 7, dtype=torch.int32, device="cuda"), torch.full((2, 64), S, device="cuda"), torch.full((2,), S, device="cuda")
+    starts = torch.zeros(3, dtype=torch.int32, device="cuda")
+    ws = X.workspace(X.xs_balance_loss_workspace_bytes, 0, 64, 2)
+    X.check(X.xs_balance_loss(g, None, 64, 0, None, starts.data_ptr(), 2, ALPHA, counts.data_ptr(), mean.data_ptr(), loss.data_ptr(), ws.data_ptr(), ws.numel(), None,
+                              _stream()))
+    torch.cuda.synchronize()
+    assert all((t == 0).all() for t in (counts, mean, loss))
+
+
+def test_thousands_of_short_sequences():
+    X = xs()
+    lens = np.random.default_rng(0).integers(0, 5, 5000)
+    lens[77] = 1200
+    starts = [0] + [int(x) for x in np.cumsum(lens)]
+    T, E, k = starts[-1], 70, 3
+    l64, dev = _logits(T, E, "f32", 0, 0)
+    idx = np.argsort(-l64, 1, kind="stable")[:, :k].astype(np.int32)
+    counts, mean, loss, st, status = _forward(_gate(E, k, "softmax", "f32"), dev, torch.from_numpy(idx).cuda(), starts, T)
+    wc, wm, wl = balance.loss(l64, idx, starts, "softmax", ALPHA)
+    rel = 2.0 ** -17 + 1264 * 2.0 ** -24
+    assert status == 0 and np.array_equal(counts.cpu().numpy(), wc)
+    assert np.all(np.abs(mean.cpu().double().numpy() - wm) <= rel * wm + 1e-38)
+    assert np.all(np.abs(loss.cpu().double().numpy() - wl) <= (rel + 2.0 ** -13) * wl)
