@@ -607,8 +607,7 @@ int xs_ulysses_copy(const void* o, int32_t heads, int32_t M, int32_t head_dim,
  *   Tq, Tk   rows of q and o, of k and v
  *   max_k    the most keys of a sequence (0: Tk)
  *   scale    0 = 1 / sqrt(head_dim)
- *   workspace  device, 16-byte aligned, xs_attention_packed_workspace_bytes() bytes (0 for calls with many rows and for short
- *            caches: NULL then)
+ *   workspace  device, 16-byte aligned, xs_attention_packed_workspace_bytes() bytes (0 for many calls: NULL then)
  * Tensors without rows (Tq or Tk 0) may be NULL.
  * A sequence whose queries do not lie in [0, Tq), whose keys do not lie in [0, Tk) or are more than max_k sets
  * XS_EBADINPUT in dev_status and is skipped. Rows of o and lse outside every sequence are not written, keys and values

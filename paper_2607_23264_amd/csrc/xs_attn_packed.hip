@@ -16,7 +16,7 @@
 //
 // Forward, four forms (form_of chooses): rows_kernel, a workgroup 128 rows over all keys that they see; wide_kernel, the same with the
 // keys dealt out evenly where such tiles do not fill the chip; narrow_kernel, a few rows a sequence, each wave its share of all keys; short_kernel,
-// a few rows over short caches in one launch. Gradients: dq_kernel by rows, dkv_kernel by keys, each recomputing P.
+// 32 rows a workgroup with the keys shared out among its waves: short caches, few or short prompts. Gradients: dq_kernel by rows, dkv_kernel by keys, each recomputing P.
 //
 // LDS tiles are rows of 2 D bytes in pieces of 16; row r keeps its piece p at p ^ swz(r). A read by rows takes one
 // piece of 16 consecutive rows at a time, a read by columns four pieces of four consecutive rows; swz
@@ -916,7 +916,7 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges
   store_joined(a, s, kvh, r, col, o, top, sum);
 }
 
-// Short caches: a workgroup a narrow unit, its eight waves each an eighth of the key tiles, added up in LDS: no second launch. One request's next token
+// Short caches and prompts: a workgroup a narrow unit, its eight waves each an eighth of the key tiles, added up in LDS: no second launch. One request's next token
 // over 80 keys: 4 us, a chain of dependent loads (starts, keys, result); 1024 keys 9.6.
 template <int D>
 __global__ __launch_bounds__(512, 2) void short_kernel(Args a) {
@@ -1491,10 +1491,13 @@ Form form_of(const pattn::Args& a) {
   // Few rows a sequence: one launch up to 1024 keys (8 units of 1024 keys 9.6 us, in two 11.4 and the time between; 256 22.0 and 29.8; of 2048
   // keys 13.3 and 11.7).
   if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq) return a.max_k <= 1024 ? Form::kShort : Form::kNarrow;
-  // Where the tiles of rows are too few for their length the keys are dealt out too. One prompt, us by rows and dealt out (two launches): 8 heads of 1100
-  // tokens 23.1 and 25.8, 2000: 35.7 and 35.5, 4000: 65.5 and 64.3, 8000: 184 and 164, 16384: 509 and 598; one head of 5000: 83 and 32; 16 heads of 2000: 39 and
-  // 47, 4000: 95 and 101; 7 chunks of 61 tokens, 32 heads, caches of 1100: 23.8 and 32.6.
-  const int64_t tiles = row_tiles(a), cus = xs_host::num_cus(), keys = long_keys(a);
+  // Eight waves for 32 rows where these fill the chip once, twice if they are long: an eighth of the keys each (one prompt, us by rows or dealt out and so:
+  // 8 heads of 100 tokens 8.1 and 5.6, 512: 15.6 and 9.8, 1000: 21.3 and 11.7, 2000: 36 and 27; one head of 5000 33 and 26; four of 250, 10 heads: 11.3
+  // and 10.3, 12 heads: 11.4 and 12.5; two of 1000, 8 heads: 22 both; 128 tokens over a cache of 4000, 8 heads: 25 and 22).
+  const int64_t units = packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv, tiles = row_tiles(a), cus = xs_host::num_cus(), keys = long_keys(a);
+  if (keys <= 4096 && (3 * units <= 4 * cus || (keys > 768 && units <= 2 * cus))) return Form::kShort;
+  // Where the tiles of 128 rows are too few for their length the keys are dealt out too. One prompt, us by rows and dealt out (two launches): 8 heads of 4000
+  // tokens 65.5 and 64.3, 8000: 184 and 164, 16384: 509 and 598; 16 heads of 2000: 39 and 47, 4000: 95 and 101.
   return keys <= 1024 || tiles > 2 * cus || tiles * 4000 > cus * keys || a.G > 128 ? Form::kRows : Form::kWide;
 }
 

@@ -152,14 +152,14 @@ def test_many_rows(lens, H, Hkv, D, layout, causal):
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("new,H,Hkv", [(1, 8, 2), (1, 1, 1), (1, 32, 1), (2, 6, 2), (5, 8, 1), (17, 4, 2), (40, 3, 3), (50, 96, 32)])
-@pytest.mark.parametrize("cap", [1024, 1700])
+@pytest.mark.parametrize("cap", [1024, 4200])
 def test_new_tokens_over_a_cache(new, H, Hkv, D, cap):
     # keys behind each sequence's rows are NaN; lengths around the tiles' ends, fewer keys than queries, none. Caches of 1024 keys take one
     # launch, in longer ones the keys are dealt out.
     lens = [new, 0, 1, 31, 32, 33, 64, 95, 127, 129, 300, cap - 24]
     spans = [(1 + i * new, new, i * cap, m) for i, m in enumerate(lens)]
     c = Case(spans, 2 + new * len(lens), cap * len(lens), H, Hkv, D, cache=True, max_k=cap, seed=new)
-    many = (new * (H // Hkv) * len(lens) // 128 + len(lens)) * Hkv * 4000 > 256 * cap
+    many = (new * (H // Hkv) * len(lens) // 128 + len(lens)) * Hkv * 4000 > 256 * cap      # tiles of rows that fill the chip
     assert (c.ws.numel() > 0) == (cap > 1024 and not many)
     c.forward()
     c.check_forward()
@@ -210,7 +210,7 @@ def test_many_sequences_of_many_rows():
 def test_groups_of_any_size_over_long_sequences(G):
     # units of as many queries as fit 128 rows; groups of more than 128 heads have none
     spans = [(0, 130, 0, 1300), (130, 1, 1300, 64), (131, 70, 1364, 65)]
-    c = Case(spans, 201, 4000, G, 1, 64, cache=True)
+    c = Case(spans, 201, 4200, G, 1, 64, cache=True)
     assert (c.ws.numel() > 0) == (G <= 128)
     c.forward()
     c.check_forward()
@@ -229,7 +229,7 @@ def test_gradients_of_more_keys_than_queries_and_fewer():
 
 
 # 512 keys and more a sequence take key tiles of 256; 70, 3 and 1 heads leave tiles inside one workgroup's share and over several
-@pytest.mark.parametrize("lens,H,Hkv", [([1025], 4, 1), ([511, 1, 1030], 6, 2), ([700, 900], 70, 35), ([513], 1, 1), ([900], 6, 2), ([521, 503], 3, 3)])
+@pytest.mark.parametrize("lens,H,Hkv", [([1025], 4, 1), ([511, 1, 1030], 6, 2), ([700, 900], 70, 35), ([513], 1, 1), ([900], 6, 2), ([521, 503], 20, 20)])
 @pytest.mark.parametrize("D,layout", [(128, "token"), (64, "room")])
 @pytest.mark.parametrize("causal", [True, False])
 def test_long_sequences(lens, H, Hkv, D, layout, causal):
@@ -240,6 +240,17 @@ def test_long_sequences(lens, H, Hkv, D, layout, causal):
     c.check_forward()
     c.backward()
     c.check_backward()
+
+
+@pytest.mark.parametrize("lens", [[4200], [4100, 1, 4200]])
+@pytest.mark.parametrize("D,layout", [(128, "token"), (64, "head")])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_prompts_whose_keys_are_dealt_out(lens, D, layout, causal):
+    spans, T = _packed(lens, gap=1)
+    c = Case(spans, T, T, 2, 1, D, layout, causal)
+    assert c.ws.numel() > 0
+    c.forward()
+    c.check_forward()
 
 
 def test_gradients_of_a_long_prefix_and_of_queries_that_see_nothing():
@@ -428,13 +439,13 @@ def test_a_training_step_in_a_graph_and_equal_bits():
             assert torch.equal(t, w)
 
 
-@pytest.mark.parametrize("new,max_k", [(3, 0), (3, 1100), (60, 0), (60, 1100)])
-def test_keys_past_2_gib_and_32_bit_offsets(new, max_k):
+@pytest.mark.parametrize("new,H,max_k", [(3, 4, 0), (3, 4, 1100), (60, 192, 0), (60, 4, 4200)])
+def test_keys_past_2_gib_and_32_bit_offsets(new, H, max_k):
     # one key head of a cache with rows 2^22 elements apart: 700 rows are 5.5 GiB; all four forms
     m, D, row = 700, 128, 1 << 22
     big = torch.empty((m, row), dtype=torch.bfloat16, device="cuda")
     k, v = big[:, :D].unflatten(1, (1, D)), big[:, D:2 * D].unflatten(1, (1, D))
-    c = Case([(0, new, 0, m)], new, m, 4, 1, D, cache=True)
+    c = Case([(0, new, 0, m)], new, m, H, 1, D, cache=True)
     k.copy_(c.k)
     v.copy_(c.v)
     X = xs()
