@@ -1105,6 +1105,125 @@ __global__ __launch_bounds__(256 * NG, 2) void dq_kernel(Args a) {
   if (w0 < end) store_rows<D>(mine, acc, a.scale, [&](int i) { return w0 + i < end ? row_at(a, a.dq, s, kvh, w0 + i) : nullptr; });
 }
 
+// dq of few or short prompts, as short_kernel: a workgroup 32 rows, its eight waves each every eighth tile of 32 keys in a slot of K and one of V
+// of their own, their sums added up in LDS. Rows that see at most 256 keys have one tile a wave, so that delta from P and dP takes no second pass.
+template <int D>
+__global__ __launch_bounds__(512, 2) void dq_short_kernel(Args a) {
+  using G = Geo<D>;
+  using Lk = Loader<D, 32, 1, kBoth>;
+  using Lv = Loader<D, 32, 1, kRows>;
+  constexpr int kTile = 32 * G::kRow, kMine = 2 * kTile;        // a wave's slots: also 32 rows of D sums
+  __shared__ __attribute__((aligned(16))) char lds[8 * kMine];
+  __shared__ float deltas[8][32];
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, up = lane >> 5;
+  lds_char* const ks = (lds_char*)lds + wv * kMine;
+  lds_char* const vs = ks + kTile;
+  Seq s;
+  int kvh, tile;
+  if (!tile_of<32>(a, &s, &kvh, &tile)) return;
+  const int R = s.nq * a.G, r0 = tile * 32, rows = min(32, R - r0), any = sees(a, r0 + rows - 1, s.nq, s.nk), all = sees(a, r0, s.nq, s.nk);
+  const int tiles = (any + 31) / 32, r = min(r0 + (lane & 31), R - 1), qi = query_of(a, r), h = kvh * a.G + (r - qi * a.G), lim = sees(a, r, s.nq, s.nk);
+  const char* const kp = at(a.k, s.k0, kvh);
+  const char* const vp = at(a.v, s.k0, kvh);
+  const Lk lk(0, lane, a.k.row);
+  const Lv lv(0, lane, a.v.row);
+  auto issue_k = [&](int j) { lk.issue(kp + static_cast<int64_t>(j) * 32 * a.k.row, s.nk - j * 32, ks, 0); };
+  auto issue_v = [&](int j) { lv.issue(vp + static_cast<int64_t>(j) * 32 * a.v.row, s.nk - j * 32, vs, 0); };
+  if (wv < tiles) {
+    issue_k(wv);
+    issue_v(wv);
+  }
+  bf16x8 qf[D / 16], df[D / 16];
+  load_frags<D>(at(a.q, s.q0 + qi, h), qf);
+  load_frags<D>(at(a.d_o, s.q0 + qi, h), df);
+  const int64_t stat = static_cast<int64_t>(h) * a.Tq + s.q0 + qi;
+  const float lse2 = lim > 0 ? a.lse[stat] * kLog2e : 0.f;
+  const RowReads<D, kBoth> rk(lane);
+  const ColReads<D, kBoth> ck(lane);
+  const RowReads<D, kRows> rv(lane);
+  f32x16 sc, dp, acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) zero(acc[db]);
+  float delta = 0.f;
+  // P of tile j into sc, and dP
+  auto scores = [&](int j) {
+    wait_vm<0>();
+    zero(sc);
+    zero(dp);
+    fed<D / 8, 4, D == 128>([&](int i) { return i & 1 ? row_operand<D>(vs, 0, rv, i >> 1) : row_operand<D>(ks, 0, rk, i >> 1); },
+                            [&](int i, bf16x8 v) { mma(i & 1 ? dp : sc, v, i & 1 ? df[i >> 1] : qf[i >> 1]); });
+    if (j * 32 + 32 > all) hide(sc, j * 32, lim, up);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], a.scale_log2e, -lse2));
+  };
+  auto product = [&] {
+    uint32_t pk[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pk[e] = pack_bf16x2(sc[2 * e] * (dp[2 * e] - delta), sc[2 * e + 1] * (dp[2 * e + 1] - delta));
+    const bf16x8 ds[2] = {operand(pk, 0), operand(pk, 1)};
+    fed<D / 16, 4, D == 128>([&](int i) { return col_operand<D>(ks, i / (D / 32), ck, i % (D / 32)); },
+                             [&](int i, bf16x8 v) { mma(acc[i % (D / 32)], v, ds[i / (D / 32)]); });
+  };
+  if (tiles <= 8) {
+    if (wv < tiles) {
+      scores(wv);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) delta = __builtin_fmaf(sc[e], dp[e], delta);
+      delta = add_halves(delta);
+    }
+    if (up == 0) deltas[wv][lane] = delta;
+    __syncthreads();
+    delta = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) delta += deltas[w][lane & 31];
+    if (wv < tiles) product();
+  } else {
+    bf16x8 of[D / 16];
+    load_frags<D>(at(a.o, s.q0 + qi, h), of);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(static_cast<float>(df[kk][e]), static_cast<float>(of[kk][e]), delta);
+    delta = add_halves(delta);
+    for (int j = wv; j < tiles; j += 8) {
+      scores(j);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // V tile j has been read
+      if (j + 8 < tiles) issue_v(j + 8);
+      product();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (j + 8 < tiles) issue_k(j + 8);
+    }
+  }
+  if (wv == 0 && lane < rows) {
+    a.delta[stat] = delta;
+    a.lse2[stat] = lse2;
+  }
+  // as in short_kernel
+  const int waves = min(8, max(1, tiles));
+  if (wv < waves) {
+    const int i = lane & 31;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(lds + wv * kMine + i * D * 4 + (((8 * db + 2 * g + up) ^ i % (D / 4)) << 4)) =
+            f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
+  }
+  __syncthreads();
+  constexpr int kLanes = D / 4;
+  const int col = threadIdx.x % kLanes;
+  for (int i = threadIdx.x / kLanes; i < rows; i += 512 / kLanes) {
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < waves; ++w) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(lds + w * kMine + i * D * 4 + ((col ^ i % kLanes) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += v[e];
+    }
+    *reinterpret_cast<u32x2*>(row_at(a, a.dq, s, kvh, r0 + i) + col * 8) =
+        u32x2{pack_bf16x2(o[0] * a.scale, o[1] * a.scale), pack_bf16x2(o[2] * a.scale, o[3] * a.scale)};
+  }
+}
+
 // dk and dv: a workgroup holds 32 NW keys of a key head (NW waves of 32), their K and V fragments beside both
 // results' accumulators in registers, and streams the rows that see them, 32 queries of one head at a time with do,
 // lse and delta, two blocks ahead in three LDS slots. Two waves share a SIMD's registers: kStash of V's fragments lie in
@@ -1485,19 +1604,24 @@ int64_t row_tiles(const pattn::Args& a) { return packed_tiles_bound(a.Tq, a.n_se
 // 5500 tokens in three, heads of 64: 51 -> 39, 54 -> 41; short ones lose: twenty of 200, 12 -> 16; as do many: 3000 tokens, 32 heads, 86 -> 103).
 bool pairs(const pattn::Args& a) { return long_keys(a) > 768 && 2 * row_tiles(a) <= 3 * int64_t(xs_host::num_cus()); }
 
+// Eight waves for 32 rows where these fill the chip once, twice if they are long: an eighth of the keys each (one prompt, us by rows or dealt out and so:
+// 8 heads of 100 tokens 8.1 and 5.6, 512: 15.6 and 9.8, 1000: 21.3 and 11.7, 2000: 36 and 27; one head of 5000 33 and 26; four of 250, 10 heads: 11.3
+// and 10.3, 12 heads: 11.4 and 12.5; two of 1000, 8 heads: 22 both; 128 tokens over a cache of 4000, 8 heads: 25 and 22).
+bool few_units(const pattn::Args& a) {
+  const int64_t units = packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv, cus = xs_host::num_cus(), keys = long_keys(a);
+  return keys <= 4096 && (3 * units <= 4 * cus || (keys > 768 && units <= 2 * cus));
+}
+
 // Which kernels a forward call takes, from what the host knows.
 enum class Form { kRows, kWide, kNarrow, kShort };
 Form form_of(const pattn::Args& a) {
   // Few rows a sequence: one launch up to 1024 keys (8 units of 1024 keys 9.6 us, in two 11.4 and the time between; 256 22.0 and 29.8; of 2048
   // keys 13.3 and 11.7).
   if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq) return a.max_k <= 1024 ? Form::kShort : Form::kNarrow;
-  // Eight waves for 32 rows where these fill the chip once, twice if they are long: an eighth of the keys each (one prompt, us by rows or dealt out and so:
-  // 8 heads of 100 tokens 8.1 and 5.6, 512: 15.6 and 9.8, 1000: 21.3 and 11.7, 2000: 36 and 27; one head of 5000 33 and 26; four of 250, 10 heads: 11.3
-  // and 10.3, 12 heads: 11.4 and 12.5; two of 1000, 8 heads: 22 both; 128 tokens over a cache of 4000, 8 heads: 25 and 22).
-  const int64_t units = packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv, tiles = row_tiles(a), cus = xs_host::num_cus(), keys = long_keys(a);
-  if (keys <= 4096 && (3 * units <= 4 * cus || (keys > 768 && units <= 2 * cus))) return Form::kShort;
+  if (few_units(a)) return Form::kShort;
   // Where the tiles of 128 rows are too few for their length the keys are dealt out too. One prompt, us by rows and dealt out (two launches): 8 heads of 4000
   // tokens 65.5 and 64.3, 8000: 184 and 164, 16384: 509 and 598; 16 heads of 2000: 39 and 47, 4000: 95 and 101.
+  const int64_t tiles = row_tiles(a), cus = xs_host::num_cus(), keys = long_keys(a);
   return keys <= 1024 || tiles > 2 * cus || tiles * 4000 > cus * keys || a.G > 128 ? Form::kRows : Form::kWide;
 }
 
@@ -1572,7 +1696,9 @@ int backward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
   a.lse2 = a.delta + static_cast<int64_t>(a.H) * a.Tq;
   a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + stats_bytes(a));
   if (a.Tq) {
-    if (pairs(a)) hipLaunchKernelGGL((pattn::dq_kernel<D, 2>), xs_host::grid_of(row_tiles(a)), dim3(512), 0, st, a);
+    if (few_units(a))
+      hipLaunchKernelGGL((pattn::dq_short_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv), dim3(512), 0, st, a);
+    else if (pairs(a)) hipLaunchKernelGGL((pattn::dq_kernel<D, 2>), xs_host::grid_of(row_tiles(a)), dim3(512), 0, st, a);
     else hipLaunchKernelGGL((pattn::dq_kernel<D, 1>), xs_host::grid_of(row_tiles(a)), dim3(256), 0, st, a);
     if (xs_host::launch_status()) return XS_EHIP;
   }
