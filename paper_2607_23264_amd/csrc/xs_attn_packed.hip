@@ -380,16 +380,16 @@ __device__ __forceinline__ Seq seq_of(const Args& a, int i) {
   return Seq{q0, q1 - q0, k0, nk};
 }
 
-// The workgroup's tile of PER rows of a sequence and key head, key heads side by side; false past the last. Every wave finds it
+// The workgroup's tile of PER rows (or keys) of a sequence and key head, key heads side by side; false past the last. Every wave finds it
 // by itself, 64 sequences a step, all that it has to know of one in a lane and on its way at once.
-template <int PER>
+template <int PER, bool KEYS = false>
 __device__ __forceinline__ bool tile_of(const Args& a, Seq* s, int* kvh, int* tile) {
   const int64_t id = block_number(), t = quot(id, a.Hkv);
   *kvh = static_cast<int>(id - t * a.Hkv);
   int left = static_cast<int>(t);
   for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
     const Seq mine = seq_of(a, s0 + (threadIdx.x & 63));
-    const int n = static_cast<int>((static_cast<int64_t>(mine.nq) * a.G + PER - 1) / PER), upto = wave_scan(n);
+    const int n = static_cast<int>((static_cast<int64_t>(KEYS ? mine.nk : mine.nq * a.G) + PER - 1) / PER), upto = wave_scan(n);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > left);
     if (hit) {
       const int l = __builtin_ctzll(hit);
@@ -1541,6 +1541,144 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
   }
 }
 
+// dk and dv of few or short prompts: a workgroup 32 keys of a key head, its eight waves each every eighth block of 32 queries of a head that sees them, in
+// slots of their own; their sums are added up in LDS, dk first, then dv: no parts, no second launch. K's and V's fragments, the same for all waves, lie in LDS.
+template <int D>
+__global__ __launch_bounds__(512, 2) void dkv_short_kernel(Args a) {
+  using G = Geo<D>;
+  using L = Loader<D, 32, 1, kBoth>;
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+  constexpr int kTile = 32 * G::kRow, kMine = 2 * kTile, kB = D / 32;
+  __shared__ __attribute__((aligned(16))) char lds[8 * kMine + 2 * kTile + 8 * 256];
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, up = lane >> 5;
+  lds_char* const qs = (lds_char*)lds + wv * kMine;
+  lds_char* const ds = qs + kTile;
+  lds_char* const vs = (lds_char*)lds + 8 * kMine;
+  lds_char* const stats = vs + 2 * kTile + wv * 256;           // lse and delta of the block's rows
+  Seq s;
+  int kvh, tile;
+  if (!tile_of<32, true>(a, &s, &kvh, &tile)) return;
+  const int key0 = tile * 32, keys = min(32, s.nk - key0), off = s.nk - s.nq, first = a.causal ? max(0, key0 - off) : 0;
+  const int per_head = (max(0, s.nq - first) + 31) / 32;
+  const int64_t blocks = static_cast<int64_t>(per_head) * a.G;
+  const L lq(0, lane, a.q.row), ld(0, lane, a.d_o.row);
+  // block b: queries t .. + 31 of head h
+  auto place = [&](int64_t b, int* h, int* t) {
+    const int g = static_cast<int>(quot(b, per_head));
+    *h = kvh * a.G + g;
+    *t = first + static_cast<int>(b - static_cast<int64_t>(g) * per_head) * 32;
+  };
+  auto issue_q = [&](int64_t b) {
+    int h, t;
+    place(b, &h, &t);
+    lq.issue(at(a.q, s.q0 + t, h), s.nq - t, qs, 0);
+    if (up == 0) {
+      const int64_t stat = static_cast<int64_t>(h) * a.Tq + s.q0 + t;
+      load_lds4(buffer_rsrc(a.lse2 + stat, min(s.nq - t, 32) * 4), lane * 4, stats);
+      load_lds4(buffer_rsrc(a.delta + stat, min(s.nq - t, 32) * 4), lane * 4, stats + 128);
+    }
+  };
+  auto issue_d = [&](int64_t b) {
+    int h, t;
+    place(b, &h, &t);
+    ld.issue(at(a.d_o, s.q0 + t, h), s.nq - t, ds, 0);
+  };
+  if (wv < blocks) {
+    issue_q(wv);
+    issue_d(wv);
+  }
+  // fragments of 16 columns, K's first: a wave one of each
+  if (wv < D / 16) {
+    const int kc = s.k0 + key0 + min(lane & 31, keys - 1);
+    const bf16x8 k = *reinterpret_cast<const bf16x8*>(at(a.k, kc, kvh) + 32 * wv + 16 * up), v = *reinterpret_cast<const bf16x8*>(at(a.v, kc, kvh) + 32 * wv + 16 * up);
+    *(lds_bf16x8*)(vs + wv * 1024 + lane * 16) = k;
+    *(lds_bf16x8*)(vs + kTile + wv * 1024 + lane * 16) = v;
+  }
+  __syncthreads();
+  const RowReads<D, kBoth> rr(lane);
+  const ColReads<D, kBoth> rc(lane);
+  f32x16 dk[kB], dv[kB];
+#pragma unroll
+  for (int db = 0; db < kB; ++db) {
+    zero(dk[db]);
+    zero(dv[db]);
+  }
+  for (int64_t b = wv; b < blocks; b += 8) {
+    int h, t;
+    place(b, &h, &t);
+    wait_vm<0>();
+    f32x16 sc, dp;
+    zero(sc);
+    zero(dp);
+    struct Pair {
+      bf16x8 a, b;
+    };
+    fed<D / 8, 2, D == 128>([&](int i) {
+                              Pair p;
+                              p.a = row_operand<D>(i < D / 16 ? qs : ds, 0, rr, i % (D / 16));
+                              p.b = *(const lds_bf16x8*)(vs + i * 1024 + lane * 16);
+                              return p;
+                            },
+                            [&](int i, const Pair& p) { mma(i < D / 16 ? sc : dp, p.a, p.b); });
+    if (a.causal && t + off < key0 + 31) {
+      const int edge = key0 + (lane & 31) - off - t;           // rows before it do not see the lane's key
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (entry_row(e, up) < edge) sc[e] = -INFINITY;
+    }
+    uint32_t pp[8], pd[8];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 ls = *(const lds_f32x4*)(stats + (8 * g + 4 * up) * 4), de = *(const lds_f32x4*)(stats + 128 + (8 * g + 4 * up) * 4);
+      float p[4], d[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * g + e], a.scale_log2e, -ls[e]));
+        d[e] = p[e] * (dp[4 * g + e] - de[e]);
+      }
+      pp[2 * g] = pack_bf16x2(p[0], p[1]);
+      pp[2 * g + 1] = pack_bf16x2(p[2], p[3]);
+      pd[2 * g] = pack_bf16x2(d[0], d[1]);
+      pd[2 * g + 1] = pack_bf16x2(d[2], d[3]);
+    }
+    const bf16x8 po[2] = {operand(pp, 0), operand(pp, 1)};
+    fed<2 * kB, 2, D == 128>([&](int i) { return col_operand<D>(ds, i / kB, rc, i % kB); }, [&](int i, bf16x8 v) { mma(dv[i % kB], v, po[i / kB]); });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // do has been read
+    if (b + 8 < blocks) issue_d(b + 8);
+    const bf16x8 so[2] = {operand(pd, 0), operand(pd, 1)};
+    fed<2 * kB, 2, D == 128>([&](int i) { return col_operand<D>(qs, i / kB, rc, i % kB); }, [&](int i, bf16x8 v) { mma(dk[i % kB], v, so[i / kB]); });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (b + 8 < blocks) issue_q(b + 8);
+  }
+  const int waves = static_cast<int>(min(static_cast<int64_t>(8), max(static_cast<int64_t>(1), blocks)));
+  constexpr int kLanes = D / 4;
+  const int col = threadIdx.x % kLanes;
+  auto sum = [&](const f32x16(&acc)[kB], const Mat& to, float c) {
+    if (wv < waves) {
+      const int i = lane & 31;
+#pragma unroll
+      for (int db = 0; db < kB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4*>(lds + wv * kMine + i * D * 4 + (((8 * db + 2 * g + up) ^ i % kLanes) << 4)) =
+              f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
+    }
+    __syncthreads();
+    for (int i = threadIdx.x / kLanes; i < keys; i += 512 / kLanes) {
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < waves; ++w) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(lds + w * kMine + i * D * 4 + ((col ^ i % kLanes) << 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += v[e];
+      }
+      *reinterpret_cast<u32x2*>(at(to, s.k0 + key0 + i, kvh) + col * 8) = u32x2{pack_bf16x2(o[0] * c, o[1] * c), pack_bf16x2(o[2] * c, o[3] * c)};
+    }
+  };
+  sum(dk, a.dk, a.scale);
+  __syncthreads();
+  sum(dv, a.dv, 1.f);
+}
+
 constexpr int kMaxSeq = 1 << 16;
 
 }  // namespace pattn
@@ -1663,6 +1801,12 @@ int forward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
   return xs_host::launch_status();
 }
 
+// dk and dv by 32 keys a workgroup, unless the first keys' rows are too many for one or there are units enough to share out longer tiles (us with the join,
+// and so; heads of 128: one prompt of 100 tokens, 8 heads: 18.7 and 6.5, 1000: 36.9 and 16, 3000: 77 and 64; two of 1500: 57 and 45; forty of 100: 36 and 34; 32 heads
+// over 8, ten of 100 tokens 30 and 21, 1000: 53 and 38; 8 heads over 2, 2000: 56 and 61; heads of 64, 1000 tokens: 24 and 10).
+bool few_keys(const pattn::Args& a) {
+  return a.Tk && long_keys(a) * a.G <= 4096 && packed_tiles_bound(a.Tk, a.n_seq, 1, 32) * a.Hkv <= 4 * int64_t(xs_host::num_cus());
+}
 // Waves of a dkv_kernel workgroup: eight (256 keys, half the rows' traffic) for sequences of 512 keys and more on average, four
 // for shorter ones and for heads of 64, where a block of 32 rows is four waves' loads.
 template <int D>
@@ -1678,7 +1822,7 @@ int dkv_ranges(const pattn::Args& a) {
 // delta and lse of every row
 int64_t stats_bytes(const pattn::Args& a) { return (static_cast<int64_t>(a.H) * a.Tq * 8 + 255) / 256 * 256; }
 template <int D>
-int64_t grad_bytes(const pattn::Args& a) { return stats_bytes(a) + dkv_ranges<D>(a) * int64_t(2 * 2 * 32 * D * 4) * dkv_waves<D>(a); }
+int64_t grad_bytes(const pattn::Args& a) { return stats_bytes(a) + (few_keys(a) ? 0 : dkv_ranges<D>(a)) * int64_t(2 * 2 * 32 * D * 4) * dkv_waves<D>(a); }
 
 template <int D, int NW>
 int dkv(const pattn::Args& a, int ranges, hipStream_t st) {
@@ -1701,6 +1845,10 @@ int backward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
     else if (pairs(a)) hipLaunchKernelGGL((pattn::dq_kernel<D, 2>), xs_host::grid_of(row_tiles(a)), dim3(512), 0, st, a);
     else hipLaunchKernelGGL((pattn::dq_kernel<D, 1>), xs_host::grid_of(row_tiles(a)), dim3(256), 0, st, a);
     if (xs_host::launch_status()) return XS_EHIP;
+  }
+  if (few_keys(a)) {
+    hipLaunchKernelGGL((pattn::dkv_short_kernel<D>), xs_host::grid_of(packed_tiles_bound(a.Tk, a.n_seq, 1, 32) * a.Hkv), dim3(512), 0, st, a);
+    return xs_host::launch_status();
   }
   const int ranges = dkv_ranges<D>(a);
   if (!ranges) return XS_OK;
