@@ -856,7 +856,8 @@ __global__ __launch_bounds__(256) void join_wide_kernel(Args a, int64_t ranges) 
 
 // Narrow units: a workgroup a row, D / 4 lanes a part, 16 parts at once in each wave (a request's next token has a few rows, and their
 // parts are many).
-template <int D>
+// Where the rows are many, and most of them finished, a wave a row (60 sequences of 30 tokens, 8 heads: 29 us otherwise).
+template <int D, bool WAVE>
 __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges) {
   constexpr int kLanes = D / 4, kParts = 64 / kLanes, kOnce = 16 / kParts;
   __shared__ __attribute__((aligned(16))) f32x4 waves[4][kLanes];
@@ -864,7 +865,7 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges
   Seq s;
   int64_t in, before, total;
   if (!locate<Narrow>(a, [&](const Seq& x) { return static_cast<int64_t>(x.nq) * a.H; },
-                      block_number(), &s, &in, &before, &total))
+                      WAVE ? block_number() * 4 + wv : block_number(), &s, &in, &before, &total))
     return;
   int kvh, r, i;
   int64_t u0;
@@ -888,7 +889,7 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges
     const float c = w + lane <= w1 ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
     sum = __builtin_fmaf(ml.y, c, sum);
     const int n = static_cast<int>(min(w1 - w + 1, static_cast<int64_t>(64)));
-    for (int p = 16 * wv; p < n; p += 64) {
+    for (int p = WAVE ? 0 : 16 * wv; p < n; p += WAVE ? 16 : 64) {
       f32x4 v[kOnce];
 #pragma unroll
       for (int q = 0; q < kOnce; ++q) v[q] = *reinterpret_cast<const f32x4*>(a.part_o + part(w + min(p + q * kParts + grp, n - 1)) * D + col);
@@ -906,13 +907,18 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(Args a, int64_t ranges
   for (int d = kLanes; d < 64; d <<= 1)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
-  if (grp == 0) waves[wv][lane] = o;
-  __syncthreads();
-  if (wv || grp) return;
+  if constexpr (!WAVE) {
+    if (grp == 0) waves[wv][lane] = o;
+    __syncthreads();
+    if (wv) return;
+  }
+  if (grp) return;
+  if constexpr (!WAVE) {
 #pragma unroll
-  for (int w = 1; w < 4; ++w)
+    for (int w = 1; w < 4; ++w)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += waves[w][lane][e];
+      for (int e = 0; e < 4; ++e) o[e] += waves[w][lane][e];
+  }
   store_joined(a, s, kvh, r, col, o, top, sum);
 }
 
@@ -1755,7 +1761,7 @@ enum class Form { kRows, kWide, kNarrow, kShort };
 Form form_of(const pattn::Args& a) {
   // Few rows a sequence: one launch up to 1024 keys (8 units of 1024 keys 9.6 us, in two 11.4 and the time between; 256 22.0 and 29.8; of 2048
   // keys 13.3 and 11.7).
-  if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq) return a.max_k <= 1024 ? Form::kShort : Form::kNarrow;
+  if (static_cast<int64_t>(a.Tq) * a.G <= 32ll * a.n_seq) return long_keys(a) <= 1024 ? Form::kShort : Form::kNarrow;
   if (few_units(a)) return Form::kShort;
   // Where the tiles of 128 rows are too few for their length the keys are dealt out too. One prompt, us by rows and dealt out (two launches): 8 heads of 4000
   // tokens 65.5 and 64.3, 8000: 184 and 164, 16384: 509 and 598; 16 heads of 2000: 39 and 47, 4000: 95 and 101.
@@ -1796,7 +1802,8 @@ int forward(pattn::Args a, void* ws, int64_t bytes, hipStream_t st) {
     hipLaunchKernelGGL((pattn::narrow_kernel<D>), grid, dim3(256), 0, st, a);
     if (xs_host::launch_status()) return XS_EHIP;
     const int64_t rows = static_cast<int64_t>(a.Tq) * a.H;
-    hipLaunchKernelGGL((pattn::join_narrow_kernel<D>), xs_host::grid_of(rows), dim3(256), 0, st, a, ranges_of(a, f));
+    if (rows <= 2048) hipLaunchKernelGGL((pattn::join_narrow_kernel<D, false>), xs_host::grid_of(rows), dim3(256), 0, st, a, ranges_of(a, f));
+    else hipLaunchKernelGGL((pattn::join_narrow_kernel<D, true>), xs_host::grid_of((rows + 3) / 4), dim3(256), 0, st, a, ranges_of(a, f));
   }
   return xs_host::launch_status();
 }

@@ -151,7 +151,7 @@ def test_many_rows(lens, H, Hkv, D, layout, causal):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("new,H,Hkv", [(1, 8, 2), (1, 1, 1), (1, 32, 1), (2, 6, 2), (5, 8, 1), (17, 4, 2), (40, 3, 3), (50, 96, 32)])
+@pytest.mark.parametrize("new,H,Hkv", [(1, 8, 2), (1, 1, 1), (1, 32, 1), (2, 6, 2), (5, 8, 1), (17, 4, 2), (40, 3, 3), (50, 96, 32), (8, 48, 16)])
 @pytest.mark.parametrize("cap", [1024, 4200])
 def test_new_tokens_over_a_cache(new, H, Hkv, D, cap):
     # keys behind each sequence's rows are NaN; lengths around the tiles' ends, fewer keys than queries, none. Caches of 1024 keys take one
