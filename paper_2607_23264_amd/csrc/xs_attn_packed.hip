@@ -16,7 +16,8 @@
 //
 // Forward, four forms (form_of chooses): rows_kernel, a workgroup 128 rows over all keys that they see; wide_kernel, the same with the
 // keys dealt out evenly where such tiles do not fill the chip; narrow_kernel, a few rows a sequence, each wave its share of all keys; short_kernel,
-// 32 rows a workgroup with the keys shared out among its waves: short caches, few or short prompts. Gradients: dq_kernel by rows, dkv_kernel by keys, each recomputing P.
+// 32 rows a workgroup with the keys shared out among its waves: short caches, few or short prompts. Gradients: dq_kernel by rows, dkv_kernel by keys, each recomputing P;
+// dq_short_kernel and dkv_short_kernel for few or short prompts.
 //
 // LDS tiles are rows of 2 D bytes in pieces of 16; row r keeps its piece p at p ^ swz(r). A read by rows takes one
 // piece of 16 consecutive rows at a time, a read by columns four pieces of four consecutive rows; swz
@@ -972,8 +973,8 @@ __global__ __launch_bounds__(512, 2) void short_kernel(Args a) {
 
 // ------------------------------------------------------------------------------ gradients
 // dq: as rows_kernel, with a second product (V times the row's do) and dS in place of the probabilities, K and V tiles in two slots each, one
-// barrier a tile. It computes delta for its rows and leaves it, and lse in powers of two, for the kernel below. 8192 tokens in 4 documents, 32 heads over 8: 285 to
-// 301 us, 1010 to 1060 TFLOP/s; matrix units busy 55% of cycles at 1.8 GHz, vector units 43%.
+// barrier a tile. It computes delta for its rows and leaves it, and lse in powers of two, for the kernel below. 8192 tokens in 4 documents, 32 heads over 8: 282 to
+// 301 us, 1010 to 1075 TFLOP/s; matrix units busy 55% of cycles at 1.8 GHz, vector units 43%.
 //
 // delta = do . o takes o's roundings (of the probabilities and of o itself) to every dS of the row alike, a
 // relative error of dq and dk of about 0.0023 / sqrt(keys that share the weight): nothing beside the 0.0017 that dS's own
@@ -1113,6 +1114,7 @@ __global__ __launch_bounds__(256 * NG, 2) void dq_kernel(Args a) {
 
 // dq of few or short prompts, as short_kernel: a workgroup 32 rows, its eight waves each every eighth tile of 32 keys in a slot of K and one of V
 // of their own, their sums added up in LDS. Rows that see at most 256 keys have one tile a wave, so that delta from P and dP takes no second pass.
+// One prompt, 8 heads: 100 tokens 8 us, 1000 16, 2000 36 (by rows 11, 26, 43); a chain of dependent steps: two loads, two products, two barriers and a store take 7.
 template <int D>
 __global__ __launch_bounds__(512, 2) void dq_short_kernel(Args a) {
   using G = Geo<D>;
@@ -1235,7 +1237,7 @@ __global__ __launch_bounds__(512, 2) void dq_short_kernel(Args a) {
 // lse and delta, two blocks ahead in three LDS slots. Two waves share a SIMD's registers: kStash of V's fragments lie in
 // LDS. Queries past the end of the sequence are zeros with lse 0: P = 1, but do = 0 and dS = 1 (0 - 0).
 //
-// The same 8192 tokens: 395 to 417 us, 970 to 1020 TFLOP/s, and 28 to join (60 to 130 MB of parts). Matrix units are busy 48% of cycles, vector units 36%, LDS 34%: both waves of
+// The same 8192 tokens: 390 to 417 us, 970 to 1035 TFLOP/s, and 28 to join (60 to 130 MB of parts). Matrix units are busy 48% of cycles, vector units 36%, LDS 34%: both waves of
 // a SIMD wait at the same barrier. One wave a SIMD with all its registers, a block's products between the next one's softmax: 684 us, some 630 instructions a
 // block at five cycles each; the softmax put between this kernel's own products: 495 us against 447 then.
 //
@@ -1548,7 +1550,8 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(Args a, int n_ranges) {
 }
 
 // dk and dv of few or short prompts: a workgroup 32 keys of a key head, its eight waves each every eighth block of 32 queries of a head that sees them, in
-// slots of their own; their sums are added up in LDS, dk first, then dv: no parts, no second launch. K's and V's fragments, the same for all waves, lie in LDS.
+// slots of their own; their sums are added up in LDS, dk first, then dv: no parts, no second launch. K's and V's fragments, the same for all waves, lie in LDS: with K's in registers 25 of them spilled, 24 us for 16.
+// One prompt, 8 heads: 100 tokens 6.5 us, 1000 16, 3000 64; about 1.8 us a block of a wave.
 template <int D>
 __global__ __launch_bounds__(512, 2) void dkv_short_kernel(Args a) {
   using G = Geo<D>;
