@@ -60,8 +60,8 @@ struct Args {
   float scale, scale_log2e;
   float* lse;            // [H][Tq]
   float *delta, *lse2;   // [H][Tq] (gradients): do . o, lse in powers of two
-  float* part_o;         // [waves][2][32][D] (split); dkv_kernel's parts
-  float* part_ml;        // [waves][2][32][2]
+  float* part_o;         // parts: two slots of each range
+  float* part_ml;        // their rows' maxima and sums
   int32_t* status;
 };
 

@@ -216,12 +216,14 @@ def test_groups_of_any_size_over_long_sequences(G):
     c.check_forward()
 
 
-def test_gradients_of_more_keys_than_queries_and_fewer():
+# 32 query heads a key head have more rows than the kernels of few or short prompts take
+@pytest.mark.parametrize("H", [4, 64])
+def test_gradients_of_more_keys_than_queries_and_fewer(H):
     # a prompt behind a prefix that has gradients too, queries that see nothing, no queries, no keys
     spans = [(0, 20, 0, 90), (20, 70, 90, 30), (90, 0, 120, 40), (90, 10, 160, 0), (100, 130, 160, 200)]
     for causal in (True, False):
         for D in (64, 128):
-            c = Case(spans, 230, 360, 4, 2, D, causal=causal)
+            c = Case(spans, 230, 360, H, 2, D, causal=causal)
             c.forward()
             c.check_forward()
             c.backward()
@@ -253,14 +255,27 @@ def test_long_prompts_whose_keys_are_dealt_out(lens, D, layout, causal):
     c.check_forward()
 
 
-def test_gradients_of_a_long_prefix_and_of_queries_that_see_nothing():
+@pytest.mark.parametrize("H,Hkv", [(4, 2), (16, 1)])
+def test_gradients_of_a_long_prefix_and_of_queries_that_see_nothing(H, Hkv):
     spans = [(0, 33, 0, 1500), (33, 600, 1500, 90), (633, 0, 1590, 257), (633, 700, 1847, 513)]
     for causal in (True, False):
-        c = Case(spans, 1333, 2360, 4, 2, 128, causal=causal)
+        c = Case(spans, 1333, 2360, H, Hkv, 128, causal=causal)
         c.forward()
         c.check_forward()
         c.backward()
         c.check_backward()
+
+
+@pytest.mark.parametrize("D,layout", [(128, "token"), (64, "head")])
+@pytest.mark.parametrize("causal", [True, False])
+def test_large_groups_over_short_sequences(D, layout, causal):
+    # key tiles of 128 whose blocks are dealt out over ranges, with parts of several
+    spans, T = _packed([300, 200, 0, 450], gap=1)
+    c = Case(spans, T, T, 32, 2, D, layout, causal)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
 
 
 def test_no_queries_or_no_keys_at_all():
@@ -369,10 +384,11 @@ def test_bad_sequences_are_skipped(what):
         assert np.all(np.abs(c.o.cpu().double().numpy()[rows] - o[rows]) <= bo[rows])
 
 
-def test_bad_sequences_have_no_gradients():
+@pytest.mark.parametrize("H", [2, 128])
+def test_bad_sequences_have_no_gradients(H):
     X = xs()
     spans, T = _packed([40, 50, 60])
-    c = Case(spans, T, T, 2, 2, 64)
+    c = Case(spans, T, T, H, 2, 64)
     c.forward()
     c.backward()
     c.check_backward()
@@ -416,9 +432,10 @@ def test_two_streams_and_replayed_graphs_with_workspaces_of_their_own():
             c.check_forward()
 
 
-def test_a_training_step_in_a_graph_and_equal_bits():
+@pytest.mark.parametrize("H", [8, 64])
+def test_a_training_step_in_a_graph_and_equal_bits(H):
     spans, T = _packed([200, 57, 300])
-    c = Case(spans, T, T, 8, 2, 128)
+    c = Case(spans, T, T, H, 2, 128)
     c.forward()
     c.backward()
     c.check_forward()
