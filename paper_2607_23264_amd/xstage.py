@@ -222,7 +222,7 @@ xs_balance_loss_backward = _sig("xs_balance_loss_backward", C.c_int, P(xs_gate),
 xs_attention_packed_workspace_bytes = _sig("xs_attention_packed_workspace_bytes", C.c_int, P(xs_attn_packed), P(i64))
 xs_attention_packed = _sig("xs_attention_packed", C.c_int, P(xs_attn_packed), vp, i64, vp, vp)
 xs_attention_packed_backward_workspace_bytes = _sig("xs_attention_packed_backward_workspace_bytes", C.c_int, P(xs_attn_packed), P(i64))
-xs_attention_packed_backward = _sig("xs_attention_packed_backward", C.c_int, P(xs_attn_packed), P(xs_attn_grads), vp, i64, vp, vp)
+_attention_packed_backward = _sig("xs_attention_packed_backward", C.c_int, P(xs_attn_packed), P(xs_attn_grads), vp, i64, vp, vp)
 
 EXPORTED = ["xs_rmsnorm", "xs_rmsnorm_backward_workspace_bytes", "xs_rmsnorm_backward", "xs_balance_loss_workspace_bytes",
             "xs_balance_loss", "xs_balance_loss_backward", "xs_attention_packed_workspace_bytes", "xs_attention_packed",
@@ -325,6 +325,18 @@ def attn_packed_grads(d_o, dq, dk, dv) -> xs_attn_grads:
     g = xs_attn_grads(ptr(d_o), ptr(dq), ptr(dk), ptr(dv), *placed)
     g._refs = (d_o, dq, dk, dv)
     return g
+
+
+def xs_attention_packed_backward(a, g, workspace, workspace_bytes, dev_status, stream):
+    """The C call, which knows the gradients by their addresses and strides alone: tensors of attn_packed_grads have
+    to be of the sizes of attn_packed's descriptor, or it would write past them."""
+    d, t = (getattr(x, "_obj", x) for x in (a, g))      # of a byref()
+    tensors, of = getattr(t, "_refs", None), getattr(d, "_refs", None)
+    if tensors and isinstance(d, xs_attn_packed):
+        for x, rows, heads in zip(tensors, (d.Tq, d.Tq, d.Tk, d.Tk), (d.heads, d.heads, d.kv_heads, d.kv_heads)):
+            if x.shape != (rows, heads, d.head_dim) or (of and x.device != of[0].device):
+                raise ValueError("d_o and dq have to be of q's shape, dk and dv of k's, on their device")
+    return _attention_packed_backward(a, g, workspace, workspace_bytes, dev_status, stream)
 
 
 def workspace(query, *args, device=None):

@@ -153,3 +153,27 @@ def test_binding_refuses_other_layouts():
     for bad in ((q[0], q, k, k), (q, q[:3], k, k), (q, q, k, k[:5]), (q, q, k[..., :64], k[..., :64]), (q.float(), q, k, k)):
         with pytest.raises(ValueError):
             X.attn_packed_grads(*bad)
+
+
+def test_gradients_of_another_shape_than_the_forward_call_s():
+    # the C call has pointers and strides alone: its binding compares the tensors' shapes with the descriptor before
+    import torch
+    X = xs()
+    t = lambda *shape, **kw: torch.zeros(shape, dtype=torch.bfloat16, **kw)
+    i32 = torch.zeros(3, dtype=torch.int32)
+    a = X.attn_packed(t(40, 4, 128), t(60, 2, 128), t(60, 2, 128), t(40, 4, 128), i32, i32, lse=torch.zeros(4, 40))
+    q, k, meta = (40, 4, 128), (60, 2, 128), dict(device="meta")
+    call = lambda g, a=a: X.xs_attention_packed_backward(a, g, None, 0, None, None)
+    grads = lambda q, k, **kw: X.attn_packed_grads(t(*q, **kw), t(*q, **kw), t(*k, **kw), t(*k, **kw))
+    assert call(grads(q, k)) == X.XS_EWORKSPACE
+    assert call(C.byref(grads(q, k)), C.byref(a)) == X.XS_EWORKSPACE
+    for bad in (((39, 4, 128), k), ((40, 3, 128), k), (q, (59, 2, 128)), (q, (60, 1, 128)), ((40, 4, 64), (60, 2, 64)), ((41, 4, 128), k)):
+        g = grads(*bad)
+        for args in ((g, a), (C.byref(g), a), (g, C.byref(a))):
+            with pytest.raises(ValueError):
+                call(*args)
+    with pytest.raises(ValueError):
+        call(grads(q, k, **meta))
+    # descriptors that were filled in by hand have no tensors to compare
+    assert X.xs_attention_packed_backward(_attn(), X.xs_attn_grads(A, A, A, A, 1024, 128, 1024, 128, 256, 128, 256, 128), None, 0, None, None) == X.XS_EWORKSPACE
+    assert X.xs_attention_packed_backward(None, None, None, 0, None, None) == X.XS_EINVAL
