@@ -356,6 +356,7 @@ extern "C" int xs_rmsnorm(const void* x, int64_t ldx, const void* residual, int6
   const auto shifted = [](const void* o, int64_t ldo, const void* i, int64_t ldi) { return o && o == i && ldo != ldi; };
   if (shifted(h, ld_h, x, ldx) || shifted(h, ld_h, residual, ld_res) || shifted(y, ld_y, x, ldx) || shifted(y, ld_y, residual, ld_res))
     return XS_EINVAL;
+  if (h && h == y) return XS_EINVAL;
   if (rows == 0) return XS_OK;
   const norm::Args a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(residual), ldx, ld_res, weight,
                      weight_type == XS_TYPE_F32, eps, rows, cols, static_cast<uint16_t*>(h), static_cast<uint16_t*>(y), ld_h, ld_y,

@@ -29,6 +29,15 @@ def test_rmsnorm():
     assert f(rows=0) == f(rows=0, x=None, r=None, h=None, y=None, c=None, s=None) == X.XS_OK
 
 
+def test_rmsnorm_h_and_y_are_not_one_matrix():
+    # y in the place of h would take the residual stream away
+    X = xs()
+    f = lambda h, y, ld=256, x=A, rows=4: X.xs_rmsnorm(x, 256, A, 256, A, X.XS_TYPE_F32, 1e-6, rows, 256, h, 256, y, ld, None, 0, None, 0, None)
+    for bad in (dict(h=2 * A, y=2 * A), dict(h=2 * A, y=2 * A, ld=264), dict(h=A, y=A), dict(h=2 * A, y=2 * A, rows=0)):
+        assert f(**bad) == X.XS_EINVAL, bad
+    assert f(h=None, y=None, rows=0) == f(h=None, y=A, rows=0) == X.XS_OK
+
+
 def test_rmsnorm_backward():
     X = xs()
 
