@@ -610,7 +610,8 @@ int xs_ulysses_copy(const void* o, int32_t heads, int32_t M, int32_t head_dim,
  *   workspace  device, 16-byte aligned, xs_attention_packed_workspace_bytes() bytes (0 for many calls: NULL then)
  * Tensors without rows (Tq or Tk 0) may be NULL.
  * A sequence whose queries do not lie in [0, Tq), whose keys do not lie in [0, Tk) or are more than max_k sets
- * XS_EBADINPUT in dev_status and is skipped. Rows of o and lse outside every sequence are not written, keys and values
+ * XS_EBADINPUT in dev_status and is skipped; where starts descend, so that other sequences' queries (for gradients: or keys)
+ * overlap, the call's outputs are not specified. Rows of o and lse outside every sequence are not written, keys and values
  * outside every sequence (also behind k_rows) are not read. A sequence's keys and values have to be finite: a query
  * may take 0 times one that causality hides from it.
  * Scores, softmax and sums are fp32; probabilities are rounded to bf16 for the second product. How keys are
