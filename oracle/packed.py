@@ -1,5 +1,5 @@
 """Oracle of attention over packed sequences with grouped heads, and of its gradients, in fp64, with bounds of
-what bf16 results computed in fp32 may differ by.
+what bf16 results computed in fp32 may differ by, each element at worst and many in the 2-norm.
 
 Pinned by explicit loops and by differences."""
 from __future__ import annotations
@@ -8,7 +8,7 @@ import math
 
 import numpy as np
 
-__all__ = ["attention", "gradients", "U"]
+__all__ = ["attention", "gradients", "deviations", "U"]
 
 U = 2.0 ** -8                 # half a step of bf16, relative
 E = 2.0 ** -24                # of fp32
@@ -87,3 +87,37 @@ def gradients(q, k, v, d_o, spans, scale=None, causal=True):
     for x in out:
         bound[x] = (1 + U) * bound[x] + U * np.abs(out[x])
     return out, bound
+
+
+def deviations(q, k, v, d_o, spans, scale=None, causal=True):
+    """Mean squares that the elements of dq, dk and dv may differ by (a dict): the sum over many of them bounds the
+    square of the 2-norm, which the bounds of gradients(), all roundings at their worst together, do not say anything
+    about (a sum of N terms may lose some sqrt(N) of them there). Roundings to bf16 are independent of each other and of mean
+    square U^2 / 3 relative to the power of two below at most; U^2 relative to the value is taken. A row's delta, d_o . o with o as it
+    was rounded (each of its columns, and each probability that went into it), is common to all of the row's dS. A score's error
+    es stands beside each rounding of P and dS."""
+    H, D = q.shape[1:]
+    G = H // k.shape[1]
+    scale = scale or 1.0 / math.sqrt(D)
+    mean = {x: np.full(t.shape, np.nan) for x, t in (("dq", q), ("dk", k), ("dv", v))}
+    for q0, n, k0, m in spans:
+        keys = slice(k0, k0 + m)
+        sums = {x: np.zeros(t[keys].shape) for x, t in (("dk", k), ("dv", v))}
+        mean["dk"][keys] = mean["dv"][keys] = 0.0
+        for h in range(H):
+            rows, kv = slice(q0, q0 + n), h // G
+            Q, K, V, dO = q[rows, h], k[keys, kv], v[keys, kv], d_o[rows, h]
+            P, o, _, es = _head(Q, K, V, scale, causal)
+            dP = dO @ V.T
+            dS = P * (dP - (dO * o).sum(1, keepdims=True))
+            u2 = U ** 2 + (2 * es) ** 2
+            m_delta = u2 * (((dO * o) ** 2).sum(1, keepdims=True) + ((P * dP) ** 2).sum(1, keepdims=True))
+            m_S = u2 * dS ** 2 + (P * ((D + 8) * E * (np.abs(dO) @ np.abs(V).T))) ** 2
+            mean["dq"][rows, h] = scale ** 2 * (m_S @ K ** 2 + m_delta * (P @ K) ** 2) + (U * scale * dS @ K) ** 2
+            mean["dk"][keys, kv] += scale ** 2 * (m_S + m_delta * P ** 2).T @ Q ** 2
+            mean["dv"][keys, kv] += u2 * (P ** 2).T @ dO ** 2
+            sums["dk"][:, kv] += scale * dS.T @ Q
+            sums["dv"][:, kv] += P.T @ dO
+        for x in sums:
+            mean[x][keys] += (U * sums[x]) ** 2
+    return mean

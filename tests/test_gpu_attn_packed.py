@@ -244,6 +244,31 @@ def test_long_sequences(lens, H, Hkv, D, layout, causal):
     c.check_backward()
 
 
+# each form of the gradients' kernels: key tiles dealt out over ranges with parts of several, and in one launch; rows by 128 and by 32
+@pytest.mark.parametrize("lens,H,Hkv,D", [([1025], 4, 1, 128), ([1025], 4, 1, 64), ([511, 1, 1030], 6, 2, 128), ([700, 900], 70, 35, 128), ([521, 503], 20, 20, 64),
+                                          ([300, 200, 0, 450], 32, 2, 128), ([300, 200, 0, 450], 32, 2, 64), ([500, 3, 97], 1, 1, 128), ([2100], 2, 1, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradients_in_the_2_norm(lens, H, Hkv, D, causal):
+    # 256 rows of a head at a time (and the whole tensor): independent roundings, so that a block of rows left out, which a bound of each
+    # element's worst case hides, stands out
+    spans, T = _packed(lens)
+    c = Case(spans, T, T, H, Hkv, D, causal=causal, seed=H + 1)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    h = c.host
+    want, _ = packed.gradients(h["q"], h["k"], h["v"], h["d_o"], spans, causal=causal)
+    mean = packed.deviations(h["q"], h["k"], h["v"], h["d_o"], spans, causal=causal)
+    for x in want:
+        off = (getattr(c, x).cpu().double().numpy() - want[x]) ** 2
+        assert off.sum() <= mean[x].sum(), f"{x}: {np.sqrt(off.sum() / mean[x].sum()):.3f} of the 2-norm"
+        for at, n, _, _ in spans:
+            for r in range(at, at + n - 63, 256):
+                rows = slice(r, min(r + 256, at + n))
+                worst = np.max(np.sqrt(off[rows].sum((0, 2)) / mean[x][rows].sum((0, 2))))
+                assert worst <= 1.0, f"{x}, rows {rows}: {worst:.3f} of the 2-norm"
+
+
 @pytest.mark.parametrize("lens", [[4200], [4100, 1, 4200]])
 @pytest.mark.parametrize("D,layout", [(128, "token"), (64, "head")])
 @pytest.mark.parametrize("causal", [True, False])

@@ -52,6 +52,39 @@ def test_attention_gradients_by_differences(causal):
     assert all((b[np.isfinite(b)] >= 0).all() for b in bound.values())
 
 
+def _bf16(x):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(x)).bfloat16().double().numpy()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_deviations_hold_roundings_and_not_a_block_left_out(causal):
+    # the kernels' roundings made in fp64, as they are and with 32 rows of one head missing from 32 keys' dk and dv
+    T, H, D = 520, 4, 64
+    rng = np.random.default_rng(3)
+    q, k, v = (_bf16(t) for t in _qkv(rng, T, T, H, 1, D))
+    d_o = _bf16(rng.standard_normal(q.shape))
+    spans = [(0, T, 0, T)]
+    want, _ = packed.gradients(q, k, v, d_o, spans, causal=causal)
+    mean = packed.deviations(q, k, v, d_o, spans, causal=causal)
+    scale = D ** -0.5
+    for missing in (False, True):
+        got = {x: np.zeros(t.shape) for x, t in want.items()}
+        for h in range(H):
+            P, _, _, _ = packed._head(q[:, h], k[:, 0], v[:, 0], scale, causal)
+            o = _bf16(_bf16(P) @ v[:, 0])
+            dS = _bf16(P * (d_o[:, h] @ v[:, 0].T - (d_o[:, h] * o).sum(1, keepdims=True)))
+            P = _bf16(P)
+            got["dq"][:, h] = scale * dS @ k[:, 0]
+            if missing and h == 1:
+                P[448:480, 32:64] = dS[448:480, 32:64] = 0
+            got["dk"][:, 0] += scale * dS.T @ q[:, h]
+            got["dv"][:, 0] += P.T @ d_o[:, h]
+        for x in got:
+            off, allowed = np.linalg.norm(_bf16(got[x]) - want[x]), math.sqrt(mean[x].sum())
+            assert off < 0.6 * allowed if not missing or x == "dq" else off > 1.2 * allowed, x
+
+
 def test_norm_by_loops_and_differences():
     rng = np.random.default_rng(2)
     h, w, dy, dh = rng.standard_normal((3, 8)), rng.standard_normal(8), rng.standard_normal((3, 8)), rng.standard_normal((3, 8))
