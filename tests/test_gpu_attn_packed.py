@@ -378,6 +378,44 @@ def test_gradients_are_the_differences_of_the_forward_call():
         assert abs((ends[0][0] - ends[1][0]) - along) <= noise + (0.0 if x == "v" else 0.25 * size), x
 
 
+@pytest.mark.parametrize("lens,H,Hkv,D", [([48, 17], 2, 1, 64), ([300, 1, 40], 4, 2, 128), ([130, 61], 24, 24, 64)])
+def test_gradients_are_the_slope_of_the_forward_call(lens, H, Hkv, D):
+    """The call's own o along +-1/8 of the sign of the (fp64) gradient, so that the change is the sum of all its magnitudes and
+    every element's counts. Values of one key lie close together and d_o is positive: the change is large beside the roundings of o, all taken
+    at their worst, as are the gradients'; the differences' curvature is the fp64 function's at the same points."""
+    spans, T = _packed(lens)
+    c = Case(spans, T, T, H, Hkv, D)
+    g = torch.Generator().manual_seed(5)
+    c.v.copy_((torch.randn((T, Hkv, 1), generator=g) + 0.25 * torch.randn((T, Hkv, D), generator=g)).bfloat16())
+    c.d_o.copy_((0.5 + torch.rand((T, H, D), generator=g)).bfloat16())
+    at = {n: getattr(c, n).cpu().double().numpy() for n in ("q", "k", "v", "d_o")}
+    want, bound = packed.gradients(at["q"], at["k"], at["v"], at["d_o"], spans)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    for x in "qkv":
+        t, base = getattr(c, x), getattr(c, x).clone()
+        got = getattr(c, "d" + x).cpu().double().numpy()
+        ends, exact, points, noise = [], [], [], 0.0
+        for s in (1, -1):
+            t.copy_(base + s * 0.125 * torch.sign(torch.from_numpy(want["d" + x])).cuda().bfloat16())
+            c.forward()
+            torch.cuda.synchronize()
+            points.append(t.cpu().double().numpy())
+            o, bo, _, _ = packed.attention(*({**at, x: points[-1]}[n] for n in "qkv"), spans)
+            ends.append((c.o.cpu().double().numpy() * at["d_o"]).sum())
+            exact.append((o * at["d_o"]).sum())
+            noise += (bo * np.abs(at["d_o"])).sum()
+        t.copy_(base)
+        moved = points[0] - points[1]               # between the points reached: some sums were rounded
+        slope = (want["d" + x] * moved).sum()
+        tolerance = noise + (bound["d" + x] * np.abs(moved)).sum() + abs(exact[0] - exact[1] - slope)
+        assert 4 * tolerance < slope, x              # so that a gradient negated, halved, doubled or of zeros is told from it
+        off = lambda grad: abs(ends[0] - ends[1] - (grad * moved).sum())
+        assert off(got) <= tolerance, x
+        assert all(off(w * got) > tolerance for w in (-1.0, 0.0, 0.5, 2.0)), x
+
+
 @pytest.mark.parametrize("what", ["q descends", "q past the end", "keys before the start", "keys past the end", "more than max_k", "negative rows"])
 def test_bad_sequences_are_skipped(what):
     X = xs()
