@@ -218,13 +218,6 @@ __device__ __forceinline__ f32x16 rows_product(const lds_char* tile, int b, cons
   return acc;
 }
 
-// acc[column of the tile][lane's column] += sum over 16 rows of the tile, from row 16 s
-template <int D, Way WAY>
-__device__ __forceinline__ void cols_product(const lds_char* tile, int s, const ColReads<D, WAY>& rd, bf16x8 b, f32x16 (&acc)[D / 32]) {
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db) mma(acc[db], col_operand<D>(tile, s, rd, db), b);
-}
-
 // Accumulator entry e of a 32-row block is row 8 (e / 4) + 4 (lane / 32) + e % 4.
 __device__ __forceinline__ int entry_row(int e, int up) { return 8 * (e >> 2) + 4 * up + (e & 3); }
 

@@ -56,7 +56,7 @@ struct GradArgs {
 
 template <typename A>
 __device__ __forceinline__ bool find(const A& a, int t, PackedTile* out) {
-  if (a.start) return packed_tile(a.start, a.n_seq, a.T, 1, a.chunk, t, out, a.status);
+  if (a.start) return packed_tile(a.start, a.n_seq, a.T, a.chunk, t, out, a.status);
   *out = PackedTile{0, t, 0, a.T};
   return static_cast<int64_t>(t) * a.chunk < a.T;
 }

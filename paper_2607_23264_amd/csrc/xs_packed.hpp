@@ -32,10 +32,10 @@ __device__ __forceinline__ T wave_scan(T v) {
   return add_dpp<0x143, 0xc>(v);    // row_bcast 31 to rows 2 and 3
 }
 
-// The t-th tile of all sequences, ceil(rows mult / per) of each; false past the last. A sequence that does not
+// The t-th tile of all sequences, ceil(rows / per) of each; false past the last. A sequence that does not
 // lie in [0, T) sets XS_EBADINPUT and has no tiles. Every wave of a workgroup finds it by itself: 64 sequences a
 // step, one a lane, which are two loads and a scan (n_seq <= 64), and no launch before that lists the tiles.
-__device__ __forceinline__ bool packed_tile(const int32_t* __restrict__ start, int n_seq, int T, int mult, int per, int t,
+__device__ __forceinline__ bool packed_tile(const int32_t* __restrict__ start, int n_seq, int T, int per, int t,
                                             PackedTile* out, int32_t* status) {
   const int lane = threadIdx.x & 63;
   int before = 0;
@@ -50,7 +50,7 @@ __device__ __forceinline__ bool packed_tile(const int32_t* __restrict__ start, i
       set_status(status, XS_EBADINPUT);
       b = a;
     }
-    const int tiles = static_cast<int>((static_cast<int64_t>(b - a) * mult + per - 1) / per);
+    const int tiles = static_cast<int>((static_cast<int64_t>(b - a) + per - 1) / per);
     const int upto = wave_scan(tiles);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(before + upto > t);
     if (hit) {
@@ -66,7 +66,7 @@ __device__ __forceinline__ bool packed_tile(const int32_t* __restrict__ start, i
   return false;
 }
 
-// At least as many tiles as packed_tile finds, from what the host knows.
+// At least as many tiles as sequences of T rows together have, `mult` rows of tiles to a row and `per` to a tile.
 inline __host__ int64_t packed_tiles_bound(int64_t T, int64_t n_seq, int64_t mult, int64_t per) {
   const int64_t whole = T * mult / per + n_seq;
   return whole < T * mult ? whole : T * mult;
