@@ -107,33 +107,41 @@ __device__ __forceinline__ void load_row(const void* m, int64_t at, int E, int s
   }
 }
 
-// Logits to shares p and, for sigmoid scores, rest = 1 - s (as 1 / (1 + e^l), which a score near 1 does not cancel).
+// Logits x to shares p and, for sigmoid scores, rest = 1 - s (as 1 / (1 + e^x), which a score near 1 does not cancel).
+// Scores below 2^-126 come out as 0 (the reciprocal does not give smaller numbers). Where a token's sum to less than 2^-64 each is e^x but for 2^-64
+// of it, and the shares are those of a softmax.
 template <int LPT, int EPL, bool REST>
-__device__ __forceinline__ void shares(bool sigmoid, float (&p)[EPL], float (&rest)[REST ? EPL : 1]) {
+__device__ __forceinline__ void shares(bool sigmoid, const float (&x)[EPL], float (&p)[EPL], float (&rest)[REST ? EPL : 1]) {
   constexpr float kLog2e = 1.4426950408889634f;
   float total = 0.f;
+  // e^(x - the token's largest x) into p, and their sum
+  auto exponentials = [&] {
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < EPL; ++i) top = fmaxf(top, x[i]);
+    top = lanes_max<LPT>(top);
+    if (top == -INFINITY) top = 0.f;          // every expert masked: all shares 0
+    total = 0.f;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      p[i] = __builtin_amdgcn_exp2f((x[i] - top) * kLog2e);
+      total += p[i];
+    }
+    total = lanes_sum<LPT>(total);
+  };
   if (sigmoid) {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
       // the reciprocal of one unit in the last place, which is what exp2 has too: a quotient takes ten instructions
-      const float x = p[i];
-      p[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * kLog2e));
-      if constexpr (REST) rest[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * kLog2e));
+      p[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x[i] * kLog2e));
+      if constexpr (REST) rest[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * kLog2e));
       total += p[i];
     }
+    total = lanes_sum<LPT>(total);
+    if (__builtin_expect(total < 0x1p-64f, 0)) exponentials();      // the same in all lanes of the token
   } else {
-    float top = p[0];
-#pragma unroll
-    for (int i = 1; i < EPL; ++i) top = fmaxf(top, p[i]);
-    top = lanes_max<LPT>(top);
-    if (top == -INFINITY) top = 0.f;          // every expert masked: all shares 0
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      p[i] = __builtin_amdgcn_exp2f((p[i] - top) * kLog2e);
-      total += p[i];
-    }
+    exponentials();
   }
-  total = lanes_sum<LPT>(total);
   const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) p[i] *= inv;
@@ -163,11 +171,11 @@ __global__ __launch_bounds__(256) void sums_kernel(Args a) {
 #pragma unroll
   for (int i = 0; i < EPL; ++i) acc[i] = 0.f;
   for (int t = grp; t < n; t += kGroups) {
-    float p[EPL], none[1];
+    float x[EPL], p[EPL], none[1];
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) p[i] = next[i];
+    for (int i = 0; i < EPL; ++i) x[i] = next[i];
     load_row<LT, V, LPT, EPL>(a.logits, (t0 + min(t + kGroups, n - 1)) * a.ld, a.E, sub, -INFINITY, next);
-    shares<LPT, EPL, false>(a.sigmoid, p, none);
+    shares<LPT, EPL, false>(a.sigmoid, x, p, none);
 #pragma unroll
     for (int i = 0; i < EPL; ++i) acc[i] += p[i];
   }
@@ -301,10 +309,10 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs a) {
     c[i] = e < a.E ? unit * static_cast<float>(a.counts[static_cast<int64_t>(s.seq) * a.E + e]) : 0.f;
   }
   for (int t = grp; t < n; t += kGroups) {
-    float p[EPL], rest[EPL], add[EPL];
-    load_row<LT, V, LPT, EPL>(a.logits, (t0 + t) * a.ld, a.E, sub, -INFINITY, p);
+    float x[EPL], p[EPL], rest[EPL], add[EPL];
+    load_row<LT, V, LPT, EPL>(a.logits, (t0 + t) * a.ld, a.E, sub, -INFINITY, x);
     load_row<LT, V, LPT, EPL>(a.d_add, (t0 + t) * a.ld_add, a.d_add ? a.E : 0, sub, 0.f, add);
-    shares<LPT, EPL, true>(a.sigmoid, p, rest);
+    shares<LPT, EPL, true>(a.sigmoid, x, p, rest);
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) dot = __builtin_fmaf(c[i], p[i], dot);

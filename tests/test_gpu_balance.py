@@ -107,6 +107,41 @@ def test_loss_and_gradient(T, E, k, starts, kind, dtype, pad):
     assert torch.equal(add[:, :E][torch.from_numpy(used).cuda()], out[:T, :E][torch.from_numpy(used).cuda()])
 
 
+@pytest.mark.parametrize("E,pad", [(16, 0), (60, 3), (256, 0), (700, 0)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sigmoid_shares_of_tokens_whose_scores_are_all_small(E, pad, dtype):
+    """Scores far below the smallest normal number still have shares; a token a sequence, so that the mean is its shares. A score's
+    exponential takes x log2 e, off by 2^-23 |x| relative (the product's rounding and the constant's), |x| at most 64 + 16 where a token's scores are
+    large enough to be added as they are, and 2^-21 of its own; a share has two of them and the sum's 64 + 10 roundings."""
+    X = xs()
+    g = torch.Generator().manual_seed(E)
+    shift = torch.tensor([0.0, -30.0, -44.0, -45.0, -60.0, -80.0, -86.9, -87.4, -88.0, -88.8, -95.0, -104.0, -200.0, -600.0])
+    l = (torch.randn((len(shift), E), generator=g) * 2 + shift[:, None]).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    l[:, 1] = -float("inf")
+    l[8, 2:] = -float("inf")
+    T, k = len(shift), 3
+    full = torch.full((T, E + pad), float("nan"), dtype=l.dtype)
+    full[:, :E] = l
+    l64, dev, gt = l.double().numpy(), full.cuda(), _gate(E, k, "sigmoid", dtype)
+    idx = np.tile(np.array([[0, 2, 5]], dtype=np.int32), (T, 1))
+    starts = list(range(T + 1))
+    counts, mean, loss, st, status = _forward(gt, dev, torch.from_numpy(idx).cuda(), starts, T)
+    _, wm, wl = balance.loss(l64, idx, starts, "sigmoid", ALPHA)
+    rel = 2 * (80 * 2.0 ** -23 + 2.0 ** -21) + 74 * 2.0 ** -24
+    assert status == 0 and np.allclose(wm.sum(1), 1.0)
+    assert np.all(np.abs(mean.cpu().double().numpy() - wm) <= rel * wm + 1e-38)
+    assert np.all(np.abs(loss.cpu().double().numpy() - wl) <= (rel + 2.0 ** -13) * wl)
+    d_loss = torch.randn(T, generator=g)
+    want, mag = balance.backward(l64, counts.cpu().numpy(), k, starts, "sigmoid", ALPHA, d_loss.double().numpy())
+    out, dl = torch.full((T, E + pad), S, dtype=dev.dtype, device="cuda"), d_loss.cuda()
+    X.check(X.xs_balance_loss_backward(gt, dev.data_ptr(), dev.stride(0), T, st.data_ptr(), T, ALPHA, counts.data_ptr(), dl.data_ptr(), None, 0, out.data_ptr(),
+                                       out.stride(0), None, _stream()))
+    torch.cuda.synchronize()
+    got = out[:, :E].cpu().double().numpy()
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    assert np.all(np.abs(got - want) <= half * np.abs(want) + (4 * rel + 2.0 ** -15) * mag + 1e-38)
+
+
 def test_one_sequence_without_starts_equals_it_with_them():
     X = xs()
     T, E, k = 777, 160, 6
