@@ -138,7 +138,7 @@ __device__ __forceinline__ void shares(bool sigmoid, const float (&x)[EPL], floa
       total += p[i];
     }
     total = lanes_sum<LPT>(total);
-    if (__builtin_expect(total < 0x1p-64f, 0)) exponentials();      // the same in all lanes of the token
+    if (total < 0x1p-64f) exponentials();      // the same in all lanes of the token
   } else {
     exponentials();
   }
