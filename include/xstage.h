@@ -780,9 +780,9 @@ int xs_swiglu_fp8_backward(const void* ck_codes, int64_t ld_ck, const float* ck_
  *   y            bf16 [rows][cols] or NULL; as h, and not h
  *   codes, scales  y in E4M3 with 1 x 128 blocks, laid out as by xs_quantize_fp8 (from y's fp32 values, not from the
  *                bf16 ones), or both NULL. One of y and codes is wanted. With no rows all of them may be NULL.
- * h is rounded first and the rest is fp32, rounded once. Every matrix has 16-byte aligned rows; eps >= 0 (a
- * row of zeros under eps = 0 gives NaN). cols a multiple of 8, at most 32768, rows below 2^31, else XS_EUNSUPPORTED; XS_EINVAL
- * on other bad arguments; nothing is launched on an error. */
+ * h is rounded first and the rest is fp32, rounded once; squares that leave fp32's range are taken of scaled values. Every matrix has
+ * 16-byte aligned rows; eps >= 0 (under eps = 0 a row of zeros gives NaN, one of subnormal numbers infinities). cols a multiple
+ * of 8, at most 32768, rows below 2^31, else XS_EUNSUPPORTED; XS_EINVAL on other bad arguments; nothing is launched on an error. */
 int xs_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld_res, const void* weight,
                int32_t weight_type, float eps, int64_t rows, int32_t cols, void* h, int64_t ld_h, void* y,
                int64_t ld_y, void* codes, int64_t ld_codes, float* scales, int64_t ld_scales, void* stream);

@@ -13,6 +13,7 @@
 //
 // Bound by memory: 16,381 x 7168 with the residual, bf16 and E4M3 results 197 us, 5.4 TB/s (a large copy: 4.9), its gradients 202 us, 4.65 TB/s, and 5.7 to
 // add dw up; 24 rows 4.3 us, a chain of two loads, a sum and a store.
+#include <cfloat>
 #include <cmath>
 
 #include "xs_common.hpp"
@@ -58,22 +59,26 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// Eight weights of columns col .. + 7 as fp32.
+// Eight weights of columns col .. + 7 as fp32. The compiler keeps every piece's address, two registers each, over a loop of rows; unless HELD it
+// gets an offset from the scalar address anew. (Gradients of 16,381 x 7168: held 208 us, anew 193; a wave a row, 8000 x 2048: 39.1 and 41.4.)
 struct W8 {
   float v[8];
 };
+template <bool HELD>
 __device__ __forceinline__ W8 weights8(const void* w, int w32, int col) {
   W8 o;
+  uint32_t at = static_cast<uint32_t>(col);
+  if constexpr (!HELD) asm volatile("" : "+v"(at));
   if (w32) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(w) + col);
-    const f32x4 b = *reinterpret_cast<const f32x4*>(static_cast<const float*>(w) + col + 4);
+    const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const char*>(w) + at * 4);
+    const f32x4 b = *reinterpret_cast<const f32x4*>(static_cast<const char*>(w) + at * 4 + 16);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       o.v[e] = a[e];
       o.v[4 + e] = b[e];
     }
   } else {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(w) + col);
+    const u32x4 a = *reinterpret_cast<const u32x4*>(static_cast<const char*>(w) + at * 2);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       o.v[2 * e] = bf_lo(a[e]);
@@ -98,6 +103,13 @@ __device__ __forceinline__ float row_sum(float v, float* red, int row) {
   return v;
 }
 
+// The power of two that a row's values are multiplied with before they are squared: 1, unless the sum ss of their squares has left fp32's range.
+// 2^-80 where it is infinite (a value of 2^56 or more; the largest are below 2^48 then), 2^80 where the mean and eps are below 2^-80, so
+// that squares which fp32 does not hold may weigh in it (values below 2^-32, then below 2^48).
+__device__ __forceinline__ float unit_of(float ss, float n, float eps) {
+  return !(ss <= FLT_MAX) ? 0x1p-80f : ss < 0x1p-80f * n && eps < 0x1p-80f ? 0x1p80f : 1.f;
+}
+
 // EARLY: the weights are read with the row, not behind its sum (few rows, where a kernel's time is its chain of loads).
 template <int NT, int NP, int RP, bool EARLY>
 __global__ __launch_bounds__(NT * RP) void norm_kernel(Args a) {
@@ -115,7 +127,7 @@ __global__ __launch_bounds__(NT * RP) void norm_kernel(Args a) {
     h[p] = kZero4;
     if (live && col < a.cols) {
       h[p] = *reinterpret_cast<const u32x4*>(a.x + row * a.ldx + col);
-      if constexpr (EARLY) early[p] = weights8(a.w, a.w32, col);
+      if constexpr (EARLY) early[p] = weights8<false>(a.w, a.w32, col);
       if (a.r) {
         const u32x4 r = *reinterpret_cast<const u32x4*>(a.r + row * a.ldr + col);
 #pragma unroll
@@ -126,14 +138,29 @@ __global__ __launch_bounds__(NT * RP) void norm_kernel(Args a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) ss = __builtin_fmaf(bf_lo(h[p][e]), bf_lo(h[p][e]), __builtin_fmaf(bf_hi(h[p][e]), bf_hi(h[p][e]), ss));
   }
-  const float inv = 1.f / sqrtf(row_sum<NT>(ss, red, in) / static_cast<float>(a.cols) + a.eps);
+  const float n = static_cast<float>(a.cols);
+  ss = row_sum<NT>(ss, red, in);
+  const float k = unit_of(ss, n, a.eps);
+  if (k != 1.f) {            // the same in the whole row, which is a wave or the workgroup
+    if (NT > 64) __syncthreads();                 // the first sums have been read
+    ss = 0.f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float h0 = bf_lo(h[p][e]) * k, h1 = bf_hi(h[p][e]) * k;
+        ss = __builtin_fmaf(h0, h0, __builtin_fmaf(h1, h1, ss));
+      }
+    ss = row_sum<NT>(ss, red, in);
+  }
+  const float inv = k / sqrtf(ss / n + a.eps * k * k);
   const int padded = (a.cols + 127) & ~127;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int col = (p * NT + t) * 8;
     float y[8] = {};
     if (col < a.cols) {
-      const W8 w = EARLY ? early[EARLY ? p : 0] : weights8(a.w, a.w32, col);
+      const W8 w = EARLY ? early[EARLY ? p : 0] : weights8<false>(a.w, a.w32, col);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         y[2 * e] = bf_lo(h[p][e]) * inv * w.v[2 * e];
@@ -174,7 +201,6 @@ __global__ __launch_bounds__(NT * RP) void norm_grad_kernel(GradArgs a) {
     const int64_t row = base + in;
     const bool live = row < a.rows;
     u32x4 h[NP], dy[NP], dh[NP];
-    float ss = 0.f, sg = 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int col = (p * NT + t) * 8;
@@ -185,11 +211,12 @@ __global__ __launch_bounds__(NT * RP) void norm_grad_kernel(GradArgs a) {
         if (a.dh) dh[p] = *reinterpret_cast<const u32x4*>(a.dh + row * a.lddh + col);
       }
     }
+    float ss = 0.f, sg = 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int col = (p * NT + t) * 8;
       if (col < a.cols) {
-        const W8 w = weights8(a.w, a.w32, col);
+        const W8 w = weights8<NT == 64>(a.w, a.w32, col);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float h0 = bf_lo(h[p][e]), h1 = bf_hi(h[p][e]);
@@ -201,13 +228,43 @@ __global__ __launch_bounds__(NT * RP) void norm_grad_kernel(GradArgs a) {
     if (NT > 64) __syncthreads();                  // the last row's sums have been read
     ss = row_sum<NT>(ss, red[0], in);
     sg = row_sum<NT>(sg, red[1], in);
-    const float inv = 1.f / sqrtf(ss / n + a.eps);
-    const float c = sg * inv / n * inv;             // of h, inside the brackets: u sum(g u) / n = h i (sg i) / n
+    const float k = unit_of(ss, n, a.eps);
+    bool again = k != 1.f;
+    if constexpr (NT > 64 && RP > 1) {             // of any of the workgroup's rows
+#pragma unroll
+      for (int r = 0; r < RP; ++r) {
+        float other = 0.f;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) other += red[0][r * (NT / 64) + i];
+        again |= unit_of(other, n, a.eps) != 1.f;
+      }
+    }
+    if (again) {
+      ss = sg = 0.f;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int col = (p * NT + t) * 8;
+        if (col < a.cols) {
+          const W8 w = weights8<NT == 64>(a.w, a.w32, col);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float h0 = bf_lo(h[p][e]) * k, h1 = bf_hi(h[p][e]) * k;
+            ss = __builtin_fmaf(h0, h0, __builtin_fmaf(h1, h1, ss));
+            sg = __builtin_fmaf(bf_lo(dy[p][e]) * w.v[2 * e], h0, __builtin_fmaf(bf_hi(dy[p][e]) * w.v[2 * e + 1], h1, sg));
+          }
+        }
+      }
+      if (NT > 64) __syncthreads();                // the first sums have been read
+      ss = row_sum<NT>(ss, red[0], in);
+      sg = row_sum<NT>(sg, red[1], in);
+    }
+    const float root = 1.f / sqrtf(ss / n + a.eps * k * k), inv = k * root;
+    const float c = sg * root / n * inv;            // of h, inside the brackets: u sum(g u) / n = h i (sg i) / n
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int col = (p * NT + t) * 8;
       if (col >= a.cols) continue;
-      const W8 w = weights8(a.w, a.w32, col);
+      const W8 w = weights8<NT == 64>(a.w, a.w32, col);
       u32x4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {

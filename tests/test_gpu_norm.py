@@ -133,6 +133,42 @@ def test_gradient(rows, cols, extra, kind, pad):
     assert torch.equal(b[:, :cols], dx[:rows, :cols])
 
 
+# each width of the forms of few rows and of many
+@pytest.mark.parametrize("rows,cols", [(33, 512), (33, 1024), (33, 7168), (33, 16384), (33, 20000), (300, 520), (300, 2048), (300, 3080), (300, 8192), (300, 9000),
+                                       (257, 32768)])
+@pytest.mark.parametrize("eps", [0.0, EPS])
+def test_rows_whose_squares_leave_the_range_of_fp32(rows, cols, eps):
+    """Rows of values around 2^-110 to 2^110, one large value among small ones, and rows beside them as ever: a row's mean square and its
+    product with the gradient come from values times a power of two, which is exact. Tolerances as above."""
+    X = xs()
+    e = torch.tensor([0, 110, -110, 0, 56, 60, 63, 64, 90, -40, -50, -60, -64, -75, -100, 10])[torch.arange(rows) % 16]
+    h = (_rand(rows, cols, 1).float() * torch.exp2(e.float())[:, None]).bfloat16()
+    h[3], h[3, 5] = 2.0 ** -20, 2.0 ** 100
+    dy, w = _rand(rows, cols, 2, 1e-2), _weight(cols, "f32")
+    y64 = norm.norm(h.double().numpy(), w.double().numpy(), eps)
+    hd, wd, gd = h.cuda(), w.cuda(), dy.cuda()
+    blocks = -(-cols // 128)
+    y = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    codes, scales = torch.zeros((rows, blocks * 128), dtype=torch.uint8, device="cuda"), torch.zeros((rows, -(-blocks // 4) * 4), device="cuda")
+    X.check(X.xs_rmsnorm(hd.data_ptr(), cols, None, 0, wd.data_ptr(), X.XS_TYPE_F32, eps, rows, cols, None, 0, y.data_ptr(), cols, codes.data_ptr(),
+                         codes.stride(0), scales.data_ptr(), scales.stride(0), _stream()))
+    torch.cuda.synchronize()
+    # below the normal numbers of bf16 half a step is 2^-134
+    assert np.all(np.abs(y.cpu().double().numpy() - y64) <= (2.0 ** -8 + 2.0 ** -17) * np.abs(y64) + 2.0 ** -133)
+    full = np.zeros((rows, blocks * 128))
+    full[:, :cols] = y64
+    amax = np.maximum(np.abs(full.reshape(rows, blocks, 128)).max(2), 2.0 ** -60) / 448
+    assert np.all(np.abs(scales[:, :blocks].cpu().double().numpy() - amax) <= 2.0 ** -16 * amax)
+    want, want_w, mag, mag_w = norm.backward(h.double().numpy(), w.double().numpy(), dy.double().numpy(), eps)
+    ws = X.workspace(X.xs_rmsnorm_backward_workspace_bytes, rows, cols)
+    dx, dw = torch.zeros_like(y), torch.zeros(cols, device="cuda")
+    X.check(X.xs_rmsnorm_backward(gd.data_ptr(), cols, None, 0, hd.data_ptr(), cols, wd.data_ptr(), X.XS_TYPE_F32, eps, rows, cols, dx.data_ptr(), cols,
+                                  dw.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
+    torch.cuda.synchronize()
+    assert np.all(np.abs(dx.cpu().double().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -15 * mag + 2.0 ** -133)
+    assert np.all(np.abs(dw.cpu().double().numpy() - want_w) <= ((rows + 64) * 2.0 ** -24 + 2.0 ** -16) * mag_w)
+
+
 def test_in_place_and_no_rows():
     X = xs()
     rows, cols = 33, 1024
