@@ -605,7 +605,7 @@ int xs_ulysses_copy(const void* o, int32_t heads, int32_t M, int32_t head_dim,
  *   lse      device fp32 [heads][Tq] out, or NULL
  *   q_start  device int32 [n_seq + 1]; k_start device int32 [n_seq + 1], with k_rows [n_seq]; k_rows device int32 [n_seq] or NULL
  *   Tq, Tk   rows of q and o, of k and v
- *   max_k    the most keys of a sequence (0: Tk)
+ *   max_k    the most keys of a sequence (0: Tk); without k_rows the kernels are chosen for 2 Tk / n_seq keys at most
  *   scale    0 = 1 / sqrt(head_dim)
  *   workspace  device, 16-byte aligned, xs_attention_packed_workspace_bytes() bytes (0 for many calls: NULL then)
  * Tensors without rows (Tq or Tk 0) may be NULL.
@@ -614,6 +614,8 @@ int xs_ulysses_copy(const void* o, int32_t heads, int32_t M, int32_t head_dim,
  * overlap, the call's outputs are not specified. Rows of o and lse outside every sequence are not written, keys and values
  * outside every sequence (also behind k_rows) are not read. A sequence's keys and values have to be finite: a query
  * may take 0 times one that causality hides from it.
+ * Sequences are looked up by each workgroup: with some thousand of them that takes longer than short caches or prompts do (one token
+ * each of 4096 caches of 64 keys, 32 heads over 8: 1.9 ms).
  * Scores, softmax and sums are fp32; probabilities are rounded to bf16 for the second product. How keys are
  * split over workgroups follows from the lengths, the descriptor and the device's CU count alone.
  * Requires head_dim 64 or 128, row strides of at most 2^23 elements, heads <= 65536, Tq heads / kv_heads < 2^30, Tq heads < 2^34, Tk <= 2^30, Tk kv_heads <

@@ -1737,7 +1737,8 @@ int check(const xs_attn_packed* A, pattn::Args* a) {
   return XS_OK;
 }
 
-// How many keys a long sequence has, as far as the host knows: a prompt's about twice their average, a cache is taken to be full.
+// How many keys a long sequence has, as far as the host knows: a prompt's about twice their average, a cache is taken to be full. (max_k only lowers it:
+// one long prompt among many short ones is taken for a short one, and its tiles follow each other in a few workgroups.)
 int64_t long_keys(const pattn::Args& a) { return a.k_rows ? a.max_k : std::min<int64_t>(a.max_k, 2 * int64_t(a.Tk) / a.n_seq); }
 int64_t row_tiles(const pattn::Args& a) { return packed_tiles_bound(a.Tq, a.n_seq, a.G, 128) * a.Hkv; }
 // Eight waves a tile of rows where the tiles are few and long (one prompt of 1000 tokens, 8 heads: rows 25.6 -> 21.5 us, dq 28.9 -> 25.6;
@@ -1746,7 +1747,7 @@ bool pairs(const pattn::Args& a) { return long_keys(a) > 768 && 2 * row_tiles(a)
 
 // Eight waves for 32 rows where these fill the chip once, twice if they are long: an eighth of the keys each (one prompt, us by rows or dealt out and so:
 // 8 heads of 100 tokens 8.1 and 5.6, 512: 15.6 and 9.8, 1000: 21.3 and 11.7, 2000: 36 and 27; one head of 5000 33 and 26; four of 250, 10 heads: 11.3
-// and 10.3, 12 heads: 11.4 and 12.5; two of 1000, 8 heads: 22 both; 128 tokens over a cache of 4000, 8 heads: 25 and 22).
+// and 10.3, 12 heads: 11.4 and 12.5, the limit between them leaves 10 heads, 350 units, by rows; two of 1000, 8 heads: 22 both; 128 tokens over a cache of 4000, 8 heads: 25 and 22).
 bool few_units(const pattn::Args& a) {
   const int64_t units = packed_tiles_bound(a.Tq, a.n_seq, a.G, 32) * a.Hkv, cus = xs_host::num_cus(), keys = long_keys(a);
   return keys <= 4096 && (3 * units <= 4 * cus || (keys > 768 && units <= 2 * cus));

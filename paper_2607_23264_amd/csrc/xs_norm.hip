@@ -11,7 +11,7 @@
 // A row is NT threads' pieces of eight values (16 bytes), held in registers from the one read to the
 // write; sixteen lanes hold a block of 128 and take its scale.
 //
-// Bound by memory: 16,381 x 7168 with the residual, bf16 and E4M3 results 197 us, 5.4 TB/s (a large copy: 4.9), its gradients 202 us, 4.65 TB/s, and 5.7 to
+// Bound by memory: 16,381 x 7168 with the residual, bf16 and E4M3 results 197 us, 5.4 TB/s (a large copy: 4.9), its gradients 189 us, 5.0 TB/s, and 4.8 to
 // add dw up; 24 rows 4.3 us, a chain of two loads, a sum and a store.
 #include <cfloat>
 #include <cmath>
