@@ -142,6 +142,29 @@ def test_sigmoid_shares_of_tokens_whose_scores_are_all_small(E, pad, dtype):
     assert np.all(np.abs(got - want) <= half * np.abs(want) + (4 * rel + 2.0 ** -15) * mag + 1e-38)
 
 
+@pytest.mark.parametrize("E", [16, 60, 256, 700])
+def test_small_and_ordinary_sigmoid_scores_side_by_side(E):
+    # tokens of one wave whose scores are all small, and others; shares within the bound of the test above
+    X = xs()
+    T, k = 203, 2
+    g = torch.Generator().manual_seed(E)
+    shift = torch.tensor([0.0, -95.0, -40.0, -600.0, 5.0, -87.4, -50.0])[torch.randint(0, 7, (T,), generator=g)]
+    l = torch.randn((T, E), generator=g) * 2 + shift[:, None]
+    l64, dev, gt = l.double().numpy(), l.cuda(), _gate(E, k, "sigmoid", "f32")
+    idx = np.argsort(-l64, 1, kind="stable")[:, :k].astype(np.int32)
+    counts, mean, loss, st, status = _forward(gt, dev, torch.from_numpy(idx).cuda(), [0, T], T)
+    wc, wm, wl = balance.loss(l64, idx, [0, T], "sigmoid", ALPHA)
+    rel = 2 * (80 * 2.0 ** -23 + 2.0 ** -21) + 74 * 2.0 ** -24
+    assert status == 0 and np.array_equal(counts.cpu().numpy(), wc)
+    assert np.all(np.abs(mean.cpu().double().numpy() - wm) <= (rel + (T + 64) * 2.0 ** -24) * wm)
+    want, mag = balance.backward(l64, wc, k, [0, T], "sigmoid", ALPHA, np.ones(1))
+    out, one = torch.zeros_like(dev), torch.ones(1, device="cuda")
+    X.check(X.xs_balance_loss_backward(gt, dev.data_ptr(), E, T, st.data_ptr(), 1, ALPHA, counts.data_ptr(), one.data_ptr(), None, 0, out.data_ptr(), E, None,
+                                       _stream()))
+    torch.cuda.synchronize()
+    assert np.all(np.abs(out.cpu().double().numpy() - want) <= 2.0 ** -24 * np.abs(want) + (4 * rel + 2.0 ** -15) * mag + 1e-38)
+
+
 def test_one_sequence_without_starts_equals_it_with_them():
     X = xs()
     T, E, k = 777, 160, 6
